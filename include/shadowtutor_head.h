@@ -262,6 +262,103 @@ int st_object_weights(const int32_t* labels, int32_t n, int32_t height, int32_t 
                       int32_t background, int32_t ignore_index, int32_t radius, int32_t factor, uint8_t* weights,
                       void* stream);
 
+/* ---- dense layers in 8-bit integers ------------------------------------------------------
+ * A dense (1x1) layer y = act(x W^T + b) over tokens: the cells of a feature map (an [n, h, w, c] map is n*h*w tokens of c channels),
+ * or any rows.  Both operands of a product are whole numbers of -127 .. 127 with one float32 scale for each row of the product they
+ * enter, the products are added exactly in int32, and the scales are applied in float32 to the sum.  A row's scale is its largest
+ * absolute value a times 1/127; its numbers are rint(x * (127 * (1/a))), every operation rounded to float32, ties to even.  A row of zeros has scale 0; a row that holds an
+ * infinity or a NaN gets scale NaN and numbers 0, so that whatever it enters is NaN.  (A row whose largest value lies below 2^-119 is
+ * taken as zeros: 127 / largest leaves float32 there.)
+ *
+ * A matrix argument has an element type (ST_F32 | ST_BF16) and two strides in elements, of which one is 1: row by row with a pitch, or
+ * column by column with a pitch (what a channel-first feature map is to its cells).  Pointers are aligned to their elements, int8
+ * matrices to 16 bytes with a pitch that is a multiple of 16 and at most 2^23.  Tokens may be 0 in number (the call then writes what an empty sum is);
+ * other sizes are at least 1.  Offsets inside a matrix are 64 bits wide; sums longer than ST_INT8_MAX_SUM are refused (ST_ERR_SHAPE)
+ * where the header says so, since int32 could not hold them.  Outputs must not overlap inputs or each other. */
+#define ST_INT8_MAX_SUM 131071
+
+typedef struct st_matrix {
+    const void* data;                /* DEVICE */
+    int32_t dtype;                   /* ST_F32 | ST_BF16 */
+    int64_t rows, cols;
+    int64_t row_stride, col_stride;  /* elements; one of them is 1 (or its dimension is) */
+} st_matrix;
+
+/* Rows of x as 8-bit integers: q [rows, q_pitch] int8, scale [rows] float32.  The bytes of a row from cols up to the next multiple of
+ * 128 are set to zero as far as the pitch reaches.  (Quantising the transpose of a matrix is this call with the strides exchanged.)
+ *   workspace  st_int8_quantize_workspace(rows, cols) bytes if x lies column by column, NULL otherwise */
+size_t st_int8_quantize_workspace(int64_t rows, int64_t cols);
+int st_int8_quantize(const st_matrix* x, int8_t* q, int64_t q_pitch, float* scale, void* workspace, void* stream);
+
+/* y [m, n] = act(x W^T + bias): the tokens x [m, k] are quantised within the call, W is n rows of 8-bit integers with a pitch and a
+ * scale each (st_int8_quantize of the float weights, once).  A row of W is read up to k rounded up to 16; what lies behind k there does
+ * not matter.
+ *   bias [n] float32 or NULL;  relu 0 | 1 (a NaN stays one);  y float32 or bfloat16, row by row with y_pitch >= n
+ *   k <= ST_INT8_MAX_SUM
+ *   workspace  st_int8_linear_workspace(m, n, k) bytes, 256-byte aligned */
+size_t st_int8_linear_workspace(int64_t m, int64_t n, int64_t k);
+int st_int8_linear(const st_matrix* x, const int8_t* wq, int64_t w_pitch, const float* w_scale, int64_t n, const float* bias,
+                   int32_t relu, void* y, int32_t y_dtype, int64_t y_pitch, void* workspace, void* stream);
+
+/* Gradients of that layer from its input x [m, k], its float weights w [n, k] (either type, either order) and dy [m, n]:
+ *   dz = dy, or where y is given (a layer with ReLU) dy where y > 0 and 0 elsewhere (a NaN of y lets nothing through)
+ *   dx [m, k] = dz W       float32 or bfloat16, both operands quantised along n (n <= ST_INT8_MAX_SUM)
+ *   dw [n, k] = dz^T x     float32, both operands quantised along m (m <= 2^23; sums of more than ST_INT8_MAX_SUM tokens are added in 64 bits)
+ *   db [n]    = sum of dz over the tokens, float32, not quantised
+ * Each of dx, dw, db may be NULL and costs nothing then.  y lies as dy does (the same one of its strides is 1), of either type.
+ * dx and dw are row by row with a pitch.  What is not needed for the outputs asked for (x without dw, w without dx) may be NULL.
+ *   workspace  st_int8_linear_backward_workspace(m, n, k) bytes, 256-byte aligned */
+size_t st_int8_linear_backward_workspace(int64_t m, int64_t n, int64_t k);
+int st_int8_linear_backward(const st_matrix* x, const st_matrix* w, const st_matrix* dy, const st_matrix* y, void* dx,
+                            int32_t dx_dtype, int64_t dx_pitch, float* dw, int64_t dw_pitch, float* db, void* workspace,
+                            void* stream);
+
+/* ---- AdamW over many tensors --------------------------------------------------------------
+ * One optimiser step on every tensor of a list, in as few launches as the list allows (ST_ADAMW_PER_LAUNCH tensors each):
+ *   g <- g * grad_scale * c          c = max_norm / norm where norm > max_norm > 0, else 1; norm: of all the list's scaled gradients
+ *   m <- beta1 m + (1 - beta1) g,    v <- beta2 v + (1 - beta2) g^2
+ *   p <- p (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * all in float32, rounded once to the parameters' type.  With max_norm > 0 and a norm that is not finite the step changes nothing.
+ *
+ * state_bits = 32: m and v are float32.  state_bits = 8: every run of ST_ADAMW_BLOCK values of a tensor (the last one shorter) has two
+ * float32 scales, and a value is one byte: m = sign(q) q^2 m_scale with q int8 of -127 .. 127, sqrt(v) = q^2 v_scale with q uint8; the
+ * scales are the run's largest |m| / 127^2 and sqrt(v) / 255^2, a code is the square root of the value's share, to the nearest whole
+ * number; a sqrt(v) > 0 never gets the code 0, so that no m meets a vanished v.  A run whose largest value lies below 2^-100 is held
+ * as zeros; one that holds an infinity or a NaN has scale NaN (all of its values become NaN: with states in 8 bits, clip).  States of
+ * zeros are all bytes zero, in both forms. */
+#define ST_ADAMW_BLOCK 256
+#define ST_ADAMW_PER_LAUNCH 48
+#define ST_ADAMW_MAX_TENSORS 65536
+typedef struct st_adamw_tensor {   /* HOST struct of DEVICE pointers, aligned to their elements */
+    void* param;                   /* [n] in/out */
+    const void* grad;              /* [n] read only */
+    void* m;                       /* [n] in/out: float32, or int8 codes  */
+    void* v;                       /* [n] in/out: float32, or uint8 codes */
+    float* m_scale;                /* [ceil(n / ST_ADAMW_BLOCK)] in/out with states in 8 bits, else NULL */
+    float* v_scale;
+    void* copy;                    /* [n] out: the new parameters as bfloat16 (operands of products), or NULL */
+    int64_t n;                     /* >= 0 */
+    double weight_decay;
+} st_adamw_tensor;
+
+typedef struct st_adamw_opts {
+    int32_t param_dtype, grad_dtype;   /* ST_F32 | ST_BF16 */
+    int32_t state_bits;                /* 8 | 32 */
+    int32_t t;                         /* steps taken on this state, this one included: >= 1 */
+    double lr, beta1, beta2, eps;      /* finite; 0 <= beta < 1; eps >= 0 */
+    double grad_scale;                 /* > 0: 1, or what takes a loss scale back out */
+    double max_norm;                   /* > 0: clip; 0: the norm is not computed unless grad_norm asks for it */
+    float* grad_norm;                  /* [1] out: norm, before clipping; or NULL */
+} st_adamw_opts;
+
+/* Bytes of device scratch for the norm (0 if the list is invalid); needed with max_norm > 0 or grad_norm only. */
+size_t st_adamw_workspace(const st_adamw_tensor* tensors, int32_t n_tensors);
+int st_adamw_step(const st_adamw_tensor* tensors, int32_t n_tensors, const st_adamw_opts* opts, void* workspace, void* stream);
+
+/* The values that a state of n values in 8 bits stands for: m [n] and v [n] float32, either NULL (and then its codes and scales too). */
+int st_adamw_state(const int8_t* m, const float* m_scale, const uint8_t* v, const float* v_scale, int64_t n, float* m_out,
+                   float* v_out, void* stream);
+
 /* ---- scheduling arithmetic around the training step (host only, no GPU work) ------------- */
 
 /* Key-frame striding, Algorithm 2: the ratio of the next stride to the current one is linear in

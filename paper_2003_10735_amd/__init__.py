@@ -23,12 +23,16 @@ ST_F32, ST_BF16 = 0, 1
 ST_NCHW, ST_NHWC = 0, 1
 ST_COMPUTE_F32, ST_COMPUTE_BF16 = 0, 1
 ST_OPTIM_SGD, ST_OPTIM_ADAM = 0, 1
+ST_INT8_MAX_SUM = 131071
+ST_ADAMW_BLOCK = 256
 
 EXPORTS = ["st_num_params", "st_workspace_bytes", "st_head_forward", "st_head_forward_noalloc", "st_partial_distill",
            "st_miou", "st_object_weights", "st_strerror", "st_last_hip_error", "st_version",
            "st_get_workspace_layout", "st_profile_enable", "st_profile_filter", "st_profile_reset", "st_profile_read",
            "st_next_stride", "st_schedule_bounds", "st_schedule_total_time",
-           "st_graph_cache_clear", "st_graph_cache_size", "st_metric_polling"]
+           "st_graph_cache_clear", "st_graph_cache_size", "st_metric_polling",
+           "st_int8_quantize_workspace", "st_int8_quantize", "st_int8_linear_workspace", "st_int8_linear",
+           "st_int8_linear_backward_workspace", "st_int8_linear_backward", "st_adamw_workspace", "st_adamw_step", "st_adamw_state"]
 
 
 class StHeadDesc(C.Structure):
@@ -66,6 +70,21 @@ class StWorkspaceLayout(C.Structure):
     _fields_ = [(k, C.c_size_t) for k in ("feat", "a1", "a2", "da1", "da2", "z", "g", "theta",
                                            "grad", "elem_size", "total", "row_pitch", "grad_copies",
                                            "grad_stride")] + [("splits", C.c_size_t * 3)]
+
+
+class StMatrix(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("dtype", C.c_int32), ("rows", C.c_int64), ("cols", C.c_int64),
+                ("row_stride", C.c_int64), ("col_stride", C.c_int64)]
+
+
+class StAdamwTensor(C.Structure):
+    _fields_ = [(k, C.c_void_p) for k in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [
+        ("n", C.c_int64), ("weight_decay", C.c_double)]
+
+
+class StAdamwOpts(C.Structure):
+    _fields_ = [(k, C.c_int32) for k in ("param_dtype", "grad_dtype", "state_bits", "t")] + [
+        (k, C.c_double) for k in ("lr", "beta1", "beta2", "eps", "grad_scale", "max_norm")] + [("grad_norm", C.c_void_p)]
 
 
 class StKernelStat(C.Structure):
@@ -129,6 +148,19 @@ def lib():
         L.st_schedule_bounds.argtypes = [C.POINTER(StScheduleParams), C.POINTER(StScheduleBounds)]
         L.st_schedule_total_time.restype = C.c_double
         L.st_schedule_total_time.argtypes = [C.POINTER(StScheduleParams)] + [C.c_double] * 4
+        i32, i64, ptr, size = C.c_int32, C.c_int64, C.c_void_p, C.c_size_t
+        for name, result, args in (
+                ("st_int8_quantize_workspace", size, [i64, i64]),
+                ("st_int8_quantize", C.c_int, [ptr, ptr, i64, ptr, ptr, ptr]),
+                ("st_int8_linear_workspace", size, [i64, i64, i64]),
+                ("st_int8_linear", C.c_int, [ptr, ptr, i64, ptr, i64, ptr, i32, ptr, i32, i64, ptr, ptr]),
+                ("st_int8_linear_backward_workspace", size, [i64, i64, i64]),
+                ("st_int8_linear_backward", C.c_int, [ptr, ptr, ptr, ptr, ptr, i32, i64, ptr, i64, ptr, ptr, ptr]),
+                ("st_adamw_workspace", size, [ptr, i32]),
+                ("st_adamw_step", C.c_int, [ptr, i32, ptr, ptr, ptr]),
+                ("st_adamw_state", C.c_int, [ptr, ptr, ptr, ptr, i64, ptr, ptr, ptr])):
+            f = getattr(L, name)
+            f.restype, f.argtypes = result, args
         L.st_graph_cache_size.restype = C.c_int
         L.st_profile_enable.argtypes = [C.c_int]
         L.st_profile_filter.argtypes = [C.c_char_p]
@@ -329,6 +361,218 @@ def st_object_weights(labels, n_classes: int, radius: int, factor: int = 5, back
     _check(lib().st_object_weights(labels.data_ptr(), n, H, W, n_classes, background, ignore_index, radius, factor,
                                    weights.data_ptr(), _stream(stream)), "st_object_weights")
     return weights
+
+
+# ---------------------------------------------------------------- dense layers in 8-bit integers
+_DTYPES = None
+
+
+def _dtype(t, where):
+    """ST_F32 or ST_BF16 of a tensor."""
+    global _DTYPES
+    if _DTYPES is None:
+        import torch
+        _DTYPES = {torch.float32: ST_F32, torch.bfloat16: ST_BF16}
+    d = _DTYPES.get(t.dtype)
+    if d is None:
+        raise StError(ST_ERR_ARG, where)
+    return d
+
+
+def _matrix(t, where):
+    """A two-dimensional tensor as the library takes it: either of its strides 1."""
+    if t.dim() != 2:
+        raise StError(ST_ERR_SHAPE, where)
+    return StMatrix(t.data_ptr(), _dtype(t, where), *t.shape, *t.stride())
+
+
+def _out_matrix(t, rows, cols, where):
+    """Checks a result that lies row by row; returns its pitch."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+        raise StError(ST_ERR_SHAPE, where)
+    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+
+
+def _float_vector(t, n, where):
+    if t.numel() != n or not t.is_contiguous() or _dtype(t, where) != ST_F32:
+        raise StError(ST_ERR_SHAPE, where)
+    return t.data_ptr()
+
+
+def _scratch(nbytes, device, where):
+    import torch
+    if nbytes == 0:
+        raise StError(ST_ERR_SHAPE, where)
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def int8_pitch(cols: int) -> int:
+    """Bytes of a row of `cols` 8-bit integers: a multiple of 16."""
+    return (cols + 15) // 16 * 16
+
+
+def new_int8_workspace(m: int, n: int, k: int, backward: bool = False, device="cuda"):
+    """Scratch for st_int8_linear (or with backward=True st_int8_linear_backward) of m tokens, k -> n channels."""
+    f = lib().st_int8_linear_backward_workspace if backward else lib().st_int8_linear_workspace
+    return _scratch(f(m, n, k), device, "new_int8_workspace")
+
+
+def st_int8_quantize(x, q=None, scale=None, workspace=None, stream=None):
+    """Rows of x [rows, cols] (float32 or bfloat16, row by row or column by column; x.t() quantises the columns) as 8-bit integers:
+    (q int8 [rows, int8_pitch(cols)], scale float32 [rows])."""
+    import torch
+    where = "st_int8_quantize"
+    mx = _matrix(x, where)
+    rows, cols = x.shape
+    if q is None:
+        q = torch.empty((rows, int8_pitch(cols)), dtype=torch.int8, device=x.device)
+    if scale is None:
+        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+    if q.dim() != 2 or q.shape[0] != rows or q.dtype != torch.int8 or q.stride(1) != 1:
+        raise StError(ST_ERR_SHAPE, where)
+    ws = workspace
+    if ws is None and cols > 1 and mx.col_stride != 1:
+        ws = _scratch(lib().st_int8_quantize_workspace(rows, cols), x.device, where)
+    _check(lib().st_int8_quantize(C.byref(mx), q.data_ptr(), q.stride(0) if rows > 1 else q.shape[1], _float_vector(scale, rows, where),
+                                  _addr(ws), _stream(stream)), where)
+    return q, scale
+
+
+def st_int8_linear(x, wq, w_scale, bias=None, relu: bool = False, out=None, out_dtype=None, workspace=None, stream=None):
+    """out [m, n] = act(x W^T + bias): x [m, k] float32 or bfloat16, row by row or column by column, its rows (tokens) quantised within
+    the call; W as st_int8_quantize(W) leaves it: wq int8 [n, >= k], w_scale float32 [n].  out: float32 or bfloat16, as given, else of
+    out_dtype, else of x's type."""
+    where = "st_int8_linear"
+    mx = _matrix(x, where)
+    m, k = x.shape
+    n = wq.shape[0]
+    if wq.dim() != 2 or wq.shape[1] < k or wq.stride(1) != 1 or wq.element_size() != 1:
+        raise StError(ST_ERR_SHAPE, where)
+    if out is None:
+        import torch
+        out = torch.empty((m, n), dtype=out_dtype or x.dtype, device=x.device)
+    pitch = _out_matrix(out, m, n, where)
+    ws = workspace if workspace is not None else new_int8_workspace(m, n, k, device=x.device)
+    _check(lib().st_int8_linear(C.byref(mx), wq.data_ptr(), wq.stride(0) if n > 1 else wq.shape[1], _float_vector(w_scale, n, where), n,
+                                None if bias is None else _float_vector(bias, n, where), 1 if relu else 0, out.data_ptr(),
+                                _dtype(out, where), pitch, ws.data_ptr(), _stream(stream)), where)
+    return out
+
+
+def st_int8_linear_backward(x, w, dy, y=None, dx=None, dw=None, db=None, workspace=None, stream=None):
+    """Gradients of a dense layer, both products in 8-bit integers: dx [m, k] (float32 or bfloat16) = dz W, dw [n, k] float32 = dz^T x,
+    db [n] float32 = sum of dz, where dz = dy, or with y (the layer's result, a layer with ReLU) dy where y > 0.  Only the outputs that
+    are given are computed; x may be None without dw, w without dx.  x, w (float weights), dy, y: float32 or bfloat16, row by row or column by
+    column, y as dy.  Returns (dx, dw, db)."""
+    where = "st_int8_linear_backward"
+    m, n = dy.shape
+    mats = [None if t is None else _matrix(t, where) for t in (x, w, dy, y)]
+    k = w.shape[1] if dx is not None and w is not None else x.shape[1] if dw is not None and x is not None else 1
+    dx_pitch = k if dx is None else _out_matrix(dx, m, k, where)
+    if dw is not None and _dtype(dw, where) != ST_F32:
+        raise StError(ST_ERR_ARG, where)
+    dw_pitch = k if dw is None else _out_matrix(dw, n, k, where)
+    ws = workspace if workspace is not None else new_int8_workspace(m, n, k, backward=True, device=dy.device)
+    _check(lib().st_int8_linear_backward(*[None if a is None else C.byref(a) for a in mats], _addr(dx),
+                                         ST_F32 if dx is None else _dtype(dx, where), dx_pitch, _addr(dw), dw_pitch,
+                                         None if db is None else _float_vector(db, n, where), ws.data_ptr(), _stream(stream)), where)
+    return dx, dw, db
+
+
+# ---------------------------------------------------------------- AdamW over many tensors
+class AdamWTensors:
+    """The list that st_adamw_step works on: parameters, gradients and states of the same lengths, contiguous, in a HOST array that is
+    filled once (the tensors are kept alive with it).  params, grads: float32 or bfloat16, one type each; m, v: float32, or int8 and uint8
+    codes with m_scales and v_scales (float32, one value for each ST_ADAMW_BLOCK values; new_adamw_state makes them); copies: bfloat16 or
+    None; weight_decay: a number or one for each tensor."""
+
+    def __init__(self, params, grads, m, v, m_scales=None, v_scales=None, copies=None, weight_decay=0.0):
+        import torch
+        where = "AdamWTensors"
+        count = len(params)
+        eight = count > 0 and m[0].dtype == torch.int8
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
+        lists = [params, grads, m, v, m_scales, v_scales, copies]
+        wanted = [params[0].dtype if count else None, grads[0].dtype if count else None, torch.int8 if eight else torch.float32,
+                  torch.uint8 if eight else torch.float32, torch.float32, torch.float32, torch.bfloat16]
+        if any(x is not None and len(x) != count for x in lists) or len(decay) != count or eight != (m_scales is not None) \
+                or eight != (v_scales is not None):
+            raise StError(ST_ERR_SHAPE, where)
+        self.array = (StAdamwTensor * max(count, 1))()
+        self.count, self.kept = count, [None if x is None else list(x) for x in lists]
+        self.state_bits = 8 if eight else 32
+        self.param_dtype, self.grad_dtype = (_dtype(params[0], where), _dtype(grads[0], where)) if count else (ST_F32, ST_F32)
+        for i in range(count):
+            n, runs = params[i].numel(), (params[i].numel() + ST_ADAMW_BLOCK - 1) // ST_ADAMW_BLOCK
+            a = self.array[i]
+            for (name, _), x, dtype in zip(StAdamwTensor._fields_, lists, wanted):
+                if x is None:
+                    continue
+                if x[i].dtype != dtype or not x[i].is_contiguous() or x[i].numel() != (runs if name.endswith("scale") else n):
+                    raise StError(ST_ERR_SHAPE, where)
+                setattr(a, name, x[i].data_ptr())
+            a.n, a.weight_decay = n, float(decay[i])
+        self.device = params[0].device if count else "cuda"
+
+    def set_grads(self, grads):
+        """Other gradient tensors (of the same type and lengths) from the next step on."""
+        if len(grads) != self.count:
+            raise StError(ST_ERR_SHAPE, "AdamWTensors")
+        for i, (g, old) in enumerate(zip(grads, self.kept[1])):
+            if g.dtype != old.dtype or g.numel() != old.numel() or not g.is_contiguous():
+                raise StError(ST_ERR_SHAPE, "AdamWTensors")
+            self.array[i].grad = g.data_ptr()
+        self.kept[1] = list(grads)
+
+
+def new_adamw_state(params, bits: int = 32):
+    """Zeroed states for a list of tensors: dict(m=, v=) with bits = 32, dict(m=, v=, m_scales=, v_scales=) with bits = 8."""
+    import torch
+    if bits not in (8, 32):
+        raise StError(ST_ERR_ARG, "new_adamw_state")
+    if bits == 32:
+        return {name: [torch.zeros(p.numel(), dtype=torch.float32, device=p.device) for p in params] for name in ("m", "v")}
+    runs = [(p.numel() + ST_ADAMW_BLOCK - 1) // ST_ADAMW_BLOCK for p in params]
+    state = {name: [torch.zeros(p.numel(), dtype=t, device=p.device) for p in params] for name, t in (("m", torch.int8), ("v", torch.uint8))}
+    for name in ("m_scales", "v_scales"):
+        state[name] = [torch.zeros(r, dtype=torch.float32, device=p.device) for r, p in zip(runs, params)]
+    return state
+
+
+def new_adamw_workspace(tensors: AdamWTensors):
+    """Scratch for st_adamw_step's norm of this list."""
+    return _scratch(lib().st_adamw_workspace(tensors.array, tensors.count), tensors.device, "new_adamw_workspace")
+
+
+def st_adamw_step(tensors: AdamWTensors, t: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
+                  max_norm: float = 0.0, grad_scale: float = 1.0, grad_norm=None, workspace=None, stream=None):
+    """Step number t (from 1 on) of AdamW on every tensor of the list, in place.  max_norm > 0 clips by the norm of all (scaled)
+    gradients, which grad_norm (float32 [1]) receives if given; a norm that is not finite then leaves everything as it was."""
+    where = "st_adamw_step"
+    ws = workspace
+    if ws is None and (max_norm > 0.0 or grad_norm is not None):
+        ws = new_adamw_workspace(tensors)
+    o = StAdamwOpts(tensors.param_dtype, tensors.grad_dtype, tensors.state_bits, t, lr, beta1, beta2, eps, grad_scale, max_norm,
+                    None if grad_norm is None else _float_vector(grad_norm, 1, where))
+    _check(lib().st_adamw_step(tensors.array, tensors.count, C.byref(o), _addr(ws), _stream(stream)), where)
+
+
+def st_adamw_state(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):
+    """The float32 values that a state in 8 bits stands for, into m_out and v_out (made if neither is given).  Returns (m_out, v_out)."""
+    where = "st_adamw_state"
+    if m_out is None and v_out is None:
+        import torch
+        m_out, v_out = (torch.empty(m.shape, dtype=torch.float32, device=m.device) for _ in range(2))
+    n = m.numel() if m_out is not None else v.numel()
+    for codes, scale, out in ((m, m_scale, m_out), (v, v_scale, v_out)):
+        if out is not None and (codes.numel() != n or codes.element_size() != 1 or not codes.is_contiguous()
+                                or scale.numel() * ST_ADAMW_BLOCK < n or not scale.is_contiguous()):
+            raise StError(ST_ERR_SHAPE, where)
+    _check(lib().st_adamw_state(_addr(m) if m_out is not None else None, _addr(m_scale) if m_out is not None else None,
+                                _addr(v) if v_out is not None else None, _addr(v_scale) if v_out is not None else None, n,
+                                None if m_out is None else _float_vector(m_out, n, where),
+                                None if v_out is None else _float_vector(v_out, n, where), _stream(stream)), where)
+    return m_out, v_out
 
 
 def st_graph_cache_clear():

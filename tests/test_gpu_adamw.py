@@ -1,0 +1,281 @@
+"""AdamW over many tensors against the formulas in 64 bits.
+
+Tolerances.  A float32 value here is the result of at most twelve roundings of 2^-24 of its parts: 1e-6 of the parts' size.  With states in
+8 bits a code has to be the square root of the value's share of the run's largest, to the nearest whole number, but for the roundings of the
+share and its root: |code - root| <= 0.5 + 255 * 1e-6 * 2.
+"""
+import math
+
+import pytest
+
+import paper_2003_10735_amd as st
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+DT = {"f32": torch.float32, "bf16": torch.bfloat16}
+RUN = st.ST_ADAMW_BLOCK
+TOL = 1e-6
+HALF = 0.5 + 255 * 2 * TOL
+
+
+def make(sizes, bits=32, param="f32", grad="f32", copies=False, seed=0, offset=0, decay=0.01):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+
+    def new(n, dtype, scale):
+        t = torch.zeros(n + offset, dtype=torch.float32, device="cuda")
+        t[offset:] = scale * torch.randn(n, device="cuda", generator=g)
+        return t.to(dtype)[offset:]
+
+    params = [new(n, DT[param], 1.0) for n in sizes]
+    grads = [new(n, DT[grad], 0.1) for n in sizes]
+    state = st.new_adamw_state(params, bits)
+    extra = [torch.zeros(n + offset, dtype=torch.bfloat16, device="cuda")[offset:] for n in sizes] if copies else None
+    decays = [decay if i % 2 == 0 else 0.0 for i in range(len(sizes))]
+    t = st.AdamWTensors(params, grads, **state, copies=extra, weight_decay=decays)
+    return t, params, grads, state, extra, decays
+
+
+def values(state, i, bits):
+    """(m, sqrt v) of tensor i in 64 bits, from what is stored."""
+    if bits == 32:
+        return state["m"][i].double(), state["v"][i].double().sqrt()
+    n = state["m"][i].numel()
+    rep = lambda s: s.double().repeat_interleave(RUN)[:n]      # noqa: E731
+    q, r = state["m"][i].double(), state["v"][i].double()
+    return q * q.abs() * rep(state["m_scales"][i]), r * r * rep(state["v_scales"][i])
+
+
+def runs_top(x):
+    pad = (-x.numel()) % RUN
+    return torch.cat([x, x.new_zeros(pad)]).view(-1, RUN).amax(1)
+
+
+def check_step(t, params, grads, state, extra, decays, bits, step, lr=1e-2, b1=0.9, b2=0.999, eps=1e-8, max_norm=0.0, grad_scale=1.0):
+    before = [(p.double().clone(), *values(state, i, bits)) for i, p in enumerate(params)]
+    norm = torch.empty(1, device="cuda")
+    st.st_adamw_step(t, step, lr, b1, b2, eps, max_norm=max_norm, grad_scale=grad_scale, grad_norm=norm)
+    torch.cuda.synchronize()
+    want_norm = math.sqrt(sum((g.double() * grad_scale).square().sum().item() for g in grads))
+    assert abs(norm.item() - want_norm) <= TOL * want_norm
+    c = max_norm / want_norm if 0 < max_norm < want_norm else 1.0
+    for i, (p0, m0, u0) in enumerate(before):
+        g = grads[i].double() * grad_scale * c
+        m, v = b1 * m0 + (1 - b1) * g, b2 * u0.square() + (1 - b2) * g.square()
+        size_m = b1 * m0.abs() + (1 - b1) * g.abs()
+        u = v.sqrt()
+        move = lr / (1 - b1 ** step) * m / (u / math.sqrt(1 - b2 ** step) + eps)
+        p = p0 * (1 - lr * decays[i]) - move
+        moved = lr / (1 - b1 ** step) * size_m / (u / math.sqrt(1 - b2 ** step) + eps)
+        far = TOL * (p0.abs() + moved) + (2.0 ** -8 * p.abs() if params[i].dtype == torch.bfloat16 else 0.0)
+        assert ((params[i].double() - p).abs() <= far).all()
+        if extra is not None:
+            assert ((extra[i].double() - p).abs() <= TOL * (p0.abs() + moved) + 2.0 ** -8 * p.abs()).all()
+        if bits == 32:
+            assert ((state["m"][i].double() - m).abs() <= TOL * size_m).all()
+            assert ((state["v"][i].double() - v).abs() <= TOL * v).all()
+            continue
+        for name, value, most in (("m", m, 127), ("v", u, 255)):
+            codes, scale = state[name][i].double(), state[name + "_scales"][i].double()
+            top = runs_top(value.abs())
+            top_size = runs_top(size_m) if name == "m" else top
+            assert ((scale - top / most ** 2).abs() <= 2 * TOL * top_size / most ** 2).all()
+            # (m's own roundings are relative to its parts, which may cancel)
+            each = top.repeat_interleave(RUN)[:value.numel()]
+            slack = TOL * size_m if name == "m" else TOL * value
+            lo, hi = (((value.abs() + d * slack).clamp(min=0) / each.clamp(min=1e-300)).sqrt() * most for d in (-1, 1))
+            code = codes.abs()
+            ok = (code <= hi + HALF) & (code >= lo - HALF)
+            if name == "v":
+                ok |= (code == 1) & (value > 0)
+                assert ((code > 0) | (value == 0)).all()
+            assert ok.all(), name
+            if name == "m":
+                assert ((codes == 0) | (codes.sign() == value.sign()) | (value.abs() <= slack)).all()
+
+
+SIZES = [1, 3, 4, 255, 256, 257, 1023, 2047, 2048, 2049, 5000, 0, 70001]
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("param", ["f32", "bf16"])
+@pytest.mark.parametrize("grad", ["f32", "bf16"])
+@pytest.mark.parametrize("offset", [0, 1])
+def test_steps(bits, param, grad, offset):
+    """Five steps on tensors of awkward lengths, aligned and one element off, with the copy where the parameters are float32."""
+    made = make(SIZES, bits, param, grad, copies=param == "f32", seed=bits, offset=offset)
+    for step in range(1, 6):
+        for g in made[2]:
+            g.mul_(-0.7).add_(0.01)
+        check_step(*made, bits, step)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("max_norm", [0.5, 1e4])
+def test_clip(bits, max_norm):
+    made = make([3000, 17, 600], bits, grad="bf16", seed=3)
+    for step in (1, 2):
+        check_step(*made, bits, step, max_norm=max_norm, grad_scale=0.25)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_many_tensors_need_several_launches(bits):
+    check_step(*make([(i * 37) % 700 for i in range(150)], bits, seed=4), bits, 1, max_norm=1.0)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("b1,b2,eps,lr,decay", [(0.0, 0.0, 1e-8, 0.1, 0.0), (0.9, 0.95, 1e-3, 1.0, 0.5), (0.99, 0.9999, 0.0, 1e-4, 0.1)])
+def test_constants(bits, b1, b2, eps, lr, decay):
+    made = make([4000, 300], bits, seed=5, decay=decay)
+    for step in (1, 2, 1000):
+        check_step(*made, bits, step, lr=lr, b1=b1, b2=b2, eps=eps)
+
+
+def test_gradients_of_zero():
+    for bits in (8, 32):
+        t, params, grads, state, _, decays = made = make([700, 256], bits, seed=6)
+        for g in grads:
+            g.zero_()
+        before = [p.clone() for p in params]
+        st.st_adamw_step(t, 1, 0.1, max_norm=1.0)
+        assert torch.equal(params[1], before[1])                       # no decay, m = 0
+        assert ((params[0] - before[0] * (1 - 0.1 * 0.01)).abs() <= 2 ** -22 * before[0].abs()).all()
+        assert all((x == 0).all() for v in state.values() for x in v)
+        made[2][0].fill_(1e-3)
+        check_step(*made, bits, 2)
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_clipped_step_with_bad_gradient_changes_nothing(bits, bad):
+    t, params, grads, state, *_ = make([700, 5000], bits, seed=7)
+    st.st_adamw_step(t, 1, 0.1)
+    grads[1][4321] = bad
+    before = [x.clone() for x in params + [x for v in state.values() for x in v]]
+    norm = torch.zeros(1, device="cuda")
+    st.st_adamw_step(t, 2, 0.1, max_norm=1.0, grad_norm=norm)
+    assert not torch.isfinite(norm).any()
+    assert all(torch.equal(a, b) for a, b in zip(before, params + [x for v in state.values() for x in v]))
+
+
+def test_norm_of_large_and_small_gradients_is_finite():
+    t, params, grads, *_ = make([1000], seed=8)
+    for value in (1e30, 1e-30):
+        grads[0].fill_(value)
+        norm = torch.zeros(1, device="cuda")
+        st.st_adamw_step(t, 1, 0.0, grad_norm=norm)
+        assert abs(norm.item() / (value * math.sqrt(1000)) - 1) <= TOL
+
+
+def test_bad_gradient_without_clip_spoils_its_run_only():
+    t, params, grads, state, *_ = make([2000], 8, seed=9)
+    grads[0][300] = float("nan")
+    st.st_adamw_step(t, 1, 0.1)
+    assert torch.isnan(state["m_scales"][0][1]) and torch.isnan(state["v_scales"][0][1])
+    others = [i for i in range(8) if i != 1]
+    assert torch.isfinite(state["m_scales"][0][others]).all()
+    assert torch.isnan(params[0][300]) and torch.isfinite(params[0][:300]).all()
+    t, params, grads, state, *_ = make([2000], 32, seed=9)
+    grads[0][300] = float("inf")
+    st.st_adamw_step(t, 1, 0.1)
+    assert torch.isinf(state["m"][0][300]) and torch.isfinite(state["m"][0][301:]).all()
+
+
+def test_tiny_gradients_beside_large_ones_keep_a_denominator():
+    """A value far below its run's largest keeps the smallest code of v, so that its step stays one of Adam's size."""
+    t, params, grads, state, *_ = make([256], 8, seed=10, decay=0.0)
+    g = grads[0]
+    before = params[0].clone()
+    for step in range(1, 30):
+        g.fill_(1e-9)
+        g[0] = 1.0
+        st.st_adamw_step(t, step, 1e-3)
+    assert (state["v"][0][1:] == 1).all()
+    assert (params[0] - before).abs().max() <= 30 * 1e-3 * 3.2
+
+
+def test_state_values():
+    for n in (1, 255, 1000, 4099):
+        g = torch.Generator(device="cuda")
+        g.manual_seed(n)
+        m = torch.randint(-127, 128, (n,), device="cuda", generator=g).to(torch.int8)
+        v = torch.randint(0, 256, (n,), device="cuda", generator=g).to(torch.uint8)
+        runs = (n + RUN - 1) // RUN
+        ms, vs = torch.rand(runs, device="cuda", generator=g), torch.rand(runs, device="cuda", generator=g)
+        state = dict(m=[m], v=[v], m_scales=[ms], v_scales=[vs])
+        wm, wu = values(state, 0, 8)
+        a, b = st.st_adamw_state(m, ms, v, vs)
+        assert ((a - wm).abs() <= TOL * wm.abs()).all() and ((b - wu.square()).abs() <= TOL * wu.square()).all()
+        only = torch.empty(n, device="cuda")
+        st.st_adamw_state(None, None, v, vs, v_out=only)
+        assert torch.equal(only, b)
+
+
+def test_same_codes_whatever_the_alignment():
+    """A tensor one element off takes other loads, and has the same result bit for bit."""
+    for bits in (8, 32):
+        a, b = make([5000], bits, seed=11, offset=0), make([5000], bits, seed=11, offset=1)
+        for x, y in zip(a[1] + a[2], b[1] + b[2]):
+            y.copy_(x)
+        for made in (a, b):
+            for step in (1, 2, 3):
+                st.st_adamw_step(made[0], step, 0.01, max_norm=0.3)
+        assert torch.equal(a[1][0], b[1][0])
+        assert all(torch.equal(x, y) for k in a[3] for x, y in zip(a[3][k], b[3][k]))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_training_reaches_the_minimum(bits):
+    """A quadratic bowl with axes of very different steepness: both forms of the state get there."""
+    n = 3000
+    target = torch.linspace(-1, 1, n, device="cuda")
+    steep = torch.logspace(-2, 2, n, device="cuda")[torch.randperm(n, generator=torch.Generator().manual_seed(0)).cuda()]
+    p = torch.zeros(n, device="cuda")
+    g = torch.empty(n, device="cuda")
+    t = st.AdamWTensors([p], [g], **st.new_adamw_state([p], bits))
+    for step in range(1, 401):
+        torch.mul(steep, p - target, out=g)
+        st.st_adamw_step(t, step, 0.02 * (1 - step / 401))
+    # Adam's steps are at most about lr a value: after the schedule every value is within a few of its last steps' sum
+    assert (p - target).abs().max() < 0.02
+
+
+def test_stream_graph_and_other_gradients():
+    made = make([3000, 100, 2500], 8, seed=12)
+    t, params, grads, state, *_ = made
+    work = st.new_adamw_workspace(t)
+    everything = params + [x for v in state.values() for x in v]
+    start = [x.clone() for x in everything]
+
+    def reset():
+        for x, y in zip(everything, start):
+            x.copy_(y)
+
+    st.st_adamw_step(t, 1, 0.01, max_norm=0.5, workspace=work)
+    torch.cuda.synchronize()
+    want = [x.clone() for x in everything]
+    reset()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        st.st_adamw_step(t, 1, 0.01, max_norm=0.5, workspace=work)
+    side.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, everything))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st.st_adamw_step(t, 1, 0.01, max_norm=0.5, workspace=work)
+    for i in range(3):
+        grads[0].mul_(1.5)
+        reset()
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [x.clone() for x in everything]
+        reset()
+        st.st_adamw_step(t, 1, 0.01, max_norm=0.5, workspace=work)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, everything)), i
+    t.set_grads([torch.zeros_like(g) for g in grads])
+    reset()
+    st.st_adamw_step(t, 1, 0.01, workspace=work)
+    assert torch.equal(params[1], start[1])
