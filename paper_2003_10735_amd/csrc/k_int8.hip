@@ -16,7 +16,8 @@ constexpr int STAGE = 128;      // bytes of the contraction a stage holds
 
 struct GemmArgs {
     Product p;
-    int tiles_m, tiles_n, splits, stages;     // stages: of the whole contraction
+    FastDiv by_tiles, by_row;                 // tiles of a split, tiles of a row of tiles
+    int splits, stages;                       // stages: of the whole contraction
     int* slabs;                               // [splits, m, n] where splits > 1
 };
 
@@ -31,6 +32,53 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t operand(const int8_t* base, in
     return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)(unsigned)(bytes < 0xffffffffll ? bytes : 0xffffffffll), 0x00020000);
 }
 
+// One value's way out: scales, bias, ReLU.
+struct Column { float scale, bias; };
+__device__ __forceinline__ float finish(float sum, float a_scale, Column c, bool relu)
+{
+    const float v = sum * a_scale * c.scale + c.bias;
+    return relu && v < 0.f ? 0.f : v;
+}
+__device__ __forceinline__ Column column_of(const Product& p, int64_t n)
+{
+    return n < p.n ? Column{p.b_scale[n], p.bias ? p.bias[n] : 0.f} : Column{0.f, 0.f};
+}
+// `count` values of one row, channels n .. n + count - 1: at once where `wide`, else those that exist one by one
+template <int COUNT> __device__ __forceinline__ void store_out(const Product& p, int64_t m, int64_t n, bool wide, const float (&v)[COUNT])
+{
+    if (p.out_bf16) {
+        bf16* o = (bf16*)p.out + m * p.out_pitch + n;
+        if (wide && n + COUNT <= p.n) {
+            typedef bf16 T __attribute__((ext_vector_type(COUNT)));
+            T u;
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) u[i] = (bf16)v[i];
+            *(T*)o = u;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) if (n + i < p.n) o[i] = (bf16)v[i];
+    } else {
+        float* o = (float*)p.out + m * p.out_pitch + n;
+        if (wide && n + COUNT <= p.n) {
+#pragma unroll
+            for (int i = 0; i < COUNT; i += 4) *(float4*)(o + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) if (n + i < p.n) o[i] = v[i];
+    }
+}
+
+// s_waitcnt vmcnt(N) alone; a barrier that memory accesses stay on their side of, without a wait of its own
+#define ST_WAIT_VM(N) __builtin_amdgcn_s_waitcnt(((N) & 15) | (((N) >> 4) << 14) | 0x0F70)
+#define ST_BARRIER()                    \
+    do {                                \
+        asm volatile("" ::: "memory");  \
+        __builtin_amdgcn_s_barrier();   \
+        asm volatile("" ::: "memory");  \
+    } while (0)
+
 // BM tokens x BN channels a block, WM x WN a wavefront.
 template <int BM, int BN, int WM, int WN>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(const GemmArgs g)
@@ -40,10 +88,9 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
     extern __shared__ __align__(16) char lds[];
     const Product& p = g.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    int tile = blockIdx.x;
-    const int tiles = g.tiles_m * g.tiles_n, split = tile / tiles;
-    tile -= split * tiles;
-    const int tm = tile / g.tiles_n, tn = tile - tm * g.tiles_n;
+    const int split = __builtin_amdgcn_readfirstlane(fast_quot((int)blockIdx.x, g.by_tiles));
+    const int tile = (int)blockIdx.x - split * (int)g.by_tiles.d;
+    const int tm = __builtin_amdgcn_readfirstlane(fast_quot(tile, g.by_row)), tn = tile - tm * (int)g.by_row.d;
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int first = (int)((int64_t)g.stages * split / g.splits), last = (int)((int64_t)g.stages * (split + 1) / g.splits);
 
@@ -52,76 +99,116 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
     const auto ra = operand(p.b + n0 * p.b_pitch, (p.n - n0 - 1) * p.b_pitch + k16);
     const auto rb = operand(p.a + m0 * p.a_pitch, (p.m - m0 - 1) * p.a_pitch + kq);
     const unsigned chunk = ((lane & 7) ^ (lane >> 3)) * 16;
-    const unsigned va = (unsigned)(lane >> 3) * (unsigned)p.b_pitch + chunk, vb = (unsigned)(lane >> 3) * (unsigned)p.a_pitch + chunk;
+    const unsigned va = (unsigned)(wave * 8 + (lane >> 3)) * (unsigned)p.b_pitch + chunk;
+    const unsigned vb = (unsigned)(wave * 8 + (lane >> 3)) * (unsigned)p.a_pitch + chunk;
+    const unsigned sa = WAVES * 8 * (unsigned)p.b_pitch, sb = WAVES * 8 * (unsigned)p.a_pitch;
     auto stage = [&](int s, int buf) {
-        char* to = lds + buf * BUF;
+        char* to = lds + buf * BUF + wave * 8 * STAGE;
+        unsigned oa = va + (unsigned)s * STAGE, ob = vb + (unsigned)s * STAGE;
 #pragma unroll
-        for (int i = 0; i < AR / 8 / WAVES; ++i) {
-            const int r = (i * WAVES + wave) * 8;
-            load_to_lds(ra, to + r * STAGE, va + (unsigned)r * (unsigned)p.b_pitch + (unsigned)s * STAGE);
-        }
+        for (int i = 0; i < AR / 8 / WAVES; ++i, oa += sa) load_to_lds(ra, to + i * WAVES * 8 * STAGE, oa);
 #pragma unroll
-        for (int i = 0; i < BR / 8 / WAVES; ++i) {
-            const int r = (i * WAVES + wave) * 8;
-            load_to_lds(rb, to + (AR + r) * STAGE, vb + (unsigned)r * (unsigned)p.a_pitch + (unsigned)s * STAGE);
-        }
+        for (int i = 0; i < BR / 8 / WAVES; ++i, ob += sb) load_to_lds(rb, to + (AR + i * WAVES * 8) * STAGE, ob);
     };
 
-    constexpr int NA = WN / 32, NB = WM / 32;
+    constexpr int NA = WN / 32, NB = WM / 32, STEPS = STAGE / 32;
     const int wn = (wave % (BN / WN)) * WN, wm = (wave / (BN / WN)) * WM;
     const int r32 = lane & 31, half = lane >> 5;
+    const int offA = (wn + r32) * STAGE, offB = (AR + wm + r32) * STAGE;
     i32x16 acc[NB][NA] = {};
-    if (first < last) stage(first, 0);
+    i32x4 a[2][NA], b[2][NB];
+    auto fetch = [&](int buf, int ks, int to) {
+        const char* L = lds + buf * BUF + ((ks * 2 + half) ^ (r32 & 7)) * 16;
+#pragma unroll
+        for (int i = 0; i < NA; ++i) a[to][i] = *(const i32x4*)(L + offA + i * 32 * STAGE);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) b[to][j] = *(const i32x4*)(L + offB + j * 32 * STAGE);
+    };
+    auto multiply = [&](int from) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int i = 0; i < NA; ++i) acc[j][i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[from][i], b[from][j], acc[j][i], 0, 0, 0);
+    };
+    // in the instruction stream: one LDS read, one matrix instruction, while there are reads
+    auto interleave = [] {
+#pragma unroll
+        for (int i = 0; i < NA + NB; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+    };
+    // Two stages are under way.  A stage's last step has its operands in registers when the barrier is passed, so what follows the barrier
+    // is: the loads of the stage after next into the buffer that is done with, the next stage's first operands, the last step's products.
+    constexpr int LOADS = (AR + BR) / 8 / WAVES;      // of a wavefront and stage
+    if (first < last) {
+        stage(first, 0);
+        if (first + 1 < last) { stage(first + 1, 1); ST_WAIT_VM(LOADS); } else ST_WAIT_VM(0);
+        ST_BARRIER();
+        fetch(0, 0, 0);
+    }
     for (int s = first; s < last; ++s) {
         const int buf = (s - first) & 1;
-        __builtin_amdgcn_s_waitcnt(0x0f70);    // vmcnt(0): this stage has arrived
-        __syncthreads();                       // .. for every wavefront, and every one is done with the other buffer
-        if (s + 1 < last) stage(s + 1, buf ^ 1);
-        const char* A = lds + buf * BUF + (wn + r32) * STAGE;
-        const char* B = lds + buf * BUF + (AR + wm + r32) * STAGE;
 #pragma unroll
-        for (int ks = 0; ks < STAGE / 32; ++ks) {
-            const int place = ((ks * 2 + half) ^ (r32 & 7)) * 16;
-            i32x4 a[NA], b[NB];
-#pragma unroll
-            for (int i = 0; i < NA; ++i) a[i] = *(const i32x4*)(A + i * 32 * STAGE + place);
-#pragma unroll
-            for (int j = 0; j < NB; ++j) b[j] = *(const i32x4*)(B + j * 32 * STAGE + place);
-#pragma unroll
-            for (int j = 0; j < NB; ++j)
-#pragma unroll
-                for (int i = 0; i < NA; ++i) acc[j][i] = __builtin_amdgcn_mfma_i32_32x32x32_i8(a[i], b[j], acc[j][i], 0, 0, 0);
+        for (int ks = 0; ks < STEPS - 1; ++ks) {
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(buf, ks + 1, (ks + 1) & 1);
+            multiply(ks & 1);
+            interleave();
         }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_waitcnt(0x0070);    // vmcnt(0), lgkmcnt(0): the next stage is there, this one is read
+        ST_BARRIER();
+        if (s + 2 < last) stage(s + 2, buf);
+        if (s + 1 < last) fetch(buf ^ 1, 0, 0);
+        multiply((STEPS - 1) & 1);
     }
 
+    // Out through LDS, 32 tokens of a wavefront at a time: sums go in four neighbouring channels at a time and come out as runs along a row.
+    __syncthreads();
+    constexpr int PITCH = WN + 4, RUNS = WN / 8, ROWS = 64 / RUNS;
+    static_assert(WAVES * 32 * PITCH * 4 <= 2 * BUF, "room for the sums");
+    int* mine = (int*)lds + wave * 32 * PITCH;
+    const int run = lane % RUNS, row = lane / RUNS;
+    const int64_t n = n0 + wn + run * 8;
+    Column col[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) col[i] = g.splits > 1 ? Column{0.f, 0.f} : column_of(p, n + i);
+    const int64_t esz = p.out_bf16 ? 2 : 4;
+    const bool wide = ((uintptr_t)p.out & 15) == 0 && (p.out_pitch * esz & 15) == 0;
+    const bool wide_slab = (p.n & 3) == 0;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-        const int64_t m = m0 + wm + j * 32 + r32;
-        if (m >= p.m) continue;
-        if (g.splits > 1) {
-            int* to = g.slabs + ((int64_t)split * p.m + m) * p.n;
-#pragma unroll
-            for (int i = 0; i < NA; ++i)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int64_t n = n0 + wn + i * 32 + 8 * (r / 4) + 4 * half + r % 4;
-                    if (n < p.n) to[n] = acc[j][i][r];
-                }
-            continue;
-        }
-        const float sm = p.a_scale[m];
 #pragma unroll
         for (int i = 0; i < NA; ++i)
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int64_t n = n0 + wn + i * 32 + 8 * (r / 4) + 4 * half + r % 4;
-                if (n >= p.n) continue;
-                float v = (float)acc[j][i][r] * sm * p.b_scale[n];
-                if (p.bias) v += p.bias[n];
-                if (p.relu) v = v < 0.f ? 0.f : v;
-                if (p.out_bf16) ((bf16*)p.out)[m * p.out_pitch + n] = (bf16)v;
-                else ((float*)p.out)[m * p.out_pitch + n] = v;
+            for (int q = 0; q < 4; ++q)
+                *(i32x4*)(mine + r32 * PITCH + i * 32 + q * 8 + half * 4) =
+                    i32x4{acc[j][i][q * 4], acc[j][i][q * 4 + 1], acc[j][i][q * 4 + 2], acc[j][i][q * 4 + 3]};
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int h = 0; h < 32 / ROWS; ++h) {
+            const int r = h * ROWS + row;
+            const int64_t m = m0 + wm + j * 32 + r;
+            const i32x4 lo = *(const i32x4*)(mine + r * PITCH + run * 8), hi = *(const i32x4*)(mine + r * PITCH + run * 8 + 4);
+            if (m >= p.m) continue;
+            if (g.splits > 1) {
+                int* to = g.slabs + ((int64_t)split * p.m + m) * p.n + n;
+                if (wide_slab && n + 8 <= p.n) { ((i32x4*)to)[0] = lo; ((i32x4*)to)[1] = hi; }
+                else
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) if (n + i < p.n) to[i] = i < 4 ? lo[i] : hi[i - 4];
+                continue;
             }
+            const float sm = p.a_scale[m];
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = finish((float)(i < 4 ? lo[i] : hi[i - 4]), sm, col[i], p.relu);
+            store_out<8>(p, m, n, wide, v);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -134,9 +221,7 @@ __global__ __launch_bounds__(256) void k_int8_join(const GemmArgs g)
         const int64_t m = at / p.n, n = at - m * p.n;
         int64_t sum = 0;
         for (int s = 0; s < g.splits; ++s) sum += g.slabs[(int64_t)s * all + at];
-        float v = (float)sum * p.a_scale[m] * p.b_scale[n];
-        if (p.bias) v += p.bias[n];
-        if (p.relu) v = v < 0.f ? 0.f : v;
+        const float v = finish((float)sum, p.a_scale[m], column_of(p, n), p.relu);
         if (p.out_bf16) ((bf16*)p.out)[m * p.out_pitch + n] = (bf16)v;
         else ((float*)p.out)[m * p.out_pitch + n] = v;
     }
@@ -171,14 +256,15 @@ static void launch(Ctx& c, const GemmArgs& g)
 {
     constexpr size_t lds = 2 * (BM + BN) * STAGE;
     ensure_dynamic_lds((const void*)k_int8_product<BM, BN, WM, WN>, lds);
-    ST_LAUNCH(c, "int8_product", (k_int8_product<BM, BN, WM, WN>), dim3((unsigned)g.tiles_m * g.tiles_n * g.splits),
+    ST_LAUNCH(c, "int8_product", (k_int8_product<BM, BN, WM, WN>), dim3(g.by_tiles.d * (unsigned)g.splits),
               dim3((BM / WM) * (BN / WN) * 64), lds, g);
 }
 
 void product(Ctx& c, const Product& p, int* slabs)
 {
     const Form f = form_of(p.m, p.n, p.k);
-    GemmArgs g{p, (int)ceil_div(p.m, f.bm), (int)ceil_div(p.n, f.bn), f.splits, (int)ceil_div(p.k, STAGE), slabs};
+    const int64_t tm = ceil_div(p.m, f.bm), tn = ceil_div(p.n, f.bn);
+    GemmArgs g{p, fast_div((int)(tm * tn)), fast_div((int)tn), f.splits, (int)ceil_div(p.k, STAGE), slabs};
     if (f.bm == 256) launch<256, 256, 128, 64>(c, g);
     else if (f.bm == 128) launch<128, 128, 64, 64>(c, g);
     else launch<64, 64, 32, 32>(c, g);
