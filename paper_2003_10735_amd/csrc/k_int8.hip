@@ -10,6 +10,8 @@
 // eight consecutive rows then read eight different groups of banks.
 #include "st_dense.hpp"
 
+#include <algorithm>
+
 namespace st {
 
 constexpr int STAGE = 128;      // bytes of the contraction a stage holds
@@ -18,8 +20,9 @@ struct GemmArgs {
     Product p;
     FastDiv by_tiles, by_row;                 // tiles of a split, tiles of a row of tiles
     int splits, stages;                       // stages: of the whole contraction
-    int* slabs;                               // [splits, m, n] where splits > 1
+    unsigned blocks;
 };
+struct GemmPair { GemmArgs g[2]; };
 
 // 16 bytes a lane from `rsrc` + voff to LDS at `lds` + 16 * lane (the whole offset is the lanes': a scalar one takes no part in the
 // comparison with the buffer's size)
@@ -81,15 +84,18 @@ template <int COUNT> __device__ __forceinline__ void store_out(const Product& p,
 
 // BM tokens x BN channels a block, WM x WN a wavefront.
 template <int BM, int BN, int WM, int WN>
-__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(const GemmArgs g)
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(const GemmPair pair)
 {
     constexpr int WAVES = (BM / WM) * (BN / WN), AR = BN, BR = BM;     // A operand: channels, B operand: tokens
     constexpr int BUF = (AR + BR) * STAGE;
     extern __shared__ __align__(16) char lds[];
+    const bool second = blockIdx.x >= pair.g[0].blocks;
+    const GemmArgs& g = pair.g[second];
     const Product& p = g.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int split = __builtin_amdgcn_readfirstlane(fast_quot((int)blockIdx.x, g.by_tiles));
-    const int tile = (int)blockIdx.x - split * (int)g.by_tiles.d;
+    const int block = (int)blockIdx.x - (second ? (int)pair.g[0].blocks : 0);
+    const int split = __builtin_amdgcn_readfirstlane(fast_quot(block, g.by_tiles));
+    const int tile = block - split * (int)g.by_tiles.d;
     const int tm = __builtin_amdgcn_readfirstlane(fast_quot(tile, g.by_row)), tn = tile - tm * (int)g.by_row.d;
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int first = (int)((int64_t)g.stages * split / g.splits), last = (int)((int64_t)g.stages * (split + 1) / g.splits);
@@ -194,7 +200,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
             const i32x4 lo = *(const i32x4*)(mine + r * PITCH + run * 8), hi = *(const i32x4*)(mine + r * PITCH + run * 8 + 4);
             if (m >= p.m) continue;
             if (g.splits > 1) {
-                int* to = g.slabs + ((int64_t)split * p.m + m) * p.n + n;
+                int* to = p.slabs + ((int64_t)split * p.m + m) * p.n + n;
                 if (wide_slab && n + 8 <= p.n) { ((i32x4*)to)[0] = lo; ((i32x4*)to)[1] = hi; }
                 else
 #pragma unroll
@@ -212,65 +218,71 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
     }
 }
 
-// The slabs of a split product, added in 64 bits, and what the product's own epilogue does otherwise.
-__global__ __launch_bounds__(256) void k_int8_join(const GemmArgs g)
+// The slabs of split products, added in 64 bits, and what the product's own epilogue does otherwise.
+__global__ __launch_bounds__(256) void k_int8_join(const GemmPair pair, int64_t first, int64_t all)
 {
-    const Product& p = g.p;
-    const int64_t all = p.m * p.n;
-    for (int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x; at < all; at += (int64_t)gridDim.x * 256) {
-        const int64_t m = at / p.n, n = at - m * p.n;
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const bool second = i >= first;
+        const GemmArgs& g = pair.g[second];
+        const Product& p = g.p;
+        const int64_t at = second ? i - first : i, size = p.m * p.n, m = at / p.n, n = at - m * p.n;
         int64_t sum = 0;
-        for (int s = 0; s < g.splits; ++s) sum += g.slabs[(int64_t)s * all + at];
-        const float v = finish((float)sum, p.a_scale[m], column_of(p, n), p.relu);
-        if (p.out_bf16) ((bf16*)p.out)[m * p.out_pitch + n] = (bf16)v;
-        else ((float*)p.out)[m * p.out_pitch + n] = v;
+#pragma unroll 4
+        for (int s = 0; s < g.splits; ++s) sum += p.slabs[(int64_t)s * size + at];
+        const float v[1] = {finish((float)sum, p.a_scale[m], column_of(p, n), p.relu)};
+        store_out<1>(p, m, n, false, v);
     }
 }
 
 // --------------------------------------------------------------------------------------- choice of tile and split
-struct Form { int bm, bn, splits; };
-static Form form_of(int64_t m, int64_t n, int64_t k)
+static int64_t tiles_of(const Extent& e, int tile) { return ceil_div(e.m, tile) * ceil_div(e.n, tile); }
+Form form_of(const Extent* e, int count)
 {
-    const int64_t stages = ceil_div(k, STAGE);
-    Form f = {64, 64, 1};
-    if (ceil_div(m, 256) * ceil_div(n, 256) >= 192) f = {256, 256, 1};
-    else if (ceil_div(m, 128) * ceil_div(n, 128) >= 192) f = {128, 128, 1};
-    const int64_t tiles = ceil_div(m, f.bm) * ceil_div(n, f.bn);
-    int64_t s = 512 / tiles;                                   // two blocks a compute unit
-    if (s > stages / 4) s = stages / 4;                        // four stages each at least
-    if (s < 1) s = 1;
-    const int64_t least = ceil_div(stages, ST_INT8_MAX_SUM / STAGE);    // what int32 can hold
-    if (s < least) s = least;
-    f.splits = (int)s;
+    auto total = [&](int tile) { int64_t t = 0; for (int i = 0; i < count; ++i) t += tiles_of(e[i], tile); return t; };
+    Form f = {64, {1, 1}};
+    if (total(256) >= 192) f.tile = 256;
+    else if (total(128) >= 192) f.tile = 128;
+    // every block about the same number of stages, 512 blocks, four stages each at least
+    int64_t work = 0;
+    for (int i = 0; i < count; ++i) work += tiles_of(e[i], f.tile) * ceil_div(e[i].k, STAGE);
+    const int64_t each = std::max<int64_t>(4, ceil_div(work, 512));
+    for (int i = 0; i < count; ++i) {
+        const int64_t stages = ceil_div(e[i].k, STAGE);
+        int64_t s = total(f.tile) < 256 ? stages / each : 1;
+        s = std::max(s, ceil_div(stages, ST_INT8_MAX_SUM / STAGE));    // what int32 can hold
+        f.splits[i] = (int)std::max<int64_t>(s, 1);
+    }
     return f;
 }
 
-size_t product_slab_bytes(int64_t m, int64_t n, int64_t k)
-{
-    const Form f = form_of(m, n, k);
-    return f.splits > 1 ? (size_t)f.splits * m * n * 4 : 0;
-}
-
 template <int BM, int BN, int WM, int WN>
-static void launch(Ctx& c, const GemmArgs& g)
+static void launch(Ctx& c, const GemmPair& g)
 {
     constexpr size_t lds = 2 * (BM + BN) * STAGE;
     ensure_dynamic_lds((const void*)k_int8_product<BM, BN, WM, WN>, lds);
-    ST_LAUNCH(c, "int8_product", (k_int8_product<BM, BN, WM, WN>), dim3(g.by_tiles.d * (unsigned)g.splits),
-              dim3((BM / WM) * (BN / WN) * 64), lds, g);
+    ST_LAUNCH(c, "int8_product", (k_int8_product<BM, BN, WM, WN>), dim3(g.g[0].blocks + g.g[1].blocks), dim3((BM / WM) * (BN / WN) * 64), lds, g);
 }
 
-void product(Ctx& c, const Product& p, int* slabs)
+void products(Ctx& c, const Product* p, int count)
 {
-    const Form f = form_of(p.m, p.n, p.k);
-    const int64_t tm = ceil_div(p.m, f.bm), tn = ceil_div(p.n, f.bn);
-    GemmArgs g{p, fast_div((int)(tm * tn)), fast_div((int)tn), f.splits, (int)ceil_div(p.k, STAGE), slabs};
-    if (f.bm == 256) launch<256, 256, 128, 64>(c, g);
-    else if (f.bm == 128) launch<128, 128, 64, 64>(c, g);
+    if (count == 0) return;
+    Extent e[2];
+    for (int i = 0; i < count; ++i) e[i] = {p[i].m, p[i].n, p[i].k};
+    const Form f = form_of(e, count);
+    GemmPair g{}, joined{};
+    int n_joined = 0;
+    int64_t cells[2] = {0, 0};
+    for (int i = 0; i < count; ++i) {
+        const int64_t tm = ceil_div(p[i].m, f.tile), tn = ceil_div(p[i].n, f.tile);
+        g.g[i] = GemmArgs{p[i], fast_div((int)(tm * tn)), fast_div((int)tn), f.splits[i], (int)ceil_div(p[i].k, STAGE), (unsigned)(tm * tn * f.splits[i])};
+        if (f.splits[i] > 1) { cells[n_joined] = p[i].m * p[i].n; joined.g[n_joined++] = g.g[i]; }
+    }
+    if (f.tile == 256) launch<256, 256, 128, 64>(c, g);
+    else if (f.tile == 128) launch<128, 128, 64, 64>(c, g);
     else launch<64, 64, 32, 32>(c, g);
-    if (f.splits > 1) {
-        const int64_t blocks = ceil_div(p.m * p.n, 256);
-        ST_LAUNCH(c, "int8_join", k_int8_join, dim3((unsigned)(blocks > 8192 ? 8192 : blocks)), dim3(256), 0, g);
+    if (n_joined) {
+        const int64_t all = cells[0] + cells[1], blocks = ceil_div(all, 256);
+        ST_LAUNCH(c, "int8_join", k_int8_join, dim3((unsigned)(blocks > 8192 ? 8192 : blocks)), dim3(256), 0, joined, cells[0], all);
     }
 }
 

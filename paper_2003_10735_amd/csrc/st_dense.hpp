@@ -23,13 +23,15 @@ struct QuantSource {
 };
 
 constexpr int64_t OPERAND_QUANTUM = 128;         // internal operands: rows of whole stages of the product
-// Transposing sources (along == 0): the contraction is cut into parts, each of which leaves a largest value (and a sum) per row.
+// Sources with along == 0 are transposed: the contraction is cut into parts, each of which leaves a largest value (and a sum) per row.
 int transpose_parts(int64_t rows, int64_t len);
-// sum [rows] or null: the plain sums of the rows; to.q null: only those
-void quantize_rows(Ctx& c, const QuantSource& s, const Quantized& to, float* sum = nullptr);
-// part_max, part_sum [parts, rows] (part_sum: where sum is asked for)
-void quantize_transposed(Ctx& c, const QuantSource& s, const Quantized& to, float* part_max, float* part_sum, float* sum);
-void column_sums(Ctx& c, const QuantSource& s, float* part_sum, float* sum);    // of a source with along == 0
+struct QuantTask {
+    QuantSource s;
+    Quantized to;                  // q null: only the sums
+    float *part_max, *part_sum;    // [parts, rows] where along == 0 (part_sum: where sum is asked for)
+    float* sum;                    // [rows]: the plain sums of the rows, or null
+};
+void quantize(Ctx& c, const QuantTask* tasks, int n);      // up to four
 
 // ------------------------------------------------------------------ products
 // out [m, n] = act((sum_k a[m][k] b[n][k]) * a_scale[m] * b_scale[n] + bias[n]).  a's rows hold zeros from k up to a multiple of
@@ -40,9 +42,14 @@ struct Product {
     int64_t m, n, k;
     void* out; int out_bf16; int64_t out_pitch;
     const float* bias; int relu;
+    int* slabs;                  // [splits, m, n], see below
 };
-size_t product_slab_bytes(int64_t m, int64_t n, int64_t k);     // scratch of one product (0: none)
-void product(Ctx& c, const Product& p, int* slabs);
+// Up to two products share a launch: one tile, and for each a number of parts that its contraction is split into.  A split product needs
+// splits * m * n ints for the parts' sums.
+struct Extent { int64_t m, n, k; };
+struct Form { int tile; int splits[2]; };
+Form form_of(const Extent* e, int count);
+void products(Ctx& c, const Product* p, int count);
 void fill_zero(Ctx& c, float* p, int64_t rows, int64_t cols, int64_t pitch);
 
 // ------------------------------------------------------------------ optimiser

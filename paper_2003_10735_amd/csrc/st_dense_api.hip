@@ -2,6 +2,7 @@
 #include "st_dense.hpp"
 
 #include <math.h>
+#include <algorithm>
 
 namespace st {
 namespace {
@@ -55,10 +56,11 @@ QuantSource source(const st_matrix& x, int along, bool transposed, const st_matr
 }
 // scratch of a source that is transposed on the way
 size_t parts_bytes(int64_t rows, int64_t len) { return (size_t)transpose_parts(rows, len) * rows * 4; }
-void quantize(Ctx& c, const QuantSource& s, const Quantized& to, float* part_max, float* part_sum = nullptr, float* sum = nullptr)
+// scratch of product `which` of those that share a launch
+size_t slab_bytes(const Extent* e, int count, int which)
 {
-    if (s.along) quantize_rows(c, s, to, sum);
-    else quantize_transposed(c, s, to, part_max, part_sum, sum);
+    const Form f = form_of(e, count);
+    return f.splits[which] > 1 ? (size_t)f.splits[which] * e[which].m * e[which].n * 4 : 0;
 }
 
 struct LinearSpace { Quantized x; float* parts; int* slabs; size_t bytes; };
@@ -68,7 +70,8 @@ LinearSpace linear_space(char* ws, int64_t m, int64_t n, int64_t k)
     LinearSpace s;
     s.x = w.operand(m, k);
     s.parts = (float*)w.take(m ? parts_bytes(m, k) : 0);
-    s.slabs = (int*)w.take(m ? product_slab_bytes(m, n, k) : 0);
+    const Extent e{m, n, k};
+    s.slabs = (int*)w.take(m ? slab_bytes(&e, 1, 0) : 0);
     s.bytes = w.used + 256;
     return s;
 }
@@ -83,8 +86,9 @@ BackwardSpace backward_space(char* ws, int64_t m, int64_t n, int64_t k)
     s.dzt_sum = (float*)w.take(m ? parts_bytes(n, m) : 0);
     s.wt_max = (float*)w.take(parts_bytes(k, n));
     s.xt_max = (float*)w.take(m ? parts_bytes(k, m) : 0);
-    s.slabs_x = (int*)w.take(m ? product_slab_bytes(m, k, n) : 0);
-    s.slabs_w = (int*)w.take(m ? product_slab_bytes(n, k, m) : 0);
+    const Extent e[2] = {{n, k, m}, {m, k, n}};       // dw, dx: either may come alone
+    s.slabs_w = (int*)w.take(m ? std::max(slab_bytes(e, 2, 0), slab_bytes(e, 1, 0)) : 0);
+    s.slabs_x = (int*)w.take(m ? std::max(slab_bytes(e, 2, 1), slab_bytes(e + 1, 1, 0)) : 0);
     s.bytes = w.used + 256;
     return s;
 }
@@ -115,7 +119,8 @@ int st_int8_quantize(const st_matrix* x, int8_t* q, int64_t q_pitch, float* scal
     if (!is_aligned(q, 16) || !is_aligned(scale, 4)) return ST_ERR_ARG;
     if (!along && (!workspace || !is_aligned(workspace, 256))) return ST_ERR_WORKSPACE;
     Ctx c{(hipStream_t)stream, ST_OK};
-    quantize(c, source(*x, along, false), Quantized{q, q_pitch, scale}, (float*)workspace);
+    const QuantTask task{source(*x, along, false), Quantized{q, q_pitch, scale}, (float*)workspace, nullptr, nullptr};
+    quantize(c, &task, 1);
     return c.status;
 }
 
@@ -141,8 +146,10 @@ int st_int8_linear(const st_matrix* x, const int8_t* wq, int64_t w_pitch, const 
     if (!workspace || !is_aligned(workspace, 256)) return ST_ERR_WORKSPACE;
     const LinearSpace s = linear_space((char*)workspace, m, n, k);
     Ctx c{(hipStream_t)stream, ST_OK};
-    quantize(c, source(*x, along, false), s.x, s.parts);
-    product(c, Product{s.x.q, s.x.pitch, s.x.scale, wq, w_pitch, w_scale, m, n, k, y, y_dtype == ST_BF16, y_pitch, bias, relu}, s.slabs);
+    const QuantTask task{source(*x, along, false), s.x, s.parts, nullptr, nullptr};
+    quantize(c, &task, 1);
+    const Product p{s.x.q, s.x.pitch, s.x.scale, wq, w_pitch, w_scale, m, n, k, y, y_dtype == ST_BF16, y_pitch, bias, relu, s.slabs};
+    products(c, &p, 1);
     return c.status;
 }
 
@@ -182,21 +189,20 @@ int st_int8_linear_backward(const st_matrix* x, const st_matrix* w, const st_mat
         return c.status;
     }
     const BackwardSpace s = backward_space((char*)workspace, m, n, k);
+    QuantTask task[4];
+    int n_tasks = 0;
     if (dx) {
-        quantize(c, source(*dy, dy_along, false, y), s.dz, s.dz_max);
-        quantize(c, source(*w, w_along, true), s.wt, s.wt_max);
-        product(c, Product{s.dz.q, s.dz.pitch, s.dz.scale, s.wt.q, s.wt.pitch, s.wt.scale, m, k, n, dx, dx_dtype == ST_BF16, dx_pitch, nullptr, 0},
-                s.slabs_x);
+        task[n_tasks++] = QuantTask{source(*dy, dy_along, false, y), s.dz, s.dz_max, nullptr, nullptr};
+        task[n_tasks++] = QuantTask{source(*w, w_along, true), s.wt, s.wt_max, nullptr, nullptr};
     }
-    const QuantSource dzt = source(*dy, dy_along, true, y);
-    if (dw) {
-        quantize(c, dzt, s.dzt, s.dzt_max, s.dzt_sum, db);
-        quantize(c, source(*x, x_along, true), s.xt, s.xt_max);
-        product(c, Product{s.dzt.q, s.dzt.pitch, s.dzt.scale, s.xt.q, s.xt.pitch, s.xt.scale, n, k, m, dw, 0, dw_pitch, nullptr, 0}, s.slabs_w);
-    } else if (db) {
-        if (dzt.along) quantize_rows(c, dzt, Quantized{nullptr, 0, nullptr}, db);
-        else column_sums(c, dzt, s.dzt_sum, db);
-    }
+    if (dw || db) task[n_tasks++] = QuantTask{source(*dy, dy_along, true, y), dw ? s.dzt : Quantized{nullptr, 0, nullptr}, s.dzt_max, s.dzt_sum, db};
+    if (dw) task[n_tasks++] = QuantTask{source(*x, x_along, true), s.xt, s.xt_max, nullptr, nullptr};
+    quantize(c, task, n_tasks);
+    Product p[2];
+    int n_products = 0;
+    if (dw) p[n_products++] = Product{s.dzt.q, s.dzt.pitch, s.dzt.scale, s.xt.q, s.xt.pitch, s.xt.scale, n, k, m, dw, 0, dw_pitch, nullptr, 0, s.slabs_w};
+    if (dx) p[n_products++] = Product{s.dz.q, s.dz.pitch, s.dz.scale, s.wt.q, s.wt.pitch, s.wt.scale, m, k, n, dx, dx_dtype == ST_BF16, dx_pitch, nullptr, 0, s.slabs_x};
+    products(c, p, n_products);
     return c.status;
 }
 
