@@ -221,18 +221,20 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-_TORCH = None
+_RAW_STREAM = None
 
 
 def _stream(stream):
-    """The stream's handle as an integer (the current stream if none is given)."""
-    global _TORCH
+    """The stream's handle as an integer (the current stream of the current device if none is given).  The handle is asked for without
+    the object around it, which takes longer to make than a launch."""
+    global _RAW_STREAM
     if stream is not None:
         return stream.cuda_stream
-    if _TORCH is None:
+    if _RAW_STREAM is None:
         import torch
-        _TORCH = torch
-    return _TORCH.cuda.current_stream().cuda_stream
+        torch.cuda.current_stream()         # initialises the device
+        _RAW_STREAM = torch._C._cuda_getCurrentRawStream, torch._C._cuda_getDevice
+    return _RAW_STREAM[0](_RAW_STREAM[1]())
 
 
 def _check(status: int, where: str):

@@ -8,7 +8,7 @@
 // A stage of 128 bytes of the contraction of a tile's rows goes from memory into LDS directly, 16 bytes a lane, eight rows a
 // wavefront and instruction.  Chunk c (of 16 bytes) of row r lies in place c ^ (r & 7) of its row: lanes that read the same chunk of
 // eight consecutive rows then read eight different groups of banks.
-#include "st_dense.hpp"
+#include "st_quantize.hpp"
 
 #include <algorithm>
 
@@ -232,6 +232,150 @@ __global__ __launch_bounds__(256) void k_int8_join(const GemmPair pair, int64_t 
         const float v[1] = {finish((float)sum, p.a_scale[m], column_of(p, n), p.relu)};
         store_out<1>(p, m, n, false, v);
     }
+}
+
+// --------------------------------------------------------------------------------------------------- few tokens
+// Up to 64 tokens: the weights are read once, by as many wavefronts as there are, and the tokens' codes many times.  A block takes 16
+// channels, each of its eight wavefronts an eighth of the contraction, 16 bytes a lane straight from memory into
+// v_mfma_i32_16x16x64_i8 (lane l supplies A[l % 16][16*(l/16) .. +15] and B[16*(l/16) .. +15][l % 16] and receives
+// D[4*(l/16) + r][l % 16]); the eighths are added in LDS.
+//
+// FUSED: every block quantises the tokens by itself, into LDS, while its first weights are on their way: the tokens are few, and a launch
+// of its own for them takes longer than the product.
+constexpr int FEW_WAVES = 8, FEW_AHEAD = 8;
+
+struct FewArgs {
+    Product p;
+    const void* x; int x_bf16, x_wide; int64_t x_pitch;      // FUSED: the tokens as they are, row by row
+    int per_wave;                                            // bytes of the contraction a wavefront takes, a multiple of 64
+    int lds_pitch;                                           // FUSED: bytes between two tokens' codes in LDS
+};
+
+template <class T> __device__ __forceinline__ void few_quantize(const FewArgs& f, char* codes, unsigned (*tops)[FEW_WAVES], float* scales)
+{
+    const Product& p = f.p;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = (int)p.m;
+    const int per_row = m == 1 ? 8 : m == 2 ? 4 : m <= 4 ? 2 : 1;       // wavefronts a token
+    const int sub = wave % per_row, first = wave / per_row, step = FEW_WAVES / per_row;
+    for (int r = first; r < m; r += step) {
+        unsigned top = 0;
+        for (int at = (sub * 64 + lane) * 8; at < p.k; at += per_row * 512) {
+            float v[8];
+            load_run<T, 8>((const T*)f.x + r * f.x_pitch + at, p.k - at, f.x_wide, v);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[i]));
+        }
+#pragma unroll
+        for (int d = 1; d < 64; d *= 2) top = max(top, (unsigned)__shfl_xor((int)top, d));
+        if (lane == 0) tops[r][sub] = top;
+    }
+    __syncthreads();
+    const int end = FEW_WAVES * f.per_wave;
+    for (int r = first; r < m; r += step) {
+        unsigned top = 0;
+        for (int i = 0; i < per_row; ++i) top = max(top, tops[r][i]);
+        float s;
+        const float mult = row_multiplier(top, &s);
+        if (lane == 0 && sub == 0) scales[r] = s;
+        for (int at = (sub * 64 + lane) * 8; at < end; at += per_row * 512) {
+            float v[8];
+            load_run<T, 8>((const T*)f.x + r * f.x_pitch + at, p.k - at, f.x_wide, v);
+            *(uint2*)(codes + r * f.lds_pitch + at) = make_uint2(pack4(code_of(v[0], mult), code_of(v[1], mult), code_of(v[2], mult), code_of(v[3], mult)),
+                                                                pack4(code_of(v[4], mult), code_of(v[5], mult), code_of(v[6], mult), code_of(v[7], mult)));
+        }
+    }
+}
+
+template <int NT, bool FUSED>
+__global__ __launch_bounds__(FEW_WAVES * 64) void k_int8_few(const FewArgs f)
+{
+    extern __shared__ __align__(16) char lds[];      // FUSED: the codes; then, and otherwise, the wavefronts' sums [8][NT * 256]
+    __shared__ unsigned tops[FUSED ? NT * 16 : 1][FEW_WAVES];
+    __shared__ float scales[NT * 16];
+    const Product& p = f.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int64_t rows = p.n - n0 < 16 ? p.n - n0 : 16;
+    const auto ra = operand(p.b + n0 * p.b_pitch, (rows - 1) * p.b_pitch + (p.k + 15) / 16 * 16);
+    const unsigned kq = (unsigned)((p.k + 63) / 64 * 64);
+    const unsigned from = (unsigned)wave * f.per_wave, to = from + f.per_wave < kq ? from + f.per_wave : kq;
+    const unsigned va = (lane & 15) * (unsigned)p.b_pitch + (lane >> 4) * 16;
+    i32x4 a[2][FEW_AHEAD];
+    auto ask = [&](unsigned k, i32x4 (&w)[FEW_AHEAD]) {
+#pragma unroll
+        for (int u = 0; u < FEW_AHEAD; ++u) {      // (an offset beyond the buffer: zeros, and nothing is read)
+            const unsigned off = k + u * 64 < to ? va + k + u * 64 : 0xfffffff0u;
+            w[u] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, (int)off, 0, 0));
+        }
+    };
+    ask(from, a[0]);
+    if constexpr (FUSED) {
+        if (f.x_bf16) few_quantize<bf16>(f, lds, tops, scales); else few_quantize<float>(f, lds, tops, scales);
+        __syncthreads();
+    }
+    int token[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) token[t] = min(t * 16 + (lane & 15), (int)p.m - 1);      // (columns beyond the tokens are not used)
+    i32x4 acc[NT] = {};
+    auto use = [&](unsigned k, const i32x4 (&w)[FEW_AHEAD]) {
+#pragma unroll
+        for (int u = 0; u < FEW_AHEAD; ++u) {
+            if (k + u * 64 >= to) break;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const unsigned at = k + u * 64 + (lane >> 4) * 16;
+                const i32x4 b = FUSED ? *(const i32x4*)(lds + token[t] * f.lds_pitch + at) : *(const i32x4*)(p.a + token[t] * p.a_pitch + at);
+                acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u], b, acc[t], 0, 0, 0);
+            }
+        }
+    };
+    for (unsigned k = from; k < to; k += 2 * FEW_AHEAD * 64) {
+        if (k + FEW_AHEAD * 64 < to) ask(k + FEW_AHEAD * 64, a[1]);
+        use(k, a[0]);
+        if (k + FEW_AHEAD * 64 >= to) break;
+        if (k + 2 * FEW_AHEAD * 64 < to) ask(k + 2 * FEW_AHEAD * 64, a[0]);
+        use(k + FEW_AHEAD * 64, a[1]);
+    }
+    if (FUSED) __syncthreads();      // the codes are read
+    int* part = (int*)lds;
+#pragma unroll
+    for (int t = 0; t < NT; ++t) *(i32x4*)(part + (wave * NT + t) * 256 + (lane & 15) * 16 + (lane >> 4) * 4) = acc[t];
+    __syncthreads();
+    for (int i = threadIdx.x; i < NT * 256; i += FEW_WAVES * 64) {
+        const int64_t m = i >> 4, n = n0 + (i & 15);
+        if (m >= p.m || n >= p.n) continue;
+        int sum = 0;
+#pragma unroll
+        for (int w = 0; w < FEW_WAVES; ++w) sum += part[w * NT * 256 + i];
+        const float v[1] = {finish((float)sum, FUSED ? scales[m] : p.a_scale[m], column_of(p, n), p.relu)};
+        store_out<1>(p, m, n, false, v);
+    }
+}
+
+constexpr int FEW_TOKENS = 64;
+constexpr int64_t FEW_LDS = 80 * 1024;       // two blocks a compute unit
+bool few_tokens(int64_t m) { return m <= FEW_TOKENS; }
+static int64_t few_per_wave(int64_t k) { return round_up(ceil_div(k, FEW_WAVES), 64); }
+static int64_t few_lds(int64_t m, int64_t k) { return m * (FEW_WAVES * few_per_wave(k) + 16); }
+// The tokens are quantised by every block: those of one matrix-core tile, as far as their codes fit.
+bool few_fused(int64_t m, int64_t k) { return m <= 16 && few_lds(m, k) <= FEW_LDS; }
+
+template <int NT, bool FUSED> static void few_launch(Ctx& c, const FewArgs& f)
+{
+    size_t lds = (size_t)FEW_WAVES * NT * 1024;
+    if (FUSED) lds = std::max(lds, (size_t)few_lds(f.p.m, f.p.k));
+    ensure_dynamic_lds((const void*)k_int8_few<NT, FUSED>, FUSED ? FEW_LDS : lds);
+    ST_LAUNCH(c, "int8_few", (k_int8_few<NT, FUSED>), dim3((unsigned)ceil_div(f.p.n, 16)), dim3(FEW_WAVES * 64), lds, f);
+}
+void product_few(Ctx& c, const Product& p, const QuantSource* x)
+{
+    FewArgs f{p, nullptr, 0, 0, 0, (int)few_per_wave(p.k), (int)(FEW_WAVES * few_per_wave(p.k) + 16)};
+    if (x) {
+        f.x = x->x; f.x_bf16 = x->bf16; f.x_pitch = x->pitch; f.x_wide = wide_ok(x->x, x->pitch, x->bf16, 8);
+        few_launch<1, true>(c, f);
+    } else if (p.m <= 16) few_launch<1, false>(c, f);
+    else if (p.m <= 32) few_launch<2, false>(c, f);
+    else few_launch<4, false>(c, f);
 }
 
 // --------------------------------------------------------------------------------------- choice of tile and split

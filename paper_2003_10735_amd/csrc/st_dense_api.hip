@@ -146,9 +146,12 @@ int st_int8_linear(const st_matrix* x, const int8_t* wq, int64_t w_pitch, const 
     if (!workspace || !is_aligned(workspace, 256)) return ST_ERR_WORKSPACE;
     const LinearSpace s = linear_space((char*)workspace, m, n, k);
     Ctx c{(hipStream_t)stream, ST_OK};
-    const QuantTask task{source(*x, along, false), s.x, s.parts, nullptr, nullptr};
-    quantize(c, &task, 1);
+    const QuantSource tokens = source(*x, along, false);
     const Product p{s.x.q, s.x.pitch, s.x.scale, wq, w_pitch, w_scale, m, n, k, y, y_dtype == ST_BF16, y_pitch, bias, relu, s.slabs};
+    if (along && few_fused(m, k)) { product_few(c, p, &tokens); return c.status; }
+    const QuantTask task{tokens, s.x, s.parts, nullptr, nullptr};
+    quantize(c, &task, 1);
+    if (few_tokens(m)) product_few(c, p, nullptr); else
     products(c, &p, 1);
     return c.status;
 }

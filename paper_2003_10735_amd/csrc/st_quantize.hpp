@@ -1,0 +1,56 @@
+// Codes and scales of rows, for the kernels that quantise (k_quantize.hip says what is computed).
+#pragma once
+#include "st_dense.hpp"
+
+namespace st {
+
+constexpr unsigned ABS_BITS = 0x7fffffffu, INF_BITS = 0x7f800000u;
+constexpr unsigned SMALLEST_TOP = 0x04000000u;     // 2^-119: 127 / a is finite from 2^-121 on
+
+__device__ __forceinline__ unsigned abs_bits(float v) { return __float_as_uint(v) & ABS_BITS; }
+
+// multiplier and scale of a row whose largest |value| has the bits `top`
+__device__ __forceinline__ float row_multiplier(unsigned top, float* scale)
+{
+    if (top < SMALLEST_TOP) { *scale = 0.f; return 0.f; }
+    if (top >= INF_BITS) { *scale = __uint_as_float(0x7fc00000u); return 0.f; }
+    const float a = __uint_as_float(top);
+    *scale = a * (1.f / 127.f);
+    return 127.f * (1.f / a);
+}
+// the code in the low byte; a multiplier of 0 stands for a row of zeros or of no numbers, whose codes are 0 whatever v is
+__device__ __forceinline__ unsigned code_of(float v, float r) { return r == 0.f ? 0u : __float_as_uint(v * r + 12582912.f); }
+__device__ __forceinline__ unsigned pack4(unsigned a, unsigned b, unsigned c, unsigned d)
+{
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400), __builtin_amdgcn_perm(b, a, 0x0c0c0400), 0x05040100);
+}
+
+// COUNT consecutive values from p, of which `n` exist; the others are 0.  wide: p is aligned for loads of all of them.
+template <class T, int COUNT> __device__ __forceinline__ void load_run(const T* p, int64_t n, bool wide, float (&v)[COUNT])
+{
+    if (wide && n >= COUNT) {
+        if constexpr (sizeof(T) == 2) {
+            typedef unsigned W __attribute__((ext_vector_type(COUNT / 2)));
+            const W w = *(const W*)p;
+#pragma unroll
+            for (int i = 0; i < COUNT / 2; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u); }
+        } else {
+#pragma unroll
+            for (int i = 0; i < COUNT; i += 4) {
+                const float4 w = *(const float4*)(p + i);
+                v[i] = w.x; v[i + 1] = w.y; v[i + 2] = w.z; v[i + 3] = w.w;
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
+}
+
+inline bool wide_ok(const void* p, int64_t pitch, int is_bf16, int run)     // runs of `run` values can be loaded at once
+{
+    const int64_t e = is_bf16 ? 2 : 4, bytes = run * e < 16 ? run * e : 16;
+    return (uintptr_t)p % bytes == 0 && pitch * e % bytes == 0;
+}
+
+}  // namespace st
