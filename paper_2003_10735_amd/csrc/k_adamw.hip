@@ -1,10 +1,13 @@
 // AdamW over a list of tensors.  A launch takes up to ST_ADAMW_PER_LAUNCH tensors, whose pointers travel with its arguments; every block
 // takes one tile of one of them.
-#include "st_dense.hpp"
+#include "st_quantize.hpp"
+
+#include <algorithm>
 
 namespace st {
 
-constexpr int TILE = 2048;                 // values a block of 256 threads
+constexpr int TILE = 2048;                 // values a block of 256 threads steps: two runs of 256 a wavefront
+constexpr int NORM_TILE = 8192, NORM_BLOCKS = 2048, NORM_PER_LAUNCH = 160;
 constexpr float TINY = 0x1p-100f;          // a run of an 8-bit state whose largest value is less holds zeros
 
 struct TensorRef { void* p; const void* g; void* m; void* v; float* ms; float* vs; void* copy; long long n; };
@@ -14,35 +17,24 @@ struct TensorList {
     unsigned first[ST_ADAMW_PER_LAUNCH + 1];   // first tile of each
     int n;
 };
-static_assert(sizeof(TensorList) + sizeof(AdamwConstants) + 64 <= 4096, "kernel arguments");
+struct GradList {
+    const void* g[NORM_PER_LAUNCH]; long long n[NORM_PER_LAUNCH];
+    unsigned first[NORM_PER_LAUNCH + 1];
+    int count;
+};
+static_assert(sizeof(TensorList) + sizeof(AdamwConstants) + 64 <= 4096 && sizeof(GradList) + 64 <= 4096, "kernel arguments");
 
-__device__ __forceinline__ int tensor_of(const TensorList& l, unsigned tile)
+// the last tensor that begins at or before the tile (tensors without values own no tile and are not in the list)
+__device__ __forceinline__ int tensor_of(const unsigned* first, int n, unsigned tile)
 {
-    int lo = 0, hi = l.n - 1;              // the last tensor that begins at or before the tile (tensors without values own no tile)
+    int lo = 0, hi = n - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
-        if (l.first[mid] <= tile) lo = mid; else hi = mid - 1;
+        if (first[mid] <= tile) lo = mid; else hi = mid - 1;
     }
     return lo;
 }
 
-// Four consecutive values from p + i, of which `n` exist (the others are 0).
-template <class T> __device__ __forceinline__ void load4(const T* p, int n, bool wide, float (&v)[4])
-{
-    if (wide && n >= 4) {
-        if (sizeof(T) == 2) {
-            const uint2 u = *(const uint2*)p;
-            v[0] = __uint_as_float(u.x << 16); v[1] = __uint_as_float(u.x & 0xffff0000u);
-            v[2] = __uint_as_float(u.y << 16); v[3] = __uint_as_float(u.y & 0xffff0000u);
-        } else {
-            const float4 u = *(const float4*)p;
-            v[0] = u.x; v[1] = u.y; v[2] = u.z; v[3] = u.w;
-        }
-        return;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
-}
 template <class T> __device__ __forceinline__ void store4(T* p, int n, bool wide, const float (&v)[4])
 {
     if (wide && n >= 4) {
@@ -54,65 +46,72 @@ template <class T> __device__ __forceinline__ void store4(T* p, int n, bool wide
     for (int i = 0; i < 4; ++i) if (i < n) p[i] = from_f32<T>(v[i]);
 }
 __device__ __forceinline__ bool aligned(const void* p, unsigned bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+__device__ __forceinline__ double block_sum(double s, double* sums)      // of 256 threads, in one order; to every thread
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+    __syncthreads();
+    return (sums[0] + sums[1]) + (sums[2] + sums[3]);
+}
 
 // ------------------------------------------------------------------------------------------------------ norm
-// Squares and their sums in float64: no gradient that is finite makes the norm infinite, and the order of the sums does not show.
+// Squares and their sums in float64: no gradient that is finite makes the norm infinite, and the order of the sums does not show.  A
+// launch has NORM_BLOCKS blocks at most, so that few parts are left to be added.
 template <class G>
-__global__ __launch_bounds__(256) void k_grad_square_sums(const TensorList l, float grad_scale, double* __restrict__ parts)
+__global__ __launch_bounds__(256) void k_grad_square_sums(const GradList l, float grad_scale, unsigned tiles, double* __restrict__ parts)
 {
     __shared__ double sums[4];
-    const int i = tensor_of(l, blockIdx.x);
-    const G* g = (const G*)l.t[i].g;
-    const long long n = l.t[i].n, base = (long long)(blockIdx.x - l.first[i]) * TILE;
-    const bool wide = aligned(g, 4 * sizeof(G));
     double s = 0.0;
+    for (unsigned tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
+        const int i = tensor_of(l.first, l.count, tile);
+        const G* g = (const G*)l.g[i];
+        const long long n = l.n[i], base = (long long)(tile - l.first[i]) * NORM_TILE + threadIdx.x * 8;
+        const bool wide = aligned(g, 16);
+        float v[NORM_TILE / 2048][8];
 #pragma unroll
-    for (int j = 0; j < TILE / 1024; ++j) {
-        const long long at = base + j * 1024 + threadIdx.x * 4;
-        if (at >= n) break;
-        float v[4];
-        load4(g + at, n - at < 4 ? (int)(n - at) : 4, wide, v);
+        for (int j = 0; j < NORM_TILE / 2048; ++j) load_run<G, 8>(g + base + j * 2048, n - base - j * 2048, wide, v[j]);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) { const double d = (double)(v[k] * grad_scale); s += d * d; }
+        for (int j = 0; j < NORM_TILE / 2048; ++j)
+#pragma unroll
+            for (int k = 0; k < 8; ++k) { const double d = (double)(v[j][k] * grad_scale); s = __builtin_fma(d, d, s); }
     }
-#pragma unroll
-    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) parts[blockIdx.x] = (sums[0] + sums[1]) + (sums[2] + sums[3]);
+    s = block_sum(s, sums);
+    if (threadIdx.x == 0) parts[blockIdx.x] = s;
 }
-__global__ __launch_bounds__(1024) void k_norm(const double* __restrict__ parts, long long n, float* __restrict__ norm, float* __restrict__ out)
+__device__ __forceinline__ float norm_of_parts(const double* __restrict__ parts, int n, double* sums)
 {
-    __shared__ double sums[16];
     double s = 0.0;
-    for (long long i = threadIdx.x; i < n; i += 1024) s += parts[i];
-#pragma unroll
-    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        s = 0.0;
-        for (int i = 0; i < 16; ++i) s += sums[i];
-        const float v = (float)sqrt(s);
-        *norm = v;
-        if (out) *out = v;
-    }
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += 256) s += parts[i];
+    return (float)sqrt(block_sum(s, sums));
+}
+__global__ __launch_bounds__(256) void k_norm(const double* __restrict__ parts, int n, float* __restrict__ norm, float* __restrict__ out)
+{
+    __shared__ double sums[4];
+    const float v = norm_of_parts(parts, n, sums);
+    if (threadIdx.x == 0) { *norm = v; if (out) *out = v; }
 }
 
 // ------------------------------------------------------------------------------------------------------ step
+// The norm, as it reaches a step: a value, or (parts > 0) the parts of it, which every block of a small launch adds by itself; the first
+// block then also writes it to `out`.
+struct NormRef { const float* norm; const double* parts; int n_parts; float* out; };
+
 // The factor on the gradients, or 0 where the step is not taken (grad_scale and max_norm are positive).
-__device__ __forceinline__ float clip_factor(const AdamwConstants& k, const float* norm)
+__device__ __forceinline__ float clip_factor(const AdamwConstants& k, float norm)
 {
-    if (!norm) return k.grad_scale;
-    const float v = *norm;
-    if (!(v < __builtin_inff())) return 0.f;
-    return v > k.max_norm ? k.grad_scale * (k.max_norm / v) : k.grad_scale;
+    if (!(norm < __builtin_inff())) return 0.f;
+    return norm > k.max_norm ? k.grad_scale * (k.max_norm / norm) : k.grad_scale;
 }
+// largest of a wavefront's values, in a scalar register: four steps inside rows of 16 lanes, two across
 __device__ __forceinline__ unsigned wave_max(unsigned v)
 {
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) v = max(v, (unsigned)__shfl_xor((int)v, d));
-    return v;
+#define ST_DPP(CTRL, ROWS) v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false))
+    ST_DPP(0x111, 0xf); ST_DPP(0x112, 0xf); ST_DPP(0x114, 0xf); ST_DPP(0x118, 0xf);      // row_shr 1, 2, 4, 8
+    ST_DPP(0x142, 0xa); ST_DPP(0x143, 0xc);                                              // row_bcast 15, 31
+#undef ST_DPP
+    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
 }
 // scale and multiplier of a run whose largest value has the bits `top`; codes^2 reach `codes2`
 __device__ __forceinline__ float run_multiplier(unsigned top, float codes2, float* scale)
@@ -123,85 +122,116 @@ __device__ __forceinline__ float run_multiplier(unsigned top, float codes2, floa
     *scale = a * (1.f / codes2);
     return codes2 * (1.f / a);
 }
-
-// One tile.  A lane takes four neighbouring values of a run of 256, a wavefront a run at a time.  Every operation is a float32 operation
-// of its own (no fused ones), in the order of the header's formulas: codes change by whole steps, so two programs that are to give the
-// same codes have to round alike.
-template <class P, class G, int BITS>
-__global__ __launch_bounds__(256) void k_adamw(const TensorList l, const AdamwConstants k, const float* __restrict__ norm)
+// Square root, rounded to the nearest float32.  The instruction's result s is off by one unit in the last place at most; s (s +- unit) is
+// s^2 beyond the middle between the two candidates, so the sign of its difference from x, which a fused multiply-add has exactly, decides.
+__device__ __forceinline__ float sqrt_rn(float x)
 {
-    const int i = tensor_of(l, blockIdx.x);
-    const TensorRef t = l.t[i];
-    const float decay = l.decay[i], factor = clip_factor(k, norm);
-    if (factor == 0.f) return;
+    if (x < 0x1p-96f && x > 0.f) return sqrtf(x);
+    const float s = __builtin_amdgcn_sqrtf(x);
+    const float lo = __uint_as_float(__float_as_uint(s) - 1), hi = __uint_as_float(__float_as_uint(s) + 1);
+    const float r_lo = __builtin_fmaf(-lo, s, x), r_hi = __builtin_fmaf(-hi, s, x);
+    const float t = r_lo <= 0.f ? lo : s;
+    return r_hi > 0.f ? hi : t;
+}
+// rint of the square root rounded to float32, for 0 <= y < 2^17: the instruction's own result settles it unless it lies next to a middle
+__device__ __forceinline__ float code_root(float y)
+{
+    const float s = __builtin_amdgcn_sqrtf(y), q = rintf(s);
+    return fabsf(s - q) > 0.4999f ? rintf(sqrt_rn(y)) : q;
+}
+
+// One tile.  A lane takes four neighbouring values of a run of 256, a wavefront two runs, all of whose loads are under way before the
+// first is used.  What the codes depend on is float32 operations of their own (no fused ones), in the order of the header's formulas:
+// codes change by whole steps, so two programs that are to give the same codes have to round alike.  The parameters' quotient is a
+// product with a reciprocal of one unit's accuracy.
+template <class P, class G, int BITS>
+__global__ __launch_bounds__(256) void k_adamw(const TensorList l, const AdamwConstants k, const NormRef nr)
+{
+    constexpr int RUNS = TILE / 1024;
+    __shared__ double sums[4];
+    const int i = tensor_of(l.first, l.n, blockIdx.x);
+    const TensorRef& t = l.t[i];
     P* pp = (P*)t.p;
     const G* gg = (const G*)t.g;
     const bool wp = aligned(pp, 4 * sizeof(P)), wg = aligned(gg, 4 * sizeof(G)), wc = aligned(t.copy, 8);
     const bool wm = aligned(t.m, BITS == 8 ? 4 : 16) && aligned(t.v, BITS == 8 ? 4 : 16);
-    const long long base = (long long)(blockIdx.x - l.first[i]) * TILE;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    for (int j = 0; j < TILE / 1024; ++j) {
-        const long long run = base + (j * 4 + wave) * 256, at = run + lane * 4;
-        if (run >= t.n) break;
-        const int n = t.n - at >= 4 ? 4 : t.n - at > 0 ? (int)(t.n - at) : 0;
-        float p[4], g[4], m[4], v[4], u[4];
-        load4(pp + at, n, wp, p);
-        load4(gg + at, n, wg, g);
-        if constexpr (BITS == 32) {
-            load4((const float*)t.m + at, n, wm, m);
-            load4((const float*)t.v + at, n, wm, v);
-        } else {
-            const float ms = t.ms[run / 256], vs = t.vs[run / 256];
-            unsigned cm = 0, cv = 0;
-            if (wm && n == 4) { cm = *(const unsigned*)((const char*)t.m + at); cv = *(const unsigned*)((const char*)t.v + at); }
-            else for (int e = 0; e < n; ++e) {
-                cm |= (unsigned)((const uint8_t*)t.m)[at + e] << (8 * e);
-                cv |= (unsigned)((const uint8_t*)t.v)[at + e] << (8 * e);
-            }
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const long long base = (long long)(blockIdx.x - l.first[i]) * TILE + wave * (RUNS * 256);
+    float p[RUNS][4], g[RUNS][4], m[RUNS][4], v[RUNS][4], ms[RUNS], vs[RUNS];
+    unsigned cm[RUNS], cv[RUNS];
+    int n[RUNS];
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const float qm = (float)(int8_t)(cm >> (8 * e)), qv = (float)(uint8_t)(cv >> (8 * e));
-                m[e] = qm * fabsf(qm) * ms;
-                const float root = qv * qv * vs;
-                v[e] = root * root;
+    for (int j = 0; j < RUNS; ++j) {
+        const long long run = base + j * 256, at = run + lane * 4;
+        n[j] = t.n - at >= 4 ? 4 : t.n - at > 0 ? (int)(t.n - at) : 0;
+        load_run<P, 4>(pp + at, n[j], wp, p[j]);
+        load_run<G, 4>(gg + at, n[j], wg, g[j]);
+        if constexpr (BITS == 32) {
+            load_run<float, 4>((const float*)t.m + at, n[j], wm, m[j]);
+            load_run<float, 4>((const float*)t.v + at, n[j], wm, v[j]);
+        } else {
+            cm[j] = cv[j] = 0; ms[j] = vs[j] = 0.f;
+            if (run < t.n) { ms[j] = t.ms[run / 256]; vs[j] = t.vs[run / 256]; }
+            if (wm && n[j] == 4) { cm[j] = *(const unsigned*)((const char*)t.m + at); cv[j] = *(const unsigned*)((const char*)t.v + at); }
+            else for (int e = 0; e < n[j]; ++e) {
+                cm[j] |= (unsigned)((const uint8_t*)t.m)[at + e] << (8 * e);
+                cv[j] |= (unsigned)((const uint8_t*)t.v)[at + e] << (8 * e);
             }
         }
+    }
+    float factor = k.grad_scale;
+    if (nr.norm || nr.parts) {
+        const float norm = nr.parts ? norm_of_parts(nr.parts, nr.n_parts, sums) : *nr.norm;
+        if (nr.parts && nr.out && blockIdx.x == 0 && threadIdx.x == 0) *nr.out = norm;
+        factor = k.max_norm > 0.f ? clip_factor(k, norm) : k.grad_scale;
+        if (factor == 0.f) return;
+    }
+    const float decay = l.decay[i];
+#pragma unroll
+    for (int j = 0; j < RUNS; ++j) {
+        const long long run = base + j * 256, at = run + lane * 4;
+        if (run >= t.n) break;
+        float u[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float ge = g[e] * factor;
-            m[e] = m[e] * k.beta1 + ge * k.one_minus_beta1;
-            v[e] = v[e] * k.beta2 + ge * ge * k.one_minus_beta2;
-            u[e] = sqrtf(v[e]);
-            p[e] = p[e] * decay - k.step_scale * (m[e] / (u[e] * k.inv_sqrt_bc2 + k.eps));
+            if constexpr (BITS == 8) {
+                const float qm = (float)(int8_t)(cm[j] >> (8 * e)), qv = (float)(uint8_t)(cv[j] >> (8 * e));
+                m[j][e] = qm * fabsf(qm) * ms[j];
+                const float root = qv * qv * vs[j];
+                v[j][e] = root * root;
+            }
+            const float ge = g[j][e] * factor;
+            m[j][e] = m[j][e] * k.beta1 + ge * k.one_minus_beta1;
+            v[j][e] = v[j][e] * k.beta2 + ge * ge * k.one_minus_beta2;
+            u[e] = BITS == 8 ? sqrt_rn(v[j][e]) : sqrtf(v[j][e]);
+            p[j][e] = p[j][e] * decay - k.step_scale * (m[j][e] * __builtin_amdgcn_rcpf(u[e] * k.inv_sqrt_bc2 + k.eps));
         }
-        store4(pp + at, n, wp, p);
-        if (t.copy) store4((bf16*)t.copy + at, n, wc, p);
+        store4(pp + at, n[j], wp, p[j]);
+        if (t.copy) store4((bf16*)t.copy + at, n[j], wc, p[j]);
         if constexpr (BITS == 32) {
-            store4((float*)t.m + at, n, wm, m);
-            store4((float*)t.v + at, n, wm, v);
+            store4((float*)t.m + at, n[j], wm, m[j]);
+            store4((float*)t.v + at, n[j], wm, v[j]);
         } else {
             unsigned tm = 0, tv = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e)
-                if (e < n) { tm = max(tm, __float_as_uint(m[e]) & 0x7fffffffu); tv = max(tv, __float_as_uint(u[e]) & 0x7fffffffu); }
-            tm = wave_max(tm); tv = wave_max(tv);
-            float ms, vs;
-            const float rm = run_multiplier(tm, 16129.f, &ms), rv = run_multiplier(tv, 65025.f, &vs);
-            if (lane == 0) { t.ms[run / 256] = ms; t.vs[run / 256] = vs; }
-            unsigned cm = 0, cv = 0;
+                if (e < n[j]) { tm = max(tm, abs_bits(m[j][e])); tv = max(tv, abs_bits(u[e])); }
+            float new_ms, new_vs;
+            const float rm = run_multiplier(wave_max(tm), 16129.f, &new_ms), rv = run_multiplier(wave_max(tv), 65025.f, &new_vs);
+            if (lane == 0) { t.ms[run / 256] = new_ms; t.vs[run / 256] = new_vs; }
+            unsigned qm = 0, qv = 0;
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                int qm = rm == 0.f ? 0 : (int)rintf(sqrtf(fabsf(m[e]) * rm));
-                if (m[e] < 0.f) qm = -qm;
-                int qv = rv == 0.f ? 0 : (int)rintf(sqrtf(u[e] * rv));
-                if (rv != 0.f && qv == 0 && u[e] > 0.f) qv = 1;
-                cm |= (unsigned)(uint8_t)qm << (8 * e);
-                cv |= (unsigned)(uint8_t)qv << (8 * e);
+                const int a = rm == 0.f ? 0 : (int)code_root(fabsf(m[j][e]) * rm);
+                int b = rv == 0.f ? 0 : (int)code_root(u[e] * rv);
+                if (rv != 0.f && b == 0 && u[e] > 0.f) b = 1;
+                qm |= (unsigned)(uint8_t)(m[j][e] < 0.f ? -a : a) << (8 * e);
+                qv |= (unsigned)(uint8_t)b << (8 * e);
             }
-            if (wm && n == 4) { *(unsigned*)((char*)t.m + at) = cm; *(unsigned*)((char*)t.v + at) = cv; }
-            else for (int e = 0; e < n; ++e) {
-                ((uint8_t*)t.m)[at + e] = (uint8_t)(cm >> (8 * e));
-                ((uint8_t*)t.v)[at + e] = (uint8_t)(cv >> (8 * e));
+            if (wm && n[j] == 4) { *(unsigned*)((char*)t.m + at) = qm; *(unsigned*)((char*)t.v + at) = qv; }
+            else for (int e = 0; e < n[j]; ++e) {
+                ((uint8_t*)t.m)[at + e] = (uint8_t)(qm >> (8 * e));
+                ((uint8_t*)t.v)[at + e] = (uint8_t)(qv >> (8 * e));
             }
         }
     }
@@ -243,13 +273,32 @@ __global__ __launch_bounds__(256) void k_adamw_state(const int8_t* __restrict__ 
 }
 
 // ------------------------------------------------------------------------------------------------------ host
-int64_t adamw_tiles(const st_adamw_tensor* t, int n)
+// The gradients in pieces that a launch of the norm can take: f(list, tiles).
+template <class F> static void for_grads(const st_adamw_tensor* t, int n, F f)
 {
-    int64_t tiles = 0;
-    for (int i = 0; i < n; ++i) tiles += ceil_div(t[i].n, TILE);
-    return tiles;
+    for (int at = 0; at < n;) {
+        GradList l;
+        l.count = 0;
+        l.first[0] = 0;
+        int64_t tiles = 0;
+        for (; at < n && l.count < NORM_PER_LAUNCH; ++at) {
+            if (t[at].n == 0) continue;
+            const int64_t more = ceil_div(t[at].n, NORM_TILE);
+            if (l.count && tiles + more > 0x7fffffff) break;
+            l.g[l.count] = t[at].grad;
+            l.n[l.count] = t[at].n;
+            tiles += more;
+            l.first[++l.count] = (unsigned)tiles;
+        }
+        if (l.count) f(l, (unsigned)tiles);
+    }
 }
-
+int64_t adamw_norm_parts(const st_adamw_tensor* t, int n)
+{
+    int64_t parts = 0;
+    for_grads(t, n, [&](const GradList&, unsigned tiles) { parts += std::min<unsigned>(tiles, NORM_BLOCKS); });
+    return parts;
+}
 // Calls f(list, tiles) for the list in pieces that a launch can take.
 template <class F> static void for_pieces(const st_adamw_tensor* t, int n, double lr, F f)
 {
@@ -271,32 +320,42 @@ template <class F> static void for_pieces(const st_adamw_tensor* t, int n, doubl
     }
 }
 
-void adamw_norm(Ctx& c, const st_adamw_tensor* t, int n, int grad_bf16, float grad_scale, double* parts, float* norm, float* out)
-{
-    int64_t done = 0;
-    for_pieces(t, n, 0.0, [&](const TensorList& l, unsigned tiles) {
-        if (grad_bf16) ST_LAUNCH(c, "grad_square_sums", k_grad_square_sums<bf16>, dim3(tiles), dim3(256), 0, l, grad_scale, parts + done);
-        else           ST_LAUNCH(c, "grad_square_sums", k_grad_square_sums<float>, dim3(tiles), dim3(256), 0, l, grad_scale, parts + done);
-        done += tiles;
-    });
-    ST_LAUNCH(c, "grad_norm", k_norm, dim3(1), dim3(1024), 0, parts, (long long)done, norm, out);
-}
-
 template <class P, class G, int BITS>
-static void step(Ctx& c, const st_adamw_tensor* t, int n, double lr, const AdamwConstants& k, const float* norm)
+static void step(Ctx& c, const st_adamw_tensor* t, int n, double lr, const AdamwConstants& k, NormRef nr)
 {
     for_pieces(t, n, lr, [&](const TensorList& l, unsigned tiles) {
-        ST_LAUNCH(c, "adamw", (k_adamw<P, G, BITS>), dim3(tiles), dim3(256), 0, l, k, norm);
+        ST_LAUNCH(c, "adamw", (k_adamw<P, G, BITS>), dim3(tiles), dim3(256), 0, l, k, nr);
+        nr.out = nullptr;
     });
 }
 
-// norm: clip by it; null: do not
-void adamw_step(Ctx& c, const st_adamw_tensor* t, int n, const st_adamw_opts& o, const AdamwConstants& k, const float* norm)
+// workspace: the norm and, 256 bytes on, its parts; null: no norm
+void adamw_step(Ctx& c, const st_adamw_tensor* t, int n, const st_adamw_opts& o, const AdamwConstants& k, char* workspace)
 {
+    NormRef nr{nullptr, nullptr, 0, nullptr};
+    int64_t tiles = 0;
+    for (int i = 0; i < n; ++i) tiles += ceil_div(t[i].n, TILE);
+    if (workspace) {
+        double* parts = (double*)(workspace + 256);
+        int done = 0;
+        for_grads(t, n, [&](const GradList& l, unsigned norm_tiles) {
+            const unsigned blocks = std::min<unsigned>(norm_tiles, NORM_BLOCKS);
+            if (o.grad_dtype == ST_BF16) ST_LAUNCH(c, "grad_square_sums", k_grad_square_sums<bf16>, dim3(blocks), dim3(256), 0, l, k.grad_scale, norm_tiles, parts + done);
+            else ST_LAUNCH(c, "grad_square_sums", k_grad_square_sums<float>, dim3(blocks), dim3(256), 0, l, k.grad_scale, norm_tiles, parts + done);
+            done += (int)blocks;
+        });
+        // Up to two rounds of blocks the step adds the parts itself: they are few then, and a launch of its own takes longer.
+        if (tiles > 0 && tiles <= 4096 && done <= 2048) nr = NormRef{nullptr, parts, done, o.grad_norm};
+        else {
+            ST_LAUNCH(c, "grad_norm", k_norm, dim3(1), dim3(256), 0, parts, done, (float*)workspace, o.grad_norm);
+            nr.norm = (const float*)workspace;
+        }
+    }
+    if (tiles == 0) return;
 #define ST_STEP(P, G)                                                  \
     do {                                                               \
-        if (o.state_bits == 8) step<P, G, 8>(c, t, n, o.lr, k, norm);  \
-        else step<P, G, 32>(c, t, n, o.lr, k, norm);                   \
+        if (o.state_bits == 8) step<P, G, 8>(c, t, n, o.lr, k, nr);    \
+        else step<P, G, 32>(c, t, n, o.lr, k, nr);                     \
     } while (0)
     if (o.param_dtype == ST_F32) { if (o.grad_dtype == ST_F32) ST_STEP(float, float); else ST_STEP(float, bf16); }
     else                         { if (o.grad_dtype == ST_F32) ST_STEP(bf16, float); else ST_STEP(bf16, bf16); }

@@ -82,8 +82,8 @@ template <int COUNT> __device__ __forceinline__ void store_out(const Product& p,
         asm volatile("" ::: "memory");  \
     } while (0)
 
-// BM tokens x BN channels a block, WM x WN a wavefront.
-template <int BM, int BN, int WM, int WN>
+// BM tokens x BN channels a block, WM x WN a wavefront, DEPTH stages under way.
+template <int BM, int BN, int WM, int WN, int DEPTH>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(const GemmPair pair)
 {
     constexpr int WAVES = (BM / WM) * (BN / WN), AR = BN, BR = BM;     // A operand: channels, B operand: tokens
@@ -144,17 +144,19 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         }
     };
-    // Two stages are under way.  A stage's last step has its operands in registers when the barrier is passed, so what follows the barrier
-    // is: the loads of the stage after next into the buffer that is done with, the next stage's first operands, the last step's products.
+    // DEPTH stages are under way.  A stage's last step has its operands in registers when the barrier is passed, so what follows the
+    // barrier is: the loads of the stage DEPTH later into the buffer that is done with, the next stage's first operands, the last step's
+    // products.
     constexpr int LOADS = (AR + BR) / 8 / WAVES;      // of a wavefront and stage
+    static_assert((DEPTH - 1) * LOADS < 64, "the counter of loads under way");
     if (first < last) {
-        stage(first, 0);
-        if (first + 1 < last) { stage(first + 1, 1); ST_WAIT_VM(LOADS); } else ST_WAIT_VM(0);
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) if (first + d < last) stage(first + d, d);
+        if (first + DEPTH <= last) ST_WAIT_VM((DEPTH - 1) * LOADS); else ST_WAIT_VM(0);
         ST_BARRIER();
         fetch(0, 0, 0);
     }
-    for (int s = first; s < last; ++s) {
-        const int buf = (s - first) & 1;
+    for (int s = first, buf = 0; s < last; ++s) {
 #pragma unroll
         for (int ks = 0; ks < STEPS - 1; ++ks) {
             __builtin_amdgcn_sched_barrier(0);
@@ -163,17 +165,20 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
             interleave();
         }
         __builtin_amdgcn_sched_barrier(0);
-        __builtin_amdgcn_s_waitcnt(0x0070);    // vmcnt(0), lgkmcnt(0): the next stage is there, this one is read
+        // the next stage is there (behind it DEPTH - 2 may still be on their way), this one is read
+        if (DEPTH > 2 && s + DEPTH <= last) ST_WAIT_VM((DEPTH - 2) * LOADS); else ST_WAIT_VM(0);
+        __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0)
         ST_BARRIER();
-        if (s + 2 < last) stage(s + 2, buf);
-        if (s + 1 < last) fetch(buf ^ 1, 0, 0);
+        if (s + DEPTH < last) stage(s + DEPTH, buf);
+        buf = buf + 1 == DEPTH ? 0 : buf + 1;
+        if (s + 1 < last) fetch(buf, 0, 0);
         multiply((STEPS - 1) & 1);
     }
 
     // Out through LDS, 32 tokens of a wavefront at a time: sums go in four neighbouring channels at a time and come out as runs along a row.
     __syncthreads();
     constexpr int PITCH = WN + 4, RUNS = WN / 8, ROWS = 64 / RUNS;
-    static_assert(WAVES * 32 * PITCH * 4 <= 2 * BUF, "room for the sums");
+    static_assert(WAVES * 32 * PITCH * 4 <= DEPTH * BUF, "room for the sums");
     int* mine = (int*)lds + wave * 32 * PITCH;
     const int run = lane % RUNS, row = lane / RUNS;
     const int64_t n = n0 + wn + run * 8;
@@ -399,12 +404,12 @@ Form form_of(const Extent* e, int count)
     return f;
 }
 
-template <int BM, int BN, int WM, int WN>
+template <int BM, int BN, int WM, int WN, int DEPTH>
 static void launch(Ctx& c, const GemmPair& g)
 {
-    constexpr size_t lds = 2 * (BM + BN) * STAGE;
-    ensure_dynamic_lds((const void*)k_int8_product<BM, BN, WM, WN>, lds);
-    ST_LAUNCH(c, "int8_product", (k_int8_product<BM, BN, WM, WN>), dim3(g.g[0].blocks + g.g[1].blocks), dim3((BM / WM) * (BN / WN) * 64), lds, g);
+    constexpr size_t lds = (size_t)DEPTH * (BM + BN) * STAGE;
+    ensure_dynamic_lds((const void*)k_int8_product<BM, BN, WM, WN, DEPTH>, lds);
+    ST_LAUNCH(c, "int8_product", (k_int8_product<BM, BN, WM, WN, DEPTH>), dim3(g.g[0].blocks + g.g[1].blocks), dim3((BM / WM) * (BN / WN) * 64), lds, g);
 }
 
 void products(Ctx& c, const Product* p, int count)
@@ -421,9 +426,9 @@ void products(Ctx& c, const Product* p, int count)
         g.g[i] = GemmArgs{p[i], fast_div((int)(tm * tn)), fast_div((int)tn), f.splits[i], (int)ceil_div(p[i].k, STAGE), (unsigned)(tm * tn * f.splits[i])};
         if (f.splits[i] > 1) { cells[n_joined] = p[i].m * p[i].n; joined.g[n_joined++] = g.g[i]; }
     }
-    if (f.tile == 256) launch<256, 256, 128, 64>(c, g);
-    else if (f.tile == 128) launch<128, 128, 64, 64>(c, g);
-    else launch<64, 64, 32, 32>(c, g);
+    if (f.tile == 256) launch<256, 256, 128, 64, 2>(c, g);
+    else if (f.tile == 128) launch<128, 128, 64, 64, 2>(c, g);
+    else launch<64, 64, 32, 32, 4>(c, g);
     if (n_joined) {
         const int64_t all = cells[0] + cells[1], blocks = ceil_div(all, 256);
         ST_LAUNCH(c, "int8_join", k_int8_join, dim3((unsigned)(blocks > 8192 ? 8192 : blocks)), dim3(256), 0, joined, cells[0], all);

@@ -58,9 +58,8 @@ void fill_zero(Ctx& c, float* p, int64_t rows, int64_t cols, int64_t pitch);
 
 // ------------------------------------------------------------------ optimiser
 struct AdamwConstants { float beta1, beta2, one_minus_beta1, one_minus_beta2, eps, step_scale, inv_sqrt_bc2, grad_scale, max_norm; };
-int64_t adamw_tiles(const st_adamw_tensor* t, int n);
-void adamw_norm(Ctx& c, const st_adamw_tensor* t, int n, int grad_bf16, float grad_scale, double* parts, float* norm, float* out);
-void adamw_step(Ctx& c, const st_adamw_tensor* t, int n, const st_adamw_opts& o, const AdamwConstants& k, const float* norm);
+int64_t adamw_norm_parts(const st_adamw_tensor* t, int n);
+void adamw_step(Ctx& c, const st_adamw_tensor* t, int n, const st_adamw_opts& o, const AdamwConstants& k, char* workspace);
 void adamw_state(Ctx& c, const int8_t* m, const float* m_scale, const uint8_t* v, const float* v_scale, int64_t n, float* m_out, float* v_out);
 
 }  // namespace st

@@ -224,7 +224,7 @@ static int check_tensors(const st_adamw_tensor* t, int32_t n)
 size_t st_adamw_workspace(const st_adamw_tensor* tensors, int32_t n_tensors)
 {
     if (check_tensors(tensors, n_tensors) != ST_OK) return 0;
-    return 256 + (size_t)adamw_tiles(tensors, n_tensors) * sizeof(double);
+    return 256 + (size_t)adamw_norm_parts(tensors, n_tensors) * sizeof(double);
 }
 
 int st_adamw_step(const st_adamw_tensor* tensors, int32_t n_tensors, const st_adamw_opts* opts, void* workspace, void* stream)
@@ -238,12 +238,10 @@ int st_adamw_step(const st_adamw_tensor* tensors, int32_t n_tensors, const st_ad
         || (o.max_norm > 0 && !((float)o.max_norm > 0)) || !is_aligned(o.grad_norm, 4))
         return ST_ERR_ARG;
     const size_t pe = elem(o.param_dtype), ge = elem(o.grad_dtype), se = o.state_bits == 8 ? 1 : 4;
-    bool any = false;
     for (int i = 0; i < n_tensors; ++i) {
         const st_adamw_tensor& t = tensors[i];
         if (!isfinite(t.weight_decay)) return ST_ERR_ARG;
         if (t.n == 0) continue;
-        any = true;
         if (!t.param || !t.grad || !t.m || !t.v || (o.state_bits == 8 && (!t.m_scale || !t.v_scale))) return ST_ERR_NULL;
         if (!is_aligned(t.param, pe) || !is_aligned(t.grad, ge) || !is_aligned(t.m, se) || !is_aligned(t.v, se) || !is_aligned(t.copy, 2)
             || (o.state_bits == 8 && (!is_aligned(t.m_scale, 4) || !is_aligned(t.v_scale, 4))))
@@ -255,9 +253,7 @@ int st_adamw_step(const st_adamw_tensor* tensors, int32_t n_tensors, const st_ad
     const double bc1 = 1.0 - pow(o.beta1, (double)o.t), bc2 = 1.0 - pow(o.beta2, (double)o.t);
     const AdamwConstants k{(float)o.beta1, (float)o.beta2, (float)(1.0 - o.beta1), (float)(1.0 - o.beta2), (float)o.eps,
                            (float)(o.lr / bc1), (float)(1.0 / sqrt(bc2)), (float)o.grad_scale, (float)o.max_norm};
-    float* norm = (float*)workspace;
-    if (clip || o.grad_norm) adamw_norm(c, tensors, n_tensors, o.grad_dtype == ST_BF16, k.grad_scale, (double*)((char*)workspace + 256), norm, o.grad_norm);
-    if (any) adamw_step(c, tensors, n_tensors, o, k, clip ? norm : nullptr);
+    adamw_step(c, tensors, n_tensors, o, k, clip || o.grad_norm ? (char*)workspace : nullptr);
     return c.status;
 }
 
