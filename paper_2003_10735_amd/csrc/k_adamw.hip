@@ -104,15 +104,6 @@ __device__ __forceinline__ float clip_factor(const AdamwConstants& k, float norm
     if (!(norm < __builtin_inff())) return 0.f;
     return norm > k.max_norm ? k.grad_scale * (k.max_norm / norm) : k.grad_scale;
 }
-// largest of a wavefront's values, in a scalar register: four steps inside rows of 16 lanes, two across
-__device__ __forceinline__ unsigned wave_max(unsigned v)
-{
-#define ST_DPP(CTRL, ROWS) v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false))
-    ST_DPP(0x111, 0xf); ST_DPP(0x112, 0xf); ST_DPP(0x114, 0xf); ST_DPP(0x118, 0xf);      // row_shr 1, 2, 4, 8
-    ST_DPP(0x142, 0xa); ST_DPP(0x143, 0xc);                                              // row_bcast 15, 31
-#undef ST_DPP
-    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
-}
 // scale and multiplier of a run whose largest value has the bits `top`; codes^2 reach `codes2`
 __device__ __forceinline__ float run_multiplier(unsigned top, float codes2, float* scale)
 {

@@ -254,48 +254,96 @@ struct FewArgs {
     const void* x; int x_bf16, x_wide; int64_t x_pitch;      // FUSED: the tokens as they are, row by row
     int per_wave;                                            // bytes of the contraction a wavefront takes, a multiple of 64
     int lds_pitch;                                           // FUSED: bytes between two tokens' codes in LDS
+    int group, per_token;                                    // FUSED: wavefronts along a token, a power of two; a thread's runs of a token
 };
 
-template <class T> __device__ __forceinline__ void few_quantize(const FewArgs& f, char* codes, unsigned (*tops)[FEW_WAVES], float* scales)
-{
-    const Product& p = f.p;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, m = (int)p.m;
-    const int per_row = m == 1 ? 8 : m == 2 ? 4 : m <= 4 ? 2 : 1;       // wavefronts a token
-    const int sub = wave % per_row, first = wave / per_row, step = FEW_WAVES / per_row;
-    for (int r = first; r < m; r += step) {
-        unsigned top = 0;
-        for (int at = (sub * 64 + lane) * 8; at < p.k; at += per_row * 512) {
-            float v[8];
-            load_run<T, 8>((const T*)f.x + r * f.x_pitch + at, p.k - at, f.x_wide, v);
+// Eight values as they lie in memory.
+template <class T> struct Raw8;
+template <> struct Raw8<bf16> {
+    static constexpr int KEEP = 8;
+    unsigned w[4];
+    __device__ __forceinline__ void load(const bf16* p, int n, bool wide)
+    {
+        if (wide) { const uint4 u = n > 0 ? *(const uint4*)p : make_uint4(0, 0, 0, 0); w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w; return; }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[i]));
+        for (int i = 0; i < 4; ++i) {
+            const unsigned lo = 2 * i < n ? ((const unsigned short*)p)[2 * i] : 0u, hi = 2 * i + 1 < n ? ((const unsigned short*)p)[2 * i + 1] : 0u;
+            w[i] = lo | hi << 16;
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+};
+template <> struct Raw8<float> {
+    static constexpr int KEEP = 4;
+    float v[8];
+    __device__ __forceinline__ void load(const float* p, int n, bool wide)
+    {
+        if (wide) {
+            const float4 a = n > 0 ? ((const float4*)p)[0] : make_float4(0, 0, 0, 0), b = n > 0 ? ((const float4*)p)[1] : make_float4(0, 0, 0, 0);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            return;
         }
 #pragma unroll
-        for (int d = 1; d < 64; d *= 2) top = max(top, (unsigned)__shfl_xor((int)top, d));
-        if (lane == 0) tops[r][sub] = top;
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+    }
+    __device__ __forceinline__ float operator[](int i) const { return v[i]; }
+};
+
+// Threads go along a token, eight values each; where a token has fewer than 512 such runs, several tokens are taken at once.  A thread
+// keeps all of its runs (KEEP at most) in registers between the search for the largest and the rounding.
+template <class T>
+__device__ __forceinline__ void few_quantize(const FewArgs& f, char* codes, unsigned* tops, float* scales)
+{
+    constexpr int KEEP = Raw8<T>::KEEP;
+    const Product& p = f.p;
+    const int m = (int)p.m, k = (int)p.k, end = FEW_WAVES * f.per_wave;
+    const int threads = f.group * 64, lane = threadIdx.x & (threads - 1);
+    const int first = __builtin_amdgcn_readfirstlane(threadIdx.x / threads), step = FEW_WAVES / f.group;
+    if ((int)threadIdx.x < m) tops[threadIdx.x] = 0;
+    Raw8<T> v[KEEP];
+    int r = first, c = 0;
+#pragma unroll
+    for (int j = 0; j < KEEP; ++j) {
+        const int at = (c * threads + lane) * 8;
+        if (r < m) v[j].load((const T*)f.x + r * f.x_pitch + at, k - at, f.x_wide);
+        if (++c == f.per_token) { c = 0; r += step; }
     }
     __syncthreads();
-    const int end = FEW_WAVES * f.per_wave;
-    for (int r = first; r < m; r += step) {
-        unsigned top = 0;
-        for (int i = 0; i < per_row; ++i) top = max(top, tops[r][i]);
-        float s;
-        const float mult = row_multiplier(top, &s);
-        if (lane == 0 && sub == 0) scales[r] = s;
-        for (int at = (sub * 64 + lane) * 8; at < end; at += per_row * 512) {
-            float v[8];
-            load_run<T, 8>((const T*)f.x + r * f.x_pitch + at, p.k - at, f.x_wide, v);
-            *(uint2*)(codes + r * f.lds_pitch + at) = make_uint2(pack4(code_of(v[0], mult), code_of(v[1], mult), code_of(v[2], mult), code_of(v[3], mult)),
-                                                                pack4(code_of(v[4], mult), code_of(v[5], mult), code_of(v[6], mult), code_of(v[7], mult)));
+    r = first; c = 0;
+#pragma unroll
+    for (int j = 0; j < KEEP; ++j) {
+        if (r < m) {
+            unsigned top = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[j][i]));
+            top = wave_max(top);
+            if ((threadIdx.x & 63) == 0) atomicMax(&tops[r], top);
         }
+        if (++c == f.per_token) { c = 0; r += step; }
+    }
+    __syncthreads();
+    r = first; c = 0;
+#pragma unroll
+    for (int j = 0; j < KEEP; ++j) {
+        if (r < m) {
+            float s;
+            const float mult = row_multiplier(tops[r], &s);
+            if (c == 0 && lane == 0) scales[r] = s;
+            const int at = (c * threads + lane) * 8;
+            if (at < end)
+                *(uint2*)(codes + r * f.lds_pitch + at) =
+                    make_uint2(pack4(code_of(v[j][0], mult), code_of(v[j][1], mult), code_of(v[j][2], mult), code_of(v[j][3], mult)),
+                               pack4(code_of(v[j][4], mult), code_of(v[j][5], mult), code_of(v[j][6], mult), code_of(v[j][7], mult)));
+        }
+        if (++c == f.per_token) { c = 0; r += step; }
     }
 }
 
 template <int NT, bool FUSED>
-__global__ __launch_bounds__(FEW_WAVES * 64) void k_int8_few(const FewArgs f)
+__global__ __launch_bounds__(FEW_WAVES * 64, 4) void k_int8_few(const FewArgs f)
 {
     extern __shared__ __align__(16) char lds[];      // FUSED: the codes; then, and otherwise, the wavefronts' sums [8][NT * 256]
-    __shared__ unsigned tops[FUSED ? NT * 16 : 1][FEW_WAVES];
+    __shared__ unsigned tops[NT * 16];
     __shared__ float scales[NT * 16];
     const Product& p = f.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -358,25 +406,38 @@ __global__ __launch_bounds__(FEW_WAVES * 64) void k_int8_few(const FewArgs f)
 }
 
 constexpr int FEW_TOKENS = 64;
-constexpr int64_t FEW_LDS = 80 * 1024;       // two blocks a compute unit
 bool few_tokens(int64_t m) { return m <= FEW_TOKENS; }
 static int64_t few_per_wave(int64_t k) { return round_up(ceil_div(k, FEW_WAVES), 64); }
 static int64_t few_lds(int64_t m, int64_t k) { return m * (FEW_WAVES * few_per_wave(k) + 16); }
-// The tokens are quantised by every block: those of one matrix-core tile, as far as their codes fit.
-bool few_fused(int64_t m, int64_t k) { return m <= 16 && few_lds(m, k) <= FEW_LDS; }
+// wavefronts along a token, and runs of eight values that a thread has of one
+static void few_shape(int64_t m, int64_t k, int* group, int* per_token)
+{
+    *group = FEW_WAVES;
+    while (*group > 1 && (*group / 2) * 512 >= FEW_WAVES * few_per_wave(k) && FEW_WAVES / *group < m) *group /= 2;
+    *per_token = (int)ceil_div(FEW_WAVES * few_per_wave(k), *group * 512);
+}
+// The tokens are quantised by every block where they are those of one matrix-core tile and a thread's share of them fits its registers.
+bool few_fused(int64_t m, int64_t k, int is_bf16)
+{
+    if (m > 16) return false;
+    int group, per_token;
+    few_shape(m, k, &group, &per_token);
+    return ceil_div(m, FEW_WAVES / group) * per_token <= (is_bf16 ? Raw8<bf16>::KEEP : Raw8<float>::KEEP);
+}
 
 template <int NT, bool FUSED> static void few_launch(Ctx& c, const FewArgs& f)
 {
     size_t lds = (size_t)FEW_WAVES * NT * 1024;
     if (FUSED) lds = std::max(lds, (size_t)few_lds(f.p.m, f.p.k));
-    ensure_dynamic_lds((const void*)k_int8_few<NT, FUSED>, FUSED ? FEW_LDS : lds);
+    ensure_dynamic_lds((const void*)k_int8_few<NT, FUSED>, FUSED ? 64 * 1024 : lds);
     ST_LAUNCH(c, "int8_few", (k_int8_few<NT, FUSED>), dim3((unsigned)ceil_div(f.p.n, 16)), dim3(FEW_WAVES * 64), lds, f);
 }
 void product_few(Ctx& c, const Product& p, const QuantSource* x)
 {
-    FewArgs f{p, nullptr, 0, 0, 0, (int)few_per_wave(p.k), (int)(FEW_WAVES * few_per_wave(p.k) + 16)};
+    FewArgs f{p, nullptr, 0, 0, 0, (int)few_per_wave(p.k), (int)(FEW_WAVES * few_per_wave(p.k) + 16), 0, 0};
     if (x) {
-        f.x = x->x; f.x_bf16 = x->bf16; f.x_pitch = x->pitch; f.x_wide = wide_ok(x->x, x->pitch, x->bf16, 8);
+        f.x = x->x; f.x_bf16 = x->bf16; f.x_pitch = x->pitch; f.x_wide = p.k % 8 == 0 && wide_ok(x->x, x->pitch, x->bf16, 8);
+        few_shape(p.m, p.k, &f.group, &f.per_token);
         few_launch<1, true>(c, f);
     } else if (p.m <= 16) few_launch<1, false>(c, f);
     else if (p.m <= 32) few_launch<2, false>(c, f);
@@ -427,7 +488,7 @@ void products(Ctx& c, const Product* p, int count)
         if (f.splits[i] > 1) { cells[n_joined] = p[i].m * p[i].n; joined.g[n_joined++] = g.g[i]; }
     }
     if (f.tile == 256) launch<256, 256, 128, 64, 2>(c, g);
-    else if (f.tile == 128) launch<128, 128, 64, 64, 2>(c, g);
+    else if (f.tile == 128) launch<128, 128, 64, 64, 4>(c, g);
     else launch<64, 64, 32, 32, 4>(c, g);
     if (n_joined) {
         const int64_t all = cells[0] + cells[1], blocks = ceil_div(all, 256);

@@ -25,6 +25,16 @@ __device__ __forceinline__ unsigned pack4(unsigned a, unsigned b, unsigned c, un
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(d, c, 0x0c0c0400), __builtin_amdgcn_perm(b, a, 0x0c0c0400), 0x05040100);
 }
 
+// largest of a wavefront's values, in a scalar register: four steps inside rows of 16 lanes, two across
+__device__ __forceinline__ unsigned wave_max(unsigned v)
+{
+#define ST_DPP(CTRL, ROWS) v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false))
+    ST_DPP(0x111, 0xf); ST_DPP(0x112, 0xf); ST_DPP(0x114, 0xf); ST_DPP(0x118, 0xf);      // row_shr 1, 2, 4, 8
+    ST_DPP(0x142, 0xa); ST_DPP(0x143, 0xc);                                              // row_bcast 15, 31
+#undef ST_DPP
+    return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+}
+
 // COUNT consecutive values from p, of which `n` exist; the others are 0.  wide: p is aligned for loads of all of them.
 template <class T, int COUNT> __device__ __forceinline__ void load_run(const T* p, int64_t n, bool wide, float (&v)[COUNT])
 {
