@@ -6,19 +6,22 @@
 // lane are four neighbouring channels of one token.
 //
 // A stage of 128 bytes of the contraction of a tile's rows goes from memory into LDS directly, 16 bytes a lane, eight rows a
-// wavefront and instruction.  Chunk c (of 16 bytes) of row r lies in place c ^ (r & 7) of its row: lanes that read the same chunk of
-// eight consecutive rows then read eight different groups of banks.
+// wavefront and instruction.  Chunk c (of 16 bytes) of row r lies in place c ^ (r / 2 % 8) of its row: two rows span the 64 banks, so lanes
+// that read the same chunk of sixteen consecutive rows read sixteen different groups of four banks.  (With c ^ (r % 8) rows r and r + 8
+// met: half of the LDS cycles were conflicts.)
 #include "st_quantize.hpp"
 
 #include <algorithm>
 
 namespace st {
 
+constexpr int BAND = 4;         // rows of tiles
 constexpr int STAGE = 128;      // bytes of the contraction a stage holds
 
 struct GemmArgs {
     Product p;
-    FastDiv by_tiles, by_row;                 // tiles of a split, tiles of a row of tiles
+    FastDiv by_tiles, by_band;                // tiles of a split, tiles of a band of BAND rows of tiles
+    int tiles_m;
     int splits, stages;                       // stages: of the whole contraction
     unsigned blocks;
 };
@@ -93,10 +96,14 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
     const GemmArgs& g = pair.g[second];
     const Product& p = g.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int block = (int)blockIdx.x - (second ? (int)pair.g[0].blocks : 0);
+    // An XCD gets a run of consecutive tiles, ordered in bands of four tiles of tokens: what its 32 compute units work on at a time is
+    // 4 x 8 tiles, and a third less goes from memory to its L2 than with rows of tiles.
+    const int block = xcd_band((int)blockIdx.x - (second ? (int)pair.g[0].blocks : 0), (int)g.blocks);
     const int split = __builtin_amdgcn_readfirstlane(fast_quot(block, g.by_tiles));
     const int tile = block - split * (int)g.by_tiles.d;
-    const int tm = __builtin_amdgcn_readfirstlane(fast_quot(tile, g.by_row)), tn = tile - tm * (int)g.by_row.d;
+    const int band = __builtin_amdgcn_readfirstlane(fast_quot(tile, g.by_band)), in_band = tile - band * (int)g.by_band.d;
+    const int high = min(BAND, g.tiles_m - band * BAND);
+    const int tn = __builtin_amdgcn_readfirstlane(in_band / high), tm = band * BAND + in_band - tn * high;
     const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
     const int first = (int)((int64_t)g.stages * split / g.splits), last = (int)((int64_t)g.stages * (split + 1) / g.splits);
 
@@ -104,7 +111,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
     const int64_t k16 = (p.k + 15) / 16 * 16, kq = (p.k + STAGE - 1) / STAGE * STAGE;
     const auto ra = operand(p.b + n0 * p.b_pitch, (p.n - n0 - 1) * p.b_pitch + k16);
     const auto rb = operand(p.a + m0 * p.a_pitch, (p.m - m0 - 1) * p.a_pitch + kq);
-    const unsigned chunk = ((lane & 7) ^ (lane >> 3)) * 16;
+    static_assert(WAVES % 2 == 0, "a wavefront's eight rows begin at an even or at an odd multiple of eight in every load");
+    const unsigned chunk = ((lane & 7) ^ ((lane >> 4) + 4 * (wave & 1))) * 16;
     const unsigned va = (unsigned)(wave * 8 + (lane >> 3)) * (unsigned)p.b_pitch + chunk;
     const unsigned vb = (unsigned)(wave * 8 + (lane >> 3)) * (unsigned)p.a_pitch + chunk;
     const unsigned sa = WAVES * 8 * (unsigned)p.b_pitch, sb = WAVES * 8 * (unsigned)p.a_pitch;
@@ -124,7 +132,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
     i32x16 acc[NB][NA] = {};
     i32x4 a[2][NA], b[2][NB];
     auto fetch = [&](int buf, int ks, int to) {
-        const char* L = lds + buf * BUF + ((ks * 2 + half) ^ (r32 & 7)) * 16;
+        const char* L = lds + buf * BUF + ((ks * 2 + half) ^ (r32 >> 1 & 7)) * 16;
 #pragma unroll
         for (int i = 0; i < NA; ++i) a[to][i] = *(const i32x4*)(L + offA + i * 32 * STAGE);
 #pragma unroll
@@ -484,7 +492,7 @@ void products(Ctx& c, const Product* p, int count)
     int64_t cells[2] = {0, 0};
     for (int i = 0; i < count; ++i) {
         const int64_t tm = ceil_div(p[i].m, f.tile), tn = ceil_div(p[i].n, f.tile);
-        g.g[i] = GemmArgs{p[i], fast_div((int)(tm * tn)), fast_div((int)tn), f.splits[i], (int)ceil_div(p[i].k, STAGE), (unsigned)(tm * tn * f.splits[i])};
+        g.g[i] = GemmArgs{p[i], fast_div((int)(tm * tn)), fast_div((int)(tn * BAND)), (int)tm, f.splits[i], (int)ceil_div(p[i].k, STAGE), (unsigned)(tm * tn * f.splits[i])};
         if (f.splits[i] > 1) { cells[n_joined] = p[i].m * p[i].n; joined.g[n_joined++] = g.g[i]; }
     }
     if (f.tile == 256) launch<256, 256, 128, 64, 2>(c, g);
