@@ -265,44 +265,14 @@ struct FewArgs {
     int group, per_token;                                    // FUSED: wavefronts along a token, a power of two; a thread's runs of a token
 };
 
-// Eight values as they lie in memory.
-template <class T> struct Raw8;
-template <> struct Raw8<bf16> {
-    static constexpr int KEEP = 8;
-    unsigned w[4];
-    __device__ __forceinline__ void load(const bf16* p, int n, bool wide)
-    {
-        if (wide) { const uint4 u = n > 0 ? *(const uint4*)p : make_uint4(0, 0, 0, 0); w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w; return; }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const unsigned lo = 2 * i < n ? ((const unsigned short*)p)[2 * i] : 0u, hi = 2 * i + 1 < n ? ((const unsigned short*)p)[2 * i + 1] : 0u;
-            w[i] = lo | hi << 16;
-        }
-    }
-    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
-};
-template <> struct Raw8<float> {
-    static constexpr int KEEP = 4;
-    float v[8];
-    __device__ __forceinline__ void load(const float* p, int n, bool wide)
-    {
-        if (wide) {
-            const float4 a = n > 0 ? ((const float4*)p)[0] : make_float4(0, 0, 0, 0), b = n > 0 ? ((const float4*)p)[1] : make_float4(0, 0, 0, 0);
-            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-            return;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
-    }
-    __device__ __forceinline__ float operator[](int i) const { return v[i]; }
-};
+template <class T> constexpr int few_keep() { return sizeof(T) == 2 ? 8 : 4; }      // runs of eight values in a thread's registers
 
 // Threads go along a token, eight values each; where a token has fewer than 512 such runs, several tokens are taken at once.  A thread
 // keeps all of its runs (KEEP at most) in registers between the search for the largest and the rounding.
 template <class T>
 __device__ __forceinline__ void few_quantize(const FewArgs& f, char* codes, unsigned* tops, float* scales)
 {
-    constexpr int KEEP = Raw8<T>::KEEP;
+    constexpr int KEEP = few_keep<T>();
     const Product& p = f.p;
     const int m = (int)p.m, k = (int)p.k, end = FEW_WAVES * f.per_wave;
     const int threads = f.group * 64, lane = threadIdx.x & (threads - 1);
@@ -430,7 +400,7 @@ bool few_fused(int64_t m, int64_t k, int is_bf16)
     if (m > 16) return false;
     int group, per_token;
     few_shape(m, k, &group, &per_token);
-    return ceil_div(m, FEW_WAVES / group) * per_token <= (is_bf16 ? Raw8<bf16>::KEEP : Raw8<float>::KEEP);
+    return ceil_div(m, FEW_WAVES / group) * per_token <= (is_bf16 ? few_keep<bf16>() : few_keep<float>());
 }
 
 template <int NT, bool FUSED> static void few_launch(Ctx& c, const FewArgs& f)
@@ -460,13 +430,14 @@ Form form_of(const Extent* e, int count)
     Form f = {64, {1, 1}};
     if (total(256) >= 192) f.tile = 256;
     else if (total(128) >= 192) f.tile = 128;
-    // every block about the same number of stages, 512 blocks, four stages each at least
+    // every block about the same number of stages, 256 blocks, eight stages each at least; up to 16 stages the parts' join costs more than
+    // it gives (333 tokens 1000 -> 1003: 11.8 us, in two parts 15.6; 65 tokens 8192 -> 128 in eight parts: 12.7, in four 15.0)
     int64_t work = 0;
     for (int i = 0; i < count; ++i) work += tiles_of(e[i], f.tile) * ceil_div(e[i].k, STAGE);
-    const int64_t each = std::max<int64_t>(4, ceil_div(work, 512));
+    const int64_t each = std::max<int64_t>(8, ceil_div(work, 256));
     for (int i = 0; i < count; ++i) {
         const int64_t stages = ceil_div(e[i].k, STAGE);
-        int64_t s = total(f.tile) < 256 ? stages / each : 1;
+        int64_t s = total(f.tile) < 256 && stages > 16 ? stages / each : 1;
         s = std::max(s, ceil_div(stages, ST_INT8_MAX_SUM / STAGE));    // what int32 can hold
         f.splits[i] = (int)std::max<int64_t>(s, 1);
     }
@@ -496,7 +467,9 @@ void products(Ctx& c, const Product* p, int count)
         if (f.splits[i] > 1) { cells[n_joined] = p[i].m * p[i].n; joined.g[n_joined++] = g.g[i]; }
     }
     if (f.tile == 256) launch<256, 256, 128, 64, 2>(c, g);
-    else if (f.tile == 128) launch<128, 128, 64, 64, 4>(c, g);
+    // (one block a compute unit: deeper; 1000 tokens 4000 -> 4000 31.0 us against 34.8; else two blocks: 4096 tokens 2048 -> 2048 32.1 against 40.4)
+    else if (f.tile == 128 && g.g[0].blocks + g.g[1].blocks <= 256) launch<128, 128, 64, 32, 4>(c, g);
+    else if (f.tile == 128) launch<128, 128, 64, 32, 2>(c, g);
     else launch<64, 64, 32, 32, 4>(c, g);
     if (n_joined) {
         const int64_t all = cells[0] + cells[1], blocks = ceil_div(all, 256);

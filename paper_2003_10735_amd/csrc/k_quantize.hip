@@ -19,10 +19,11 @@ struct Job {
     int8_t* q;
     float *scale, *sum, *part_max, *part_sum;
     int parts;
-    unsigned len_tiles, first1, first2;      // first block of the job in the two launches
+    unsigned len_tiles;
+    // wide, mask_wide: aligned for the role's loads (rows: and a whole number of runs)
     uint8_t bf16_, mask_bf16, wide, mask_wide, along;
 };
-struct Jobs { Job job[4]; int n; };
+struct Jobs { unsigned first1[4], first2[4]; int n; Job job[4]; };      // first block of each job in the two launches
 
 // COUNT values at `at` of row (or position) `line`, zero where the mask is not positive
 template <class T, int COUNT>
@@ -37,7 +38,14 @@ __device__ __forceinline__ void read(const Job& j, int64_t line, int64_t at, int
         for (int i = 0; i < COUNT; ++i) v[i] = m[i] > 0.f ? v[i] : 0.f;
     }
 }
-__device__ __forceinline__ float sum8(const float (&v)[8]) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
+template <class M, class T> __device__ __forceinline__ void clear_masked(const M* m, int n, bool wide, Raw8<T>& v)
+{
+    Raw8<M> on;
+    on.load(m, n, wide);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) if (!(on[i] > 0.f)) v.clear(i);
+}
+template <class T> __device__ __forceinline__ float sum8(const Raw8<T>& v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 
 struct Shared {
     union {
@@ -48,28 +56,38 @@ struct Shared {
 };
 
 // ------------------------------------------------------------------------------------ rows that lie along memory
-// LANES threads a row.  A thread holds four runs of eight values of its row in registers between the search for the largest and the
-// rounding, so a row of up to 32 * LANES values is read once; longer rows read the rest twice.
-template <class T, int LANES> __device__ __forceinline__ void rows_role(const Job& j, unsigned block, Shared& sh)
+// LANES threads a row.  A thread holds KEEP runs of eight values of its row, as they came, between the search for the largest and the
+// rounding, so a row of up to 8 * KEEP * LANES values is read once; longer rows read the rest twice.  A wavefront takes a row of up to 4096
+// bfloat16 values by itself: no barrier, eight loads under way.
+template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_role(const Job& j, unsigned block, Shared& sh)
 {
-    constexpr int KEEP = 4;
     const int lane = threadIdx.x % LANES;
     const int64_t row = (int64_t)block * (256 / LANES) + threadIdx.x / LANES;
     const bool there = row < j.rows;
-    float v[KEEP][8];
+    const int len = (int)j.len;
+    const T* x = (const T*)j.x + row * j.pitch;
     unsigned top = 0;
     double total = 0.0;
-    auto take = [&](int64_t at, float (&w)[8]) {
-        read<T, 8>(j, there ? row : 0, at, there ? j.len - at : 0, w);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) top = max(top, abs_bits(w[i]));
-        if (j.sum) total += sum8(w);
+    auto load = [&](int at, Raw8<T>& v) { v.load(x + at, there ? len - at : 0, j.wide); };
+    auto mask = [&](int at, Raw8<T>& v) {
+        if (!j.mask) return;
+        const int n = there ? len - at : 0;
+        if (j.mask_bf16) clear_masked((const bf16*)j.mask + row * j.mask_pitch + at, n, j.mask_wide, v);
+        else clear_masked((const float*)j.mask + row * j.mask_pitch + at, n, j.mask_wide, v);
     };
+    auto see = [&](const Raw8<T>& v) {
 #pragma unroll
-    for (int k = 0; k < KEEP; ++k) take((int64_t)(k * LANES + lane) * 8, v[k]);
-    for (int64_t at = (int64_t)(KEEP * LANES + lane) * 8; at < j.len; at += LANES * 8) {
-        float w[8];
-        take(at, w);
+        for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[i]));
+        if (j.sum) total += sum8(v);
+    };
+    Raw8<T> v[KEEP];
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) load((k * LANES + lane) * 8, v[k]);
+#pragma unroll
+    for (int k = 0; k < KEEP; ++k) { mask((k * LANES + lane) * 8, v[k]); see(v[k]); }
+    for (int at = (KEEP * LANES + lane) * 8; at < len; at += LANES * 8) {
+        Raw8<T> w;
+        load(at, w); mask(at, w); see(w);
     }
     if (j.sum) {
 #pragma unroll
@@ -82,8 +100,7 @@ template <class T, int LANES> __device__ __forceinline__ void rows_role(const Jo
         if (there && lane == 0) j.sum[row] = (float)total;
     }
     if (!j.q) return;
-#pragma unroll
-    for (int d = 1; d < (LANES < 64 ? LANES : 64); d *= 2) top = max(top, (unsigned)__shfl_xor((int)top, d));
+    top = LANES == 32 ? half_max(top) : wave_max(top);
     if (LANES == 256) {
         if ((threadIdx.x & 63) == 0) sh.rows.tops[threadIdx.x >> 6] = top;
         __syncthreads();
@@ -93,23 +110,24 @@ template <class T, int LANES> __device__ __forceinline__ void rows_role(const Jo
     float s;
     const float r = row_multiplier(top, &s);
     if (lane == 0) j.scale[row] = s;
-    int64_t end = (j.len + OPERAND_QUANTUM - 1) / OPERAND_QUANTUM * OPERAND_QUANTUM;
-    if (end > j.q_pitch) end = j.q_pitch;
+    const int64_t padded = (j.len + OPERAND_QUANTUM - 1) / OPERAND_QUANTUM * OPERAND_QUANTUM;
+    const int end = (int)(padded < j.q_pitch ? padded : j.q_pitch);
     int8_t* qr = j.q + row * j.q_pitch;
-    auto put = [&](int64_t at, const float (&w)[8]) {
+    auto put = [&](int at, const Raw8<T>& w) {
         if (at >= end) return;      // (pitch and quantum are multiples of 8: a run is written whole or not at all)
         *(uint2*)(qr + at) = make_uint2(pack4(code_of(w[0], r), code_of(w[1], r), code_of(w[2], r), code_of(w[3], r)),
                                         pack4(code_of(w[4], r), code_of(w[5], r), code_of(w[6], r), code_of(w[7], r)));
     };
 #pragma unroll
-    for (int k = 0; k < KEEP; ++k) put((int64_t)(k * LANES + lane) * 8, v[k]);
-    for (int64_t at = (int64_t)(KEEP * LANES + lane) * 8; at < end; at += LANES * 8) {
-        float w[8];
-        read<T, 8>(j, row, at, j.len - at, w);
+    for (int k = 0; k < KEEP; ++k) put((k * LANES + lane) * 8, v[k]);
+    for (int at = (KEEP * LANES + lane) * 8; at < end; at += LANES * 8) {
+        Raw8<T> w;
+        load(at, w); mask(at, w);
         put(at, w);
     }
 }
-static __host__ __device__ __forceinline__ int row_lanes(int64_t len) { return len <= 1024 ? 32 : len <= 2048 ? 64 : 256; }
+template <class T> constexpr int row_keep() { return sizeof(T) == 2 ? 8 : 4; }
+static __host__ __device__ __forceinline__ int row_lanes(int64_t len, int is_bf16) { return len <= 1024 ? 32 : len <= (is_bf16 ? 4096 : 2048) ? 64 : 256; }
 
 // --------------------------------------------------------------------------------------- rows that lie across it
 // The source is a matrix [len][pitch] whose columns are the operand's rows.  Sixteen threads take 64 columns of a position, sixteen
@@ -208,25 +226,25 @@ template <class T> __device__ __forceinline__ void turn_role(const Job& j, unsig
 template <class T> __device__ __forceinline__ void first_role(const Job& j, unsigned block, Shared& sh)
 {
     if (!j.along) parts_role<T>(j, block, sh);
-    else if (row_lanes(j.len) == 32) rows_role<T, 32>(j, block, sh);
-    else if (row_lanes(j.len) == 64) rows_role<T, 64>(j, block, sh);
-    else rows_role<T, 256>(j, block, sh);
+    else if (row_lanes(j.len, sizeof(T) == 2) == 32) rows_role<T, 32, 4>(j, block, sh);
+    else if (row_lanes(j.len, sizeof(T) == 2) == 64) rows_role<T, 64, row_keep<T>()>(j, block, sh);
+    else rows_role<T, 256, row_keep<T>()>(j, block, sh);
 }
 __global__ __launch_bounds__(256) void k_quantize_first(const Jobs jobs)
 {
     __shared__ Shared sh;
     int i = 0;
-    while (i + 1 < jobs.n && blockIdx.x >= jobs.job[i + 1].first1) ++i;
+    while (i + 1 < jobs.n && blockIdx.x >= jobs.first1[i + 1]) ++i;
     const Job& j = jobs.job[i];
-    if (j.bf16_) first_role<bf16>(j, blockIdx.x - j.first1, sh); else first_role<float>(j, blockIdx.x - j.first1, sh);
+    if (j.bf16_) first_role<bf16>(j, blockIdx.x - jobs.first1[i], sh); else first_role<float>(j, blockIdx.x - jobs.first1[i], sh);
 }
 __global__ __launch_bounds__(256) void k_quantize_turn(const Jobs jobs)
 {
     __shared__ Shared sh;
     int i = 0;
-    while (i + 1 < jobs.n && blockIdx.x >= jobs.job[i + 1].first2) ++i;
+    while (i + 1 < jobs.n && blockIdx.x >= jobs.first2[i + 1]) ++i;
     const Job& j = jobs.job[i];
-    if (j.bf16_) turn_role<bf16>(j, blockIdx.x - j.first2, sh); else turn_role<float>(j, blockIdx.x - j.first2, sh);
+    if (j.bf16_) turn_role<bf16>(j, blockIdx.x - jobs.first2[i], sh); else turn_role<float>(j, blockIdx.x - jobs.first2[i], sh);
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -250,12 +268,14 @@ void quantize(Ctx& c, const QuantTask* tasks, int n)
             const QuantTask& t = tasks[i];
             const QuantSource& s = t.s;
             if (s.along != pass || s.rows == 0) continue;
+            jobs.first1[jobs.n] = (unsigned)blocks1; jobs.first2[jobs.n] = (unsigned)blocks2;
             Job& j = jobs.job[jobs.n++];
+            const int run = s.along ? 8 : 4;
+            const bool whole = !s.along || s.len % 8 == 0;
             j = Job{s.x, s.mask, s.pitch, s.mask_pitch, s.rows, s.len, t.to.pitch, 0, t.to.q, t.to.scale, t.sum, t.to.q ? t.part_max : nullptr,
-                    t.sum ? t.part_sum : nullptr, 1, 1, (unsigned)blocks1, (unsigned)blocks2, (uint8_t)s.bf16, (uint8_t)s.mask_bf16,
-                    (uint8_t)wide_ok(s.x, s.pitch, s.bf16, s.along ? 8 : 4), (uint8_t)wide_ok(s.mask, s.mask_pitch, s.mask_bf16, s.along ? 8 : 4),
-                    (uint8_t)s.along};
-            if (s.along) { blocks1 += ceil_div(s.rows, 256 / row_lanes(s.len)); continue; }
+                    t.sum ? t.part_sum : nullptr, 1, 1, (uint8_t)s.bf16, (uint8_t)s.mask_bf16, (uint8_t)(whole && wide_ok(s.x, s.pitch, s.bf16, run)),
+                    (uint8_t)(whole && wide_ok(s.mask, s.mask_pitch, s.mask_bf16, run)), (uint8_t)s.along};
+            if (s.along) { blocks1 += ceil_div(s.rows, 256 / row_lanes(s.len, s.bf16)); continue; }
             j.parts = transpose_parts(s.rows, s.len);
             j.per_part = ceil_div(s.len, j.parts);
             j.len_tiles = t.to.q ? (unsigned)ceil_div(s.len, 128) : 1;
@@ -267,7 +287,7 @@ void quantize(Ctx& c, const QuantTask* tasks, int n)
     Jobs turn;
     turn.n = 0;
     for (int i = 0; i < jobs.n; ++i)
-        if (!jobs.job[i].along) turn.job[turn.n++] = jobs.job[i];
+        if (!jobs.job[i].along) { turn.first2[turn.n] = jobs.first2[i]; turn.job[turn.n++] = jobs.job[i]; }
     ST_LAUNCH(c, "quantize_turn", k_quantize_turn, dim3((unsigned)blocks2), dim3(256), 0, turn);
 }
 

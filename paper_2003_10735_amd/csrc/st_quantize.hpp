@@ -26,14 +26,22 @@ __device__ __forceinline__ unsigned pack4(unsigned a, unsigned b, unsigned c, un
 }
 
 // largest of a wavefront's values, in a scalar register: four steps inside rows of 16 lanes, two across
+#define ST_DPP(CTRL, ROWS) v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false))
 __device__ __forceinline__ unsigned wave_max(unsigned v)
 {
-#define ST_DPP(CTRL, ROWS) v = max(v, (unsigned)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false))
     ST_DPP(0x111, 0xf); ST_DPP(0x112, 0xf); ST_DPP(0x114, 0xf); ST_DPP(0x118, 0xf);      // row_shr 1, 2, 4, 8
     ST_DPP(0x142, 0xa); ST_DPP(0x143, 0xc);                                              // row_bcast 15, 31
-#undef ST_DPP
     return (unsigned)__builtin_amdgcn_readlane((int)v, 63);
 }
+// .. of each half of a wavefront's lanes
+__device__ __forceinline__ unsigned half_max(unsigned v)
+{
+    ST_DPP(0x111, 0xf); ST_DPP(0x112, 0xf); ST_DPP(0x114, 0xf); ST_DPP(0x118, 0xf);
+    ST_DPP(0x142, 0xa);
+    const unsigned lo = (unsigned)__builtin_amdgcn_readlane((int)v, 31), hi = (unsigned)__builtin_amdgcn_readlane((int)v, 63);
+    return threadIdx.x & 32 ? hi : lo;
+}
+#undef ST_DPP
 
 // COUNT consecutive values from p, of which `n` exist; the others are 0.  wide: p is aligned for loads of all of them.
 template <class T, int COUNT> __device__ __forceinline__ void load_run(const T* p, int64_t n, bool wide, float (&v)[COUNT])
@@ -56,6 +64,38 @@ template <class T, int COUNT> __device__ __forceinline__ void load_run(const T* 
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) v[i] = i < n ? to_f32(p[i]) : 0.f;
 }
+
+// Eight consecutive values as they lie in memory, those from n on zeros.  wide: loaded at once, and n is either 8 or more or 0 or less.
+template <class T> struct Raw8;
+template <> struct Raw8<bf16> {
+    unsigned w[4];
+    __device__ __forceinline__ void load(const bf16* p, int n, bool wide)
+    {
+        if (wide) { const uint4 u = n > 0 ? *(const uint4*)p : make_uint4(0, 0, 0, 0); w[0] = u.x; w[1] = u.y; w[2] = u.z; w[3] = u.w; return; }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const unsigned lo = 2 * i < n ? ((const unsigned short*)p)[2 * i] : 0u, hi = 2 * i + 1 < n ? ((const unsigned short*)p)[2 * i + 1] : 0u;
+            w[i] = lo | hi << 16;
+        }
+    }
+    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+    __device__ __forceinline__ void clear(int i) { w[i >> 1] &= i & 1 ? 0x0000ffffu : 0xffff0000u; }
+};
+template <> struct Raw8<float> {
+    float v[8];
+    __device__ __forceinline__ void load(const float* p, int n, bool wide)
+    {
+        if (wide) {
+            const float4 a = n > 0 ? ((const float4*)p)[0] : make_float4(0, 0, 0, 0), b = n > 0 ? ((const float4*)p)[1] : make_float4(0, 0, 0, 0);
+            v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+    }
+    __device__ __forceinline__ float operator[](int i) const { return v[i]; }
+    __device__ __forceinline__ void clear(int i) { v[i] = 0.f; }
+};
 
 inline bool wide_ok(const void* p, int64_t pitch, int is_bf16, int run)     // runs of `run` values can be loaded at once
 {
