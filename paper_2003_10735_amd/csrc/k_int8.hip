@@ -305,6 +305,7 @@ __device__ __forceinline__ void few_quantize(const FewArgs& f, char* codes, unsi
     for (int j = 0; j < KEEP; ++j) {
         if (r < m) {
             float s;
+            v[j].repack();
             const float mult = row_multiplier(tops[r], &s);
             if (c == 0 && lane == 0) scales[r] = s;
             const int at = (c * threads + lane) * 8;

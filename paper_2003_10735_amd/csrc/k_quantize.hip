@@ -11,6 +11,8 @@
 // LDS as codes.  (Sources that share a launch do not wait for one another: a backward pass has four, of which some are a few tiles.)
 #include "st_quantize.hpp"
 
+#include <type_traits>
+
 namespace st {
 
 struct Job {
@@ -25,18 +27,50 @@ struct Job {
 };
 struct Jobs { unsigned first1[4], first2[4]; int n; Job job[4]; };      // first block of each job in the two launches
 
-// COUNT values at `at` of row (or position) `line`, zero where the mask is not positive
-template <class T, int COUNT>
-__device__ __forceinline__ void read(const Job& j, int64_t line, int64_t at, int64_t n, float (&v)[COUNT])
+// Four neighbouring values, one load.
+template <class T> struct Raw4;
+template <> struct Raw4<bf16> {
+    uint2 u;
+    __device__ __forceinline__ void load(const bf16* p) { u = *(const uint2*)p; }
+    __device__ __forceinline__ float operator[](int i) const { const unsigned w = i & 2 ? u.y : u.x; return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16); }
+};
+template <> struct Raw4<float> {
+    float4 u;
+    __device__ __forceinline__ void load(const float* p) { u = *(const float4*)p; }
+    __device__ __forceinline__ float operator[](int i) const { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
+};
+template <> struct Raw4<void> {};      // no mask
+
+// Four values at `at` of position `line`, of which `n` exist, zero where the mask is not positive: the way of any alignment.
+template <class T> __device__ __forceinline__ void read(const Job& j, int64_t line, int64_t at, int64_t n, float (&v)[4])
 {
-    load_run<T, COUNT>((const T*)j.x + line * j.pitch + at, n, j.wide, v);
-    if (j.mask) {
-        float m[COUNT];
-        if (j.mask_bf16) load_run<bf16, COUNT>((const bf16*)j.mask + line * j.mask_pitch + at, n, j.mask_wide, m);
-        else load_run<float, COUNT>((const float*)j.mask + line * j.mask_pitch + at, n, j.mask_wide, m);
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) v[i] = m[i] > 0.f ? v[i] : 0.f;
+    for (int i = 0; i < 4; ++i) v[i] = i < n ? to_f32(((const T*)j.x)[line * j.pitch + at + i]) : 0.f;
+    if (!j.mask) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int64_t m = line * j.mask_pitch + at + i;
+        if (i < n && !((j.mask_bf16 ? to_f32(((const bf16*)j.mask)[m]) : ((const float*)j.mask)[m]) > 0.f)) v[i] = 0.f;
     }
+}
+// COUNT of them, `step` positions apart, by wide loads that are all under way before the first is used.  M: the mask's type, or void.
+template <class T, class M, int COUNT>
+__device__ __forceinline__ void read_wide(const Job& j, int64_t line, int step, int64_t at, float (&v)[COUNT][4])
+{
+    Raw4<T> x[COUNT];
+    Raw4<M> m[COUNT];
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        x[i].load((const T*)j.x + (line + i * step) * j.pitch + at);
+        if constexpr (!std::is_void<M>::value) m[i].load((const M*)j.mask + (line + i * step) * j.mask_pitch + at);
+    }
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[i][e] = x[i][e];
+            if constexpr (!std::is_void<M>::value) v[i][e] = m[i][e] > 0.f ? v[i][e] : 0.f;
+        }
 }
 template <class M, class T> __device__ __forceinline__ void clear_masked(const M* m, int n, bool wide, Raw8<T>& v)
 {
@@ -59,8 +93,9 @@ struct Shared {
 // LANES threads a row.  A thread holds KEEP runs of eight values of its row, as they came, between the search for the largest and the
 // rounding, so a row of up to 8 * KEEP * LANES values is read once; longer rows read the rest twice.  A wavefront takes a row of up to 4096
 // bfloat16 values by itself: no barrier, eight loads under way.
-template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_role(const Job& j, unsigned block, Shared& sh)
+template <class T, int LANES, int KEEP, bool WIDE> __device__ __forceinline__ void rows_role(const Job& j, unsigned block, Shared& sh)
 {
+    constexpr int MORE = WIDE ? 4 : 1;      // runs under way beyond those
     const int lane = threadIdx.x % LANES;
     const int64_t row = (int64_t)block * (256 / LANES) + threadIdx.x / LANES;
     const bool there = row < j.rows;
@@ -68,12 +103,12 @@ template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_rol
     const T* x = (const T*)j.x + row * j.pitch;
     unsigned top = 0;
     double total = 0.0;
-    auto load = [&](int at, Raw8<T>& v) { v.load(x + at, there ? len - at : 0, j.wide); };
+    auto load = [&](int at, Raw8<T>& v) { v.load(x + at, there ? len - at : 0, WIDE); };
     auto mask = [&](int at, Raw8<T>& v) {
         if (!j.mask) return;
         const int n = there ? len - at : 0;
-        if (j.mask_bf16) clear_masked((const bf16*)j.mask + row * j.mask_pitch + at, n, j.mask_wide, v);
-        else clear_masked((const float*)j.mask + row * j.mask_pitch + at, n, j.mask_wide, v);
+        if (j.mask_bf16) clear_masked((const bf16*)j.mask + row * j.mask_pitch + at, n, WIDE, v);
+        else clear_masked((const float*)j.mask + row * j.mask_pitch + at, n, WIDE, v);
     };
     auto see = [&](const Raw8<T>& v) {
 #pragma unroll
@@ -85,9 +120,12 @@ template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_rol
     for (int k = 0; k < KEEP; ++k) load((k * LANES + lane) * 8, v[k]);
 #pragma unroll
     for (int k = 0; k < KEEP; ++k) { mask((k * LANES + lane) * 8, v[k]); see(v[k]); }
-    for (int at = (KEEP * LANES + lane) * 8; at < len; at += LANES * 8) {
-        Raw8<T> w;
-        load(at, w); mask(at, w); see(w);
+    for (int at = (KEEP * LANES + lane) * 8; at < len; at += MORE * LANES * 8) {
+        Raw8<T> w[MORE];
+#pragma unroll
+        for (int k = 0; k < MORE; ++k) load(at + k * LANES * 8, w[k]);
+#pragma unroll
+        for (int k = 0; k < MORE; ++k) { mask(at + k * LANES * 8, w[k]); see(w[k]); }
     }
     if (j.sum) {
 #pragma unroll
@@ -119,11 +157,15 @@ template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_rol
                                         pack4(code_of(w[4], r), code_of(w[5], r), code_of(w[6], r), code_of(w[7], r)));
     };
 #pragma unroll
+    for (int k = 0; k < KEEP; ++k) v[k].repack();
+#pragma unroll
     for (int k = 0; k < KEEP; ++k) put((k * LANES + lane) * 8, v[k]);
-    for (int at = (KEEP * LANES + lane) * 8; at < end; at += LANES * 8) {
-        Raw8<T> w;
-        load(at, w); mask(at, w);
-        put(at, w);
+    for (int at = (KEEP * LANES + lane) * 8; at < end; at += MORE * LANES * 8) {
+        Raw8<T> w[MORE];
+#pragma unroll
+        for (int k = 0; k < MORE; ++k) load(at + k * LANES * 8, w[k]);
+#pragma unroll
+        for (int k = 0; k < MORE; ++k) { mask(at + k * LANES * 8, w[k]); put(at + k * LANES * 8, w[k]); }
     }
 }
 template <class T> constexpr int row_keep() { return sizeof(T) == 2 ? 8 : 4; }
@@ -132,27 +174,47 @@ static __host__ __device__ __forceinline__ int row_lanes(int64_t len, int is_bf1
 // --------------------------------------------------------------------------------------- rows that lie across it
 // The source is a matrix [len][pitch] whose columns are the operand's rows.  Sixteen threads take 64 columns of a position, sixteen
 // positions at once: whole lines of memory are read.  A block leaves the largest value and the sum of 64 columns over one part.
+template <class T, class M> __device__ __forceinline__ void parts_loop(const Job& j, int64_t col, int64_t from, int64_t to, int group, bool wide,
+                                                                       unsigned (&top)[4], double (&total)[4])
+{
+    for (int64_t piece = from + group; piece < to; piece += 1024) {     // float32 sums of 64 values, added in float64
+        float s[4] = {};
+        const int64_t end = piece + 1024 < to ? piece + 1024 : to;
+        int64_t k = piece;
+        auto see = [&](const float (&v)[4]) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) { top[e] = max(top[e], abs_bits(v[e])); s[e] += v[e]; }
+        };
+        if (wide)
+            for (; k + 48 < end; k += 64) {
+                float v[4][4];
+                read_wide<T, M, 4>(j, k, 16, col, v);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) see(v[i]);
+            }
+        for (; k < end; k += 16) {
+            float v[4];
+            read<T>(j, k, col, j.rows - col, v);
+            see(v);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) total[e] += s[e];
+    }
+}
 template <class T> __device__ __forceinline__ void parts_role(const Job& j, unsigned block, Shared& sh)
 {
     const unsigned tile = block / (unsigned)j.parts, part = block - tile * (unsigned)j.parts;
     const int c = (threadIdx.x & 15) * 4, group = threadIdx.x >> 4;
-    const int64_t col = (int64_t)tile * 64 + c, n = j.rows - col;
+    const int64_t col = (int64_t)tile * 64 + c;
     const int64_t from = part * j.per_part, to = from + j.per_part < j.len ? from + j.per_part : j.len;
+    const bool wide = j.wide && j.mask_wide && col + 4 <= j.rows;
     unsigned top[4] = {};
     double total[4] = {};
-    if (n > 0)
-        for (int64_t piece = from + group; piece < to; piece += 1024) {     // float32 sums of 64 values, added in float64
-            float s[4] = {};
-#pragma unroll 4
-            for (int64_t k = piece; k < to && k < piece + 1024; k += 16) {
-                float v[4];
-                read<T, 4>(j, k, col, n, v);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { top[i] = max(top[i], abs_bits(v[i])); s[i] += v[i]; }
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i) total[i] += s[i];
-        }
+    if (col < j.rows) {
+        if (!j.mask) parts_loop<T, void>(j, col, from, to, group, wide, top, total);
+        else if (j.mask_bf16) parts_loop<T, bf16>(j, col, from, to, group, wide, top, total);
+        else parts_loop<T, float>(j, col, from, to, group, wide, top, total);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) { sh.parts.tops[group][c + i] = top[i]; sh.parts.sums[group][c + i] = (float)total[i]; }
     __syncthreads();
@@ -177,12 +239,17 @@ template <class T> __device__ __forceinline__ void turn_role(const Job& j, unsig
     const bool sums = j.sum && len_tile == 0;
     const int c = (threadIdx.x & 15) * 4, group = threadIdx.x >> 4;
     float v[8][4] = {};
-    if (j.q && row0 + c < j.rows)
+    if (j.q && row0 + c < j.rows) {
+        const int64_t k = k0 + group * 8;
+        if (j.wide && j.mask_wide && row0 + c + 4 <= j.rows && k + 8 <= j.len) {
+            if (!j.mask) read_wide<T, void, 8>(j, k, 1, row0 + c, v);
+            else if (j.mask_bf16) read_wide<T, bf16, 8>(j, k, 1, row0 + c, v);
+            else read_wide<T, float, 8>(j, k, 1, row0 + c, v);
+        } else
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int64_t k = k0 + group * 8 + i;
-            if (k < j.len) read<T, 4>(j, k, row0 + c, j.rows - row0 - c, v[i]);
-        }
+            for (int i = 0; i < 8; ++i)
+                if (k + i < j.len) read<T>(j, k + i, row0 + c, j.rows - row0 - c, v[i]);
+    }
     unsigned top = 0;
     double total = 0.0;
     if (mine < j.rows) {
@@ -223,12 +290,21 @@ template <class T> __device__ __forceinline__ void turn_role(const Job& j, unsig
     }
 }
 
+template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_of(const Job& j, unsigned block, Shared& sh)
+{
+    if (j.wide && j.mask_wide) rows_role<T, LANES, KEEP, true>(j, block, sh); else rows_role<T, LANES, 1, false>(j, block, sh);
+}
+template <class T> __device__ __forceinline__ void rows_any(const Job& j, unsigned block, Shared& sh)
+{
+    const int lanes = row_lanes(j.len, sizeof(T) == 2);
+    if (lanes == 32) rows_of<T, 32, 4>(j, block, sh);
+    else if (lanes == 64) rows_of<T, 64, row_keep<T>()>(j, block, sh);
+    else rows_of<T, 256, row_keep<T>()>(j, block, sh);
+}
 template <class T> __device__ __forceinline__ void first_role(const Job& j, unsigned block, Shared& sh)
 {
     if (!j.along) parts_role<T>(j, block, sh);
-    else if (row_lanes(j.len, sizeof(T) == 2) == 32) rows_role<T, 32, 4>(j, block, sh);
-    else if (row_lanes(j.len, sizeof(T) == 2) == 64) rows_role<T, 64, row_keep<T>()>(j, block, sh);
-    else rows_role<T, 256, row_keep<T>()>(j, block, sh);
+    else rows_any<T>(j, block, sh);
 }
 __global__ __launch_bounds__(256) void k_quantize_first(const Jobs jobs)
 {
@@ -237,6 +313,20 @@ __global__ __launch_bounds__(256) void k_quantize_first(const Jobs jobs)
     while (i + 1 < jobs.n && blockIdx.x >= jobs.first1[i + 1]) ++i;
     const Job& j = jobs.job[i];
     if (j.bf16_) first_role<bf16>(j, blockIdx.x - jobs.first1[i], sh); else first_role<float>(j, blockIdx.x - jobs.first1[i], sh);
+}
+// one source that lies along memory: the forward pass
+template <class T, int LANES, int KEEP> __global__ __launch_bounds__(256) void k_quantize_rows(const Job j)
+{
+    __shared__ Shared sh;
+    rows_of<T, LANES, KEEP>(j, blockIdx.x, sh);
+}
+template <class T> static void rows_launch(Ctx& c, const Job& j, unsigned blocks)
+{
+    switch (row_lanes(j.len, sizeof(T) == 2)) {
+    case 32: ST_LAUNCH(c, "quantize_rows", (k_quantize_rows<T, 32, 4>), dim3(blocks), dim3(256), 0, j); break;
+    case 64: ST_LAUNCH(c, "quantize_rows", (k_quantize_rows<T, 64, row_keep<T>()>), dim3(blocks), dim3(256), 0, j); break;
+    default: ST_LAUNCH(c, "quantize_rows", (k_quantize_rows<T, 256, row_keep<T>()>), dim3(blocks), dim3(256), 0, j);
+    }
 }
 __global__ __launch_bounds__(256) void k_quantize_turn(const Jobs jobs)
 {
@@ -282,7 +372,9 @@ void quantize(Ctx& c, const QuantTask* tasks, int n)
             blocks1 += ceil_div(s.rows, 64) * j.parts;
             blocks2 += ceil_div(s.rows, 64) * j.len_tiles;
         }
-    if (blocks1) ST_LAUNCH(c, "quantize_first", k_quantize_first, dim3((unsigned)blocks1), dim3(256), 0, jobs);
+    if (jobs.n == 1 && jobs.job[0].along) {
+        if (jobs.job[0].bf16_) rows_launch<bf16>(c, jobs.job[0], (unsigned)blocks1); else rows_launch<float>(c, jobs.job[0], (unsigned)blocks1);
+    } else if (blocks1) ST_LAUNCH(c, "quantize_first", k_quantize_first, dim3((unsigned)blocks1), dim3(256), 0, jobs);
     if (!blocks2) return;
     Jobs turn;
     turn.n = 0;

@@ -79,6 +79,8 @@ template <> struct Raw8<bf16> {
         }
     }
     __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
+    // what follows unpacks the values again, instead of keeping them unpacked all the time
+    __device__ __forceinline__ void repack() { asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3])); }
     __device__ __forceinline__ void clear(int i) { w[i >> 1] &= i & 1 ? 0x0000ffffu : 0xffff0000u; }
 };
 template <> struct Raw8<float> {
@@ -94,6 +96,7 @@ template <> struct Raw8<float> {
         for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
     }
     __device__ __forceinline__ float operator[](int i) const { return v[i]; }
+    __device__ __forceinline__ void repack() {}
     __device__ __forceinline__ void clear(int i) { v[i] = 0.f; }
 };
 
