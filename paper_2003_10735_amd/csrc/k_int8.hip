@@ -423,6 +423,116 @@ void product_few(Ctx& c, const Product& p, const QuantSource* x)
     else few_launch<4, false>(c, f);
 }
 
+// ------------------------------------------------------------------------------------------------- narrow layers
+// Many tokens through a small layer (the cells of a feature map): a block takes 32 tokens, quantises them into LDS and multiplies them by
+// all of the weights, 32 channels a wavefront and v_mfma_i32_32x32x32_i8 at a time, which come from a cache.  The tokens are read once, no
+// codes go through memory and one launch does it all.  Eight threads take a token, eight values at a time; RUNS of them cover a token.
+struct NarrowArgs { Product p; const void* x; int x_wide; int64_t x_pitch; };
+constexpr int NARROW_TOKENS = 32;
+
+template <class T, int RUNS> __global__ __launch_bounds__(256) void k_int8_narrow(const NarrowArgs f)
+{
+    constexpr int STEPS = RUNS * 2, PITCH = RUNS * 64 + 16, OUT = 128 + 4;       // codes: 16 bytes on, so that rows begin on other banks
+    __shared__ __align__(16) char codes[NARROW_TOKENS * PITCH];
+    __shared__ __align__(16) int sums[NARROW_TOKENS * OUT];
+    __shared__ float scales[NARROW_TOKENS];
+    const Product& p = f.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t m0 = (int64_t)blockIdx.x * NARROW_TOKENS;
+    const int k = (int)p.k, n = (int)p.n;
+    const int r32 = lane & 31, half = lane >> 5;
+    i32x4 w[STEPS];
+    auto weights = [&](int n0) {
+        const int rows = min(32, n - n0);
+        if (rows <= 0) return;
+        const auto rsrc = operand(p.b + n0 * p.b_pitch, (rows - 1) * p.b_pitch + (k + 15) / 16 * 16);
+        const unsigned at = r32 * (unsigned)p.b_pitch + half * 16;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s)
+            w[s] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, (int)(s * 32 < k ? at + s * 32 : 0xfffffff0u), 0, 0));
+    };
+
+    const int token = threadIdx.x >> 3, t8 = threadIdx.x & 7;
+    const bool there = m0 + token < p.m;
+    const T* x = (const T*)f.x + (m0 + token) * f.x_pitch;
+    Raw8<T> v[RUNS];
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i) v[i].load(x + (i * 8 + t8) * 8, there ? k - (i * 8 + t8) * 8 : 0, f.x_wide);
+    weights(wave * 32);
+    unsigned top = 0;
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top = max(top, abs_bits(v[i][e]));
+#define ST_DPP(CTRL) top = max(top, (unsigned)__builtin_amdgcn_update_dpp(0, (int)top, CTRL, 0xf, 0xf, false))
+    ST_DPP(0xb1); ST_DPP(0x4e); ST_DPP(0x141);      // lanes 1 and 2 across in fours, then the eight's other four
+#undef ST_DPP
+    float scale;
+    const float mult = row_multiplier(top, &scale);
+    if (t8 == 0) scales[token] = scale;
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i) {
+        v[i].repack();
+        *(uint2*)(codes + token * PITCH + (i * 8 + t8) * 8) =
+            make_uint2(pack4(code_of(v[i][0], mult), code_of(v[i][1], mult), code_of(v[i][2], mult), code_of(v[i][3], mult)),
+                       pack4(code_of(v[i][4], mult), code_of(v[i][5], mult), code_of(v[i][6], mult), code_of(v[i][7], mult)));
+    }
+    __syncthreads();
+    const int64_t esz = p.out_bf16 ? 2 : 4;
+    const bool wide = ((uintptr_t)p.out & 15) == 0 && (p.out_pitch * esz & 15) == 0;
+    const int run = threadIdx.x & 15, row = threadIdx.x >> 4;
+    for (int base = 0; base < n; base += 128) {
+        if (base + wave * 32 < n) {
+            i32x16 acc = {};
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+                if (s * 32 < k) acc = __builtin_amdgcn_mfma_i32_32x32x32_i8(w[s], *(const i32x4*)(codes + r32 * PITCH + s * 32 + half * 16), acc, 0, 0, 0);
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *(i32x4*)(sums + r32 * OUT + wave * 32 + q * 8 + half * 4) = i32x4{acc[q * 4], acc[q * 4 + 1], acc[q * 4 + 2], acc[q * 4 + 3]};
+        }
+        if (base + 128 < n) weights(base + 128 + wave * 32);
+        __syncthreads();
+        const int c = base + run * 8;
+        if (c < n) {
+            Column col[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) col[i] = column_of(p, c + i);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int r = h * 16 + row;
+                if (m0 + r >= p.m) break;
+                const i32x4 lo = *(const i32x4*)(sums + r * OUT + run * 8), hi = *(const i32x4*)(sums + r * OUT + run * 8 + 4);
+                float o[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) o[i] = finish((float)(i < 4 ? lo[i] : hi[i - 4]), scales[r], col[i], p.relu);
+                store_out<8>(p, m0 + r, c, wide, o);
+            }
+        }
+        if (base + 128 < n) __syncthreads();
+    }
+}
+
+// Every block reads all of the weights: up to 64 KB of them.  Against a quantising launch and the tiled product, us a call: 14400 tokens
+// 256 -> 128 6.7 and 11.6, 256 -> 256 10.8 and 13.3, 512 -> 128 9.6 and 15.0, 200000 tokens 256 -> 128 57.5 and 91.7; but 1000 tokens 512 -> 256
+// 11.1 and 9.2, 60000 tokens 512 -> 256 56 and 41.
+bool narrow_layer(int64_t m, int64_t n, int64_t k)
+{
+    return m > FEW_TOKENS && k <= 512 && n <= 256 && k * n <= 65536;
+}
+template <class T> static void narrow_launch(Ctx& c, const NarrowArgs& f)
+{
+    const dim3 grid((unsigned)ceil_div(f.p.m, NARROW_TOKENS));
+    if (f.p.k <= 128) ST_LAUNCH(c, "int8_narrow", (k_int8_narrow<T, 2>), grid, dim3(256), 0, f);
+    else if (f.p.k <= 256) ST_LAUNCH(c, "int8_narrow", (k_int8_narrow<T, 4>), grid, dim3(256), 0, f);
+    else ST_LAUNCH(c, "int8_narrow", (k_int8_narrow<T, 8>), grid, dim3(256), 0, f);
+}
+void product_narrow(Ctx& c, const Product& p, const QuantSource& x)
+{
+    const NarrowArgs f{p, x.x, p.k % 8 == 0 && wide_ok(x.x, x.pitch, x.bf16, 8), x.pitch};
+    if (x.bf16) narrow_launch<bf16>(c, f); else narrow_launch<float>(c, f);
+}
+
 // --------------------------------------------------------------------------------------- choice of tile and split
 static int64_t tiles_of(const Extent& e, int tile) { return ceil_div(e.m, tile) * ceil_div(e.n, tile); }
 Form form_of(const Extent* e, int count)

@@ -54,6 +54,9 @@ void products(Ctx& c, const Product* p, int count);
 bool few_tokens(int64_t m);
 bool few_fused(int64_t m, int64_t k, int is_bf16);
 void product_few(Ctx& c, const Product& p, const QuantSource* x);
+// One product of many tokens by few weights, which quantises the tokens (row by row) itself.
+bool narrow_layer(int64_t m, int64_t n, int64_t k);
+void product_narrow(Ctx& c, const Product& p, const QuantSource& x);
 void fill_zero(Ctx& c, float* p, int64_t rows, int64_t cols, int64_t pitch);
 
 // ------------------------------------------------------------------ optimiser

@@ -149,6 +149,22 @@ def test_linear_large_tiles_and_splits(m, k, n):
     check_linear(m, k, n, "bf16", "f32", bias=False)
 
 
+@pytest.mark.parametrize("k", [1, 16, 63, 64, 65, 128, 129, 250, 256, 257, 512, 513])
+@pytest.mark.parametrize("n", [1, 32, 33, 120, 128, 129, 256, 257])
+def test_linear_narrow_layers(k, n):
+    """Around the sizes up to which a block takes a layer whole."""
+    for m, x_type, y_type, order in ((65, "bf16", "f32", "rows"), (97, "f32", "bf16", "inside"), (1000, "bf16", "bf16", "rows")):
+        check_linear(m, k, n, x_type, y_type, order, bias=m != 97, relu=m == 1000)
+
+
+@pytest.mark.parametrize("m", [1, 2, 3, 4, 5, 7, 8, 9, 11, 16])
+@pytest.mark.parametrize("k", [4, 200, 511, 512, 513, 1024, 2056, 4096, 4104, 8200, 32768, 40000])
+def test_linear_few_tokens(m, k):
+    """Around the sizes up to which every block quantises the tokens itself, in both types, aligned and not."""
+    check_linear(m, k, 50, "bf16", "f32")
+    check_linear(m, k, 17, "f32", "bf16", "inside")
+
+
 @pytest.mark.parametrize("m", [1, 70])
 def test_longest_sum_fits_32_bits(m):
     k, n = st.ST_INT8_MAX_SUM, 20
