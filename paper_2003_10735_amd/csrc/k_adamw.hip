@@ -7,7 +7,9 @@
 namespace st {
 
 constexpr int TILE = 2048;                 // values a block of 256 threads steps: two runs of 256 a wavefront
-constexpr int NORM_TILE = 8192, NORM_BLOCKS = 2048, NORM_PER_LAUNCH = 160;
+constexpr int NORM_BLOCKS = 2048, NORM_PER_LAUNCH = 160;
+// values of a tile of the norm: small lists are spread over more blocks
+static int norm_tile(int64_t all) { return all <= (int64_t)NORM_BLOCKS * 2048 ? 2048 : 8192; }
 constexpr float TINY = 0x1p-100f;          // a run of an 8-bit state whose largest value is less holds zeros
 
 struct TensorRef { void* p; const void* g; void* m; void* v; float* ms; float* vs; void* copy; long long n; };
@@ -24,15 +26,18 @@ struct GradList {
 };
 static_assert(sizeof(TensorList) + sizeof(AdamwConstants) + 64 <= 4096 && sizeof(GradList) + 64 <= 4096, "kernel arguments");
 
-// the last tensor that begins at or before the tile (tensors without values own no tile and are not in the list)
-__device__ __forceinline__ int tensor_of(const unsigned* first, int n, unsigned tile)
+// The last tensor that begins at or before the tile (tensors without values own no tile and are not in the list).  Every lane looks at a
+// few of them: one trip to memory, where a search by halves takes one after the other.
+template <int MOST> __device__ __forceinline__ int tensor_of(const unsigned* first, int n, unsigned tile)
 {
-    int lo = 0, hi = n - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (first[mid] <= tile) lo = mid; else hi = mid - 1;
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+#pragma unroll
+    for (int c = 0; c < MOST; c += 64) {
+        const bool there = c + lane < n;
+        before += __popcll(__ballot(there && first[there ? c + lane : 0] <= tile));
     }
-    return lo;
+    return before - 1;
 }
 
 template <class T> __device__ __forceinline__ void store4(T* p, int n, bool wide, const float (&v)[4])
@@ -58,21 +63,30 @@ __device__ __forceinline__ double block_sum(double s, double* sums)      // of 2
 // ------------------------------------------------------------------------------------------------------ norm
 // Squares and their sums in float64: no gradient that is finite makes the norm infinite, and the order of the sums does not show.  A
 // launch has NORM_BLOCKS blocks at most, so that few parts are left to be added.
-template <class G>
+template <class G, int RUNS>
 __global__ __launch_bounds__(256) void k_grad_square_sums(const GradList l, float grad_scale, unsigned tiles, double* __restrict__ parts)
 {
     __shared__ double sums[4];
+    // a block's tiles follow one another, so that the tensor is searched once
+    const unsigned each = tiles / gridDim.x, rest = tiles - each * gridDim.x;
+    unsigned tile = blockIdx.x * each + min(blockIdx.x, rest);
+    const unsigned end = tile + each + (blockIdx.x < rest ? 1 : 0);
+    int i = tensor_of<NORM_PER_LAUNCH>(l.first, l.count, tile);
     double s = 0.0;
-    for (unsigned tile = blockIdx.x; tile < tiles; tile += gridDim.x) {
-        const int i = tensor_of(l.first, l.count, tile);
+    for (; tile < end; ++tile) {
+        while (i + 1 < l.count && tile >= l.first[i + 1]) ++i;
         const G* g = (const G*)l.g[i];
-        const long long n = l.n[i], base = (long long)(tile - l.first[i]) * NORM_TILE + threadIdx.x * 8;
-        const bool wide = aligned(g, 16);
-        float v[NORM_TILE / 2048][8];
+        const long long base = (long long)(tile - l.first[i]) * (RUNS * 2048) + threadIdx.x * 8, left = l.n[i] - base;
+        // (the last run of a tensor may be no whole one)
+        const bool wide = aligned(g, 16) && (l.n[i] & 7) == 0;
+        Raw8<G> v[RUNS];
 #pragma unroll
-        for (int j = 0; j < NORM_TILE / 2048; ++j) load_run<G, 8>(g + base + j * 2048, n - base - j * 2048, wide, v[j]);
+        for (int j = 0; j < RUNS; ++j) {
+            const long long n = left - j * 2048;
+            v[j].load(g + base + j * 2048, n > 8 ? 8 : n > 0 ? (int)n : 0, wide);
+        }
 #pragma unroll
-        for (int j = 0; j < NORM_TILE / 2048; ++j)
+        for (int j = 0; j < RUNS; ++j)
 #pragma unroll
             for (int k = 0; k < 8; ++k) { const double d = (double)(v[j][k] * grad_scale); s = __builtin_fma(d, d, s); }
     }
@@ -140,7 +154,7 @@ __global__ __launch_bounds__(256) void k_adamw(const TensorList l, const AdamwCo
 {
     constexpr int RUNS = TILE / 1024;
     __shared__ double sums[4];
-    const int i = tensor_of(l.first, l.n, blockIdx.x);
+    const int i = tensor_of<ST_ADAMW_PER_LAUNCH>(l.first, l.n, blockIdx.x);
     const TensorRef& t = l.t[i];
     P* pp = (P*)t.p;
     const G* gg = (const G*)t.g;
@@ -267,6 +281,9 @@ __global__ __launch_bounds__(256) void k_adamw_state(const int8_t* __restrict__ 
 // The gradients in pieces that a launch of the norm can take: f(list, tiles).
 template <class F> static void for_grads(const st_adamw_tensor* t, int n, F f)
 {
+    int64_t all = 0;
+    for (int i = 0; i < n; ++i) all += t[i].n;
+    const int tile = norm_tile(all);
     for (int at = 0; at < n;) {
         GradList l;
         l.count = 0;
@@ -274,20 +291,20 @@ template <class F> static void for_grads(const st_adamw_tensor* t, int n, F f)
         int64_t tiles = 0;
         for (; at < n && l.count < NORM_PER_LAUNCH; ++at) {
             if (t[at].n == 0) continue;
-            const int64_t more = ceil_div(t[at].n, NORM_TILE);
+            const int64_t more = ceil_div(t[at].n, tile);
             if (l.count && tiles + more > 0x7fffffff) break;
             l.g[l.count] = t[at].grad;
             l.n[l.count] = t[at].n;
             tiles += more;
             l.first[++l.count] = (unsigned)tiles;
         }
-        if (l.count) f(l, (unsigned)tiles);
+        if (l.count) f(l, (unsigned)tiles, tile);
     }
 }
 int64_t adamw_norm_parts(const st_adamw_tensor* t, int n)
 {
     int64_t parts = 0;
-    for_grads(t, n, [&](const GradList&, unsigned tiles) { parts += std::min<unsigned>(tiles, NORM_BLOCKS); });
+    for_grads(t, n, [&](const GradList&, unsigned tiles, int) { parts += std::min<unsigned>(tiles, NORM_BLOCKS); });
     return parts;
 }
 // Calls f(list, tiles) for the list in pieces that a launch can take.
@@ -329,10 +346,13 @@ void adamw_step(Ctx& c, const st_adamw_tensor* t, int n, const st_adamw_opts& o,
     if (workspace) {
         double* parts = (double*)(workspace + 256);
         int done = 0;
-        for_grads(t, n, [&](const GradList& l, unsigned norm_tiles) {
+        for_grads(t, n, [&](const GradList& l, unsigned norm_tiles, int tile) {
             const unsigned blocks = std::min<unsigned>(norm_tiles, NORM_BLOCKS);
-            if (o.grad_dtype == ST_BF16) ST_LAUNCH(c, "grad_square_sums", k_grad_square_sums<bf16>, dim3(blocks), dim3(256), 0, l, k.grad_scale, norm_tiles, parts + done);
-            else ST_LAUNCH(c, "grad_square_sums", k_grad_square_sums<float>, dim3(blocks), dim3(256), 0, l, k.grad_scale, norm_tiles, parts + done);
+#define ST_SUMS(G, RUNS)                                                                                                          \
+    ST_LAUNCH(c, "grad_square_sums", (k_grad_square_sums<G, RUNS>), dim3(blocks), dim3(256), 0, l, k.grad_scale, norm_tiles, parts + done)
+            if (o.grad_dtype == ST_BF16) { if (tile == 2048) ST_SUMS(bf16, 1); else ST_SUMS(bf16, 4); }
+            else                         { if (tile == 2048) ST_SUMS(float, 1); else ST_SUMS(float, 4); }
+#undef ST_SUMS
             done += (int)blocks;
         });
         // Up to two rounds of blocks the step adds the parts itself: they are few then, and a launch of its own takes longer.
