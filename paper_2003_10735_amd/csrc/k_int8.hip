@@ -248,14 +248,14 @@ __global__ __launch_bounds__(256) void k_int8_join(const GemmPair pair, int64_t 
 }
 
 // --------------------------------------------------------------------------------------------------- few tokens
-// Up to 64 tokens: the weights are read once, by as many wavefronts as there are, and the tokens' codes many times.  A block takes 16
+// Up to 32 tokens: the weights are read once, by as many wavefronts as there are, and the tokens' codes many times.  A block takes 16
 // channels, each of its eight wavefronts an eighth of the contraction, 16 bytes a lane straight from memory into
 // v_mfma_i32_16x16x64_i8 (lane l supplies A[l % 16][16*(l/16) .. +15] and B[16*(l/16) .. +15][l % 16] and receives
 // D[4*(l/16) + r][l % 16]); the eighths are added in LDS.
 //
 // FUSED: every block quantises the tokens by itself, into LDS, while its first weights are on their way: the tokens are few, and a launch
 // of its own for them takes longer than the product.
-constexpr int FEW_WAVES = 8, FEW_AHEAD = 8;
+constexpr int FEW_WAVES = 8;
 
 struct FewArgs {
     Product p;
@@ -321,71 +321,90 @@ __device__ __forceinline__ void few_quantize(const FewArgs& f, char* codes, unsi
 template <int NT, bool FUSED>
 __global__ __launch_bounds__(FEW_WAVES * 64, 4) void k_int8_few(const FewArgs f)
 {
-    extern __shared__ __align__(16) char lds[];      // FUSED: the codes; then, and otherwise, the wavefronts' sums [8][NT * 256]
+    constexpr int AHEAD = FUSED ? 8 : 4;             // 64 bytes of the contraction each: loads under way twice over
+    extern __shared__ __align__(16) char lds[];      // the wavefronts' sums [8][NT * 256]; FUSED: the codes behind them
     __shared__ unsigned tops[NT * 16];
     __shared__ float scales[NT * 16];
     const Product& p = f.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t n0 = (int64_t)blockIdx.x * 16;
-    const int64_t rows = p.n - n0 < 16 ? p.n - n0 : 16;
-    const auto ra = operand(p.b + n0 * p.b_pitch, (rows - 1) * p.b_pitch + (p.k + 15) / 16 * 16);
+    char* codes = lds + FEW_WAVES * NT * 1024;
+    const auto rb = operand(p.a, FUSED ? 0 : p.m * p.a_pitch);
     const unsigned kq = (unsigned)((p.k + 63) / 64 * 64);
     const unsigned from = (unsigned)wave * f.per_wave, to = from + f.per_wave < kq ? from + f.per_wave : kq;
     const unsigned va = (lane & 15) * (unsigned)p.b_pitch + (lane >> 4) * 16;
-    i32x4 a[2][FEW_AHEAD];
-    auto ask = [&](unsigned k, i32x4 (&w)[FEW_AHEAD]) {
+    struct Group { i32x4 a[AHEAD], b[FUSED ? 1 : NT][FUSED ? 1 : AHEAD]; };
+    unsigned vb[NT];
 #pragma unroll
-        for (int u = 0; u < FEW_AHEAD; ++u) {      // (an offset beyond the buffer: zeros, and nothing is read)
-            const unsigned off = k + u * 64 < to ? va + k + u * 64 : 0xfffffff0u;
-            w[u] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, (int)off, 0, 0));
+    for (int t = 0; t < NT; ++t) {      // (columns beyond the tokens are not used)
+        const unsigned token = min(t * 16 + (lane & 15), (int)p.m - 1);
+        vb[t] = token * (unsigned)(FUSED ? f.lds_pitch : p.a_pitch) + (lane >> 4) * 16;
+    }
+    auto channels = [&](int64_t n0) {
+        const int64_t rows = p.n - n0 < 16 ? p.n - n0 : 16;
+        return operand(p.b + n0 * p.b_pitch, (rows - 1) * p.b_pitch + (p.k + 15) / 16 * 16);
+    };
+    auto ask = [&](__amdgpu_buffer_rsrc_t ra, unsigned k, Group& w) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {      // (an offset beyond the buffer: zeros, and nothing is read)
+            const bool there = k + u * 64 < to;
+            w.a[u] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(ra, (int)(there ? va + k + u * 64 : 0xfffffff0u), 0, 0));
+            if constexpr (!FUSED)
+#pragma unroll
+                for (int t = 0; t < NT; ++t)
+                    w.b[t][u] = __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(rb, (int)(there ? vb[t] + k + u * 64 : 0xfffffff0u), 0, 0));
         }
     };
-    ask(from, a[0]);
+    int64_t n0 = (int64_t)blockIdx.x * 16;
+    auto ra = channels(n0);
+    Group g[2];
+    ask(ra, from, g[0]);
     if constexpr (FUSED) {
-        if (f.x_bf16) few_quantize<bf16>(f, lds, tops, scales); else few_quantize<float>(f, lds, tops, scales);
+        if (f.x_bf16) few_quantize<bf16>(f, codes, tops, scales); else few_quantize<float>(f, codes, tops, scales);
         __syncthreads();
     }
-    int token[NT];
+    i32x4 acc[NT];
+    auto use = [&](unsigned k, const Group& w) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) token[t] = min(t * 16 + (lane & 15), (int)p.m - 1);      // (columns beyond the tokens are not used)
-    i32x4 acc[NT] = {};
-    auto use = [&](unsigned k, const i32x4 (&w)[FEW_AHEAD]) {
+        for (int u = 0; u < AHEAD; ++u) {
+            if constexpr (FUSED) {
+                if (k + u * 64 >= to) break;
+                acc[0] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w.a[u], *(const i32x4*)(codes + vb[0] + k + u * 64), acc[0], 0, 0, 0);
+            } else
 #pragma unroll
-        for (int u = 0; u < FEW_AHEAD; ++u) {
-            if (k + u * 64 >= to) break;
-#pragma unroll
-            for (int t = 0; t < NT; ++t) {
-                const unsigned at = k + u * 64 + (lane >> 4) * 16;
-                const i32x4 b = FUSED ? *(const i32x4*)(lds + token[t] * f.lds_pitch + at) : *(const i32x4*)(p.a + token[t] * p.a_pitch + at);
-                acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[u], b, acc[t], 0, 0, 0);
-            }
+                for (int t = 0; t < NT; ++t) acc[t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(w.a[u], w.b[t][u], acc[t], 0, 0, 0);
         }
     };
-    for (unsigned k = from; k < to; k += 2 * FEW_AHEAD * 64) {
-        if (k + FEW_AHEAD * 64 < to) ask(k + FEW_AHEAD * 64, a[1]);
-        use(k, a[0]);
-        if (k + FEW_AHEAD * 64 >= to) break;
-        if (k + 2 * FEW_AHEAD * 64 < to) ask(k + 2 * FEW_AHEAD * 64, a[0]);
-        use(k + FEW_AHEAD * 64, a[1]);
-    }
-    if (FUSED) __syncthreads();      // the codes are read
-    int* part = (int*)lds;
+    while (true) {
 #pragma unroll
-    for (int t = 0; t < NT; ++t) *(i32x4*)(part + (wave * NT + t) * 256 + (lane & 15) * 16 + (lane >> 4) * 4) = acc[t];
-    __syncthreads();
-    for (int i = threadIdx.x; i < NT * 256; i += FEW_WAVES * 64) {
-        const int64_t m = i >> 4, n = n0 + (i & 15);
-        if (m >= p.m || n >= p.n) continue;
-        int sum = 0;
+        for (int t = 0; t < NT; ++t) acc[t] = i32x4{0, 0, 0, 0};
+        for (unsigned k = from; k < to; k += 2 * AHEAD * 64) {
+            if (k + AHEAD * 64 < to) ask(ra, k + AHEAD * 64, g[1]);
+            use(k, g[0]);
+            if (k + AHEAD * 64 >= to) break;
+            if (k + 2 * AHEAD * 64 < to) ask(ra, k + 2 * AHEAD * 64, g[0]);
+            use(k + AHEAD * 64, g[1]);
+        }
+        const int64_t at = n0, next = FUSED ? n0 + (int64_t)gridDim.x * 16 : p.n;
+        if (next < p.n) { ra = channels(next); ask(ra, from, g[0]); }      // the next channels' weights, while these are added
+        int* part = (int*)lds;
 #pragma unroll
-        for (int w = 0; w < FEW_WAVES; ++w) sum += part[w * NT * 256 + i];
-        const float v[1] = {finish((float)sum, FUSED ? scales[m] : p.a_scale[m], column_of(p, n), p.relu)};
-        store_out<1>(p, m, n, false, v);
+        for (int t = 0; t < NT; ++t) *(i32x4*)(part + (wave * NT + t) * 256 + (lane & 15) * 16 + (lane >> 4) * 4) = acc[t];
+        __syncthreads();
+        for (int i = threadIdx.x; i < NT * 256; i += FEW_WAVES * 64) {
+            const int64_t m = i >> 4, n = at + (i & 15);
+            if (m >= p.m || n >= p.n) continue;
+            int sum = 0;
+#pragma unroll
+            for (int w = 0; w < FEW_WAVES; ++w) sum += part[w * NT * 256 + i];
+            const float v[1] = {finish((float)sum, FUSED ? scales[m] : p.a_scale[m], column_of(p, n), p.relu)};
+            store_out<1>(p, m, n, false, v);
+        }
+        if (next >= p.n) break;
+        n0 = next;
+        __syncthreads();
     }
 }
 
-constexpr int FEW_TOKENS = 64;
-bool few_tokens(int64_t m) { return m <= FEW_TOKENS; }
 static int64_t few_per_wave(int64_t k) { return round_up(ceil_div(k, FEW_WAVES), 64); }
 static int64_t few_lds(int64_t m, int64_t k) { return m * (FEW_WAVES * few_per_wave(k) + 16); }
 // wavefronts along a token, and runs of eight values that a thread has of one
@@ -395,21 +414,27 @@ static void few_shape(int64_t m, int64_t k, int* group, int* per_token)
     while (*group > 1 && (*group / 2) * 512 >= FEW_WAVES * few_per_wave(k) && FEW_WAVES / *group < m) *group /= 2;
     *per_token = (int)ceil_div(FEW_WAVES * few_per_wave(k), *group * 512);
 }
-// The tokens are quantised by every block where they are those of one matrix-core tile and a thread's share of them fits its registers.
-bool few_fused(int64_t m, int64_t k, int is_bf16)
+// FUSED where the tokens are those of one matrix-core tile and a thread's share of them fits its registers.  From five tokens on the
+// tiled product with a quantising launch before it streams large weights faster (us a call: 8 tokens 4096 -> 4096 9.5 and 14.1, 4096 -> 14336
+// 18.7 and 15.6; 4 tokens 4096 -> 14336 16.0 and 15.5, one token 12.8 and 15.3).
+bool few_fused(int64_t m, int64_t n, int64_t k, int is_bf16)
 {
-    if (m > 16) return false;
+    if (m > 16 || (m > 4 && n * k > 40000000)) return false;
     int group, per_token;
     few_shape(m, k, &group, &per_token);
     return ceil_div(m, FEW_WAVES / group) * per_token <= (is_bf16 ? few_keep<bf16>() : few_keep<float>());
 }
+// Otherwise, behind a quantising launch, against the tiled product: 12 tokens 4096 -> 4096 10.2 and 14.1, 32 tokens 11.6 and 14.3, 17 tokens
+// 4096 -> 1024 10.4 and 14.2; but 16 tokens 4096 -> 14336 22.6 and 15.6, 32 tokens 8192 -> 500 16.4 and 14.2, 64 tokens 4096 -> 4096 15.8 and 14.5.
+bool few_tokens(int64_t m, int64_t n, int64_t k) { return m <= 32 && n <= 8192 && k <= 4096; }
 
 template <int NT, bool FUSED> static void few_launch(Ctx& c, const FewArgs& f)
 {
-    size_t lds = (size_t)FEW_WAVES * NT * 1024;
-    if (FUSED) lds = std::max(lds, (size_t)few_lds(f.p.m, f.p.k));
-    ensure_dynamic_lds((const void*)k_int8_few<NT, FUSED>, FUSED ? 64 * 1024 : lds);
-    ST_LAUNCH(c, "int8_few", (k_int8_few<NT, FUSED>), dim3((unsigned)ceil_div(f.p.n, 16)), dim3(FEW_WAVES * 64), lds, f);
+    const size_t sums = (size_t)FEW_WAVES * NT * 1024, lds = sums + (FUSED ? (size_t)few_lds(f.p.m, f.p.k) : 0);
+    ensure_dynamic_lds((const void*)k_int8_few<NT, FUSED>, FUSED ? 80 * 1024 : lds);
+    // FUSED: two blocks a compute unit, every one with as many groups of channels as the others or one less
+    const int64_t groups = ceil_div(f.p.n, 16), each = FUSED ? ceil_div(groups, 512) : 1;
+    ST_LAUNCH(c, "int8_few", (k_int8_few<NT, FUSED>), dim3((unsigned)ceil_div(groups, each)), dim3(FEW_WAVES * 64), lds, f);
 }
 void product_few(Ctx& c, const Product& p, const QuantSource* x)
 {
@@ -419,8 +444,7 @@ void product_few(Ctx& c, const Product& p, const QuantSource* x)
         few_shape(p.m, p.k, &f.group, &f.per_token);
         few_launch<1, true>(c, f);
     } else if (p.m <= 16) few_launch<1, false>(c, f);
-    else if (p.m <= 32) few_launch<2, false>(c, f);
-    else few_launch<4, false>(c, f);
+    else few_launch<2, false>(c, f);
 }
 
 // ------------------------------------------------------------------------------------------------- narrow layers
@@ -518,7 +542,7 @@ template <class T, int RUNS> __global__ __launch_bounds__(256) void k_int8_narro
 // 11.1 and 9.2, 60000 tokens 512 -> 256 56 and 41.
 bool narrow_layer(int64_t m, int64_t n, int64_t k)
 {
-    return m > FEW_TOKENS && k <= 512 && n <= 256 && k * n <= 65536;
+    return m > 32 && k <= 512 && n <= 256 && k * n <= 65536;
 }
 template <class T> static void narrow_launch(Ctx& c, const NarrowArgs& f)
 {

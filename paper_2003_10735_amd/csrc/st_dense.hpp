@@ -51,8 +51,8 @@ struct Form { int tile; int splits[2]; };
 Form form_of(const Extent* e, int count);
 void products(Ctx& c, const Product* p, int count);
 // One product of few tokens: a launch of its own kind.  x: the tokens, row by row, which it quantises itself; null: p.a holds their codes.
-bool few_tokens(int64_t m);
-bool few_fused(int64_t m, int64_t k, int is_bf16);
+bool few_tokens(int64_t m, int64_t n, int64_t k);
+bool few_fused(int64_t m, int64_t n, int64_t k, int is_bf16);
 void product_few(Ctx& c, const Product& p, const QuantSource* x);
 // One product of many tokens by few weights, which quantises the tokens (row by row) itself.
 bool narrow_layer(int64_t m, int64_t n, int64_t k);

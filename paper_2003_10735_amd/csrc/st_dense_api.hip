@@ -148,11 +148,11 @@ int st_int8_linear(const st_matrix* x, const int8_t* wq, int64_t w_pitch, const 
     Ctx c{(hipStream_t)stream, ST_OK};
     const QuantSource tokens = source(*x, along, false);
     const Product p{s.x.q, s.x.pitch, s.x.scale, wq, w_pitch, w_scale, m, n, k, y, y_dtype == ST_BF16, y_pitch, bias, relu, s.slabs};
-    if (along && few_fused(m, k, tokens.bf16)) { product_few(c, p, &tokens); return c.status; }
+    if (along && few_fused(m, n, k, tokens.bf16)) { product_few(c, p, &tokens); return c.status; }
     if (along && narrow_layer(m, n, k)) { product_narrow(c, p, tokens); return c.status; }
     const QuantTask task{tokens, s.x, s.parts, nullptr, nullptr};
     quantize(c, &task, 1);
-    if (few_tokens(m)) product_few(c, p, nullptr); else
+    if (few_tokens(m, n, k)) product_few(c, p, nullptr); else
     products(c, &p, 1);
     return c.status;
 }
