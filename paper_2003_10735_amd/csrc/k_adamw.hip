@@ -40,17 +40,30 @@ template <int MOST> __device__ __forceinline__ int tensor_of(const unsigned* fir
     return before - 1;
 }
 
-template <class T> __device__ __forceinline__ void store4(T* p, int n, bool wide, const float (&v)[4])
+template <class T> __device__ __forceinline__ void store4(T* p, int n, const float (&v)[4])
 {
-    if (wide && n >= 4) {
+    if (n >= 4) {
         typedef T T4 __attribute__((ext_vector_type(4)));
-        *(T4*)p = T4{from_f32<T>(v[0]), from_f32<T>(v[1]), from_f32<T>(v[2]), from_f32<T>(v[3])};
+        typedef T4 T4any __attribute__((aligned(sizeof(T))));
+        *(T4any*)p = T4{from_f32<T>(v[0]), from_f32<T>(v[1]), from_f32<T>(v[2]), from_f32<T>(v[3])};
         return;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) if (i < n) p[i] = from_f32<T>(v[i]);
 }
-__device__ __forceinline__ bool aligned(const void* p, unsigned bytes) { return ((uintptr_t)p & (bytes - 1)) == 0; }
+// four codes, of which `n` exist
+__device__ __forceinline__ unsigned load_codes(const void* p, int n)
+{
+    if (n >= 4) return *(const u32_1*)p;
+    unsigned c = 0;
+    for (int e = 0; e < n; ++e) c |= (unsigned)((const uint8_t*)p)[e] << (8 * e);
+    return c;
+}
+__device__ __forceinline__ void store_codes(void* p, int n, unsigned c)
+{
+    if (n >= 4) { *(u32_1*)p = c; return; }
+    for (int e = 0; e < n; ++e) ((uint8_t*)p)[e] = (uint8_t)(c >> (8 * e));
+}
 __device__ __forceinline__ double block_sum(double s, double* sums)      // of 256 threads, in one order; to every thread
 {
 #pragma unroll
@@ -77,13 +90,11 @@ __global__ __launch_bounds__(256) void k_grad_square_sums(const GradList l, floa
         while (i + 1 < l.count && tile >= l.first[i + 1]) ++i;
         const G* g = (const G*)l.g[i];
         const long long base = (long long)(tile - l.first[i]) * (RUNS * 2048) + threadIdx.x * 8, left = l.n[i] - base;
-        // (the last run of a tensor may be no whole one)
-        const bool wide = aligned(g, 16) && (l.n[i] & 7) == 0;
         Raw8<G> v[RUNS];
 #pragma unroll
         for (int j = 0; j < RUNS; ++j) {
             const long long n = left - j * 2048;
-            v[j].load(g + base + j * 2048, n > 8 ? 8 : n > 0 ? (int)n : 0, wide);
+            v[j].load(g + base + j * 2048, n > 8 ? 8 : n > 0 ? (int)n : 0);
         }
 #pragma unroll
         for (int j = 0; j < RUNS; ++j)
@@ -158,8 +169,6 @@ __global__ __launch_bounds__(256) void k_adamw(const TensorList l, const AdamwCo
     const TensorRef& t = l.t[i];
     P* pp = (P*)t.p;
     const G* gg = (const G*)t.g;
-    const bool wp = aligned(pp, 4 * sizeof(P)), wg = aligned(gg, 4 * sizeof(G)), wc = aligned(t.copy, 8);
-    const bool wm = aligned(t.m, BITS == 8 ? 4 : 16) && aligned(t.v, BITS == 8 ? 4 : 16);
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const long long base = (long long)(blockIdx.x - l.first[i]) * TILE + wave * (RUNS * 256);
     float p[RUNS][4], g[RUNS][4], m[RUNS][4], v[RUNS][4], ms[RUNS], vs[RUNS];
@@ -169,19 +178,15 @@ __global__ __launch_bounds__(256) void k_adamw(const TensorList l, const AdamwCo
     for (int j = 0; j < RUNS; ++j) {
         const long long run = base + j * 256, at = run + lane * 4;
         n[j] = t.n - at >= 4 ? 4 : t.n - at > 0 ? (int)(t.n - at) : 0;
-        load_run<P, 4>(pp + at, n[j], wp, p[j]);
-        load_run<G, 4>(gg + at, n[j], wg, g[j]);
+        load4(pp + at, n[j], p[j]);
+        load4(gg + at, n[j], g[j]);
         if constexpr (BITS == 32) {
-            load_run<float, 4>((const float*)t.m + at, n[j], wm, m[j]);
-            load_run<float, 4>((const float*)t.v + at, n[j], wm, v[j]);
+            load4((const float*)t.m + at, n[j], m[j]);
+            load4((const float*)t.v + at, n[j], v[j]);
         } else {
-            cm[j] = cv[j] = 0; ms[j] = vs[j] = 0.f;
+            ms[j] = vs[j] = 0.f;
             if (run < t.n) { ms[j] = t.ms[run / 256]; vs[j] = t.vs[run / 256]; }
-            if (wm && n[j] == 4) { cm[j] = *(const unsigned*)((const char*)t.m + at); cv[j] = *(const unsigned*)((const char*)t.v + at); }
-            else for (int e = 0; e < n[j]; ++e) {
-                cm[j] |= (unsigned)((const uint8_t*)t.m)[at + e] << (8 * e);
-                cv[j] |= (unsigned)((const uint8_t*)t.v)[at + e] << (8 * e);
-            }
+            cm[j] = load_codes((const char*)t.m + at, n[j]); cv[j] = load_codes((const char*)t.v + at, n[j]);
         }
     }
     float factor = k.grad_scale;
@@ -211,11 +216,11 @@ __global__ __launch_bounds__(256) void k_adamw(const TensorList l, const AdamwCo
             u[e] = BITS == 8 ? sqrt_rn(v[j][e]) : sqrtf(v[j][e]);
             p[j][e] = p[j][e] * decay - k.step_scale * (m[j][e] * __builtin_amdgcn_rcpf(u[e] * k.inv_sqrt_bc2 + k.eps));
         }
-        store4(pp + at, n[j], wp, p[j]);
-        if (t.copy) store4((bf16*)t.copy + at, n[j], wc, p[j]);
+        store4(pp + at, n[j], p[j]);
+        if (t.copy) store4((bf16*)t.copy + at, n[j], p[j]);
         if constexpr (BITS == 32) {
-            store4((float*)t.m + at, n[j], wm, m[j]);
-            store4((float*)t.v + at, n[j], wm, v[j]);
+            store4((float*)t.m + at, n[j], m[j]);
+            store4((float*)t.v + at, n[j], v[j]);
         } else {
             unsigned tm = 0, tv = 0;
 #pragma unroll
@@ -233,11 +238,7 @@ __global__ __launch_bounds__(256) void k_adamw(const TensorList l, const AdamwCo
                 qm |= (unsigned)(uint8_t)(m[j][e] < 0.f ? -a : a) << (8 * e);
                 qv |= (unsigned)(uint8_t)b << (8 * e);
             }
-            if (wm && n[j] == 4) { *(unsigned*)((char*)t.m + at) = qm; *(unsigned*)((char*)t.v + at) = qv; }
-            else for (int e = 0; e < n[j]; ++e) {
-                ((uint8_t*)t.m)[at + e] = (uint8_t)(qm >> (8 * e));
-                ((uint8_t*)t.v)[at + e] = (uint8_t)(qv >> (8 * e));
-            }
+            store_codes((char*)t.m + at, n[j], qm); store_codes((char*)t.v + at, n[j], qv);
         }
     }
 }
@@ -248,32 +249,27 @@ __global__ __launch_bounds__(256) void k_adamw_state(const int8_t* __restrict__ 
 {
     const long long at = ((long long)blockIdx.x * 256 + threadIdx.x) * 4;
     if (at >= n) return;
-    const int cnt = n - at >= 4 ? 4 : (int)(n - at);
-    const bool whole = cnt == 4;
+    const int count = n - at >= 4 ? 4 : (int)(n - at);
+    float o[4];
     if (m_out) {
         const float s = ms[at / 256];
-        float o[4];
-        const bool wide = whole && aligned(m, 4);
-        const unsigned c = wide ? *(const unsigned*)(m + at) : 0;
+        const unsigned c = load_codes(m + at, count);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float q = (float)(wide ? (int8_t)(c >> (8 * e)) : e < cnt ? m[at + e] : (int8_t)0);
+            const float q = (float)(int8_t)(c >> (8 * e));
             o[e] = q * fabsf(q) * s;
         }
-        store4(m_out + at, cnt, aligned(m_out, 16), o);
+        store4(m_out + at, count, o);
     }
     if (v_out) {
         const float s = vs[at / 256];
-        float o[4];
-        const bool wide = whole && aligned(v, 4);
-        const unsigned c = wide ? *(const unsigned*)(v + at) : 0;
+        const unsigned c = load_codes(v + at, count);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            const float q = (float)(wide ? (uint8_t)(c >> (8 * e)) : e < cnt ? v[at + e] : (uint8_t)0);
-            const float root = q * q * s;
+            const float q = (float)(uint8_t)(c >> (8 * e)), root = q * q * s;
             o[e] = root * root;
         }
-        store4(v_out + at, cnt, aligned(v_out, 16), o);
+        store4(v_out + at, count, o);
     }
 }
 

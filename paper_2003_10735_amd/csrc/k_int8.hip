@@ -49,26 +49,29 @@ __device__ __forceinline__ Column column_of(const Product& p, int64_t n)
 {
     return n < p.n ? Column{p.b_scale[n], p.bias ? p.bias[n] : 0.f} : Column{0.f, 0.f};
 }
-// `count` values of one row, channels n .. n + count - 1: at once where `wide`, else those that exist one by one
-template <int COUNT> __device__ __forceinline__ void store_out(const Product& p, int64_t m, int64_t n, bool wide, const float (&v)[COUNT])
+// COUNT values of one row, channels n .. n + COUNT - 1: at once, or at the end of the row those that exist one by one
+template <int COUNT> __device__ __forceinline__ void store_out(const Product& p, int64_t m, int64_t n, const float (&v)[COUNT])
 {
     if (p.out_bf16) {
         bf16* o = (bf16*)p.out + m * p.out_pitch + n;
-        if (wide && n + COUNT <= p.n) {
+        if (n + COUNT <= p.n) {
             typedef bf16 T __attribute__((ext_vector_type(COUNT)));
+            typedef T T2 __attribute__((aligned(2)));
             T u;
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) u[i] = (bf16)v[i];
-            *(T*)o = u;
+            *(T2*)o = u;
             return;
         }
 #pragma unroll
         for (int i = 0; i < COUNT; ++i) if (n + i < p.n) o[i] = (bf16)v[i];
     } else {
         float* o = (float*)p.out + m * p.out_pitch + n;
-        if (wide && n + COUNT <= p.n) {
+        if (n + COUNT <= p.n) {
+            if constexpr (COUNT == 1) *o = v[0];
+            else
 #pragma unroll
-            for (int i = 0; i < COUNT; i += 4) *(float4*)(o + i) = make_float4(v[i], v[i + 1], v[i + 2], v[i + 3]);
+                for (int i = 0; i < COUNT; i += 4) *(f32x4_4*)(o + i) = f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
             return;
         }
 #pragma unroll
@@ -193,9 +196,6 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
     Column col[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) col[i] = g.splits > 1 ? Column{0.f, 0.f} : column_of(p, n + i);
-    const int64_t esz = p.out_bf16 ? 2 : 4;
-    const bool wide = ((uintptr_t)p.out & 15) == 0 && (p.out_pitch * esz & 15) == 0;
-    const bool wide_slab = (p.n & 3) == 0;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
 #pragma unroll
@@ -214,7 +214,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
             if (m >= p.m) continue;
             if (g.splits > 1) {
                 int* to = p.slabs + ((int64_t)split * p.m + m) * p.n + n;
-                if (wide_slab && n + 8 <= p.n) { ((i32x4*)to)[0] = lo; ((i32x4*)to)[1] = hi; }
+                if (n + 8 <= p.n) { ((i32x4_4*)to)[0] = lo; ((i32x4_4*)to)[1] = hi; }
                 else
 #pragma unroll
                     for (int i = 0; i < 8; ++i) if (n + i < p.n) to[i] = i < 4 ? lo[i] : hi[i - 4];
@@ -224,7 +224,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = finish((float)(i < 4 ? lo[i] : hi[i - 4]), sm, col[i], p.relu);
-            store_out<8>(p, m, n, wide, v);
+            store_out<8>(p, m, n, v);
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -243,7 +243,7 @@ __global__ __launch_bounds__(256) void k_int8_join(const GemmPair pair, int64_t 
 #pragma unroll 4
         for (int s = 0; s < g.splits; ++s) sum += p.slabs[(int64_t)s * size + at];
         const float v[1] = {finish((float)sum, p.a_scale[m], column_of(p, n), p.relu)};
-        store_out<1>(p, m, n, false, v);
+        store_out<1>(p, m, n, v);
     }
 }
 
@@ -259,7 +259,7 @@ constexpr int FEW_WAVES = 8;
 
 struct FewArgs {
     Product p;
-    const void* x; int x_bf16, x_wide; int64_t x_pitch;      // FUSED: the tokens as they are, row by row
+    const void* x; int x_bf16; int64_t x_pitch;      // FUSED: the tokens as they are, row by row
     int per_wave;                                            // bytes of the contraction a wavefront takes, a multiple of 64
     int lds_pitch;                                           // FUSED: bytes between two tokens' codes in LDS
     int group, per_token;                                    // FUSED: wavefronts along a token, a power of two; a thread's runs of a token
@@ -283,7 +283,7 @@ __device__ __forceinline__ void few_quantize(const FewArgs& f, char* codes, unsi
 #pragma unroll
     for (int j = 0; j < KEEP; ++j) {
         const int at = (c * threads + lane) * 8;
-        if (r < m) v[j].load((const T*)f.x + r * f.x_pitch + at, k - at, f.x_wide);
+        if (r < m) v[j].load((const T*)f.x + r * f.x_pitch + at, k - at);
         if (++c == f.per_token) { c = 0; r += step; }
     }
     __syncthreads();
@@ -397,7 +397,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 4) void k_int8_few(const FewArgs f)
 #pragma unroll
             for (int w = 0; w < FEW_WAVES; ++w) sum += part[w * NT * 256 + i];
             const float v[1] = {finish((float)sum, FUSED ? scales[m] : p.a_scale[m], column_of(p, n), p.relu)};
-            store_out<1>(p, m, n, false, v);
+            store_out<1>(p, m, n, v);
         }
         if (next >= p.n) break;
         n0 = next;
@@ -438,9 +438,9 @@ template <int NT, bool FUSED> static void few_launch(Ctx& c, const FewArgs& f)
 }
 void product_few(Ctx& c, const Product& p, const QuantSource* x)
 {
-    FewArgs f{p, nullptr, 0, 0, 0, (int)few_per_wave(p.k), (int)(FEW_WAVES * few_per_wave(p.k) + 16), 0, 0};
+    FewArgs f{p, nullptr, 0, 0, (int)few_per_wave(p.k), (int)(FEW_WAVES * few_per_wave(p.k) + 16), 0, 0};
     if (x) {
-        f.x = x->x; f.x_bf16 = x->bf16; f.x_pitch = x->pitch; f.x_wide = p.k % 8 == 0 && wide_ok(x->x, x->pitch, x->bf16, 8);
+        f.x = x->x; f.x_bf16 = x->bf16; f.x_pitch = x->pitch;
         few_shape(p.m, p.k, &f.group, &f.per_token);
         few_launch<1, true>(c, f);
     } else if (p.m <= 16) few_launch<1, false>(c, f);
@@ -451,7 +451,7 @@ void product_few(Ctx& c, const Product& p, const QuantSource* x)
 // Many tokens through a small layer (the cells of a feature map): a block takes 32 tokens, quantises them into LDS and multiplies them by
 // all of the weights, 32 channels a wavefront and v_mfma_i32_32x32x32_i8 at a time, which come from a cache.  The tokens are read once, no
 // codes go through memory and one launch does it all.  Eight threads take a token, eight values at a time; RUNS of them cover a token.
-struct NarrowArgs { Product p; const void* x; int x_wide; int64_t x_pitch; };
+struct NarrowArgs { Product p; const void* x; int64_t x_pitch; };
 constexpr int NARROW_TOKENS = 32;
 
 template <class T, int RUNS> __global__ __launch_bounds__(256) void k_int8_narrow(const NarrowArgs f)
@@ -481,7 +481,7 @@ template <class T, int RUNS> __global__ __launch_bounds__(256) void k_int8_narro
     const T* x = (const T*)f.x + (m0 + token) * f.x_pitch;
     Raw8<T> v[RUNS];
 #pragma unroll
-    for (int i = 0; i < RUNS; ++i) v[i].load(x + (i * 8 + t8) * 8, there ? k - (i * 8 + t8) * 8 : 0, f.x_wide);
+    for (int i = 0; i < RUNS; ++i) v[i].load(x + (i * 8 + t8) * 8, there ? k - (i * 8 + t8) * 8 : 0);
     weights(wave * 32);
     unsigned top = 0;
 #pragma unroll
@@ -502,8 +502,6 @@ template <class T, int RUNS> __global__ __launch_bounds__(256) void k_int8_narro
                        pack4(code_of(v[i][4], mult), code_of(v[i][5], mult), code_of(v[i][6], mult), code_of(v[i][7], mult)));
     }
     __syncthreads();
-    const int64_t esz = p.out_bf16 ? 2 : 4;
-    const bool wide = ((uintptr_t)p.out & 15) == 0 && (p.out_pitch * esz & 15) == 0;
     const int run = threadIdx.x & 15, row = threadIdx.x >> 4;
     for (int base = 0; base < n; base += 128) {
         if (base + wave * 32 < n) {
@@ -530,7 +528,7 @@ template <class T, int RUNS> __global__ __launch_bounds__(256) void k_int8_narro
                 float o[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[i] = finish((float)(i < 4 ? lo[i] : hi[i - 4]), scales[r], col[i], p.relu);
-                store_out<8>(p, m0 + r, c, wide, o);
+                store_out<8>(p, m0 + r, c, o);
             }
         }
         if (base + 128 < n) __syncthreads();
@@ -553,7 +551,7 @@ template <class T> static void narrow_launch(Ctx& c, const NarrowArgs& f)
 }
 void product_narrow(Ctx& c, const Product& p, const QuantSource& x)
 {
-    const NarrowArgs f{p, x.x, p.k % 8 == 0 && wide_ok(x.x, x.pitch, x.bf16, 8), x.pitch};
+    const NarrowArgs f{p, x.x, x.pitch};
     if (x.bf16) narrow_launch<bf16>(c, f); else narrow_launch<float>(c, f);
 }
 
@@ -572,7 +570,7 @@ Form form_of(const Extent* e, int count)
     const int64_t each = std::max<int64_t>(8, ceil_div(work, 256));
     for (int i = 0; i < count; ++i) {
         const int64_t stages = ceil_div(e[i].k, STAGE);
-        int64_t s = total(f.tile) < 256 && stages > 16 ? stages / each : 1;
+        int64_t s = stages > 16 ? stages / each : 1;
         s = std::max(s, ceil_div(stages, ST_INT8_MAX_SUM / STAGE));    // what int32 can hold
         f.splits[i] = (int)std::max<int64_t>(s, 1);
     }

@@ -22,40 +22,39 @@ struct Job {
     float *scale, *sum, *part_max, *part_sum;
     int parts;
     unsigned len_tiles;
-    // wide, mask_wide: aligned for the role's loads (rows: and a whole number of runs)
-    uint8_t bf16_, mask_bf16, wide, mask_wide, along;
+    uint8_t bf16_, mask_bf16, along;
 };
 struct Jobs { unsigned first1[4], first2[4]; int n; Job job[4]; };      // first block of each job in the two launches
 
 // Four neighbouring values, one load.
 template <class T> struct Raw4;
 template <> struct Raw4<bf16> {
-    uint2 u;
-    __device__ __forceinline__ void load(const bf16* p) { u = *(const uint2*)p; }
-    __device__ __forceinline__ float operator[](int i) const { const unsigned w = i & 2 ? u.y : u.x; return __uint_as_float(i & 1 ? w & 0xffff0000u : w << 16); }
+    u32x2 u;
+    __device__ __forceinline__ void load(const bf16* p) { u = *(const u32x2_2*)p; }
+    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i & 1 ? u[i >> 1] & 0xffff0000u : u[i >> 1] << 16); }
 };
 template <> struct Raw4<float> {
-    float4 u;
-    __device__ __forceinline__ void load(const float* p) { u = *(const float4*)p; }
-    __device__ __forceinline__ float operator[](int i) const { return i == 0 ? u.x : i == 1 ? u.y : i == 2 ? u.z : u.w; }
+    f32x4_t u;
+    __device__ __forceinline__ void load(const float* p) { u = *(const f32x4_4*)p; }
+    __device__ __forceinline__ float operator[](int i) const { return u[i]; }
 };
 template <> struct Raw4<void> {};      // no mask
 
-// Four values at `at` of position `line`, of which `n` exist, zero where the mask is not positive: the way of any alignment.
+// Four values at `at` of position `line`, of which `n` exist, zero where the mask is not positive.
 template <class T> __device__ __forceinline__ void read(const Job& j, int64_t line, int64_t at, int64_t n, float (&v)[4])
 {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = i < n ? to_f32(((const T*)j.x)[line * j.pitch + at + i]) : 0.f;
+    const int count = n < 4 ? (int)n : 4;
+    load4((const T*)j.x + line * j.pitch + at, count, v);
     if (!j.mask) return;
+    float m[4];
+    if (j.mask_bf16) load4((const bf16*)j.mask + line * j.mask_pitch + at, count, m);
+    else load4((const float*)j.mask + line * j.mask_pitch + at, count, m);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int64_t m = line * j.mask_pitch + at + i;
-        if (i < n && !((j.mask_bf16 ? to_f32(((const bf16*)j.mask)[m]) : ((const float*)j.mask)[m]) > 0.f)) v[i] = 0.f;
-    }
+    for (int i = 0; i < 4; ++i) v[i] = m[i] > 0.f ? v[i] : 0.f;
 }
-// COUNT of them, `step` positions apart, by wide loads that are all under way before the first is used.  M: the mask's type, or void.
+// COUNT fours, `step` positions apart, all under way before the first is used.  M: the mask's type, or void.
 template <class T, class M, int COUNT>
-__device__ __forceinline__ void read_wide(const Job& j, int64_t line, int step, int64_t at, float (&v)[COUNT][4])
+__device__ __forceinline__ void read_all(const Job& j, int64_t line, int step, int64_t at, float (&v)[COUNT][4])
 {
     Raw4<T> x[COUNT];
     Raw4<M> m[COUNT];
@@ -72,10 +71,10 @@ __device__ __forceinline__ void read_wide(const Job& j, int64_t line, int step, 
             if constexpr (!std::is_void<M>::value) v[i][e] = m[i][e] > 0.f ? v[i][e] : 0.f;
         }
 }
-template <class M, class T> __device__ __forceinline__ void clear_masked(const M* m, int n, bool wide, Raw8<T>& v)
+template <class M, class T> __device__ __forceinline__ void clear_masked(const M* m, int n, Raw8<T>& v)
 {
     Raw8<M> on;
-    on.load(m, n, wide);
+    on.load(m, n);
 #pragma unroll
     for (int i = 0; i < 8; ++i) if (!(on[i] > 0.f)) v.clear(i);
 }
@@ -93,9 +92,9 @@ struct Shared {
 // LANES threads a row.  A thread holds KEEP runs of eight values of its row, as they came, between the search for the largest and the
 // rounding, so a row of up to 8 * KEEP * LANES values is read once; longer rows read the rest twice.  A wavefront takes a row of up to 4096
 // bfloat16 values by itself: no barrier, eight loads under way.
-template <class T, int LANES, int KEEP, bool WIDE> __device__ __forceinline__ void rows_role(const Job& j, unsigned block, Shared& sh)
+template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_role(const Job& j, unsigned block, Shared& sh)
 {
-    constexpr int MORE = WIDE ? 4 : 1;      // runs under way beyond those
+    constexpr int MORE = 4;      // runs under way beyond those
     const int lane = threadIdx.x % LANES;
     const int64_t row = (int64_t)block * (256 / LANES) + threadIdx.x / LANES;
     const bool there = row < j.rows;
@@ -103,12 +102,12 @@ template <class T, int LANES, int KEEP, bool WIDE> __device__ __forceinline__ vo
     const T* x = (const T*)j.x + row * j.pitch;
     unsigned top = 0;
     double total = 0.0;
-    auto load = [&](int at, Raw8<T>& v) { v.load(x + at, there ? len - at : 0, WIDE); };
+    auto load = [&](int at, Raw8<T>& v) { v.load(x + at, there ? len - at : 0); };
     auto mask = [&](int at, Raw8<T>& v) {
         if (!j.mask) return;
         const int n = there ? len - at : 0;
-        if (j.mask_bf16) clear_masked((const bf16*)j.mask + row * j.mask_pitch + at, n, WIDE, v);
-        else clear_masked((const float*)j.mask + row * j.mask_pitch + at, n, WIDE, v);
+        if (j.mask_bf16) clear_masked((const bf16*)j.mask + row * j.mask_pitch + at, n, v);
+        else clear_masked((const float*)j.mask + row * j.mask_pitch + at, n, v);
     };
     auto see = [&](const Raw8<T>& v) {
 #pragma unroll
@@ -174,7 +173,7 @@ static __host__ __device__ __forceinline__ int row_lanes(int64_t len, int is_bf1
 // --------------------------------------------------------------------------------------- rows that lie across it
 // The source is a matrix [len][pitch] whose columns are the operand's rows.  Sixteen threads take 64 columns of a position, sixteen
 // positions at once: whole lines of memory are read.  A block leaves the largest value and the sum of 64 columns over one part.
-template <class T, class M> __device__ __forceinline__ void parts_loop(const Job& j, int64_t col, int64_t from, int64_t to, int group, bool wide,
+template <class T, class M> __device__ __forceinline__ void parts_loop(const Job& j, int64_t col, int64_t from, int64_t to, int group, bool whole,
                                                                        unsigned (&top)[4], double (&total)[4])
 {
     for (int64_t piece = from + group; piece < to; piece += 1024) {     // float32 sums of 64 values, added in float64
@@ -185,10 +184,10 @@ template <class T, class M> __device__ __forceinline__ void parts_loop(const Job
 #pragma unroll
             for (int e = 0; e < 4; ++e) { top[e] = max(top[e], abs_bits(v[e])); s[e] += v[e]; }
         };
-        if (wide)
+        if (whole)
             for (; k + 48 < end; k += 64) {
                 float v[4][4];
-                read_wide<T, M, 4>(j, k, 16, col, v);
+                read_all<T, M, 4>(j, k, 16, col, v);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) see(v[i]);
             }
@@ -207,13 +206,13 @@ template <class T> __device__ __forceinline__ void parts_role(const Job& j, unsi
     const int c = (threadIdx.x & 15) * 4, group = threadIdx.x >> 4;
     const int64_t col = (int64_t)tile * 64 + c;
     const int64_t from = part * j.per_part, to = from + j.per_part < j.len ? from + j.per_part : j.len;
-    const bool wide = j.wide && j.mask_wide && col + 4 <= j.rows;
+    const bool whole = col + 4 <= j.rows;
     unsigned top[4] = {};
     double total[4] = {};
     if (col < j.rows) {
-        if (!j.mask) parts_loop<T, void>(j, col, from, to, group, wide, top, total);
-        else if (j.mask_bf16) parts_loop<T, bf16>(j, col, from, to, group, wide, top, total);
-        else parts_loop<T, float>(j, col, from, to, group, wide, top, total);
+        if (!j.mask) parts_loop<T, void>(j, col, from, to, group, whole, top, total);
+        else if (j.mask_bf16) parts_loop<T, bf16>(j, col, from, to, group, whole, top, total);
+        else parts_loop<T, float>(j, col, from, to, group, whole, top, total);
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) { sh.parts.tops[group][c + i] = top[i]; sh.parts.sums[group][c + i] = (float)total[i]; }
@@ -241,10 +240,10 @@ template <class T> __device__ __forceinline__ void turn_role(const Job& j, unsig
     float v[8][4] = {};
     if (j.q && row0 + c < j.rows) {
         const int64_t k = k0 + group * 8;
-        if (j.wide && j.mask_wide && row0 + c + 4 <= j.rows && k + 8 <= j.len) {
-            if (!j.mask) read_wide<T, void, 8>(j, k, 1, row0 + c, v);
-            else if (j.mask_bf16) read_wide<T, bf16, 8>(j, k, 1, row0 + c, v);
-            else read_wide<T, float, 8>(j, k, 1, row0 + c, v);
+        if (row0 + c + 4 <= j.rows && k + 8 <= j.len) {
+            if (!j.mask) read_all<T, void, 8>(j, k, 1, row0 + c, v);
+            else if (j.mask_bf16) read_all<T, bf16, 8>(j, k, 1, row0 + c, v);
+            else read_all<T, float, 8>(j, k, 1, row0 + c, v);
         } else
 #pragma unroll
             for (int i = 0; i < 8; ++i)
@@ -290,16 +289,12 @@ template <class T> __device__ __forceinline__ void turn_role(const Job& j, unsig
     }
 }
 
-template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_of(const Job& j, unsigned block, Shared& sh)
-{
-    if (j.wide && j.mask_wide) rows_role<T, LANES, KEEP, true>(j, block, sh); else rows_role<T, LANES, 1, false>(j, block, sh);
-}
 template <class T> __device__ __forceinline__ void rows_any(const Job& j, unsigned block, Shared& sh)
 {
     const int lanes = row_lanes(j.len, sizeof(T) == 2);
-    if (lanes == 32) rows_of<T, 32, 4>(j, block, sh);
-    else if (lanes == 64) rows_of<T, 64, row_keep<T>()>(j, block, sh);
-    else rows_of<T, 256, row_keep<T>()>(j, block, sh);
+    if (lanes == 32) rows_role<T, 32, 4>(j, block, sh);
+    else if (lanes == 64) rows_role<T, 64, row_keep<T>()>(j, block, sh);
+    else rows_role<T, 256, row_keep<T>()>(j, block, sh);
 }
 template <class T> __device__ __forceinline__ void first_role(const Job& j, unsigned block, Shared& sh)
 {
@@ -318,7 +313,7 @@ __global__ __launch_bounds__(256) void k_quantize_first(const Jobs jobs)
 template <class T, int LANES, int KEEP> __global__ __launch_bounds__(256) void k_quantize_rows(const Job j)
 {
     __shared__ Shared sh;
-    rows_of<T, LANES, KEEP>(j, blockIdx.x, sh);
+    rows_role<T, LANES, KEEP>(j, blockIdx.x, sh);
 }
 template <class T> static void rows_launch(Ctx& c, const Job& j, unsigned blocks)
 {
@@ -360,11 +355,8 @@ void quantize(Ctx& c, const QuantTask* tasks, int n)
             if (s.along != pass || s.rows == 0) continue;
             jobs.first1[jobs.n] = (unsigned)blocks1; jobs.first2[jobs.n] = (unsigned)blocks2;
             Job& j = jobs.job[jobs.n++];
-            const int run = s.along ? 8 : 4;
-            const bool whole = !s.along || s.len % 8 == 0;
             j = Job{s.x, s.mask, s.pitch, s.mask_pitch, s.rows, s.len, t.to.pitch, 0, t.to.q, t.to.scale, t.sum, t.to.q ? t.part_max : nullptr,
-                    t.sum ? t.part_sum : nullptr, 1, 1, (uint8_t)s.bf16, (uint8_t)s.mask_bf16, (uint8_t)(whole && wide_ok(s.x, s.pitch, s.bf16, run)),
-                    (uint8_t)(whole && wide_ok(s.mask, s.mask_pitch, s.mask_bf16, run)), (uint8_t)s.along};
+                    t.sum ? t.part_sum : nullptr, 1, 1, (uint8_t)s.bf16, (uint8_t)s.mask_bf16, (uint8_t)s.along};
             if (s.along) { blocks1 += ceil_div(s.rows, 256 / row_lanes(s.len, s.bf16)); continue; }
             j.parts = transpose_parts(s.rows, s.len);
             j.per_part = ceil_div(s.len, j.parts);

@@ -5,6 +5,7 @@
 namespace st {
 
 typedef int i32x4 __attribute__((ext_vector_type(4)));
+typedef i32x4 i32x4_4 __attribute__((aligned(4)));
 typedef int i32x16 __attribute__((ext_vector_type(16)));
 
 inline int64_t round_up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
