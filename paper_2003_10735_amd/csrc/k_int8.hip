@@ -560,14 +560,15 @@ static int64_t tiles_of(const Extent& e, int tile) { return ceil_div(e.m, tile) 
 Form form_of(const Extent* e, int count)
 {
     auto total = [&](int tile) { int64_t t = 0; for (int i = 0; i < count; ++i) t += tiles_of(e[i], tile); return t; };
+    auto stages_of = [&](int tile) { int64_t w = 0; for (int i = 0; i < count; ++i) w += tiles_of(e[i], tile) * ceil_div(e[i].k, STAGE); return w; };
     Form f = {64, {1, 1}};
-    if (total(256) >= 192) f.tile = 256;
+    // (a tile of five stages or fewer is begun and ended most of its time: smaller ones, two a compute unit, overlap; 5480 tokens 532 -> 6367
+    // 48.5 us against 62, 14400 tokens 256 -> 2048 33.0 against 36.4; but 8192 tokens 1024 -> 8192 107 against 96)
+    if (total(256) >= 192 && stages_of(256) > 5 * total(256)) f.tile = 256;
     else if (total(128) >= 192) f.tile = 128;
     // every block about the same number of stages, 256 blocks, eight stages each at least; up to 16 stages the parts' join costs more than
     // it gives (333 tokens 1000 -> 1003: 11.8 us, in two parts 15.6; 65 tokens 8192 -> 128 in eight parts: 12.7, in four 15.0)
-    int64_t work = 0;
-    for (int i = 0; i < count; ++i) work += tiles_of(e[i], f.tile) * ceil_div(e[i].k, STAGE);
-    const int64_t each = std::max<int64_t>(8, ceil_div(work, 256));
+    const int64_t each = std::max<int64_t>(8, ceil_div(stages_of(f.tile), 256));
     for (int i = 0; i < count; ++i) {
         const int64_t stages = ceil_div(e[i].k, STAGE);
         int64_t s = stages > 16 ? stages / each : 1;

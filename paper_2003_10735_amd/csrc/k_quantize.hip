@@ -294,7 +294,7 @@ template <class T> __device__ __forceinline__ void rows_any(const Job& j, unsign
     const int lanes = row_lanes(j.len, sizeof(T) == 2);
     if (lanes == 32) rows_role<T, 32, 4>(j, block, sh);
     else if (lanes == 64) rows_role<T, 64, row_keep<T>()>(j, block, sh);
-    else rows_role<T, 256, row_keep<T>()>(j, block, sh);
+    else rows_role<T, 256, 4>(j, block, sh);
 }
 template <class T> __device__ __forceinline__ void first_role(const Job& j, unsigned block, Shared& sh)
 {
@@ -320,7 +320,7 @@ template <class T> static void rows_launch(Ctx& c, const Job& j, unsigned blocks
     switch (row_lanes(j.len, sizeof(T) == 2)) {
     case 32: ST_LAUNCH(c, "quantize_rows", (k_quantize_rows<T, 32, 4>), dim3(blocks), dim3(256), 0, j); break;
     case 64: ST_LAUNCH(c, "quantize_rows", (k_quantize_rows<T, 64, row_keep<T>()>), dim3(blocks), dim3(256), 0, j); break;
-    default: ST_LAUNCH(c, "quantize_rows", (k_quantize_rows<T, 256, row_keep<T>()>), dim3(blocks), dim3(256), 0, j);
+    default: ST_LAUNCH(c, "quantize_rows", (k_quantize_rows<T, 256, 4>), dim3(blocks), dim3(256), 0, j);
     }
 }
 __global__ __launch_bounds__(256) void k_quantize_turn(const Jobs jobs)
