@@ -89,13 +89,9 @@ __global__ __launch_bounds__(256) void k_grad_square_sums(const GradList l, floa
     for (; tile < end; ++tile) {
         while (i + 1 < l.count && tile >= l.first[i + 1]) ++i;
         const G* g = (const G*)l.g[i];
-        const long long base = (long long)(tile - l.first[i]) * (RUNS * 2048) + threadIdx.x * 8, left = l.n[i] - base;
+        const long long base = (long long)(tile - l.first[i]) * (RUNS * 2048) + threadIdx.x * 8;
         Raw8<G> v[RUNS];
-#pragma unroll
-        for (int j = 0; j < RUNS; ++j) {
-            const long long n = left - j * 2048;
-            v[j].load(g + base + j * 2048, n > 8 ? 8 : n > 0 ? (int)n : 0);
-        }
+        load_row(g, l.n[i], [&](int j) { return base + j * 2048; }, v);
 #pragma unroll
         for (int j = 0; j < RUNS; ++j)
 #pragma unroll

@@ -283,7 +283,10 @@ __device__ __forceinline__ void few_quantize(const FewArgs& f, char* codes, unsi
 #pragma unroll
     for (int j = 0; j < KEEP; ++j) {
         const int at = (c * threads + lane) * 8;
-        if (r < m) v[j].load((const T*)f.x + r * f.x_pitch + at, k - at);
+        if (r < m) {
+            if (k < 8) v[j].load_short((const T*)f.x + r * f.x_pitch + at, k - at);
+            else v[j].load((const T*)f.x + r * f.x_pitch + run_start<8>(at, k));
+        }
         if (++c == f.per_token) { c = 0; r += step; }
     }
     __syncthreads();
@@ -291,6 +294,8 @@ __device__ __forceinline__ void few_quantize(const FewArgs& f, char* codes, unsi
 #pragma unroll
     for (int j = 0; j < KEEP; ++j) {
         if (r < m) {
+            const int d = (c * threads + lane) * 8 - (k - 8);
+            if (k >= 8 && d > 0) v[j].down(min(d, 8));
             unsigned top = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[j][i]));
@@ -478,10 +483,9 @@ template <class T, int RUNS> __global__ __launch_bounds__(256) void k_int8_narro
 
     const int token = threadIdx.x >> 3, t8 = threadIdx.x & 7;
     const bool there = m0 + token < p.m;
-    const T* x = (const T*)f.x + (m0 + token) * f.x_pitch;
+    const T* x = (const T*)f.x + (there ? m0 + token : 0) * f.x_pitch;
     Raw8<T> v[RUNS];
-#pragma unroll
-    for (int i = 0; i < RUNS; ++i) v[i].load(x + (i * 8 + t8) * 8, there ? k - (i * 8 + t8) * 8 : 0);
+    load_row(x, k, [&](int i) { return (i * 8 + t8) * 8; }, v);
     weights(wave * 32);
     unsigned top = 0;
 #pragma unroll

@@ -11,6 +11,7 @@
 // LDS as codes.  (Sources that share a launch do not wait for one another: a backward pass has four, of which some are a few tiles.)
 #include "st_quantize.hpp"
 
+#include <algorithm>
 #include <type_traits>
 
 namespace st {
@@ -21,70 +22,27 @@ struct Job {
     int8_t* q;
     float *scale, *sum, *part_max, *part_sum;
     int parts;
-    unsigned len_tiles;
+    unsigned len_tiles, tiles_each, len_blocks;      // second launch: tiles of 128 positions, of a block, blocks of a row of tiles
     uint8_t bf16_, mask_bf16, along;
 };
 struct Jobs { unsigned first1[4], first2[4]; int n; Job job[4]; };      // first block of each job in the two launches
 
-// Four neighbouring values, one load.
-template <class T> struct Raw4;
-template <> struct Raw4<bf16> {
-    u32x2 u;
-    __device__ __forceinline__ void load(const bf16* p) { u = *(const u32x2_2*)p; }
-    __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i & 1 ? u[i >> 1] & 0xffff0000u : u[i >> 1] << 16); }
-};
-template <> struct Raw4<float> {
-    f32x4_t u;
-    __device__ __forceinline__ void load(const float* p) { u = *(const f32x4_4*)p; }
-    __device__ __forceinline__ float operator[](int i) const { return u[i]; }
-};
-template <> struct Raw4<void> {};      // no mask
-
-// Four values at `at` of position `line`, of which `n` exist, zero where the mask is not positive.
-template <class T> __device__ __forceinline__ void read(const Job& j, int64_t line, int64_t at, int64_t n, float (&v)[4])
+template <class M, class T, int COUNT, class F> __device__ __forceinline__ void clear_masked(const M* row, int len, F at, Raw8<T> (&v)[COUNT])
 {
-    const int count = n < 4 ? (int)n : 4;
-    load4((const T*)j.x + line * j.pitch + at, count, v);
-    if (!j.mask) return;
-    float m[4];
-    if (j.mask_bf16) load4((const bf16*)j.mask + line * j.mask_pitch + at, count, m);
-    else load4((const float*)j.mask + line * j.mask_pitch + at, count, m);
+    Raw8<M> on[COUNT];
+    load_row<M, COUNT, int>(row, len, at, on);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[i] = m[i] > 0.f ? v[i] : 0.f;
-}
-// COUNT fours, `step` positions apart, all under way before the first is used.  M: the mask's type, or void.
-template <class T, class M, int COUNT>
-__device__ __forceinline__ void read_all(const Job& j, int64_t line, int step, int64_t at, float (&v)[COUNT][4])
-{
-    Raw4<T> x[COUNT];
-    Raw4<M> m[COUNT];
+    for (int k = 0; k < COUNT; ++k)
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
-        x[i].load((const T*)j.x + (line + i * step) * j.pitch + at);
-        if constexpr (!std::is_void<M>::value) m[i].load((const M*)j.mask + (line + i * step) * j.mask_pitch + at);
-    }
-#pragma unroll
-    for (int i = 0; i < COUNT; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[i][e] = x[i][e];
-            if constexpr (!std::is_void<M>::value) v[i][e] = m[i][e] > 0.f ? v[i][e] : 0.f;
-        }
-}
-template <class M, class T> __device__ __forceinline__ void clear_masked(const M* m, int n, Raw8<T>& v)
-{
-    Raw8<M> on;
-    on.load(m, n);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) if (!(on[i] > 0.f)) v.clear(i);
+        for (int i = 0; i < 8; ++i) if (!(on[k][i] > 0.f)) v[k].clear(i);
 }
 template <class T> __device__ __forceinline__ float sum8(const Raw8<T>& v) { return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])); }
 
 struct Shared {
     union {
         struct { unsigned tops[4]; double sums[4]; } rows;
-        struct { unsigned tops[16][64]; float sums[16][64]; } parts;
-        struct { unsigned tops[4][64]; double sums[4][64]; float mult[64]; unsigned tile[64][33]; } turn;   // 33: rows begin on other banks
+        struct { unsigned tops[32][64]; float sums[32][64]; } parts;
+        struct { unsigned tops[4][64]; double sums[4][64]; float mult[64]; unsigned tile[2][64][33]; } turn;   // 33: rows begin on other banks
     };
 };
 
@@ -96,18 +54,18 @@ template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_rol
 {
     constexpr int MORE = 4;      // runs under way beyond those
     const int lane = threadIdx.x % LANES;
-    const int64_t row = (int64_t)block * (256 / LANES) + threadIdx.x / LANES;
+    int64_t row = (int64_t)block * (256 / LANES) + threadIdx.x / LANES;
     const bool there = row < j.rows;
+    row = there ? row : j.rows - 1;      // (what a thread without a row finds is not used)
     const int len = (int)j.len;
     const T* x = (const T*)j.x + row * j.pitch;
     unsigned top = 0;
     double total = 0.0;
-    auto load = [&](int at, Raw8<T>& v) { v.load(x + at, there ? len - at : 0); };
-    auto mask = [&](int at, Raw8<T>& v) {
+    auto load = [&](auto at, auto& v) {
+        load_row(x, len, at, v);
         if (!j.mask) return;
-        const int n = there ? len - at : 0;
-        if (j.mask_bf16) clear_masked((const bf16*)j.mask + row * j.mask_pitch + at, n, v);
-        else clear_masked((const float*)j.mask + row * j.mask_pitch + at, n, v);
+        if (j.mask_bf16) clear_masked((const bf16*)j.mask + row * j.mask_pitch, len, at, v);
+        else clear_masked((const float*)j.mask + row * j.mask_pitch, len, at, v);
     };
     auto see = [&](const Raw8<T>& v) {
 #pragma unroll
@@ -115,16 +73,14 @@ template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_rol
         if (j.sum) total += sum8(v);
     };
     Raw8<T> v[KEEP];
+    load([&](int k) { return (k * LANES + lane) * 8; }, v);
 #pragma unroll
-    for (int k = 0; k < KEEP; ++k) load((k * LANES + lane) * 8, v[k]);
-#pragma unroll
-    for (int k = 0; k < KEEP; ++k) { mask((k * LANES + lane) * 8, v[k]); see(v[k]); }
+    for (int k = 0; k < KEEP; ++k) see(v[k]);
     for (int at = (KEEP * LANES + lane) * 8; at < len; at += MORE * LANES * 8) {
         Raw8<T> w[MORE];
+        load([&](int k) { return at + k * LANES * 8; }, w);
 #pragma unroll
-        for (int k = 0; k < MORE; ++k) load(at + k * LANES * 8, w[k]);
-#pragma unroll
-        for (int k = 0; k < MORE; ++k) { mask(at + k * LANES * 8, w[k]); see(w[k]); }
+        for (int k = 0; k < MORE; ++k) see(w[k]);
     }
     if (j.sum) {
 #pragma unroll
@@ -161,132 +117,191 @@ template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_rol
     for (int k = 0; k < KEEP; ++k) put((k * LANES + lane) * 8, v[k]);
     for (int at = (KEEP * LANES + lane) * 8; at < end; at += MORE * LANES * 8) {
         Raw8<T> w[MORE];
+        load([&](int k) { return at + k * LANES * 8; }, w);
 #pragma unroll
-        for (int k = 0; k < MORE; ++k) load(at + k * LANES * 8, w[k]);
-#pragma unroll
-        for (int k = 0; k < MORE; ++k) { mask(at + k * LANES * 8, w[k]); put(at + k * LANES * 8, w[k]); }
+        for (int k = 0; k < MORE; ++k) put(at + k * LANES * 8, w[k]);
     }
 }
 template <class T> constexpr int row_keep() { return sizeof(T) == 2 ? 8 : 4; }
 static __host__ __device__ __forceinline__ int row_lanes(int64_t len, int is_bf16) { return len <= 1024 ? 32 : len <= (is_bf16 ? 4096 : 2048) ? 64 : 256; }
 
 // --------------------------------------------------------------------------------------- rows that lie across it
-// The source is a matrix [len][pitch] whose columns are the operand's rows.  Sixteen threads take 64 columns of a position, sixteen
-// positions at once: whole lines of memory are read.  A block leaves the largest value and the sum of 64 columns over one part.
-template <class T, class M> __device__ __forceinline__ void parts_loop(const Job& j, int64_t col, int64_t from, int64_t to, int group, bool whole,
-                                                                       unsigned (&top)[4], double (&total)[4])
+// The source is a matrix [len][pitch] whose columns are the operand's rows.  A thread takes 16 bytes of a position, so that 64 columns of
+// it are eight (bfloat16) or sixteen (float32) threads and whole lines of memory are read.
+template <class T> constexpr int across() { return 16 / (int)sizeof(T); }              // columns of a thread
+template <class T> constexpr int groups() { return 4 * across<T>(); }                  // positions a block takes at once
+
+// A run of a position and what masks it, on their way; settle() before they are used.
+struct Columns { int64_t col, from, rows; int down; };      // of a thread: its first, where its runs are loaded from, how far they are moved
+template <class T> __device__ __forceinline__ Columns columns_of(int64_t col, int64_t rows)
 {
-    for (int64_t piece = from + group; piece < to; piece += 1024) {     // float32 sums of 64 values, added in float64
-        float s[4] = {};
-        const int64_t end = piece + 1024 < to ? piece + 1024 : to;
+    constexpr int V = across<T>();
+    const int64_t from = run_start<V, int64_t>(col, rows), d = col - from;
+    return Columns{col, from, rows, d < V ? (int)d : V};
+}
+template <class T, class M, bool SHORT> struct Masked {
+    static constexpr int V = across<T>();
+    Run<T, V> x;
+    Run<M, V> m;
+    __device__ __forceinline__ void load(const Job& j, int64_t line, const Columns& c)
+    {
+        const int n = SHORT && c.col < c.rows ? (int)(c.rows - c.col) : 0;
+        if constexpr (SHORT) x.load_short((const T*)j.x + line * j.pitch + c.col, n);
+        else x.load((const T*)j.x + line * j.pitch + c.from);
+        if constexpr (!std::is_void<M>::value) {
+            if constexpr (SHORT) m.load_short((const M*)j.mask + line * j.mask_pitch + c.col, n);
+            else m.load((const M*)j.mask + line * j.mask_pitch + c.from);
+        }
+    }
+    __device__ __forceinline__ void settle(const Columns& c)
+    {
+        if (SHORT || c.down == 0) return;
+        x.down(c.down);
+        if constexpr (!std::is_void<M>::value) m.down(c.down);
+    }
+    __device__ __forceinline__ float operator[](int i) const
+    {
+        if constexpr (!std::is_void<M>::value) return m[i] > 0.f ? x[i] : 0.f;
+        else return x[i];
+    }
+};
+
+// First launch: a block leaves the largest value and the sum of 64 columns over one part of the contraction.
+template <class T, class M, bool SHORT> __device__ __forceinline__ void parts_loop(const Job& j, const Columns& col, int64_t from, int64_t to, int group,
+                                                                       unsigned (&top)[across<T>()], double (&total)[across<T>()])
+{
+    constexpr int V = across<T>(), STEP = groups<T>(), AHEAD = SHORT ? 1 : std::is_void<M>::value ? 8 : 4;
+    for (int64_t piece = from + group; piece < to; piece += 64 * STEP) {     // float32 sums of 64 values, added in float64
+        float s[V] = {};
+        const int64_t end = piece + 64 * STEP < to ? piece + 64 * STEP : to;
         int64_t k = piece;
-        auto see = [&](const float (&v)[4]) {
+        auto see = [&](const Masked<T, M, SHORT>& v) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) { top[e] = max(top[e], abs_bits(v[e])); s[e] += v[e]; }
+            for (int e = 0; e < V; ++e) { const float f = v[e]; top[e] = max(top[e], abs_bits(f)); s[e] += f; }
         };
-        if (whole)
-            for (; k + 48 < end; k += 64) {
-                float v[4][4];
-                read_all<T, M, 4>(j, k, 16, col, v);
+        for (; k + (AHEAD - 1) * STEP < end; k += AHEAD * STEP) {
+            Masked<T, M, SHORT> v[AHEAD];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) see(v[i]);
-            }
-        for (; k < end; k += 16) {
-            float v[4];
-            read<T>(j, k, col, j.rows - col, v);
+            for (int i = 0; i < AHEAD; ++i) v[i].load(j, k + i * STEP, col);
+#pragma unroll
+            for (int i = 0; i < AHEAD; ++i) { v[i].settle(col); see(v[i]); }
+        }
+        for (; k < end; k += STEP) {
+            Masked<T, M, SHORT> v;
+            v.load(j, k, col);
+            v.settle(col);
             see(v);
         }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) total[e] += s[e];
+        for (int e = 0; e < V; ++e) total[e] += s[e];
     }
 }
-template <class T> __device__ __forceinline__ void parts_role(const Job& j, unsigned block, Shared& sh)
+template <class T, bool SHORT> __device__ __forceinline__ void parts_role(const Job& j, unsigned block, Shared& sh)
 {
+    constexpr int V = across<T>(), LANES = 64 / V, GROUPS = groups<T>();
     const unsigned tile = block / (unsigned)j.parts, part = block - tile * (unsigned)j.parts;
-    const int c = (threadIdx.x & 15) * 4, group = threadIdx.x >> 4;
+    const int c = (threadIdx.x % LANES) * V, group = threadIdx.x / LANES;
     const int64_t col = (int64_t)tile * 64 + c;
     const int64_t from = part * j.per_part, to = from + j.per_part < j.len ? from + j.per_part : j.len;
-    const bool whole = col + 4 <= j.rows;
-    unsigned top[4] = {};
-    double total[4] = {};
+    unsigned top[V] = {};
+    double total[V] = {};
     if (col < j.rows) {
-        if (!j.mask) parts_loop<T, void>(j, col, from, to, group, whole, top, total);
-        else if (j.mask_bf16) parts_loop<T, bf16>(j, col, from, to, group, whole, top, total);
-        else parts_loop<T, float>(j, col, from, to, group, whole, top, total);
+        const Columns mine = columns_of<T>(col, j.rows);
+        if (!j.mask) parts_loop<T, void, SHORT>(j, mine, from, to, group, top, total);
+        else if (j.mask_bf16) parts_loop<T, bf16, SHORT>(j, mine, from, to, group, top, total);
+        else parts_loop<T, float, SHORT>(j, mine, from, to, group, top, total);
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) { sh.parts.tops[group][c + i] = top[i]; sh.parts.sums[group][c + i] = (float)total[i]; }
+    for (int i = 0; i < V; ++i) { sh.parts.tops[group][c + i] = top[i]; sh.parts.sums[group][c + i] = (float)total[i]; }
     __syncthreads();
     const int64_t mine = (int64_t)tile * 64 + threadIdx.x;
     if (threadIdx.x < 64 && mine < j.rows) {
         unsigned t = 0;
         double s = 0.0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) { t = max(t, sh.parts.tops[i][threadIdx.x]); s += sh.parts.sums[i][threadIdx.x]; }
+        for (int i = 0; i < GROUPS; ++i) { t = max(t, sh.parts.tops[i][threadIdx.x]); s += sh.parts.sums[i][threadIdx.x]; }
         if (j.part_max) j.part_max[(int64_t)part * j.rows + mine] = __uint_as_float(t);
         if (j.part_sum) j.part_sum[(int64_t)part * j.rows + mine] = (float)s;
     }
 }
 
-// Tiles of 64 columns x 128 positions.  A thread takes eight positions of four columns: two words of codes for each of four rows.
-template <class T> __device__ __forceinline__ void turn_role(const Job& j, unsigned block, Shared& sh)
+// Second launch: tiles of 64 columns x 128 positions, several of them one after the other where there are many, the next one's loads under
+// way while one is stored.  A thread takes POS neighbouring positions of its columns: words of four codes for each of them.
+template <class T, class M, bool SHORT> __device__ __forceinline__ void turn_tiles(const Job& j, int64_t row0, unsigned len_tile, unsigned count, Shared& sh)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const unsigned row_tile = block / j.len_tiles, len_tile = block - row_tile * j.len_tiles;
-    const int64_t row0 = (int64_t)row_tile * 64, k0 = (int64_t)len_tile * 128;
-    const int64_t mine = row0 + lane;
-    const bool sums = j.sum && len_tile == 0;
-    const int c = (threadIdx.x & 15) * 4, group = threadIdx.x >> 4;
-    float v[8][4] = {};
-    if (j.q && row0 + c < j.rows) {
-        const int64_t k = k0 + group * 8;
-        if (row0 + c + 4 <= j.rows && k + 8 <= j.len) {
-            if (!j.mask) read_all<T, void, 8>(j, k, 1, row0 + c, v);
-            else if (j.mask_bf16) read_all<T, bf16, 8>(j, k, 1, row0 + c, v);
-            else read_all<T, float, 8>(j, k, 1, row0 + c, v);
-        } else
+    constexpr int V = across<T>(), LANES = 64 / V, POS = 128 / groups<T>();
+    const int c = (threadIdx.x % LANES) * V, group = threadIdx.x / LANES;
+    const Columns col = columns_of<T>(row0 + c, j.rows);
+    Masked<T, M, SHORT> v[POS];
+    auto load = [&](unsigned tile) {       // (positions behind the last one: the last one, and codes of 0 below)
+        const int64_t k = (int64_t)tile * 128 + group * POS;
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (k + i < j.len) read<T>(j, k + i, row0 + c, j.rows - row0 - c, v[i]);
-    }
+        for (int i = 0; i < POS; ++i) v[i].load(j, k + i < j.len ? k + i : j.len - 1, col);
+    };
+    load(len_tile);
+    // the parts' largest values, and the multipliers
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t mine = row0 + lane;
     unsigned top = 0;
-    double total = 0.0;
-    if (mine < j.rows) {
-        if (j.q)
+    if (mine < j.rows)
 #pragma unroll 8
-            for (int p = wave; p < j.parts; p += 4) top = max(top, __float_as_uint(j.part_max[(int64_t)p * j.rows + mine]));
-        if (sums)
-            for (int p = wave; p < j.parts; p += 4) total += j.part_sum[(int64_t)p * j.rows + mine];
-    }
+        for (int p = wave; p < j.parts; p += 4) top = max(top, __float_as_uint(j.part_max[(int64_t)p * j.rows + mine]));
     sh.turn.tops[wave][lane] = top;
-    sh.turn.sums[wave][lane] = total;
     __syncthreads();
     if (wave == 0) {
         float s;
         sh.turn.mult[lane] = row_multiplier(max(max(sh.turn.tops[0][lane], sh.turn.tops[1][lane]), max(sh.turn.tops[2][lane], sh.turn.tops[3][lane])), &s);
-        if (len_tile == 0 && j.q && mine < j.rows) j.scale[mine] = s;
+        if (len_tile == 0 && mine < j.rows) j.scale[mine] = s;
     }
-    if (wave == 1 && sums && mine < j.rows)
-        j.sum[mine] = (float)((sh.turn.sums[0][lane] + sh.turn.sums[1][lane]) + (sh.turn.sums[2][lane] + sh.turn.sums[3][lane]));
+    __syncthreads();
+    float mult[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) mult[i] = sh.turn.mult[c + i];
+    for (unsigned t = 0; t < count; ++t) {
+        unsigned (&tile)[64][33] = sh.turn.tile[t & 1];
+#pragma unroll
+        for (int i = 0; i < POS; ++i) v[i].settle(col);
+        const int64_t k = (int64_t)(len_tile + t) * 128 + group * POS;
+        const int left = j.len - k < POS ? (j.len > k ? (int)(j.len - k) : 0) : POS;
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+#pragma unroll
+            for (int h = 0; h < POS / 4; ++h) {
+                unsigned w = pack4(code_of(v[h * 4][i], mult[i]), code_of(v[h * 4 + 1][i], mult[i]), code_of(v[h * 4 + 2][i], mult[i]),
+                                   code_of(v[h * 4 + 3][i], mult[i]));
+                if (left < POS) w = left <= h * 4 ? 0u : left >= h * 4 + 4 ? w : w & (0xffffffffu >> (8 * (h * 4 + 4 - left)));
+                tile[c + i][group * (POS / 4) + h] = w;
+            }
+        if (t + 1 < count) load(len_tile + t + 1);
+        __syncthreads();          // (one a tile is enough: the tile after next is written behind the next one's)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {           // a row's 128 bytes by eight lanes
+            const int u = threadIdx.x + h * 256, rr = u >> 3, w = (u & 7) * 4;
+            const int64_t row = row0 + rr, at = (int64_t)(len_tile + t) * 128 + w * 4;
+            if (row < j.rows && at < j.q_pitch)
+                *(uint4*)(j.q + row * j.q_pitch + at) = make_uint4(tile[rr][w], tile[rr][w + 1], tile[rr][w + 2], tile[rr][w + 3]);
+        }
+    }
+}
+template <class T, bool SHORT> __device__ __forceinline__ void turn_role(const Job& j, unsigned block, Shared& sh)
+{
+    const unsigned row_tile = block / j.len_blocks, first = (block - row_tile * j.len_blocks) * j.tiles_each;
+    const unsigned count = min(j.tiles_each, j.len_tiles - first);
+    const int64_t row0 = (int64_t)row_tile * 64;
+    if (j.sum && first == 0) {
+        const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+        double total = 0.0;
+        if (row0 + lane < j.rows)
+            for (int p = wave; p < j.parts; p += 4) total += j.part_sum[(int64_t)p * j.rows + row0 + lane];
+        sh.turn.sums[wave][lane] = total;
+        __syncthreads();
+        if (wave == 1 && row0 + lane < j.rows)
+            j.sum[row0 + lane] = (float)((sh.turn.sums[0][lane] + sh.turn.sums[1][lane]) + (sh.turn.sums[2][lane] + sh.turn.sums[3][lane]));
+    }
     if (!j.q) return;
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float r = sh.turn.mult[c + i];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-            sh.turn.tile[c + i][group * 2 + h] = pack4(code_of(v[h * 4][i], r), code_of(v[h * 4 + 1][i], r), code_of(v[h * 4 + 2][i], r),
-                                                       code_of(v[h * 4 + 3][i], r));
-    }
-    __syncthreads();
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {           // a row's 128 bytes by eight lanes
-        const int t = threadIdx.x + h * 256, rr = t >> 3, w = (t & 7) * 4;
-        const int64_t row = row0 + rr, at = k0 + w * 4;
-        if (row < j.rows && at < j.q_pitch)
-            *(uint4*)(j.q + row * j.q_pitch + at) =
-                make_uint4(sh.turn.tile[rr][w], sh.turn.tile[rr][w + 1], sh.turn.tile[rr][w + 2], sh.turn.tile[rr][w + 3]);
-    }
+    if (!j.mask) turn_tiles<T, void, SHORT>(j, row0, first, count, sh);
+    else if (j.mask_bf16) turn_tiles<T, bf16, SHORT>(j, row0, first, count, sh);
+    else turn_tiles<T, float, SHORT>(j, row0, first, count, sh);
 }
 
 template <class T> __device__ __forceinline__ void rows_any(const Job& j, unsigned block, Shared& sh)
@@ -298,10 +313,10 @@ template <class T> __device__ __forceinline__ void rows_any(const Job& j, unsign
 }
 template <class T> __device__ __forceinline__ void first_role(const Job& j, unsigned block, Shared& sh)
 {
-    if (!j.along) parts_role<T>(j, block, sh);
+    if (!j.along) { if (j.rows < across<T>()) parts_role<T, true>(j, block, sh); else parts_role<T, false>(j, block, sh); }
     else rows_any<T>(j, block, sh);
 }
-__global__ __launch_bounds__(256) void k_quantize_first(const Jobs jobs)
+__global__ __launch_bounds__(256, 3) void k_quantize_first(const Jobs jobs)
 {
     __shared__ Shared sh;
     int i = 0;
@@ -323,13 +338,15 @@ template <class T> static void rows_launch(Ctx& c, const Job& j, unsigned blocks
     default: ST_LAUNCH(c, "quantize_rows", (k_quantize_rows<T, 256, 4>), dim3(blocks), dim3(256), 0, j);
     }
 }
-__global__ __launch_bounds__(256) void k_quantize_turn(const Jobs jobs)
+__global__ __launch_bounds__(256, 4) void k_quantize_turn(const Jobs jobs)
 {
     __shared__ Shared sh;
     int i = 0;
     while (i + 1 < jobs.n && blockIdx.x >= jobs.first2[i + 1]) ++i;
     const Job& j = jobs.job[i];
-    if (j.bf16_) turn_role<bf16>(j, blockIdx.x - jobs.first2[i], sh); else turn_role<float>(j, blockIdx.x - jobs.first2[i], sh);
+    const unsigned block = blockIdx.x - jobs.first2[i];
+    if (j.bf16_) { if (j.rows < across<bf16>()) turn_role<bf16, true>(j, block, sh); else turn_role<bf16, false>(j, block, sh); }
+    else         { if (j.rows < across<float>()) turn_role<float, true>(j, block, sh); else turn_role<float, false>(j, block, sh); }
 }
 
 // ------------------------------------------------------------------------------------------------------------- host
@@ -356,13 +373,15 @@ void quantize(Ctx& c, const QuantTask* tasks, int n)
             jobs.first1[jobs.n] = (unsigned)blocks1; jobs.first2[jobs.n] = (unsigned)blocks2;
             Job& j = jobs.job[jobs.n++];
             j = Job{s.x, s.mask, s.pitch, s.mask_pitch, s.rows, s.len, t.to.pitch, 0, t.to.q, t.to.scale, t.sum, t.to.q ? t.part_max : nullptr,
-                    t.sum ? t.part_sum : nullptr, 1, 1, (uint8_t)s.bf16, (uint8_t)s.mask_bf16, (uint8_t)s.along};
+                    t.sum ? t.part_sum : nullptr, 1, 1, 1, 1, (uint8_t)s.bf16, (uint8_t)s.mask_bf16, (uint8_t)s.along};
             if (s.along) { blocks1 += ceil_div(s.rows, 256 / row_lanes(s.len, s.bf16)); continue; }
             j.parts = transpose_parts(s.rows, s.len);
             j.per_part = ceil_div(s.len, j.parts);
             j.len_tiles = t.to.q ? (unsigned)ceil_div(s.len, 128) : 1;
+            j.tiles_each = (unsigned)std::min<int64_t>(4, std::max<int64_t>(1, ceil_div(s.rows, 64) * j.len_tiles / 1024));
+            j.len_blocks = (unsigned)ceil_div(j.len_tiles, j.tiles_each);
             blocks1 += ceil_div(s.rows, 64) * j.parts;
-            blocks2 += ceil_div(s.rows, 64) * j.len_tiles;
+            blocks2 += ceil_div(s.rows, 64) * j.len_blocks;
         }
     if (jobs.n == 1 && jobs.job[0].along) {
         if (jobs.job[0].bf16_) rows_launch<bf16>(c, jobs.job[0], (unsigned)blocks1); else rows_launch<float>(c, jobs.job[0], (unsigned)blocks1);

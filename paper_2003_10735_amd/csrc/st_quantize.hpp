@@ -76,43 +76,91 @@ __device__ __forceinline__ void load4(const float* p, int n, float (&v)[4])
     for (int i = 0; i < 4; ++i) v[i] = i < n ? p[i] : 0.f;
 }
 
-// Eight consecutive values as they lie in memory, those from n on zeros.
-template <class T> struct Raw8;
-template <> struct Raw8<bf16> {
-    unsigned w[4];
-    __device__ __forceinline__ void load(const bf16* p, int n)
+// V (4 or 8) consecutive values as they lie in memory.  The run at `at` of a row of `len` values that ends inside it is loaded from
+// run_start(): the row's last V values, which down() then moves to their places, zeros behind them.  Rows of fewer than V values are
+// loaded one by one (load_short).
+template <int V, class I> __device__ __forceinline__ I run_start(I at, I len) { return at < len - V ? at : len - V; }
+template <class T, int V> struct Run;
+template <int V> struct Run<bf16, V> {
+    unsigned w[V / 2];
+    __device__ __forceinline__ void load(const bf16* p)
     {
-        if (n >= 8) {
-            const u32x4_t u = *(const u32x4_2*)p;
-            w[0] = u[0]; w[1] = u[1]; w[2] = u[2]; w[3] = u[3];
-            return;
-        }
+        if constexpr (V == 8) { const u32x4_t u = *(const u32x4_2*)p; w[0] = u[0]; w[1] = u[1]; w[2] = u[2]; w[3] = u[3]; }
+        else { const u32x2 u = *(const u32x2_2*)p; w[0] = u[0]; w[1] = u[1]; }
+    }
+    __device__ __forceinline__ void load_short(const bf16* p, int n)
+    {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < V / 2; ++i) {
             const unsigned lo = 2 * i < n ? ((const unsigned short*)p)[2 * i] : 0u, hi = 2 * i + 1 < n ? ((const unsigned short*)p)[2 * i + 1] : 0u;
             w[i] = lo | hi << 16;
         }
     }
+    __device__ __forceinline__ void down(int d)
+    {
+#pragma unroll
+        for (int s = 1; s < V / 2; s *= 2)
+#pragma unroll
+            for (int i = 0; i < V / 2; ++i) w[i] = d & (2 * s) ? (i + s < V / 2 ? w[i + s] : 0u) : w[i];
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            const unsigned odd = w[i] >> 16 | (i + 1 < V / 2 ? w[i + 1] << 16 : 0u);
+            w[i] = d >= V ? 0u : d & 1 ? odd : w[i];
+        }
+    }
     __device__ __forceinline__ float operator[](int i) const { return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16); }
     // what follows unpacks the values again, instead of keeping them unpacked all the time
-    __device__ __forceinline__ void repack() { asm volatile("" : "+v"(w[0]), "+v"(w[1]), "+v"(w[2]), "+v"(w[3])); }
+    __device__ __forceinline__ void repack()
+    {
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) asm volatile("" : "+v"(w[i]));
+    }
     __device__ __forceinline__ void clear(int i) { w[i >> 1] &= i & 1 ? 0x0000ffffu : 0xffff0000u; }
 };
-template <> struct Raw8<float> {
-    float v[8];
-    __device__ __forceinline__ void load(const float* p, int n)
+template <int V> struct Run<float, V> {
+    float v[V];
+    __device__ __forceinline__ void load(const float* p)
     {
-        if (n >= 8) {
-            const f32x4_t a = *(const f32x4_4*)p, b = *(const f32x4_4*)(p + 4);
-            v[0] = a[0]; v[1] = a[1]; v[2] = a[2]; v[3] = a[3]; v[4] = b[0]; v[5] = b[1]; v[6] = b[2]; v[7] = b[3];
-            return;
-        }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+        for (int i = 0; i < V; i += 4) { const f32x4_t a = *(const f32x4_4*)(p + i); v[i] = a[0]; v[i + 1] = a[1]; v[i + 2] = a[2]; v[i + 3] = a[3]; }
+    }
+    __device__ __forceinline__ void load_short(const float* p, int n)
+    {
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = i < n ? p[i] : 0.f;
+    }
+    __device__ __forceinline__ void down(int d)
+    {
+#pragma unroll
+        for (int s = 1; s < V; s *= 2)
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = d & s ? (i + s < V ? v[i + s] : 0.f) : v[i];
+#pragma unroll
+        for (int i = 0; i < V; ++i) v[i] = d >= V ? 0.f : v[i];
     }
     __device__ __forceinline__ float operator[](int i) const { return v[i]; }
     __device__ __forceinline__ void repack() {}
     __device__ __forceinline__ void clear(int i) { v[i] = 0.f; }
 };
+template <int V> struct Run<void, V> {};      // no mask
+template <class T> using Raw8 = Run<T, 8>;
+
+// COUNT runs of eight of a row, run i at at(i): all under way before one of them is moved.
+template <class T, int COUNT, class I, class F>
+__device__ __forceinline__ void load_row(const T* row, I len, F at, Raw8<T> (&v)[COUNT])
+{
+    if (len < 8) {
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i].load_short(row + at(i), at(i) < len ? (int)(len - at(i)) : 0);
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i].load(row + run_start<8, I>(at(i), len));
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) {
+        const I d = at(i) - (len - 8);
+        if (d > 0) v[i].down(d < 8 ? (int)d : 8);
+    }
+}
 
 }  // namespace st
