@@ -273,7 +273,7 @@ int st_object_weights(const int32_t* labels, int32_t n, int32_t height, int32_t 
  * A matrix argument has an element type (ST_F32 | ST_BF16) and two strides in elements, of which one is 1: row by row with a pitch, or
  * column by column with a pitch (what a channel-first feature map is to its cells).  Pointers are aligned to their elements, int8
  * matrices to 16 bytes with a pitch that is a multiple of 16 and at most 2^23.  Tokens may be 0 in number (the call then writes what an empty sum is);
- * other sizes are at least 1.  Offsets inside a matrix are 64 bits wide; sums longer than ST_INT8_MAX_SUM are refused (ST_ERR_SHAPE)
+ * other sizes are at least 1, and all of them are less than 2^24.  Offsets inside a matrix are 64 bits wide; sums longer than ST_INT8_MAX_SUM are refused (ST_ERR_SHAPE)
  * where the header says so, since int32 could not hold them.  Outputs must not overlap inputs or each other. */
 #define ST_INT8_MAX_SUM 131071
 
@@ -337,7 +337,7 @@ typedef struct st_adamw_tensor {   /* HOST struct of DEVICE pointers, aligned to
     float* m_scale;                /* [ceil(n / ST_ADAMW_BLOCK)] in/out with states in 8 bits, else NULL */
     float* v_scale;
     void* copy;                    /* [n] out: the new parameters as bfloat16 (operands of products), or NULL */
-    int64_t n;                     /* >= 0 */
+    int64_t n;                     /* >= 0; at most 2^33, as is the sum over the list */
     double weight_decay;
 } st_adamw_tensor;
 

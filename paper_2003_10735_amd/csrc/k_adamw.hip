@@ -284,7 +284,7 @@ template <class F> static void for_grads(const st_adamw_tensor* t, int n, F f)
         for (; at < n && l.count < NORM_PER_LAUNCH; ++at) {
             if (t[at].n == 0) continue;
             const int64_t more = ceil_div(t[at].n, tile);
-            if (l.count && tiles + more > 0x7fffffff) break;
+            if (l.count && tiles + more > 0xffffff) break;
             l.g[l.count] = t[at].grad;
             l.n[l.count] = t[at].n;
             tiles += more;
@@ -310,7 +310,7 @@ template <class F> static void for_pieces(const st_adamw_tensor* t, int n, doubl
         for (; at < n && l.n < ST_ADAMW_PER_LAUNCH; ++at) {
             if (t[at].n == 0) continue;
             const int64_t more = ceil_div(t[at].n, TILE);
-            if (l.n && tiles + more > 0x7fffffff) break;
+            if (l.n && tiles + more > 0xffffff) break;
             l.t[l.n] = TensorRef{t[at].param, t[at].grad, t[at].m, t[at].v, t[at].m_scale, t[at].v_scale, t[at].copy, t[at].n};
             l.decay[l.n] = (float)(1.0 - lr * t[at].weight_decay);
             tiles += more;

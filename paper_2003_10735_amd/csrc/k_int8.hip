@@ -259,7 +259,7 @@ constexpr int FEW_WAVES = 8;
 
 struct FewArgs {
     Product p;
-    const void* x; int x_bf16; int64_t x_pitch;      // FUSED: the tokens as they are, row by row
+    const void* x; int x_bf16; int64_t x_row, x_step;        // FUSED: the tokens as they are: elements between two, and between two values
     int per_wave;                                            // bytes of the contraction a wavefront takes, a multiple of 64
     int lds_pitch;                                           // FUSED: bytes between two tokens' codes in LDS
     int group, per_token;                                    // FUSED: wavefronts along a token, a power of two; a thread's runs of a token
@@ -277,6 +277,7 @@ __device__ __forceinline__ void few_quantize(const FewArgs& f, char* codes, unsi
     const int m = (int)p.m, k = (int)p.k, end = FEW_WAVES * f.per_wave;
     const int threads = f.group * 64, lane = threadIdx.x & (threads - 1);
     const int first = __builtin_amdgcn_readfirstlane(threadIdx.x / threads), step = FEW_WAVES / f.group;
+    const bool whole = k >= 8 && f.x_step == 1;
     if ((int)threadIdx.x < m) tops[threadIdx.x] = 0;
     Raw8<T> v[KEEP];
     int r = first, c = 0;
@@ -284,8 +285,8 @@ __device__ __forceinline__ void few_quantize(const FewArgs& f, char* codes, unsi
     for (int j = 0; j < KEEP; ++j) {
         const int at = (c * threads + lane) * 8;
         if (r < m) {
-            if (k < 8) v[j].load_short((const T*)f.x + r * f.x_pitch + at, k - at);
-            else v[j].load((const T*)f.x + r * f.x_pitch + run_start<8>(at, k));
+            const T* row = (const T*)f.x + r * f.x_row;
+            if (whole) v[j].load(row + run_start<8>(at, k)); else v[j].load_short(row + at * f.x_step, k - at, f.x_step);
         }
         if (++c == f.per_token) { c = 0; r += step; }
     }
@@ -295,7 +296,7 @@ __device__ __forceinline__ void few_quantize(const FewArgs& f, char* codes, unsi
     for (int j = 0; j < KEEP; ++j) {
         if (r < m) {
             const int d = (c * threads + lane) * 8 - (k - 8);
-            if (k >= 8 && d > 0) v[j].down(min(d, 8));
+            if (whole && d > 0) v[j].down(min(d, 8));
             unsigned top = 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) top = max(top, abs_bits(v[j][i]));
@@ -443,9 +444,9 @@ template <int NT, bool FUSED> static void few_launch(Ctx& c, const FewArgs& f)
 }
 void product_few(Ctx& c, const Product& p, const QuantSource* x)
 {
-    FewArgs f{p, nullptr, 0, 0, (int)few_per_wave(p.k), (int)(FEW_WAVES * few_per_wave(p.k) + 16), 0, 0};
+    FewArgs f{p, nullptr, 0, 0, 0, (int)few_per_wave(p.k), (int)(FEW_WAVES * few_per_wave(p.k) + 16), 0, 0};
     if (x) {
-        f.x = x->x; f.x_bf16 = x->bf16; f.x_pitch = x->pitch;
+        f.x = x->x; f.x_bf16 = x->bf16; f.x_row = x->along ? x->pitch : 1; f.x_step = x->along ? 1 : x->pitch;
         few_shape(p.m, p.k, &f.group, &f.per_token);
         few_launch<1, true>(c, f);
     } else if (p.m <= 16) few_launch<1, false>(c, f);

@@ -51,7 +51,7 @@ struct Extent { int64_t m, n, k; };
 struct Form { int tile; int splits[2]; };
 Form form_of(const Extent* e, int count);
 void products(Ctx& c, const Product* p, int count);
-// One product of few tokens: a launch of its own kind.  x: the tokens, row by row, which it quantises itself; null: p.a holds their codes.
+// One product of few tokens: a launch of its own kind.  x: the tokens, which it quantises itself; null: p.a holds their codes.
 bool few_tokens(int64_t m, int64_t n, int64_t k);
 bool few_fused(int64_t m, int64_t n, int64_t k, int is_bf16);
 void product_few(Ctx& c, const Product& p, const QuantSource* x);

@@ -7,7 +7,8 @@
 namespace st {
 namespace {
 
-constexpr int64_t MAX_DIM = 0x7fffffff, MAX_PITCH = 1 << 23;
+// A launch holds fewer than 2^32 threads: rows that take a block each, tiles of 512 threads, tiles of an optimiser step.
+constexpr int64_t MAX_DIM = (1 << 24) - 1, MAX_PITCH = 1 << 23, MAX_VALUES = (int64_t)1 << 33;
 
 struct Carve {      // 256-byte aligned pieces of a workspace
     char* base; size_t used = 0;
@@ -92,7 +93,14 @@ BackwardSpace backward_space(char* ws, int64_t m, int64_t n, int64_t k)
     s.bytes = w.used + 256;
     return s;
 }
-bool tiles_ok(int64_t a, int64_t b) { return ceil_div(a, 64) * ceil_div(b, 64) <= MAX_DIM / 512; }
+bool tiles_ok(int64_t a, int64_t b) { return ceil_div(a, 64) * ceil_div(b, 64) < (1 << 23); }
+bool products_ok(const Extent* e, int count)
+{
+    const Form f = form_of(e, count);
+    int64_t blocks = 0;
+    for (int i = 0; i < count; ++i) blocks += ceil_div(e[i].m, f.tile) * ceil_div(e[i].n, f.tile) * f.splits[i];
+    return blocks < (1 << 23);
+}
 
 }  // namespace
 }  // namespace st
@@ -148,7 +156,7 @@ int st_int8_linear(const st_matrix* x, const int8_t* wq, int64_t w_pitch, const 
     Ctx c{(hipStream_t)stream, ST_OK};
     const QuantSource tokens = source(*x, along, false);
     const Product p{s.x.q, s.x.pitch, s.x.scale, wq, w_pitch, w_scale, m, n, k, y, y_dtype == ST_BF16, y_pitch, bias, relu, s.slabs};
-    if (along && few_fused(m, n, k, tokens.bf16)) { product_few(c, p, &tokens); return c.status; }
+    if (few_fused(m, n, k, tokens.bf16)) { product_few(c, p, &tokens); return c.status; }
     if (along && narrow_layer(m, n, k)) { product_narrow(c, p, tokens); return c.status; }
     const QuantTask task{tokens, s.x, s.parts, nullptr, nullptr};
     quantize(c, &task, 1);
@@ -162,6 +170,8 @@ size_t st_int8_linear_backward_workspace(int64_t m, int64_t n, int64_t k)
     if (!size_ok(m, 0) || !size_ok(n, 1) || !size_ok(k, 1) || n > MAX_PITCH || k > MAX_PITCH || !tiles_ok(m, n) || !tiles_ok(m, k)
         || !tiles_ok(n, k))
         return 0;
+    const Extent e[2] = {{n, k, std::max<int64_t>(m, 1)}, {std::max<int64_t>(m, 1), k, n}};
+    if (!products_ok(e, 2) || !products_ok(e, 1) || !products_ok(e + 1, 1)) return 0;
     return backward_space(nullptr, m, n, k).bytes;
 }
 
@@ -216,10 +226,10 @@ static int check_tensors(const st_adamw_tensor* t, int32_t n)
     if (n && !t) return ST_ERR_NULL;
     int64_t all = 0;
     for (int i = 0; i < n; ++i) {
-        if (t[i].n < 0 || t[i].n > (int64_t)1 << 40) return ST_ERR_SHAPE;
+        if (t[i].n < 0 || t[i].n > MAX_VALUES) return ST_ERR_SHAPE;
         all += t[i].n;
     }
-    return all > (int64_t)1 << 40 ? ST_ERR_SHAPE : ST_OK;
+    return all > MAX_VALUES ? ST_ERR_SHAPE : ST_OK;
 }
 
 size_t st_adamw_workspace(const st_adamw_tensor* tensors, int32_t n_tensors)
@@ -261,7 +271,7 @@ int st_adamw_step(const st_adamw_tensor* tensors, int32_t n_tensors, const st_ad
 int st_adamw_state(const int8_t* m, const float* m_scale, const uint8_t* v, const float* v_scale, int64_t n, float* m_out,
                    float* v_out, void* stream)
 {
-    if (n < 0 || n > (int64_t)1 << 40) return ST_ERR_SHAPE;
+    if (n < 0 || n > MAX_VALUES) return ST_ERR_SHAPE;
     if (n == 0 || (!m_out && !v_out)) return ST_OK;
     if ((m_out && (!m || !m_scale)) || (v_out && (!v || !v_scale))) return ST_ERR_NULL;
     if (!is_aligned(m_out, 4) || !is_aligned(v_out, 4) || !is_aligned(m_scale, 4) || !is_aligned(v_scale, 4)) return ST_ERR_ARG;

@@ -88,11 +88,12 @@ template <int V> struct Run<bf16, V> {
         if constexpr (V == 8) { const u32x4_t u = *(const u32x4_2*)p; w[0] = u[0]; w[1] = u[1]; w[2] = u[2]; w[3] = u[3]; }
         else { const u32x2 u = *(const u32x2_2*)p; w[0] = u[0]; w[1] = u[1]; }
     }
-    __device__ __forceinline__ void load_short(const bf16* p, int n)
+    __device__ __forceinline__ void load_short(const bf16* p, int n, int64_t step = 1)      // one by one, `step` apart
     {
+        const unsigned short* u = (const unsigned short*)p;
 #pragma unroll
         for (int i = 0; i < V / 2; ++i) {
-            const unsigned lo = 2 * i < n ? ((const unsigned short*)p)[2 * i] : 0u, hi = 2 * i + 1 < n ? ((const unsigned short*)p)[2 * i + 1] : 0u;
+            const unsigned lo = 2 * i < n ? u[2 * i * step] : 0u, hi = 2 * i + 1 < n ? u[(2 * i + 1) * step] : 0u;
             w[i] = lo | hi << 16;
         }
     }
@@ -124,10 +125,10 @@ template <int V> struct Run<float, V> {
 #pragma unroll
         for (int i = 0; i < V; i += 4) { const f32x4_t a = *(const f32x4_4*)(p + i); v[i] = a[0]; v[i + 1] = a[1]; v[i + 2] = a[2]; v[i + 3] = a[3]; }
     }
-    __device__ __forceinline__ void load_short(const float* p, int n)
+    __device__ __forceinline__ void load_short(const float* p, int n, int64_t step = 1)
     {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = i < n ? p[i] : 0.f;
+        for (int i = 0; i < V; ++i) v[i] = i < n ? p[i * step] : 0.f;
     }
     __device__ __forceinline__ void down(int d)
     {

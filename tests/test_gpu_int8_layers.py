@@ -163,6 +163,7 @@ def test_linear_few_tokens(m, k):
     """Around the sizes up to which every block quantises the tokens itself, in both types, aligned and not."""
     check_linear(m, k, 50, "bf16", "f32")
     check_linear(m, k, 17, "f32", "bf16", "inside")
+    check_linear(m, k, 33, "bf16" if m % 2 else "f32", "f32", "columns")
 
 
 @pytest.mark.parametrize("m", [1, 70])
