@@ -279,3 +279,27 @@ def test_stream_graph_and_other_gradients():
     reset()
     st.st_adamw_step(t, 1, 0.01, workspace=work)
     assert torch.equal(params[1], start[1])
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_offsets_that_pass_32_bits(bits):
+    """A tensor of more than 2^31 values: its end is what the same values are in a tensor of their own."""
+    n, tail = (1 << 31) + 5 * RUN + 77, 3 * RUN + 77
+    big = [torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    small = [torch.empty(tail, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    g = torch.Generator(device="cuda")
+    g.manual_seed(13)
+    for b, s in zip(big, small):
+        s.normal_(generator=g)
+        b[n - tail:] = s
+    states = [st.new_adamw_state([x], bits) for x in (big[0], small[0])]
+    for x, state in zip((big, small), states):
+        t = st.AdamWTensors([x[0]], [x[1]], **state, weight_decay=0.01)
+        st.st_adamw_step(t, 1, 0.01, max_norm=1.0)
+        st.st_adamw_step(t, 2, 0.01, max_norm=1.0)
+    # (the norms are of the same squares, added in another order: the factor may differ in its last place)
+    assert ((big[0][n - tail:].float() - small[0].float()).abs() <= 2.0 ** -7 * small[0].float().abs()).all()
+    for name in ("m", "v"):
+        a, b = states[0][name][0][n - tail:].float(), states[1][name][0].float()
+        assert ((a - b).abs() <= (1 if bits == 8 else TOL * b.abs())).all()
+    assert (big[0][:1000] == 0).all()

@@ -362,3 +362,26 @@ def test_other_stream_and_graph():
         call()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, [y] + outs)), i
+
+
+def test_offsets_that_pass_32_bits():
+    """More than 2^31 values of x, of its codes, and of the result: rows at the end are what the same rows are alone."""
+    m, k, n = 40000, 60000, 17
+    base = rand((8, k), 1, "bf16")
+    x = base.repeat(m // 8, 1)
+    _, wq, ws = weights(n, k, 2)
+    y = st.st_int8_linear(x, wq, ws, out_dtype=torch.float32)
+    alone = st.st_int8_linear(base, wq, ws, out_dtype=torch.float32)
+    for first in (0, 35784, m - 8):          # 35784 * k is where 31 bits end
+        assert torch.equal(y[first:first + 8], alone)
+    q, s = st.st_int8_quantize(x)
+    q1, s1 = st.st_int8_quantize(base)
+    assert torch.equal(q[m - 8:], q1) and torch.equal(s[m - 8:], s1)
+    del x, q
+    m, n = 70000, 33000
+    x = base[:, :64].contiguous().repeat(m // 8, 1)
+    _, wq, ws = weights(n, 64, 3)
+    y = st.st_int8_linear(x, wq, ws)
+    alone = st.st_int8_linear(base[:, :64].contiguous(), wq, ws)
+    for first in (0, 65072, m - 8):
+        assert torch.equal(y[first:first + 8], alone)
