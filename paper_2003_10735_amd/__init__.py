@@ -369,13 +369,16 @@ def st_object_weights(labels, n_classes: int, radius: int, factor: int = 5, back
 _DTYPES = None
 
 
+def _types():
+    global _DTYPES
+    import torch
+    _DTYPES = {torch.float32: ST_F32, torch.bfloat16: ST_BF16}
+    return _DTYPES
+
+
 def _dtype(t, where):
     """ST_F32 or ST_BF16 of a tensor."""
-    global _DTYPES
-    if _DTYPES is None:
-        import torch
-        _DTYPES = {torch.float32: ST_F32, torch.bfloat16: ST_BF16}
-    d = _DTYPES.get(t.dtype)
+    d = (_DTYPES or _types()).get(t.dtype)
     if d is None:
         raise StError(ST_ERR_ARG, where)
     return d
@@ -383,20 +386,24 @@ def _dtype(t, where):
 
 def _matrix(t, where):
     """A two-dimensional tensor as the library takes it: either of its strides 1."""
-    if t.dim() != 2:
+    shape = t.shape
+    if len(shape) != 2:
         raise StError(ST_ERR_SHAPE, where)
-    return StMatrix(t.data_ptr(), _dtype(t, where), *t.shape, *t.stride())
+    return StMatrix(t.data_ptr(), _dtype(t, where), *shape, *t.stride())
 
 
 def _out_matrix(t, rows, cols, where):
     """Checks a result that lies row by row; returns its pitch."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or (cols > 1 and t.stride(1) != 1):
+    if t.shape != (rows, cols):
         raise StError(ST_ERR_SHAPE, where)
-    return t.stride(0) if rows > 1 else max(cols, t.stride(0))
+    pitch, step = t.stride()
+    if step != 1 and cols > 1:
+        raise StError(ST_ERR_SHAPE, where)
+    return pitch if rows > 1 or pitch > cols else cols
 
 
 def _float_vector(t, n, where):
-    if t.numel() != n or not t.is_contiguous() or _dtype(t, where) != ST_F32:
+    if t.numel() != n or not t.is_contiguous() or (_DTYPES or _types()).get(t.dtype) != ST_F32:
         raise StError(ST_ERR_SHAPE, where)
     return t.data_ptr()
 
@@ -446,18 +453,25 @@ def st_int8_linear(x, wq, w_scale, bias=None, relu: bool = False, out=None, out_
     out_dtype, else of x's type."""
     where = "st_int8_linear"
     mx = _matrix(x, where)
-    m, k = x.shape
-    n = wq.shape[0]
-    if wq.dim() != 2 or wq.shape[1] < k or wq.stride(1) != 1 or wq.element_size() != 1:
+    m, k = mx.rows, mx.cols
+    if wq.dim() != 2:
+        raise StError(ST_ERR_SHAPE, where)
+    n, width = wq.shape
+    w_pitch, step = wq.stride()
+    if width < k or step != 1 or wq.element_size() != 1:
         raise StError(ST_ERR_SHAPE, where)
     if out is None:
         import torch
         out = torch.empty((m, n), dtype=out_dtype or x.dtype, device=x.device)
     pitch = _out_matrix(out, m, n, where)
-    ws = workspace if workspace is not None else new_int8_workspace(m, n, k, device=x.device)
-    _check(lib().st_int8_linear(C.byref(mx), wq.data_ptr(), wq.stride(0) if n > 1 else wq.shape[1], _float_vector(w_scale, n, where), n,
-                                None if bias is None else _float_vector(bias, n, where), 1 if relu else 0, out.data_ptr(),
-                                _dtype(out, where), pitch, ws.data_ptr(), _stream(stream)), where)
+    if workspace is None:
+        workspace = new_int8_workspace(m, n, k, device=x.device)
+    status = (_LIB or lib()).st_int8_linear(
+        C.byref(mx), wq.data_ptr(), w_pitch if n > 1 else width, _float_vector(w_scale, n, where), n,
+        None if bias is None else _float_vector(bias, n, where), 1 if relu else 0, out.data_ptr(), _dtype(out, where), pitch,
+        workspace.data_ptr(), _stream(stream))
+    if status:
+        raise StError(status, where)
     return out
 
 

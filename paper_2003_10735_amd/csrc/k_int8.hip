@@ -160,6 +160,13 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
     // products.
     constexpr int LOADS = (AR + BR) / 8 / WAVES;      // of a wavefront and stage
     static_assert((DEPTH - 1) * LOADS < 64, "the counter of loads under way");
+    // what the sums meet on their way out is asked for before the loop
+    constexpr int PITCH = WN + 4, RUNS = WN / 8, ROWS = 64 / RUNS;
+    const int run = lane % RUNS, row = lane / RUNS;
+    const int64_t n = n0 + wn + run * 8;
+    Column col[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) col[i] = column_of(p, n + i);
     if (first < last) {
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) if (first + d < last) stage(first + d, d);
@@ -188,16 +195,13 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
 
     // Out through LDS, 32 tokens of a wavefront at a time: sums go in four neighbouring channels at a time and come out as runs along a row.
     __syncthreads();
-    constexpr int PITCH = WN + 4, RUNS = WN / 8, ROWS = 64 / RUNS;
     static_assert(WAVES * 32 * PITCH * 4 <= DEPTH * BUF, "room for the sums");
     int* mine = (int*)lds + wave * 32 * PITCH;
-    const int run = lane % RUNS, row = lane / RUNS;
-    const int64_t n = n0 + wn + run * 8;
-    Column col[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) col[i] = g.splits > 1 ? Column{0.f, 0.f} : column_of(p, n + i);
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
+        float sm[32 / ROWS];
+#pragma unroll
+        for (int h = 0; h < 32 / ROWS; ++h) sm[h] = p.a_scale[min(m0 + wm + j * 32 + h * ROWS + row, p.m - 1)];
 #pragma unroll
         for (int i = 0; i < NA; ++i)
 #pragma unroll
@@ -220,10 +224,9 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
                     for (int i = 0; i < 8; ++i) if (n + i < p.n) to[i] = i < 4 ? lo[i] : hi[i - 4];
                 continue;
             }
-            const float sm = p.a_scale[m];
             float v[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = finish((float)(i < 4 ? lo[i] : hi[i - 4]), sm, col[i], p.relu);
+            for (int i = 0; i < 8; ++i) v[i] = finish((float)(i < 4 ? lo[i] : hi[i - 4]), sm[h], col[i], p.relu);
             store_out<8>(p, m, n, v);
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
@@ -364,6 +367,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 4) void k_int8_few(const FewArgs f)
     auto ra = channels(n0);
     Group g[2];
     ask(ra, from, g[0]);
+    Column col = column_of(p, n0 + (threadIdx.x & 15));
     if constexpr (FUSED) {
         if (f.x_bf16) few_quantize<bf16>(f, codes, tops, scales); else few_quantize<float>(f, codes, tops, scales);
         __syncthreads();
@@ -391,7 +395,12 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 4) void k_int8_few(const FewArgs f)
             use(k + AHEAD * 64, g[1]);
         }
         const int64_t at = n0, next = FUSED ? n0 + (int64_t)gridDim.x * 16 : p.n;
-        if (next < p.n) { ra = channels(next); ask(ra, from, g[0]); }      // the next channels' weights, while these are added
+        const Column mine = col;
+        if (next < p.n) {      // the next channels' weights, while these are added
+            ra = channels(next);
+            ask(ra, from, g[0]);
+            col = column_of(p, next + (threadIdx.x & 15));
+        }
         int* part = (int*)lds;
 #pragma unroll
         for (int t = 0; t < NT; ++t) *(i32x4*)(part + (wave * NT + t) * 256 + (lane & 15) * 16 + (lane >> 4) * 4) = acc[t];
@@ -402,7 +411,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 4) void k_int8_few(const FewArgs f)
             int sum = 0;
 #pragma unroll
             for (int w = 0; w < FEW_WAVES; ++w) sum += part[w * NT * 256 + i];
-            const float v[1] = {finish((float)sum, FUSED ? scales[m] : p.a_scale[m], column_of(p, n), p.relu)};
+            const float v[1] = {finish((float)sum, FUSED ? scales[m] : p.a_scale[m], mine, p.relu)};
             store_out<1>(p, m, n, v);
         }
         if (next >= p.n) break;
@@ -509,6 +518,10 @@ template <class T, int RUNS> __global__ __launch_bounds__(256) void k_int8_narro
     __syncthreads();
     const int run = threadIdx.x & 15, row = threadIdx.x >> 4;
     for (int base = 0; base < n; base += 128) {
+        const int c = base + run * 8;
+        Column col[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) col[i] = column_of(p, c + i);
         if (base + wave * 32 < n) {
             i32x16 acc = {};
 #pragma unroll
@@ -520,11 +533,7 @@ template <class T, int RUNS> __global__ __launch_bounds__(256) void k_int8_narro
         }
         if (base + 128 < n) weights(base + 128 + wave * 32);
         __syncthreads();
-        const int c = base + run * 8;
         if (c < n) {
-            Column col[8];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) col[i] = column_of(p, c + i);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const int r = h * 16 + row;
