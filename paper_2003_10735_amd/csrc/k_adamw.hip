@@ -6,7 +6,9 @@
 
 namespace st {
 
-constexpr int TILE = 2048;                 // values a block of 256 threads steps: two runs of 256 a wavefront
+// Values a block of 256 threads steps: runs of 256 a wavefront, two with states in 8 bits, one with 32 (77 M values with states in 32 bits,
+// the whole call, 435 us with 1024, 447 with 2048, 459 with 4096; 436 M with 8 bits 2112, 2032, 2093).
+constexpr int tile_of(int bits) { return bits == 8 ? 2048 : 1024; }
 constexpr int NORM_BLOCKS = 2048, NORM_PER_LAUNCH = 160;
 // values of a tile of the norm: small lists are spread over more blocks
 static int norm_tile(int64_t all) { return all <= (int64_t)NORM_BLOCKS * 2048 ? 2048 : 8192; }
@@ -152,21 +154,21 @@ __device__ __forceinline__ float code_root(float y)
     return fabsf(s - q) > 0.4999f ? rintf(sqrt_rn(y)) : q;
 }
 
-// One tile.  A lane takes four neighbouring values of a run of 256, a wavefront two runs, all of whose loads are under way before the
+// One tile.  A lane takes four neighbouring values of a run of 256, a wavefront one or two runs, whose loads are all under way before the
 // first is used.  What the codes depend on is float32 operations of their own (no fused ones), in the order of the header's formulas:
 // codes change by whole steps, so two programs that are to give the same codes have to round alike.  The parameters' quotient is a
 // product with a reciprocal of one unit's accuracy.
 template <class P, class G, int BITS>
 __global__ __launch_bounds__(256) void k_adamw(const TensorList l, const AdamwConstants k, const NormRef nr)
 {
-    constexpr int RUNS = TILE / 1024;
+    constexpr int RUNS = tile_of(BITS) / 1024;
     __shared__ double sums[4];
     const int i = tensor_of<ST_ADAMW_PER_LAUNCH>(l.first, l.n, blockIdx.x);
     const TensorRef& t = l.t[i];
     P* pp = (P*)t.p;
     const G* gg = (const G*)t.g;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const long long base = (long long)(blockIdx.x - l.first[i]) * TILE + wave * (RUNS * 256);
+    const long long base = (long long)(blockIdx.x - l.first[i]) * tile_of(BITS) + wave * (RUNS * 256);
     float p[RUNS][4], g[RUNS][4], m[RUNS][4], v[RUNS][4], ms[RUNS], vs[RUNS];
     unsigned cm[RUNS], cv[RUNS];
     int n[RUNS];
@@ -300,7 +302,7 @@ int64_t adamw_norm_parts(const st_adamw_tensor* t, int n)
     return parts;
 }
 // Calls f(list, tiles) for the list in pieces that a launch can take.
-template <class F> static void for_pieces(const st_adamw_tensor* t, int n, double lr, F f)
+template <class F> static void for_pieces(const st_adamw_tensor* t, int n, double lr, int tile, F f)
 {
     for (int at = 0; at < n;) {
         TensorList l;
@@ -309,7 +311,7 @@ template <class F> static void for_pieces(const st_adamw_tensor* t, int n, doubl
         int64_t tiles = 0;
         for (; at < n && l.n < ST_ADAMW_PER_LAUNCH; ++at) {
             if (t[at].n == 0) continue;
-            const int64_t more = ceil_div(t[at].n, TILE);
+            const int64_t more = ceil_div(t[at].n, tile);
             if (l.n && tiles + more > 0xffffff) break;
             l.t[l.n] = TensorRef{t[at].param, t[at].grad, t[at].m, t[at].v, t[at].m_scale, t[at].v_scale, t[at].copy, t[at].n};
             l.decay[l.n] = (float)(1.0 - lr * t[at].weight_decay);
@@ -323,7 +325,7 @@ template <class F> static void for_pieces(const st_adamw_tensor* t, int n, doubl
 template <class P, class G, int BITS>
 static void step(Ctx& c, const st_adamw_tensor* t, int n, double lr, const AdamwConstants& k, NormRef nr)
 {
-    for_pieces(t, n, lr, [&](const TensorList& l, unsigned tiles) {
+    for_pieces(t, n, lr, tile_of(BITS), [&](const TensorList& l, unsigned tiles) {
         ST_LAUNCH(c, "adamw", (k_adamw<P, G, BITS>), dim3(tiles), dim3(256), 0, l, k, nr);
         nr.out = nullptr;
     });
@@ -334,7 +336,7 @@ void adamw_step(Ctx& c, const st_adamw_tensor* t, int n, const st_adamw_opts& o,
 {
     NormRef nr{nullptr, nullptr, 0, nullptr};
     int64_t tiles = 0;
-    for (int i = 0; i < n; ++i) tiles += ceil_div(t[i].n, TILE);
+    for (int i = 0; i < n; ++i) tiles += ceil_div(t[i].n, tile_of(o.state_bits));
     if (workspace) {
         double* parts = (double*)(workspace + 256);
         int done = 0;
@@ -348,7 +350,7 @@ void adamw_step(Ctx& c, const st_adamw_tensor* t, int n, const st_adamw_opts& o,
             done += (int)blocks;
         });
         // Up to two rounds of blocks the step adds the parts itself: they are few then, and a launch of its own takes longer.
-        if (tiles > 0 && tiles <= 4096 && done <= 2048) nr = NormRef{nullptr, parts, done, o.grad_norm};
+        if (tiles > 0 && tiles <= 4096 && done <= NORM_BLOCKS) nr = NormRef{nullptr, parts, done, o.grad_norm};
         else {
             ST_LAUNCH(c, "grad_norm", k_norm, dim3(1), dim3(256), 0, parts, done, (float*)workspace, o.grad_norm);
             nr.norm = (const float*)workspace;
