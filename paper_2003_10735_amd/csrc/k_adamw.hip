@@ -136,22 +136,35 @@ __device__ __forceinline__ float run_multiplier(unsigned top, float codes2, floa
     *scale = a * (1.f / codes2);
     return codes2 * (1.f / a);
 }
-// Square root, rounded to the nearest float32.  The instruction's result s is off by one unit in the last place at most; s (s +- unit) is
-// s^2 beyond the middle between the two candidates, so the sign of its difference from x, which a fused multiply-add has exactly, decides.
+// Square root, rounded to the nearest float32, of 0 and of normal numbers from 2^-96 on (and of infinity and NaN).  The instruction's
+// result s is off by one unit in the last place at most; s (s +- unit) is s^2 beyond the middle between the two candidates, so the sign of
+// its difference from x, which a fused multiply-add has exactly, decides.
 __device__ __forceinline__ float sqrt_rn(float x)
 {
-    if (x < 0x1p-96f && x > 0.f) return sqrtf(x);
     const float s = __builtin_amdgcn_sqrtf(x);
     const float lo = __uint_as_float(__float_as_uint(s) - 1), hi = __uint_as_float(__float_as_uint(s) + 1);
     const float r_lo = __builtin_fmaf(-lo, s, x), r_hi = __builtin_fmaf(-hi, s, x);
     const float t = r_lo <= 0.f ? lo : s;
     return r_hi > 0.f ? hi : t;
 }
-// rint of the square root rounded to float32, for 0 <= y < 2^17: the instruction's own result settles it unless it lies next to a middle
-__device__ __forceinline__ float code_root(float y)
+constexpr unsigned SQRT_LEAST = 0x0f800000u;      // 2^-96
+constexpr float ROUND = 12582912.f;               // 1.5 * 2^23: a sum with it ends in the other number's nearest whole number, low byte first
+
+// Codes of four values: their shares y times the sign of `of`, as four bytes.  The instruction's root settles the whole number unless it
+// lies next to a middle, which one look at all four finds out.  A value that is no number, or a share of one, gets the byte 0.
+__device__ __forceinline__ unsigned codes_of(const float (&y)[4], const float (&of)[4], const float (&least)[4])
 {
-    const float s = __builtin_amdgcn_sqrtf(y), q = rintf(s);
-    return fabsf(s - q) > 0.4999f ? rintf(sqrt_rn(y)) : q;
+    float t[4], off = 0.f;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float s = __builtin_copysignf(fmaxf(__builtin_amdgcn_sqrtf(y[e]), least[e]), of[e]);
+        t[e] = s + ROUND;
+        off = fmaxf(off, fabsf(s - (t[e] - ROUND)));
+    }
+    if (off > 0.4999f)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) t[e] = __builtin_copysignf(fmaxf(sqrt_rn(y[e]), least[e]), of[e]) + ROUND;
+    return pack4(__float_as_uint(t[0]), __float_as_uint(t[1]), __float_as_uint(t[2]), __float_as_uint(t[3]));
 }
 
 // One tile.  A lane takes four neighbouring values of a run of 256, a wavefront one or two runs, whose loads are all under way before the
@@ -212,30 +225,39 @@ __global__ __launch_bounds__(256) void k_adamw(const TensorList l, const AdamwCo
             m[j][e] = m[j][e] * k.beta1 + ge * k.one_minus_beta1;
             v[j][e] = v[j][e] * k.beta2 + ge * ge * k.one_minus_beta2;
             u[e] = BITS == 8 ? sqrt_rn(v[j][e]) : sqrtf(v[j][e]);
-            p[j][e] = p[j][e] * decay - k.step_scale * (m[j][e] * __builtin_amdgcn_rcpf(u[e] * k.inv_sqrt_bc2 + k.eps));
         }
+        if constexpr (BITS == 8) {
+            unsigned least = 0xffffffffu;      // (0 is none of the small ones)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) least = min(least, __float_as_uint(v[j][e]) - 1);
+            if (least < SQRT_LEAST - 1)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) u[e] = sqrtf(v[j][e]);
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            p[j][e] = __builtin_fmaf(-k.step_scale, m[j][e] * __builtin_amdgcn_rcpf(__builtin_fmaf(u[e], k.inv_sqrt_bc2, k.eps)), p[j][e] * decay);
         store4(pp + at, n[j], p[j]);
         if (t.copy) store4((bf16*)t.copy + at, n[j], p[j]);
         if constexpr (BITS == 32) {
             store4((float*)t.m + at, n[j], m[j]);
             store4((float*)t.v + at, n[j], v[j]);
         } else {
-            unsigned tm = 0, tv = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < n[j]) { tm = max(tm, abs_bits(m[j][e])); tv = max(tv, abs_bits(u[e])); }
+            // (values that do not exist are zeros: their gradient and state were)
+            const unsigned tm = max(max(abs_bits(m[j][0]), abs_bits(m[j][1])), max(abs_bits(m[j][2]), abs_bits(m[j][3])));
+            const unsigned tv = max(max(__float_as_uint(u[0]) & ABS_BITS, __float_as_uint(u[1]) & ABS_BITS),
+                                    max(__float_as_uint(u[2]) & ABS_BITS, __float_as_uint(u[3]) & ABS_BITS));
             float new_ms, new_vs;
             const float rm = run_multiplier(wave_max(tm), 16129.f, &new_ms), rv = run_multiplier(wave_max(tv), 65025.f, &new_vs);
             if (lane == 0) { t.ms[run / 256] = new_ms; t.vs[run / 256] = new_vs; }
-            unsigned qm = 0, qv = 0;
+            const float one = rv == 0.f ? 0.f : 1.f;
+            float ym[4], yv[4], none[4], some[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const int a = rm == 0.f ? 0 : (int)code_root(fabsf(m[j][e]) * rm);
-                int b = rv == 0.f ? 0 : (int)code_root(u[e] * rv);
-                if (rv != 0.f && b == 0 && u[e] > 0.f) b = 1;
-                qm |= (unsigned)(uint8_t)(m[j][e] < 0.f ? -a : a) << (8 * e);
-                qv |= (unsigned)(uint8_t)b << (8 * e);
+                ym[e] = fabsf(m[j][e]) * rm; none[e] = 0.f;
+                yv[e] = u[e] * rv; some[e] = u[e] > 0.f ? one : 0.f;
             }
+            const unsigned qm = codes_of(ym, m[j], none), qv = codes_of(yv, u, some);
             store_codes((char*)t.m + at, n[j], qm); store_codes((char*)t.v + at, n[j], qv);
         }
     }
