@@ -42,28 +42,29 @@ template <int MOST> __device__ __forceinline__ int tensor_of(const unsigned* fir
     return before - 1;
 }
 
+// What a step writes is read by the next one: its stores do not ask for room in L2.
 template <class T> __device__ __forceinline__ void store4(T* p, int n, const float (&v)[4])
 {
     if (n >= 4) {
         typedef T T4 __attribute__((ext_vector_type(4)));
         typedef T4 T4any __attribute__((aligned(sizeof(T))));
-        *(T4any*)p = T4{from_f32<T>(v[0]), from_f32<T>(v[1]), from_f32<T>(v[2]), from_f32<T>(v[3])};
+        __builtin_nontemporal_store(T4{from_f32<T>(v[0]), from_f32<T>(v[1]), from_f32<T>(v[2]), from_f32<T>(v[3])}, (T4any*)p);
         return;
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) if (i < n) p[i] = from_f32<T>(v[i]);
 }
 // four codes, of which `n` exist
-__device__ __forceinline__ unsigned load_codes(const void* p, int n)
+template <bool NT = false> __device__ __forceinline__ unsigned load_codes(const void* p, int n)
 {
-    if (n >= 4) return *(const u32_1*)p;
+    if (n >= 4) return ST_LOAD(NT, u32_1, p);
     unsigned c = 0;
     for (int e = 0; e < n; ++e) c |= (unsigned)((const uint8_t*)p)[e] << (8 * e);
     return c;
 }
 __device__ __forceinline__ void store_codes(void* p, int n, unsigned c)
 {
-    if (n >= 4) { *(u32_1*)p = c; return; }
+    if (n >= 4) { __builtin_nontemporal_store(c, (u32_1*)p); return; }
     for (int e = 0; e < n; ++e) ((uint8_t*)p)[e] = (uint8_t)(c >> (8 * e));
 }
 __device__ __forceinline__ double block_sum(double s, double* sums)      // of 256 threads, in one order; to every thread
@@ -171,7 +172,8 @@ __device__ __forceinline__ unsigned codes_of(const float (&y)[4], const float (&
 // first is used.  What the codes depend on is float32 operations of their own (no fused ones), in the order of the header's formulas:
 // codes change by whole steps, so two programs that are to give the same codes have to round alike.  The parameters' quotient is a
 // product with a reciprocal of one unit's accuracy.
-template <class P, class G, int BITS>
+// STREAM: the list is more than the cache behind L2 holds, and its loads do not ask for room either.
+template <class P, class G, int BITS, bool STREAM>
 __global__ __launch_bounds__(256) void k_adamw(const TensorList l, const AdamwConstants k, const NormRef nr)
 {
     constexpr int RUNS = tile_of(BITS) / 1024;
@@ -189,15 +191,15 @@ __global__ __launch_bounds__(256) void k_adamw(const TensorList l, const AdamwCo
     for (int j = 0; j < RUNS; ++j) {
         const long long run = base + j * 256, at = run + lane * 4;
         n[j] = t.n - at >= 4 ? 4 : t.n - at > 0 ? (int)(t.n - at) : 0;
-        load4(pp + at, n[j], p[j]);
-        load4(gg + at, n[j], g[j]);
+        load4<STREAM>(pp + at, n[j], p[j]);
+        load4<STREAM>(gg + at, n[j], g[j]);
         if constexpr (BITS == 32) {
-            load4((const float*)t.m + at, n[j], m[j]);
-            load4((const float*)t.v + at, n[j], v[j]);
+            load4<STREAM>((const float*)t.m + at, n[j], m[j]);
+            load4<STREAM>((const float*)t.v + at, n[j], v[j]);
         } else {
             ms[j] = vs[j] = 0.f;
             if (run < t.n) { ms[j] = t.ms[run / 256]; vs[j] = t.vs[run / 256]; }
-            cm[j] = load_codes((const char*)t.m + at, n[j]); cv[j] = load_codes((const char*)t.v + at, n[j]);
+            cm[j] = load_codes<STREAM>((const char*)t.m + at, n[j]); cv[j] = load_codes<STREAM>((const char*)t.v + at, n[j]);
         }
     }
     float factor = k.grad_scale;
@@ -345,10 +347,11 @@ template <class F> static void for_pieces(const st_adamw_tensor* t, int n, doubl
 }
 
 template <class P, class G, int BITS>
-static void step(Ctx& c, const st_adamw_tensor* t, int n, double lr, const AdamwConstants& k, NormRef nr)
+static void step(Ctx& c, const st_adamw_tensor* t, int n, double lr, const AdamwConstants& k, bool stream, NormRef nr)
 {
     for_pieces(t, n, lr, tile_of(BITS), [&](const TensorList& l, unsigned tiles) {
-        ST_LAUNCH(c, "adamw", (k_adamw<P, G, BITS>), dim3(tiles), dim3(256), 0, l, k, nr);
+        if (stream) ST_LAUNCH(c, "adamw", (k_adamw<P, G, BITS, true>), dim3(tiles), dim3(256), 0, l, k, nr);
+        else ST_LAUNCH(c, "adamw", (k_adamw<P, G, BITS, false>), dim3(tiles), dim3(256), 0, l, k, nr);
         nr.out = nullptr;
     });
 }
@@ -379,10 +382,16 @@ void adamw_step(Ctx& c, const st_adamw_tensor* t, int n, const st_adamw_opts& o,
         }
     }
     if (tiles == 0) return;
+    // One list stepped again and again, us a step with plain loads and with these: heads of 445 075 values, states in 32 bits, 24 of them
+    // (171 MB) 65 and 68, 48 (342 MB) 153 and 136, 200 683 and 566; in 8 bits, 48 (214 MB) 106 and 106, 96 (428 MB) 244 and 211.
+    const int64_t each = (o.param_dtype == ST_BF16 ? 2 : 4) + (o.grad_dtype == ST_BF16 ? 2 : 4) + (o.state_bits == 8 ? 2 : 8);
+    int64_t values = 0;
+    for (int i = 0; i < n; ++i) values += t[i].n;
+    const bool stream = values * each > (int64_t)256 << 20;
 #define ST_STEP(P, G)                                                  \
     do {                                                               \
-        if (o.state_bits == 8) step<P, G, 8>(c, t, n, o.lr, k, nr);    \
-        else step<P, G, 32>(c, t, n, o.lr, k, nr);                     \
+        if (o.state_bits == 8) step<P, G, 8>(c, t, n, o.lr, k, stream, nr);    \
+        else step<P, G, 32>(c, t, n, o.lr, k, stream, nr);                     \
     } while (0)
     if (o.param_dtype == ST_F32) { if (o.grad_dtype == ST_F32) ST_STEP(float, float); else ST_STEP(float, bf16); }
     else                         { if (o.grad_dtype == ST_F32) ST_STEP(bf16, float); else ST_STEP(bf16, bf16); }

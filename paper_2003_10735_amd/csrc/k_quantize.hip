@@ -30,7 +30,7 @@ struct Jobs { unsigned first1[4], first2[4]; int n; Job job[4]; };      // first
 template <class M, class T, int COUNT, class F> __device__ __forceinline__ void clear_masked(const M* row, int len, F at, Raw8<T> (&v)[COUNT])
 {
     Raw8<M> on[COUNT];
-    load_row<M, COUNT, int>(row, len, at, on);
+    load_row(row, len, at, on);
 #pragma unroll
     for (int k = 0; k < COUNT; ++k)
 #pragma unroll
@@ -50,7 +50,7 @@ struct Shared {
 // LANES threads a row.  A thread holds KEEP runs of eight values of its row, as they came, between the search for the largest and the
 // rounding, so a row of up to 8 * KEEP * LANES values is read once; longer rows read the rest twice.  A wavefront takes a row of up to 4096
 // bfloat16 values by itself: no barrier, eight loads under way.
-template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_role(const Job& j, unsigned block, Shared& sh)
+template <class T, int LANES, int KEEP, bool NT = false> __device__ __forceinline__ void rows_role(const Job& j, unsigned block, Shared& sh)
 {
     constexpr int MORE = 4;      // runs under way beyond those
     const int lane = threadIdx.x % LANES;
@@ -62,7 +62,7 @@ template <class T, int LANES, int KEEP> __device__ __forceinline__ void rows_rol
     unsigned top = 0;
     double total = 0.0;
     auto load = [&](auto at, auto& v) {
-        load_row(x, len, at, v);
+        load_row<NT>(x, len, at, v);
         if (!j.mask) return;
         if (j.mask_bf16) clear_masked((const bf16*)j.mask + row * j.mask_pitch, len, at, v);
         else clear_masked((const float*)j.mask + row * j.mask_pitch, len, at, v);
@@ -139,7 +139,7 @@ template <class T> __device__ __forceinline__ Columns columns_of(int64_t col, in
     const int64_t from = run_start<V, int64_t>(col, rows), d = col - from;
     return Columns{col, from, rows, d < V ? (int)d : V};
 }
-template <class T, class M, bool SHORT> struct Masked {
+template <class T, class M, bool SHORT, bool NT> struct Masked {
     static constexpr int V = across<T>();
     Run<T, V> x;
     Run<M, V> m;
@@ -147,10 +147,10 @@ template <class T, class M, bool SHORT> struct Masked {
     {
         const int n = SHORT && c.col < c.rows ? (int)(c.rows - c.col) : 0;
         if constexpr (SHORT) x.load_short((const T*)j.x + line * j.pitch + c.col, n);
-        else x.load((const T*)j.x + line * j.pitch + c.from);
+        else x.template load<NT>((const T*)j.x + line * j.pitch + c.from);
         if constexpr (!std::is_void<M>::value) {
             if constexpr (SHORT) m.load_short((const M*)j.mask + line * j.mask_pitch + c.col, n);
-            else m.load((const M*)j.mask + line * j.mask_pitch + c.from);
+            else m.template load<NT>((const M*)j.mask + line * j.mask_pitch + c.from);
         }
     }
     __device__ __forceinline__ void settle(const Columns& c)
@@ -175,19 +175,19 @@ template <class T, class M, bool SHORT> __device__ __forceinline__ void parts_lo
         float s[V] = {};
         const int64_t end = piece + 64 * STEP < to ? piece + 64 * STEP : to;
         int64_t k = piece;
-        auto see = [&](const Masked<T, M, SHORT>& v) {
+        auto see = [&](const Masked<T, M, SHORT, false>& v) {
 #pragma unroll
             for (int e = 0; e < V; ++e) { const float f = v[e]; top[e] = max(top[e], abs_bits(f)); s[e] += f; }
         };
         for (; k + (AHEAD - 1) * STEP < end; k += AHEAD * STEP) {
-            Masked<T, M, SHORT> v[AHEAD];
+            Masked<T, M, SHORT, false> v[AHEAD];
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) v[i].load(j, k + i * STEP, col);
 #pragma unroll
             for (int i = 0; i < AHEAD; ++i) { v[i].settle(col); see(v[i]); }
         }
         for (; k < end; k += STEP) {
-            Masked<T, M, SHORT> v;
+            Masked<T, M, SHORT, false> v;
             v.load(j, k, col);
             v.settle(col);
             see(v);
@@ -232,7 +232,7 @@ template <class T, class M, bool SHORT> __device__ __forceinline__ void turn_til
     constexpr int V = across<T>(), LANES = 64 / V, POS = 128 / groups<T>();
     const int c = (threadIdx.x % LANES) * V, group = threadIdx.x / LANES;
     const Columns col = columns_of<T>(row0 + c, j.rows);
-    Masked<T, M, SHORT> v[POS];
+    Masked<T, M, SHORT, true> v[POS];
     auto load = [&](unsigned tile) {       // (positions behind the last one: the last one, and codes of 0 below)
         const int64_t k = (int64_t)tile * 128 + group * POS;
 #pragma unroll
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(256, 3) void k_quantize_first(const Jobs jobs)
 template <class T, int LANES, int KEEP> __global__ __launch_bounds__(256) void k_quantize_rows(const Job j)
 {
     __shared__ Shared sh;
-    rows_role<T, LANES, KEEP>(j, blockIdx.x, sh);
+    rows_role<T, LANES, KEEP, true>(j, blockIdx.x, sh);
 }
 template <class T> static void rows_launch(Ctx& c, const Job& j, unsigned blocks)
 {

@@ -53,11 +53,15 @@ typedef u32x2 u32x2_2 __attribute__((aligned(2)));
 typedef f32x4_t f32x4_4 __attribute__((aligned(4)));
 typedef unsigned u32_1 __attribute__((aligned(1)));
 
+// A load of what is not read again soon, past the caches' order of use (NT), or a plain one.  (A macro: a template would lose the type's
+// alignment.)
+#define ST_LOAD(NT, TYPE, P) ((NT) ? __builtin_nontemporal_load((const TYPE*)(P)) : *(const TYPE*)(P))
+
 // Four consecutive values from p, of which `n` exist; the others are 0.
-__device__ __forceinline__ void load4(const bf16* p, int n, float (&v)[4])
+template <bool NT = false> __device__ __forceinline__ void load4(const bf16* p, int n, float (&v)[4])
 {
     if (n >= 4) {
-        const u32x2 w = *(const u32x2_2*)p;
+        const u32x2 w = ST_LOAD(NT, u32x2_2, p);
         v[0] = __uint_as_float(w[0] << 16); v[1] = __uint_as_float(w[0] & 0xffff0000u);
         v[2] = __uint_as_float(w[1] << 16); v[3] = __uint_as_float(w[1] & 0xffff0000u);
         return;
@@ -65,10 +69,10 @@ __device__ __forceinline__ void load4(const bf16* p, int n, float (&v)[4])
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = i < n ? (float)p[i] : 0.f;
 }
-__device__ __forceinline__ void load4(const float* p, int n, float (&v)[4])
+template <bool NT = false> __device__ __forceinline__ void load4(const float* p, int n, float (&v)[4])
 {
     if (n >= 4) {
-        const f32x4_t w = *(const f32x4_4*)p;
+        const f32x4_t w = ST_LOAD(NT, f32x4_4, p);
         v[0] = w[0]; v[1] = w[1]; v[2] = w[2]; v[3] = w[3];
         return;
     }
@@ -83,10 +87,10 @@ template <int V, class I> __device__ __forceinline__ I run_start(I at, I len) { 
 template <class T, int V> struct Run;
 template <int V> struct Run<bf16, V> {
     unsigned w[V / 2];
-    __device__ __forceinline__ void load(const bf16* p)
+    template <bool NT = false> __device__ __forceinline__ void load(const bf16* p)
     {
-        if constexpr (V == 8) { const u32x4_t u = *(const u32x4_2*)p; w[0] = u[0]; w[1] = u[1]; w[2] = u[2]; w[3] = u[3]; }
-        else { const u32x2 u = *(const u32x2_2*)p; w[0] = u[0]; w[1] = u[1]; }
+        if constexpr (V == 8) { const u32x4_t u = ST_LOAD(NT, u32x4_2, p); w[0] = u[0]; w[1] = u[1]; w[2] = u[2]; w[3] = u[3]; }
+        else { const u32x2 u = ST_LOAD(NT, u32x2_2, p); w[0] = u[0]; w[1] = u[1]; }
     }
     __device__ __forceinline__ void load_short(const bf16* p, int n, int64_t step = 1)      // one by one, `step` apart
     {
@@ -120,10 +124,10 @@ template <int V> struct Run<bf16, V> {
 };
 template <int V> struct Run<float, V> {
     float v[V];
-    __device__ __forceinline__ void load(const float* p)
+    template <bool NT = false> __device__ __forceinline__ void load(const float* p)
     {
 #pragma unroll
-        for (int i = 0; i < V; i += 4) { const f32x4_t a = *(const f32x4_4*)(p + i); v[i] = a[0]; v[i + 1] = a[1]; v[i + 2] = a[2]; v[i + 3] = a[3]; }
+        for (int i = 0; i < V; i += 4) { const f32x4_t a = ST_LOAD(NT, f32x4_4, (p + i)); v[i] = a[0]; v[i + 1] = a[1]; v[i + 2] = a[2]; v[i + 3] = a[3]; }
     }
     __device__ __forceinline__ void load_short(const float* p, int n, int64_t step = 1)
     {
@@ -147,7 +151,7 @@ template <int V> struct Run<void, V> {};      // no mask
 template <class T> using Raw8 = Run<T, 8>;
 
 // COUNT runs of eight of a row, run i at at(i): all under way before one of them is moved.
-template <class T, int COUNT, class I, class F>
+template <bool NT = false, class T, int COUNT, class I, class F>
 __device__ __forceinline__ void load_row(const T* row, I len, F at, Raw8<T> (&v)[COUNT])
 {
     if (len < 8) {
@@ -156,7 +160,7 @@ __device__ __forceinline__ void load_row(const T* row, I len, F at, Raw8<T> (&v)
         return;
     }
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) v[i].load(row + run_start<8, I>(at(i), len));
+    for (int i = 0; i < COUNT; ++i) v[i].template load<NT>(row + run_start<8, I>(at(i), len));
 #pragma unroll
     for (int i = 0; i < COUNT; ++i) {
         const I d = at(i) - (len - 8);
