@@ -49,14 +49,10 @@ __device__ __forceinline__ Column column_of(const Product& p, int64_t n)
 {
     return n < p.n ? Column{p.b_scale[n], p.bias ? p.bias[n] : 0.f} : Column{0.f, 0.f};
 }
-// COUNT values of one row, channels n .. n + COUNT - 1: at once, or at the end of the row those that exist one by one.  through: rows begin
-// at multiples of 16 bytes, whole lines are written, and they need not stay in L2 (8192 tokens 4096 -> 14336 464 -> 443 us, 2048 tokens
-// 2048 -> 2048 20.6 -> 19.8; with odd pitches, whose lines are written in parts, 5480 tokens 532 -> 6367 49.5 -> 58.6).
-__device__ __forceinline__ bool whole_lines(const Product& p)
-{
-    return (((uintptr_t)p.out | (uintptr_t)(p.out_pitch * (p.out_bf16 ? 2 : 4))) & 15) == 0;
-}
-template <int COUNT> __device__ __forceinline__ void store_out(const Product& p, int64_t m, int64_t n, bool through, const float (&v)[COUNT])
+// COUNT values of one row, channels n .. n + COUNT - 1: at once, or at the end of the row those that exist one by one.  (Stores that do not
+// ask for room in L2 lose more than they give here: 8192 tokens 4096 -> 14336 444 us against 454, but 14400 tokens 256 -> 128 8.5 against 8.0,
+// and odd pitches, whose lines are written in parts, 58.6 against 49.5 at 5480 tokens 532 -> 6367.)
+template <int COUNT> __device__ __forceinline__ void store_out(const Product& p, int64_t m, int64_t n, const float (&v)[COUNT])
 {
     if (p.out_bf16) {
         bf16* o = (bf16*)p.out + m * p.out_pitch + n;
@@ -66,7 +62,7 @@ template <int COUNT> __device__ __forceinline__ void store_out(const Product& p,
             T u;
 #pragma unroll
             for (int i = 0; i < COUNT; ++i) u[i] = (bf16)v[i];
-            if (through) __builtin_nontemporal_store(u, (T2*)o); else *(T2*)o = u;
+            *(T2*)o = u;
             return;
         }
 #pragma unroll
@@ -77,10 +73,7 @@ template <int COUNT> __device__ __forceinline__ void store_out(const Product& p,
             if constexpr (COUNT == 1) *o = v[0];
             else
 #pragma unroll
-                for (int i = 0; i < COUNT; i += 4) {
-                    const f32x4_t u = {v[i], v[i + 1], v[i + 2], v[i + 3]};
-                    if (through) __builtin_nontemporal_store(u, (f32x4_4*)(o + i)); else *(f32x4_4*)(o + i) = u;
-                }
+                for (int i = 0; i < COUNT; i += 4) *(f32x4_4*)(o + i) = f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
             return;
         }
 #pragma unroll
@@ -206,7 +199,6 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
     __syncthreads();
     static_assert(WAVES * 32 * PITCH * 4 <= DEPTH * BUF, "room for the sums");
     int* mine = (int*)lds + wave * 32 * PITCH;
-    const bool through = whole_lines(p);
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
         float sm[32 / ROWS];
@@ -237,7 +229,7 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
             float v[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) v[i] = finish((float)(i < 4 ? lo[i] : hi[i - 4]), sm[h], col[i], p.relu);
-            store_out<8>(p, m, n, through, v);
+            store_out<8>(p, m, n, v);
         }
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
@@ -256,7 +248,7 @@ __global__ __launch_bounds__(256) void k_int8_join(const GemmPair pair, int64_t 
 #pragma unroll 4
         for (int s = 0; s < g.splits; ++s) sum += p.slabs[(int64_t)s * size + at];
         const float v[1] = {finish((float)sum, p.a_scale[m], column_of(p, n), p.relu)};
-        store_out<1>(p, m, n, false, v);
+        store_out<1>(p, m, n, v);
     }
 }
 
@@ -422,7 +414,7 @@ __global__ __launch_bounds__(FEW_WAVES * 64, 4) void k_int8_few(const FewArgs f)
 #pragma unroll
             for (int w = 0; w < FEW_WAVES; ++w) sum += part[w * NT * 256 + i];
             const float v[1] = {finish((float)sum, FUSED ? scales[m] : p.a_scale[m], mine, p.relu)};
-            store_out<1>(p, m, n, false, v);
+            store_out<1>(p, m, n, v);
         }
         if (next >= p.n) break;
         n0 = next;
@@ -527,7 +519,6 @@ template <class T, int RUNS> __global__ __launch_bounds__(256) void k_int8_narro
     }
     __syncthreads();
     const int run = threadIdx.x & 15, row = threadIdx.x >> 4;
-    const bool through = whole_lines(p);
     for (int base = 0; base < n; base += 128) {
         const int c = base + run * 8;
         Column col[8];
@@ -553,7 +544,7 @@ template <class T, int RUNS> __global__ __launch_bounds__(256) void k_int8_narro
                 float o[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) o[i] = finish((float)(i < 4 ? lo[i] : hi[i - 4]), scales[r], col[i], p.relu);
-                store_out<8>(p, m0 + r, c, through, o);
+                store_out<8>(p, m0 + r, c, o);
             }
         }
         if (base + 128 < n) __syncthreads();
