@@ -83,7 +83,7 @@ __device__ __forceinline__ double block_sum(double s, double* sums)      // of 2
 }
 
 // ------------------------------------------------------------------------------------------------------ norm
-// Squares and their sums in float64: no gradient that is finite makes the norm infinite, and the order of the sums does not show.  A
+// Squares and their sums in float64: no square of a finite gradient is infinite, and the order of the sums does not show.  A
 // launch has NORM_BLOCKS blocks at most, so that few parts are left to be added.
 template <class G, int RUNS>
 __global__ __launch_bounds__(256) void k_grad_square_sums(const GradList l, float grad_scale, unsigned tiles, double* __restrict__ parts)
@@ -128,10 +128,10 @@ __global__ __launch_bounds__(256) void k_norm(const double* __restrict__ parts, 
 // block then also writes it to `out`.
 struct NormRef { const float* norm; const double* parts; int n_parts; float* out; };
 
-// The factor on the gradients, or 0 where the step is not taken (grad_scale and max_norm are positive).
+// The factor on the gradients, or -1 where the step is not taken (grad_scale and max_norm are positive; their product may vanish).
 __device__ __forceinline__ float clip_factor(const AdamwConstants& k, float norm)
 {
-    if (!(norm < __builtin_inff())) return 0.f;
+    if (!(norm < __builtin_inff())) return -1.f;
     return norm > k.max_norm ? k.grad_scale * (k.max_norm / norm) : k.grad_scale;
 }
 // scale and multiplier of a run whose largest value has the bits `top`; codes^2 reach `codes2`
@@ -213,7 +213,7 @@ __global__ __launch_bounds__(256) void k_adamw(const TensorList l, const AdamwCo
         const float norm = nr.parts ? norm_of_parts(nr.parts, nr.n_parts, sums) : *nr.norm;
         if (nr.parts && nr.out && blockIdx.x == 0 && threadIdx.x == 0) *nr.out = norm;
         factor = k.max_norm > 0.f ? clip_factor(k, norm) : k.grad_scale;
-        if (factor == 0.f) return;
+        if (factor < 0.f) return;
     }
     const float decay = l.decay[i];
 #pragma unroll

@@ -159,6 +159,22 @@ def test_clipped_step_with_bad_gradient_changes_nothing(bits, bad):
     assert all(torch.equal(a, b) for a, b in zip(before, params + [x for v in state.values() for x in v]))
 
 
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("sizes", [[700, 256], [9_000_000, 300]])      # (the norm in the step's blocks, and in a launch of its own)
+def test_clip_factor_that_vanishes(bits, sizes):
+    """A finite norm so large that max_norm / norm is 0 in float32: the step is taken, with gradients of 0."""
+    t, params, grads, state, *_ = make(sizes, bits, seed=11)
+    for g in grads:
+        g.fill_(1e30)
+    before = [p.clone() for p in params]
+    norm = torch.zeros(1, device="cuda")
+    st.st_adamw_step(t, 1, 0.1, max_norm=1e-30, grad_norm=norm)
+    assert torch.isfinite(norm).all()
+    assert torch.equal(params[1], before[1])                           # no decay, m = 0
+    assert ((params[0] - before[0] * (1 - 0.1 * 0.01)).abs() <= 2 ** -22 * before[0].abs()).all()
+    assert all((x == 0).all() for v in state.values() for x in v)
+
+
 def test_norm_of_large_and_small_gradients_is_finite():
     t, params, grads, *_ = make([1000], seed=8)
     for value in (1e30, 1e-30):
