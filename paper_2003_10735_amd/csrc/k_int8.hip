@@ -158,8 +158,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
         }
     };
     // DEPTH stages are under way.  A stage's last step has its operands in registers when the barrier is passed, so what follows the
-    // barrier is: the next stage's first operands, the last step's products, the loads of the stage DEPTH later into the buffer that is done
-    // with.  (Loads first, the wavefronts wait for their turn with the products not begun: 8192 tokens 4096 -> 14336 441 us against 432.)
+    // barrier is: the loads of the stage DEPTH later into the buffer that is done with, the next stage's first operands, the last step's
+    // products.
     constexpr int LOADS = (AR + BR) / 8 / WAVES;      // of a wavefront and stage
     static_assert((DEPTH - 1) * LOADS < 64, "the counter of loads under way");
     // what the sums meet on their way out is asked for before the loop
@@ -189,13 +189,10 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
         if (DEPTH > 2 && s + DEPTH <= last) ST_WAIT_VM((DEPTH - 2) * LOADS); else ST_WAIT_VM(0);
         __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0)
         ST_BARRIER();
-        const int done = buf;
+        if (s + DEPTH < last) stage(s + DEPTH, buf);
         buf = buf + 1 == DEPTH ? 0 : buf + 1;
         if (s + 1 < last) fetch(buf, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
         multiply((STEPS - 1) & 1);
-        __builtin_amdgcn_sched_barrier(0);
-        if (s + DEPTH < last) stage(s + DEPTH, done);
     }
 
     // Out through LDS, 32 tokens of a wavefront at a time: sums go in four neighbouring channels at a time and come out as runs along a row.
