@@ -159,7 +159,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
     };
     // DEPTH stages are under way.  A stage's last step has its operands in registers when the barrier is passed, so what follows the
     // barrier is: the loads of the stage DEPTH later into the buffer that is done with, the next stage's first operands, the last step's
-    // products.
+    // products.  (8192 tokens 4096 -> 14336 with the loads last: 432 us a call instead of 441 with operands that a cache holds, 460 instead of
+    // 447 with others every call.)
     constexpr int LOADS = (AR + BR) / 8 / WAVES;      // of a wavefront and stage
     static_assert((DEPTH - 1) * LOADS < 64, "the counter of loads under way");
     // what the sums meet on their way out is asked for before the loop

@@ -166,6 +166,16 @@ template <class T, class M, bool SHORT, bool NT> struct Masked {
     }
 };
 
+// Which 64 columns a block takes, and which of `parts` pieces of the contraction: neighbouring columns of a piece follow one another on one
+// XCD, whose L2 then has the lines that two blocks share.  (Pieces of the same columns in turn, us a backward pass: 12305 tokens 523 -> 1195
+// 104.0 against 94.9, 6376 tokens 2189 -> 3610 247.9 against 224.3; 8192 tokens 4096 -> 4096, no line shared, 351 against 346.)
+__device__ __forceinline__ unsigned column_tile(const Job& j, unsigned block, unsigned parts, unsigned* piece)
+{
+    const unsigned tiles = (unsigned)((j.rows + 63) / 64), at = (unsigned)xcd_band((int)block, (int)(tiles * parts));
+    *piece = at / tiles;
+    return at - *piece * tiles;
+}
+
 // First launch: a block leaves the largest value and the sum of 64 columns over one part of the contraction.
 template <class T, class M, bool SHORT> __device__ __forceinline__ void parts_loop(const Job& j, const Columns& col, int64_t from, int64_t to, int group,
                                                                        unsigned (&top)[across<T>()], double (&total)[across<T>()])
@@ -199,7 +209,8 @@ template <class T, class M, bool SHORT> __device__ __forceinline__ void parts_lo
 template <class T, bool SHORT> __device__ __forceinline__ void parts_role(const Job& j, unsigned block, Shared& sh)
 {
     constexpr int V = across<T>(), LANES = 64 / V, GROUPS = groups<T>();
-    const unsigned tile = block / (unsigned)j.parts, part = block - tile * (unsigned)j.parts;
+    unsigned part;
+    const unsigned tile = column_tile(j, block, (unsigned)j.parts, &part);
     const int c = (threadIdx.x % LANES) * V, group = threadIdx.x / LANES;
     const int64_t col = (int64_t)tile * 64 + c;
     const int64_t from = part * j.per_part, to = from + j.per_part < j.len ? from + j.per_part : j.len;
@@ -285,7 +296,8 @@ template <class T, class M, bool SHORT> __device__ __forceinline__ void turn_til
 }
 template <class T, bool SHORT> __device__ __forceinline__ void turn_role(const Job& j, unsigned block, Shared& sh)
 {
-    const unsigned row_tile = block / j.len_blocks, first = (block - row_tile * j.len_blocks) * j.tiles_each;
+    unsigned len_block;
+    const unsigned row_tile = column_tile(j, block, j.len_blocks, &len_block), first = len_block * j.tiles_each;
     const unsigned count = min(j.tiles_each, j.len_tiles - first);
     const int64_t row0 = (int64_t)row_tile * 64;
     if (j.sum && first == 0) {
