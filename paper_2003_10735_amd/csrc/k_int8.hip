@@ -582,7 +582,9 @@ Form form_of(const Extent* e, int count)
     // (a tile of five stages or fewer is begun and ended most of its time: smaller ones, two a compute unit, overlap; 5480 tokens 532 -> 6367
     // 48.5 us against 62, 14400 tokens 256 -> 2048 33.0 against 36.4; but 8192 tokens 1024 -> 8192 107 against 96)
     if (total(256) >= 192 && stages_of(256) > 5 * total(256)) f.tile = 256;
-    else if (total(128) >= 192) f.tile = 128;
+    // (small tiles fill the card with two a compute unit: 1536 tokens 4096 -> 1536, 576 of them, 33.9 us, with large ones 27.1; 1500 tokens
+    // 2048 -> 1700, 648, 21.7 and 18.7; but 512 tokens 4096 -> 4096, 512, 23.1 and 33.6, 2000 tokens 1000 -> 1000, 512, 11.7 and 12.7)
+    else if (total(64) > 512) f.tile = 128;
     // every block about the same number of stages, 256 blocks, eight stages each at least; up to 16 stages the parts' join costs more than
     // it gives (333 tokens 1000 -> 1003: 11.8 us, in two parts 15.6; 65 tokens 8192 -> 128 in eight parts: 12.7, in four 15.0)
     const int64_t each = std::max<int64_t>(8, ceil_div(stages_of(f.tile), 256));
