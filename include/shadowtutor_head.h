@@ -266,15 +266,16 @@ int st_object_weights(const int32_t* labels, int32_t n, int32_t height, int32_t 
  * A dense (1x1) layer y = act(x W^T + b) over tokens: the cells of a feature map (an [n, h, w, c] map is n*h*w tokens of c channels),
  * or any rows.  Both operands of a product are whole numbers of -127 .. 127 with one float32 scale for each row of the product they
  * enter, the products are added exactly in int32, and the scales are applied in float32 to the sum.  A row's scale is its largest
- * absolute value a times 1/127; its numbers are rint(x * (127 * (1/a))), every operation rounded to float32, ties to even.  A row of zeros has scale 0; a row that holds an
- * infinity or a NaN gets scale NaN and numbers 0, so that whatever it enters is NaN.  (A row whose largest value lies below 2^-119 is
- * taken as zeros: 127 / largest leaves float32 there.)
+ * absolute value a times 1/127; its numbers are rint(x * (127 * (1/a))), every operation rounded to float32, ties to even.  A row of
+ * zeros has scale 0; a row that holds an infinity or a NaN gets scale NaN and numbers 0, so that whatever it enters is NaN.  (A row whose
+ * largest value lies below 2^-119 is taken as zeros: 127 / largest leaves float32 there.)
  *
  * A matrix argument has an element type (ST_F32 | ST_BF16) and two strides in elements, of which one is 1: row by row with a pitch, or
  * column by column with a pitch (what a channel-first feature map is to its cells).  Pointers are aligned to their elements, int8
- * matrices to 16 bytes with a pitch that is a multiple of 16 and at most 2^23.  Tokens may be 0 in number (the call then writes what an empty sum is);
- * other sizes are at least 1, and all of them are less than 2^24.  Offsets inside a matrix are 64 bits wide; sums longer than ST_INT8_MAX_SUM are refused (ST_ERR_SHAPE)
- * where the header says so, since int32 could not hold them.  Outputs must not overlap inputs or each other. */
+ * matrices to 16 bytes with a pitch that is a multiple of 16 and at most 2^23.  Tokens may be 0 in number (the call then writes what an
+ * empty sum is); other sizes are at least 1, and all of them are less than 2^24.  Offsets inside a matrix are 64 bits wide; sums longer
+ * than ST_INT8_MAX_SUM are refused (ST_ERR_SHAPE) where the header says so, since int32 could not hold them.  Outputs must not overlap
+ * inputs or each other. */
 #define ST_INT8_MAX_SUM 131071
 
 typedef struct st_matrix {
@@ -286,7 +287,7 @@ typedef struct st_matrix {
 
 /* Rows of x as 8-bit integers: q [rows, q_pitch] int8, scale [rows] float32.  The bytes of a row from cols up to the next multiple of
  * 128 are set to zero as far as the pitch reaches.  (Quantising the transpose of a matrix is this call with the strides exchanged.)
- *   workspace  st_int8_quantize_workspace(rows, cols) bytes if x lies column by column, NULL otherwise */
+ *   workspace  st_int8_quantize_workspace(rows, cols) bytes, 256-byte aligned, if x lies column by column; NULL otherwise */
 size_t st_int8_quantize_workspace(int64_t rows, int64_t cols);
 int st_int8_quantize(const st_matrix* x, int8_t* q, int64_t q_pitch, float* scale, void* workspace, void* stream);
 
@@ -351,7 +352,7 @@ typedef struct st_adamw_opts {
     float* grad_norm;                  /* [1] out: norm, before clipping; or NULL */
 } st_adamw_opts;
 
-/* Bytes of device scratch for the norm (0 if the list is invalid); needed with max_norm > 0 or grad_norm only. */
+/* Bytes of device scratch for the norm (0 if the list is invalid), 256-byte aligned; needed with max_norm > 0 or grad_norm only. */
 size_t st_adamw_workspace(const st_adamw_tensor* tensors, int32_t n_tensors);
 int st_adamw_step(const st_adamw_tensor* tensors, int32_t n_tensors, const st_adamw_opts* opts, void* workspace, void* stream);
 

@@ -160,8 +160,7 @@ int st_int8_linear(const st_matrix* x, const int8_t* wq, int64_t w_pitch, const 
     if (along && narrow_layer(m, n, k)) { product_narrow(c, p, tokens); return c.status; }
     const QuantTask task{tokens, s.x, s.parts, nullptr, nullptr};
     quantize(c, &task, 1);
-    if (few_tokens(m, n, k)) product_few(c, p, nullptr); else
-    products(c, &p, 1);
+    if (few_tokens(m, n, k)) product_few(c, p, nullptr); else products(c, &p, 1);
     return c.status;
 }
 
@@ -192,7 +191,7 @@ int st_int8_linear_backward(const st_matrix* x, const st_matrix* w, const st_mat
         if (const int v = check(y, m, n, &y_along)) return v;
         if (y_along != dy_along && m > 1 && n > 1) return ST_ERR_SHAPE;
     }
-    if ((dx && (!dtype_ok(dx_dtype)))) return ST_ERR_ARG;
+    if (dx && !dtype_ok(dx_dtype)) return ST_ERR_ARG;
     if ((dx && dx_pitch < k) || (dw && dw_pitch < k)) return ST_ERR_SHAPE;
     if ((dx && !is_aligned(dx, elem(dx_dtype))) || !is_aligned(dw, 4) || !is_aligned(db, 4)) return ST_ERR_ARG;
     if (!workspace || !is_aligned(workspace, 256)) return ST_ERR_WORKSPACE;
