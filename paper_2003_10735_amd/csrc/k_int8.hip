@@ -90,7 +90,10 @@ template <int COUNT> __device__ __forceinline__ void store_out(const Product& p,
         asm volatile("" ::: "memory");  \
     } while (0)
 
-// BM tokens x BN channels a block, WM x WN a wavefront, DEPTH stages under way.
+// BM tokens x BN channels a block, WM x WN a wavefront, DEPTH stages under way.  Large products are bound by the matrix cores at the
+// clock that they leave (8192 tokens 4096 -> 14336: 436 us, 2.2 POP/s, 54 % busy at some 1.7 GHz; the same product of zeros takes 15 % less);
+// tiles of 128 and 64 by what a compute unit gets into LDS, about 50 bytes a ns (1024 tokens 2048 -> 1024: 8.6 us, 0.28 a stage, with 3 to 8
+// stages under way alike).
 template <int BM, int BN, int WM, int WN, int DEPTH>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(const GemmPair pair)
 {
@@ -237,7 +240,8 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(con
     }
 }
 
-// The slabs of split products, added in 64 bits, and what the product's own epilogue does otherwise.
+// The slabs of split products, added in 64 bits, and what the product's own epilogue does otherwise.  3.5 us where there is little to add
+// (a launch and two trips to memory), 14 for 2188 x 1185 in two parts.
 __global__ __launch_bounds__(256) void k_int8_join(const GemmPair pair, int64_t first, int64_t all)
 {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
@@ -257,7 +261,8 @@ __global__ __launch_bounds__(256) void k_int8_join(const GemmPair pair, int64_t 
 // Up to 32 tokens: the weights are read once, by as many wavefronts as there are, and the tokens' codes many times.  A block takes 16
 // channels, each of its eight wavefronts an eighth of the contraction, 16 bytes a lane straight from memory into
 // v_mfma_i32_16x16x64_i8 (lane l supplies A[l % 16][16*(l/16) .. +15] and B[16*(l/16) .. +15][l % 16] and receives
-// D[4*(l/16) + r][l % 16]); the eighths are added in LDS.
+// D[4*(l/16) + r][l % 16]); the eighths are added in LDS.  Latency bounds it: 1 token 2048 -> 5632 6.0 us (11.6 MB of weights, 1.9 TB/s),
+// 12 tokens 4096 -> 4096 5.9 (17 MB, 2.9 TB/s).
 //
 // FUSED: every block quantises the tokens by itself, into LDS, while its first weights are on their way: the tokens are few, and a launch
 // of its own for them takes longer than the product.
@@ -469,6 +474,7 @@ void product_few(Ctx& c, const Product& p, const QuantSource* x)
 // Many tokens through a small layer (the cells of a feature map): a block takes 32 tokens, quantises them into LDS and multiplies them by
 // all of the weights, 32 channels a wavefront and v_mfma_i32_32x32x32_i8 at a time, which come from a cache.  The tokens are read once, no
 // codes go through memory and one launch does it all.  Eight threads take a token, eight values at a time; RUNS of them cover a token.
+// 14400 tokens 256 -> 128: 7.6 us, 1.5 TB/s, in 450 blocks that each read, quantise, multiply and store once, so their latencies add up.
 struct NarrowArgs { Product p; const void* x; int64_t x_pitch; };
 constexpr int NARROW_TOKENS = 32;
 
@@ -619,7 +625,8 @@ void products(Ctx& c, const Product* p, int count)
     int64_t cells[2] = {0, 0};
     for (int i = 0; i < count; ++i) {
         const int64_t tm = ceil_div(p[i].m, f.tile), tn = ceil_div(p[i].n, f.tile);
-        g.g[i] = GemmArgs{p[i], fast_div((int)(tm * tn)), fast_div((int)(tn * BAND)), (int)tm, f.splits[i], (int)ceil_div(p[i].k, STAGE), (unsigned)(tm * tn * f.splits[i])};
+        g.g[i] = GemmArgs{p[i], fast_div((int)(tm * tn)), fast_div((int)(tn * BAND)), (int)tm, f.splits[i],
+                          (int)ceil_div(p[i].k, STAGE), (unsigned)(tm * tn * f.splits[i])};
         if (f.splits[i] > 1) { cells[n_joined] = p[i].m * p[i].n; joined.g[n_joined++] = g.g[i]; }
     }
     if (f.tile == 256) launch<256, 256, 128, 64, 2>(c, g);

@@ -44,7 +44,7 @@ __device__ __forceinline__ unsigned half_max(unsigned v)
 #undef ST_DPP
 
 // Several values at once, from or to any address that is a multiple of their own size: the card splits what is not aligned.  (Rows with an
-// odd pitch value by value: 5480 tokens 532 -> 6367, 111 us instead of 65.)
+// odd pitch value by value took 1.7 times as long: 5480 tokens 532 -> 6367.)
 typedef unsigned u32x4_t __attribute__((ext_vector_type(4)));
 typedef unsigned u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
