@@ -259,6 +259,14 @@ def test_backward_large():
     check_backward(2300, 2200, 2100, "bf16", "bf16", "bf16", relu=True)
 
 
+@pytest.mark.parametrize("order", ["rows", "columns"])
+def test_many_tokens(order):
+    """Backward: tiles of 128, and the weights' gradient, whose blocks would outlast the other product's, in two parts.  Forward: the same
+    tiles."""
+    check_backward(5930, 657, 1331, "bf16", "f32", "bf16", order, relu=True)
+    check_linear(5001, 1100, 450, "bf16", "bf16", order)
+
+
 def test_more_tokens_than_a_32_bit_sum_holds():
     m = st.ST_INT8_MAX_SUM + 9000
     x, dy = torch.full((m, 3), 2.0, device="cuda"), torch.full((m, 2), -3.0, device="cuda")
