@@ -204,12 +204,11 @@ int st_int8_linear_backward(const st_matrix* x, const st_matrix* w, const st_mat
     const BackwardSpace s = backward_space((char*)workspace, m, n, k);
     QuantTask task[4];
     int n_tasks = 0;
-    if (dx) {
-        task[n_tasks++] = QuantTask{source(*dy, dy_along, false, y), s.dz, s.dz_max, nullptr, nullptr};
-        task[n_tasks++] = QuantTask{source(*w, w_along, true), s.wt, s.wt_max, nullptr, nullptr};
-    }
+    // both readings of dz one after the other, the weights last: 8192 tokens 4096 -> 4096 351 us a call, weights second 357, dz^T last 361
+    if (dx) task[n_tasks++] = QuantTask{source(*dy, dy_along, false, y), s.dz, s.dz_max, nullptr, nullptr};
     if (dw || db) task[n_tasks++] = QuantTask{source(*dy, dy_along, true, y), dw ? s.dzt : Quantized{nullptr, 0, nullptr}, s.dzt_max, s.dzt_sum, db};
     if (dw) task[n_tasks++] = QuantTask{source(*x, x_along, true), s.xt, s.xt_max, nullptr, nullptr};
+    if (dx) task[n_tasks++] = QuantTask{source(*w, w_along, true), s.wt, s.wt_max, nullptr, nullptr};
     quantize(c, task, n_tasks);
     Product p[2];
     int n_products = 0;
