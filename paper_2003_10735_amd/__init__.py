@@ -11,6 +11,7 @@ from __future__ import annotations
 import ctypes as C
 import os
 from dataclasses import dataclass
+from functools import lru_cache
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libshadowtutor_head.so")
@@ -389,6 +390,8 @@ def _matrix(t, where):
     shape = t.shape
     if len(shape) != 2:
         raise StError(ST_ERR_SHAPE, where)
+    if not t.is_cuda:
+        raise StError(ST_ERR_ARG, where)
     return StMatrix(t.data_ptr(), _dtype(t, where), *shape, *t.stride())
 
 
@@ -396,6 +399,8 @@ def _out_matrix(t, rows, cols, where):
     """Checks a result that lies row by row; returns its pitch."""
     if t.shape != (rows, cols):
         raise StError(ST_ERR_SHAPE, where)
+    if not t.is_cuda:
+        raise StError(ST_ERR_ARG, where)
     pitch, step = t.stride()
     if step != 1 and cols > 1:
         raise StError(ST_ERR_SHAPE, where)
@@ -405,6 +410,8 @@ def _out_matrix(t, rows, cols, where):
 def _float_vector(t, n, where):
     if t.numel() != n or not t.is_contiguous() or (_DTYPES or _types()).get(t.dtype) != ST_F32:
         raise StError(ST_ERR_SHAPE, where)
+    if not t.is_cuda:
+        raise StError(ST_ERR_ARG, where)
     return t.data_ptr()
 
 
@@ -415,6 +422,19 @@ def _scratch(nbytes, device, where):
     return torch.empty(nbytes, dtype=torch.uint8, device=device)
 
 
+@lru_cache(maxsize=1024)
+def _int8_bytes(m: int, n: int, k: int, backward: bool) -> int:
+    """Bytes of scratch that the sizes ask for; 0: they are refused."""
+    return (lib().st_int8_linear_backward_workspace if backward else lib().st_int8_linear_workspace)(m, n, k)
+
+
+def _given(ws, nbytes, where):
+    """Address of a caller's scratch of at least `nbytes` (where sizes are refused, 0, the library says so)."""
+    if not ws.is_cuda or ws.nbytes < nbytes:
+        raise StError(ST_ERR_WORKSPACE, where)
+    return ws.data_ptr()
+
+
 def int8_pitch(cols: int) -> int:
     """Bytes of a row of `cols` 8-bit integers: a multiple of 16."""
     return (cols + 15) // 16 * 16
@@ -422,8 +442,7 @@ def int8_pitch(cols: int) -> int:
 
 def new_int8_workspace(m: int, n: int, k: int, backward: bool = False, device="cuda"):
     """Scratch for st_int8_linear (or with backward=True st_int8_linear_backward) of m tokens, k -> n channels."""
-    f = lib().st_int8_linear_backward_workspace if backward else lib().st_int8_linear_workspace
-    return _scratch(f(m, n, k), device, "new_int8_workspace")
+    return _scratch(_int8_bytes(m, n, k, bool(backward)), device, "new_int8_workspace")
 
 
 def st_int8_quantize(x, q=None, scale=None, workspace=None, stream=None):
@@ -439,9 +458,14 @@ def st_int8_quantize(x, q=None, scale=None, workspace=None, stream=None):
         scale = torch.empty(rows, dtype=torch.float32, device=x.device)
     if q.dim() != 2 or q.shape[0] != rows or q.dtype != torch.int8 or q.stride(1) != 1:
         raise StError(ST_ERR_SHAPE, where)
+    if not q.is_cuda:
+        raise StError(ST_ERR_ARG, where)
     ws = workspace
-    if ws is None and cols > 1 and mx.col_stride != 1:
-        ws = _scratch(lib().st_int8_quantize_workspace(rows, cols), x.device, where)
+    if cols > 1 and mx.col_stride != 1:
+        nbytes = lib().st_int8_quantize_workspace(rows, cols)
+        if ws is None:
+            ws = _scratch(nbytes, x.device, where)
+        _given(ws, nbytes, where)
     _check(lib().st_int8_quantize(C.byref(mx), q.data_ptr(), q.stride(0) if rows > 1 else q.shape[1], _float_vector(scale, rows, where),
                                   _addr(ws), _stream(stream)), where)
     return q, scale
@@ -460,6 +484,8 @@ def st_int8_linear(x, wq, w_scale, bias=None, relu: bool = False, out=None, out_
     w_pitch, step = wq.stride()
     if width < k or step != 1 or wq.element_size() != 1:
         raise StError(ST_ERR_SHAPE, where)
+    if not wq.is_cuda:
+        raise StError(ST_ERR_ARG, where)
     if out is None:
         import torch
         out = torch.empty((m, n), dtype=out_dtype or x.dtype, device=x.device)
@@ -469,7 +495,7 @@ def st_int8_linear(x, wq, w_scale, bias=None, relu: bool = False, out=None, out_
     status = (_LIB or lib()).st_int8_linear(
         C.byref(mx), wq.data_ptr(), w_pitch if n > 1 else width, _float_vector(w_scale, n, where), n,
         None if bias is None else _float_vector(bias, n, where), 1 if relu else 0, out.data_ptr(), _dtype(out, where), pitch,
-        workspace.data_ptr(), _stream(stream))
+        _given(workspace, _int8_bytes(m, n, k, False), where), _stream(stream))
     if status:
         raise StError(status, where)
     return out
@@ -491,7 +517,8 @@ def st_int8_linear_backward(x, w, dy, y=None, dx=None, dw=None, db=None, workspa
     ws = workspace if workspace is not None else new_int8_workspace(m, n, k, backward=True, device=dy.device)
     _check(lib().st_int8_linear_backward(*[None if a is None else C.byref(a) for a in mats], _addr(dx),
                                          ST_F32 if dx is None else _dtype(dx, where), dx_pitch, _addr(dw), dw_pitch,
-                                         None if db is None else _float_vector(db, n, where), ws.data_ptr(), _stream(stream)), where)
+                                         None if db is None else _float_vector(db, n, where),
+                                         _given(ws, _int8_bytes(m, n, k, True), where), _stream(stream)), where)
     return dx, dw, db
 
 
@@ -518,23 +545,34 @@ class AdamWTensors:
         self.count, self.kept = count, [None if x is None else list(x) for x in lists]
         self.state_bits = 8 if eight else 32
         self.param_dtype, self.grad_dtype = (_dtype(params[0], where), _dtype(grads[0], where)) if count else (ST_F32, ST_F32)
-        for i in range(count):
-            n, runs = params[i].numel(), (params[i].numel() + ST_ADAMW_BLOCK - 1) // ST_ADAMW_BLOCK
-            a = self.array[i]
-            for (name, _), x, dtype in zip(StAdamwTensor._fields_, lists, wanted):
-                if x is None:
-                    continue
-                if x[i].dtype != dtype or not x[i].is_contiguous() or x[i].numel() != (runs if name.endswith("scale") else n):
+        fields = [(name, x, dtype, name.endswith("scale")) for (name, _), x, dtype in zip(StAdamwTensor._fields_, lists, wanted)
+                  if x is not None]
+        for i, a in enumerate(self.array[:count]):
+            n = params[i].numel()
+            runs = (n + ST_ADAMW_BLOCK - 1) // ST_ADAMW_BLOCK
+            for name, x, dtype, scale in fields:
+                t = x[i]
+                if t.dtype != dtype or t.numel() != (runs if scale else n) or not t.is_contiguous():
                     raise StError(ST_ERR_SHAPE, where)
-                setattr(a, name, x[i].data_ptr())
+                setattr(a, name, t.data_ptr())
             a.n, a.weight_decay = n, float(decay[i])
         self.device = params[0].device if count else "cuda"
+        self._norm_bytes = None
+        self.on_device = all(t.is_cuda for x in lists if x is not None for t in x)
+
+    def norm_bytes(self) -> int:
+        """Bytes of scratch that the norm of this list asks for."""
+        if self._norm_bytes is None:
+            self._norm_bytes = lib().st_adamw_workspace(self.array, self.count)
+        return self._norm_bytes
 
     def set_grads(self, grads):
         """Other gradient tensors (of the same type and lengths) from the next step on."""
         if len(grads) != self.count:
             raise StError(ST_ERR_SHAPE, "AdamWTensors")
         for i, (g, old) in enumerate(zip(grads, self.kept[1])):
+            if self.on_device and not g.is_cuda:
+                raise StError(ST_ERR_ARG, "AdamWTensors")
             if g.dtype != old.dtype or g.numel() != old.numel() or not g.is_contiguous():
                 raise StError(ST_ERR_SHAPE, "AdamWTensors")
             self.array[i].grad = g.data_ptr()
@@ -557,7 +595,7 @@ def new_adamw_state(params, bits: int = 32):
 
 def new_adamw_workspace(tensors: AdamWTensors):
     """Scratch for st_adamw_step's norm of this list."""
-    return _scratch(lib().st_adamw_workspace(tensors.array, tensors.count), tensors.device, "new_adamw_workspace")
+    return _scratch(tensors.norm_bytes(), tensors.device, "new_adamw_workspace")
 
 
 def st_adamw_step(tensors: AdamWTensors, t: int, lr: float, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8,
@@ -565,9 +603,13 @@ def st_adamw_step(tensors: AdamWTensors, t: int, lr: float, beta1: float = 0.9, 
     """Step number t (from 1 on) of AdamW on every tensor of the list, in place.  max_norm > 0 clips by the norm of all (scaled)
     gradients, which grad_norm (float32 [1]) receives if given; a norm that is not finite then leaves everything as it was."""
     where = "st_adamw_step"
+    if not tensors.on_device:
+        raise StError(ST_ERR_ARG, where)
     ws = workspace
-    if ws is None and (max_norm > 0.0 or grad_norm is not None):
-        ws = new_adamw_workspace(tensors)
+    if max_norm > 0.0 or grad_norm is not None:
+        if ws is None:
+            ws = new_adamw_workspace(tensors)
+        _given(ws, tensors.norm_bytes(), where)
     o = StAdamwOpts(tensors.param_dtype, tensors.grad_dtype, tensors.state_bits, t, lr, beta1, beta2, eps, grad_scale, max_norm,
                     None if grad_norm is None else _float_vector(grad_norm, 1, where))
     _check(lib().st_adamw_step(tensors.array, tensors.count, C.byref(o), _addr(ws), _stream(stream)), where)
@@ -582,8 +624,10 @@ def st_adamw_state(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):
     n = m.numel() if m_out is not None else v.numel()
     for codes, scale, out in ((m, m_scale, m_out), (v, v_scale, v_out)):
         if out is not None and (codes.numel() != n or codes.element_size() != 1 or not codes.is_contiguous()
-                                or scale.numel() * ST_ADAMW_BLOCK < n or not scale.is_contiguous()):
+                                or scale.numel() * ST_ADAMW_BLOCK < n or not scale.is_contiguous() or scale.element_size() != 4):
             raise StError(ST_ERR_SHAPE, where)
+        if out is not None and not (codes.is_cuda and scale.is_cuda):
+            raise StError(ST_ERR_ARG, where)
     _check(lib().st_adamw_state(_addr(m) if m_out is not None else None, _addr(m_scale) if m_out is not None else None,
                                 _addr(v) if v_out is not None else None, _addr(v_scale) if v_out is not None else None, n,
                                 None if m_out is None else _float_vector(m_out, n, where),

@@ -319,3 +319,19 @@ def test_offsets_that_pass_32_bits(bits):
         a, b = states[0][name][0][n - tail:].float(), states[1][name][0].float()
         assert ((a - b).abs() <= (1 if bits == 8 else TOL * b.abs())).all()
     assert (big[0][:1000] == 0).all()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_host_tensors_and_small_workspaces_are_refused(bits):
+    t, params, grads, state, *_ = make([700, 5000], bits, seed=12)
+    with pytest.raises(st.StError):
+        st.st_adamw_step(t, 1, 0.1, max_norm=1.0, workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))
+    with pytest.raises(st.StError):
+        st.st_adamw_step(t, 1, 0.1, grad_norm=torch.zeros(1))
+    with pytest.raises(st.StError):
+        t.set_grads([g.cpu() for g in grads])
+    with pytest.raises(st.StError):
+        st.st_adamw_step(st.AdamWTensors(params, [grads[0], grads[1].cpu()], **state), 1, 0.1)
+    if bits == 8:
+        with pytest.raises(st.StError):
+            st.st_adamw_state(state["m"][0].cpu(), state["m_scales"][0], state["v"][0], state["v_scales"][0])

@@ -393,3 +393,20 @@ def test_offsets_that_pass_32_bits():
     alone = st.st_int8_linear(base[:, :64].contiguous(), wq, ws)
     for first in (0, 65072, m - 8):
         assert torch.equal(y[first:first + 8], alone)
+
+
+def test_host_tensors_and_small_workspaces_are_refused():
+    x, dy = rand((40, 64), 1), rand((40, 32), 2)
+    w = rand((32, 64), 3)
+    wq, ws = st.st_int8_quantize(w)
+    small = torch.empty(256, dtype=torch.uint8, device="cuda")
+    dw = torch.empty_like(w)
+    calls = [lambda: st.st_int8_quantize(x.cpu()), lambda: st.st_int8_quantize(x, q=wq.new_empty((40, 64)).cpu()),
+             lambda: st.st_int8_quantize(x.t(), workspace=small), lambda: st.st_int8_linear(x.cpu(), wq, ws, out=dy),
+             lambda: st.st_int8_linear(x, wq.cpu(), ws), lambda: st.st_int8_linear(x, wq, ws.cpu()),
+             lambda: st.st_int8_linear(x, wq, ws, bias=torch.zeros(32)), lambda: st.st_int8_linear(x, wq, ws, out=dy.cpu()),
+             lambda: st.st_int8_linear(x, wq, ws, workspace=small), lambda: st.st_int8_linear_backward(x, w, dy.cpu(), dw=dw),
+             lambda: st.st_int8_linear_backward(x, w, dy, dw=dw.cpu()), lambda: st.st_int8_linear_backward(x, w, dy, dw=dw, workspace=small)]
+    for call in calls:
+        with pytest.raises(st.StError):
+            call()
