@@ -306,7 +306,8 @@ int st_int8_linear(const st_matrix* x, const int8_t* wq, int64_t w_pitch, const 
  *   dx [m, k] = dz W       float32 or bfloat16, both operands quantised along n (n <= ST_INT8_MAX_SUM)
  *   dw [n, k] = dz^T x     float32, both operands quantised along m (m <= 2^23; sums of more than ST_INT8_MAX_SUM tokens are added in 64 bits)
  *   db [n]    = sum of dz over the tokens, float32, not quantised
- * Each of dx, dw, db may be NULL and costs nothing then.  y lies as dy does (the same one of its strides is 1), of either type.
+ * Each of dx, dw, db may be NULL and costs nothing then.  y lies as dy does (the same one of its strides is 1; for one token either may
+ * have any step between its channels), of either type.
  * dx and dw are row by row with a pitch.  What is not needed for the outputs asked for (x without dw, w without dx) may be NULL.
  *   workspace  st_int8_linear_backward_workspace(m, n, k) bytes, 256-byte aligned */
 size_t st_int8_linear_backward_workspace(int64_t m, int64_t n, int64_t k);

@@ -190,6 +190,8 @@ int st_int8_linear_backward(const st_matrix* x, const st_matrix* w, const st_mat
     if (y) {
         if (const int v = check(y, m, n, &y_along)) return v;
         if (y_along != dy_along && m > 1 && n > 1) return ST_ERR_SHAPE;
+        // One token: both are read across memory, each with its own step, unless both lie along it.  (With one channel check() has set both.)
+        if (m == 1 && !y_along) dy_along = 0;
     }
     if (dx && !dtype_ok(dx_dtype)) return ST_ERR_ARG;
     if ((dx && dx_pitch < k) || (dw && dw_pitch < k)) return ST_ERR_SHAPE;
