@@ -447,7 +447,8 @@ def new_int8_workspace(m: int, n: int, k: int, backward: bool = False, device="c
 
 def st_int8_quantize(x, q=None, scale=None, workspace=None, stream=None):
     """Rows of x [rows, cols] (float32 or bfloat16, row by row or column by column; x.t() quantises the columns) as 8-bit integers:
-    (q int8 [rows, int8_pitch(cols)], scale float32 [rows])."""
+    (q int8 [rows, int8_pitch(cols)], scale float32 [rows]).  A row's bytes from cols up to the next multiple of 128 become zeros as far
+    as the step between two rows of q reaches; a q that is too narrow to hold them (a part of a wider matrix's columns) is refused."""
     import torch
     where = "st_int8_quantize"
     mx = _matrix(x, where)
@@ -458,6 +459,9 @@ def st_int8_quantize(x, q=None, scale=None, workspace=None, stream=None):
         scale = torch.empty(rows, dtype=torch.float32, device=x.device)
     if q.dim() != 2 or q.shape[0] != rows or q.dtype != torch.int8 or q.stride(1) != 1:
         raise StError(ST_ERR_SHAPE, where)
+    pitch = q.stride(0) if rows > 1 else q.shape[1]
+    if q.shape[1] < max(cols, min((cols + 127) // 128 * 128, pitch)):
+        raise StError(ST_ERR_SHAPE, where)
     if not q.is_cuda:
         raise StError(ST_ERR_ARG, where)
     ws = workspace
@@ -466,7 +470,7 @@ def st_int8_quantize(x, q=None, scale=None, workspace=None, stream=None):
         if ws is None:
             ws = _scratch(nbytes, x.device, where)
         _given(ws, nbytes, where)
-    _check(lib().st_int8_quantize(C.byref(mx), q.data_ptr(), q.stride(0) if rows > 1 else q.shape[1], _float_vector(scale, rows, where),
+    _check(lib().st_int8_quantize(C.byref(mx), q.data_ptr(), pitch, _float_vector(scale, rows, where),
                                   _addr(ws), _stream(stream)), where)
     return q, scale
 
