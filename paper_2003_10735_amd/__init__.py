@@ -238,6 +238,20 @@ def _stream(stream):
     return _RAW_STREAM[0](_RAW_STREAM[1]())
 
 
+def _own(stream, make, result=False):
+    """A tensor that a call makes itself.  Where the call is given a stream, the tensor is made on that stream: the allocator then neither
+    takes memory that another stream's work still uses nor hands this on while the call's work is under way.  A result may be used on
+    the caller's current stream as well."""
+    if stream is None:
+        return make()
+    import torch
+    with torch.cuda.stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(stream.cuda_stream)):
+        t = make()
+    if result:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
 def _check(status: int, where: str):
     if status != ST_OK:
         raise StError(status, where)
@@ -273,7 +287,7 @@ def st_head_forward(desc: HeadDesc, features, head_params, logits_lowres=None, p
                     workspace=None, stream=None):
     """features [n,c_in,h,w] (float32 or bfloat16 cuda tensor), head_params float32 [num_params]
     ([n, num_params] for a grouped descriptor).  Fills logits_lowres [n,C,h,w] float32 and/or pred [n,8h,8w] uint8 when given."""
-    ws = workspace if workspace is not None else new_workspace(desc, features.device)
+    ws = workspace if workspace is not None else _own(stream, lambda: new_workspace(desc, features.device))
     _check(lib().st_head_forward(desc._ref(), _addr(features), _addr(head_params), _addr(logits_lowres), _addr(pred),
                                  _addr(ws), _stream(stream)), "st_head_forward")
     return logits_lowres, pred
@@ -303,7 +317,7 @@ def st_partial_distill(desc: HeadDesc, features, teacher_labels, head_params, st
     gradients at once instead of scoring first (st_distill_opts.expect_key_frame).
     Returns (steps_taken, best_metric or None); with a threshold the returned tuple also carries
     `.first_metric`, the metric before any update."""
-    ws = workspace if workspace is not None else new_workspace(desc, features.device)
+    ws = workspace if workspace is not None else _own(stream, lambda: new_workspace(desc, features.device))
     opts = None
     if (momentum != 0.0 or threshold > 0.0 or velocity is not None or adam is not None or pixel_weights is not None
             or feature_grad is not None or graph or best_params is not None or expect_key_frame):
@@ -345,9 +359,9 @@ def st_miou(pred, labels, n_classes: int, ignore_index: int = -1, confusion=None
     if confusion is None or miou is None:
         import torch
         if confusion is None:
-            confusion = torch.empty((n_classes, n_classes), dtype=torch.int64, device=pred.device)
+            confusion = _own(stream, lambda: torch.empty((n_classes, n_classes), dtype=torch.int64, device=pred.device), result=True)
         if miou is None:
-            miou = torch.empty(1, dtype=torch.float64, device=pred.device)
+            miou = _own(stream, lambda: torch.empty(1, dtype=torch.float64, device=pred.device), result=True)
     _check(lib().st_miou(_addr(pred), _addr(labels), pred.numel(), n_classes, ignore_index,
                          confusion.data_ptr(), miou.data_ptr(), _stream(stream)), "st_miou")
     return confusion, miou
@@ -360,7 +374,7 @@ def st_object_weights(labels, n_classes: int, radius: int, factor: int = 5, back
     n, H, W = labels.shape
     if weights is None:
         import torch
-        weights = torch.empty((n, H, W), dtype=torch.uint8, device=labels.device)
+        weights = _own(stream, lambda: torch.empty((n, H, W), dtype=torch.uint8, device=labels.device), result=True)
     _check(lib().st_object_weights(labels.data_ptr(), n, H, W, n_classes, background, ignore_index, radius, factor,
                                    weights.data_ptr(), _stream(stream)), "st_object_weights")
     return weights
@@ -454,9 +468,9 @@ def st_int8_quantize(x, q=None, scale=None, workspace=None, stream=None):
     mx = _matrix(x, where)
     rows, cols = x.shape
     if q is None:
-        q = torch.empty((rows, int8_pitch(cols)), dtype=torch.int8, device=x.device)
+        q = _own(stream, lambda: torch.empty((rows, int8_pitch(cols)), dtype=torch.int8, device=x.device), result=True)
     if scale is None:
-        scale = torch.empty(rows, dtype=torch.float32, device=x.device)
+        scale = _own(stream, lambda: torch.empty(rows, dtype=torch.float32, device=x.device), result=True)
     if q.dim() != 2 or q.shape[0] != rows or q.dtype != torch.int8 or q.stride(1) != 1:
         raise StError(ST_ERR_SHAPE, where)
     pitch = q.stride(0) if rows > 1 else q.shape[1]
@@ -468,7 +482,7 @@ def st_int8_quantize(x, q=None, scale=None, workspace=None, stream=None):
     if cols > 1 and mx.col_stride != 1:
         nbytes = lib().st_int8_quantize_workspace(rows, cols)
         if ws is None:
-            ws = _scratch(nbytes, x.device, where)
+            ws = _own(stream, lambda: _scratch(nbytes, x.device, where))
         _given(ws, nbytes, where)
     _check(lib().st_int8_quantize(C.byref(mx), q.data_ptr(), pitch, _float_vector(scale, rows, where),
                                   _addr(ws), _stream(stream)), where)
@@ -492,10 +506,10 @@ def st_int8_linear(x, wq, w_scale, bias=None, relu: bool = False, out=None, out_
         raise StError(ST_ERR_ARG, where)
     if out is None:
         import torch
-        out = torch.empty((m, n), dtype=out_dtype or x.dtype, device=x.device)
+        out = _own(stream, lambda: torch.empty((m, n), dtype=out_dtype or x.dtype, device=x.device), result=True)
     pitch = _out_matrix(out, m, n, where)
     if workspace is None:
-        workspace = new_int8_workspace(m, n, k, device=x.device)
+        workspace = _own(stream, lambda: new_int8_workspace(m, n, k, device=x.device))
     status = (_LIB or lib()).st_int8_linear(
         C.byref(mx), wq.data_ptr(), w_pitch if n > 1 else width, _float_vector(w_scale, n, where), n,
         None if bias is None else _float_vector(bias, n, where), 1 if relu else 0, out.data_ptr(), _dtype(out, where), pitch,
@@ -518,7 +532,7 @@ def st_int8_linear_backward(x, w, dy, y=None, dx=None, dw=None, db=None, workspa
     if dw is not None and _dtype(dw, where) != ST_F32:
         raise StError(ST_ERR_ARG, where)
     dw_pitch = k if dw is None else _out_matrix(dw, n, k, where)
-    ws = workspace if workspace is not None else new_int8_workspace(m, n, k, backward=True, device=dy.device)
+    ws = workspace if workspace is not None else _own(stream, lambda: new_int8_workspace(m, n, k, backward=True, device=dy.device))
     _check(lib().st_int8_linear_backward(*[None if a is None else C.byref(a) for a in mats], _addr(dx),
                                          ST_F32 if dx is None else _dtype(dx, where), dx_pitch, _addr(dw), dw_pitch,
                                          None if db is None else _float_vector(db, n, where),
@@ -612,7 +626,7 @@ def st_adamw_step(tensors: AdamWTensors, t: int, lr: float, beta1: float = 0.9, 
     ws = workspace
     if max_norm > 0.0 or grad_norm is not None:
         if ws is None:
-            ws = new_adamw_workspace(tensors)
+            ws = _own(stream, lambda: new_adamw_workspace(tensors))
         _given(ws, tensors.norm_bytes(), where)
     o = StAdamwOpts(tensors.param_dtype, tensors.grad_dtype, tensors.state_bits, t, lr, beta1, beta2, eps, grad_scale, max_norm,
                     None if grad_norm is None else _float_vector(grad_norm, 1, where))
@@ -624,7 +638,7 @@ def st_adamw_state(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):
     where = "st_adamw_state"
     if m_out is None and v_out is None:
         import torch
-        m_out, v_out = (torch.empty(m.shape, dtype=torch.float32, device=m.device) for _ in range(2))
+        m_out, v_out = (_own(stream, lambda: torch.empty(m.shape, dtype=torch.float32, device=m.device), result=True) for _ in range(2))
     n = m.numel() if m_out is not None else v.numel()
     for codes, scale, out in ((m, m_scale, m_out), (v, v_scale, v_out)):
         if out is not None and (codes.numel() != n or codes.element_size() != 1 or not codes.is_contiguous()

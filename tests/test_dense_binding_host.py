@@ -3,6 +3,8 @@
 The tensors are host tensors that say they are on a device, and the entry points are stand-ins that record their arguments (other
 functions, those that give sizes among them, are the library's own): a call that gets through reaches the stand-in and nothing else.
 """
+import types
+
 import pytest
 
 import paper_2003_10735_amd as st
@@ -14,7 +16,8 @@ class OnDevice(torch.Tensor):
     is_cuda = True
 
 
-ENTRY_POINTS = ("st_int8_quantize", "st_int8_linear", "st_int8_linear_backward", "st_adamw_step", "st_adamw_state")
+ENTRY_POINTS = ("st_int8_quantize", "st_int8_linear", "st_int8_linear_backward", "st_adamw_step", "st_adamw_state",
+                "st_head_forward", "st_partial_distill", "st_miou", "st_object_weights")
 
 
 class Recorder:
@@ -75,3 +78,66 @@ def test_codes_are_written_inside_what_is_given(rows, cols, width, first, end, f
     pitch, written = args[2], min((cols + 127) // 128 * 128, args[2])
     assert name == "st_int8_quantize" and args[1] == q.data_ptr()
     assert pitch == (q.stride(0) if rows > 1 else q.shape[1]) and written <= q.shape[1]
+
+
+class Streams:
+    """Stands in for torch's current stream: which one every tensor was made on, and which others may use it."""
+
+    def __init__(self, monkeypatch):
+        self.current, self.made, empty = "current", [], torch.empty
+
+        class Scope:
+            def __init__(scope, stream):
+                scope.stream = stream
+
+            def __enter__(scope):
+                scope.before, self.current = self.current, scope.stream
+
+            def __exit__(scope, *e):
+                self.current = scope.before
+
+        def make(*a, **k):
+            k.pop("device", None)
+            t = empty(*a, **k).as_subclass(OnDevice)
+            self.made.append([t.data_ptr(), self.current, None, t])
+            return t
+
+        def record(t, stream):
+            next(m for m in self.made if m[0] == t.data_ptr())[2] = stream
+
+        monkeypatch.setattr(torch, "empty", make)
+        monkeypatch.setattr(torch.cuda, "stream", Scope)
+        monkeypatch.setattr(torch.cuda, "ExternalStream", lambda handle: ("stream", handle))
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: self.current)
+        monkeypatch.setattr(OnDevice, "record_stream", record, raising=False)
+
+
+SMALL = st.HeadDesc(1, 8, 4, 4, 8, 8, 3, compute=st.ST_COMPUTE_F32)
+# a call without its workspace and its results, how many of each it makes, and the entry point
+CALLS = {
+    "quantize rows": (lambda s: st.st_int8_quantize(dev(5, 24), stream=s), 0, 2),
+    "quantize columns": (lambda s: st.st_int8_quantize(dev(24, 5).t(), stream=s), 1, 2),
+    "linear": (lambda s: st.st_int8_linear(dev(5, 16), dev(7, 16, dtype=torch.int8), dev(7), stream=s), 1, 1),
+    "backward": (lambda s: st.st_int8_linear_backward(dev(5, 16), dev(7, 16), dev(5, 7), dw=dev(7, 16), stream=s), 1, 0),
+    "adamw": (lambda s: st.st_adamw_step(st.AdamWTensors([dev(9)], [dev(9)], [dev(9)], [dev(9)]), 1, 0.1, max_norm=1.0, stream=s), 1, 0),
+    "state": (lambda s: st.st_adamw_state(dev(9, dtype=torch.int8), dev(1), dev(9, dtype=torch.uint8), dev(1), stream=s), 0, 2),
+    "head forward": (lambda s: st.st_head_forward(SMALL, dev(1), dev(1), stream=s), 1, 0),
+    "distill": (lambda s: st.st_partial_distill(SMALL, dev(1), dev(1), dev(1), 1, 0.1, stream=s), 1, 0),
+    "miou": (lambda s: st.st_miou(dev(4, dtype=torch.uint8), dev(4, dtype=torch.int32), 3, stream=s), 0, 2),
+    "object weights": (lambda s: st.st_object_weights(dev(1, 4, 4, dtype=torch.int32), 3, 1, stream=s), 0, 1),
+}
+
+
+@pytest.mark.parametrize("name", CALLS)
+@pytest.mark.parametrize("given", [False, True])
+def test_what_a_call_makes_belongs_to_its_stream(name, given, library, monkeypatch):
+    """Scratch and results are made on the stream that the call works on; results may be used on the caller's stream too."""
+    call, scratch, results = CALLS[name]
+    streams = Streams(monkeypatch)
+    call(types.SimpleNamespace(cuda_stream=77) if given else None)
+    assert [args[-1] for _, args in library.calls] == [77 if given else 0]
+    assert len(streams.made) == scratch + results
+    for address, made_on, also_on, _ in streams.made:
+        assert made_on == (("stream", 77) if given else "current")
+    assert sum(also_on is not None for _, _, also_on, _ in streams.made) == (results if given else 0)
+    assert all(also_on in (None, "current") for _, _, also_on, _ in streams.made)
