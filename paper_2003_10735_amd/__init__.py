@@ -586,15 +586,17 @@ class AdamWTensors:
 
     def set_grads(self, grads):
         """Other gradient tensors (of the same type and lengths) from the next step on."""
+        grads, where = list(grads), "AdamWTensors"
         if len(grads) != self.count:
-            raise StError(ST_ERR_SHAPE, "AdamWTensors")
-        for i, (g, old) in enumerate(zip(grads, self.kept[1])):
+            raise StError(ST_ERR_SHAPE, where)
+        for g, old in zip(grads, self.kept[1]):      # all of them before any is taken: a refused list changes nothing
             if self.on_device and not g.is_cuda:
-                raise StError(ST_ERR_ARG, "AdamWTensors")
+                raise StError(ST_ERR_ARG, where)
             if g.dtype != old.dtype or g.numel() != old.numel() or not g.is_contiguous():
-                raise StError(ST_ERR_SHAPE, "AdamWTensors")
-            self.array[i].grad = g.data_ptr()
-        self.kept[1] = list(grads)
+                raise StError(ST_ERR_SHAPE, where)
+        for a, g in zip(self.array, grads):
+            a.grad = g.data_ptr()
+        self.kept[1] = grads
 
 
 def new_adamw_state(params, bits: int = 32):

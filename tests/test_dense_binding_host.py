@@ -141,3 +141,26 @@ def test_what_a_call_makes_belongs_to_its_stream(name, given, library, monkeypat
         assert made_on == (("stream", 77) if given else "current")
     assert sum(also_on is not None for _, _, also_on, _ in streams.made) == (results if given else 0)
     assert all(also_on in (None, "current") for _, _, also_on, _ in streams.made)
+
+
+BAD_GRADIENTS = {                                    # made from the length that is wanted
+    "length": (lambda n: dev(n + 1), st.ST_ERR_SHAPE), "type": (lambda n: dev(n, dtype=torch.bfloat16), st.ST_ERR_SHAPE),
+    "order": (lambda n: dev(n, 2)[:, 0], st.ST_ERR_SHAPE), "host": (lambda n: torch.zeros(n), st.ST_ERR_ARG),
+}
+
+
+@pytest.mark.parametrize("bad", BAD_GRADIENTS)
+@pytest.mark.parametrize("at", [0, 1, 2])
+def test_refused_gradients_change_nothing(bad, at, library):
+    """Whichever tensor of the new list is refused: the list goes on with the gradients that it had, and keeps them."""
+    make, status = BAD_GRADIENTS[bad]
+    params, first, second, m, v = ([dev(4), dev(5), dev(7)] for _ in range(5))
+    tensors = st.AdamWTensors(params, first, m, v)
+    wrong = list(second)
+    wrong[at] = make(params[at].numel())
+    refused(status, lambda: tensors.set_grads(wrong), library)
+    assert [a.grad for a in tensors.array] == [t.data_ptr() for t in first] and all(a is b for a, b in zip(tensors.kept[1], first))
+    refused(st.ST_ERR_SHAPE, lambda: tensors.set_grads(second[:2]), library)
+    assert [a.grad for a in tensors.array] == [t.data_ptr() for t in first]
+    tensors.set_grads(second)
+    assert [a.grad for a in tensors.array] == [t.data_ptr() for t in second] and all(a is b for a, b in zip(tensors.kept[1], second))
