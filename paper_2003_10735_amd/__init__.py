@@ -381,12 +381,13 @@ def st_object_weights(labels, n_classes: int, radius: int, factor: int = 5, back
 
 
 # ---------------------------------------------------------------- dense layers in 8-bit integers
-_DTYPES = None
+_DTYPES = _INT8 = None
 
 
 def _types():
-    global _DTYPES
+    global _DTYPES, _INT8
     import torch
+    _INT8 = torch.int8
     _DTYPES = {torch.float32: ST_F32, torch.bfloat16: ST_BF16}
     return _DTYPES
 
@@ -500,7 +501,7 @@ def st_int8_linear(x, wq, w_scale, bias=None, relu: bool = False, out=None, out_
         raise StError(ST_ERR_SHAPE, where)
     n, width = wq.shape
     w_pitch, step = wq.stride()
-    if width < k or step != 1 or wq.element_size() != 1:
+    if width < k or step != 1 or wq.dtype != _INT8:
         raise StError(ST_ERR_SHAPE, where)
     if not wq.is_cuda:
         raise StError(ST_ERR_ARG, where)
@@ -636,15 +637,16 @@ def st_adamw_step(tensors: AdamWTensors, t: int, lr: float, beta1: float = 0.9, 
 
 
 def st_adamw_state(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):
-    """The float32 values that a state in 8 bits stands for, into m_out and v_out (made if neither is given).  Returns (m_out, v_out)."""
+    """The float32 values that a state in 8 bits (m int8, v uint8, scales float32) stands for, into m_out and v_out (made if neither is
+    given).  Returns (m_out, v_out)."""
+    import torch
     where = "st_adamw_state"
     if m_out is None and v_out is None:
-        import torch
         m_out, v_out = (_own(stream, lambda: torch.empty(m.shape, dtype=torch.float32, device=m.device), result=True) for _ in range(2))
     n = m.numel() if m_out is not None else v.numel()
-    for codes, scale, out in ((m, m_scale, m_out), (v, v_scale, v_out)):
-        if out is not None and (codes.numel() != n or codes.element_size() != 1 or not codes.is_contiguous()
-                                or scale.numel() * ST_ADAMW_BLOCK < n or not scale.is_contiguous() or scale.element_size() != 4):
+    for codes, scale, out, dtype in ((m, m_scale, m_out, torch.int8), (v, v_scale, v_out, torch.uint8)):
+        if out is not None and (codes.numel() != n or codes.dtype != dtype or not codes.is_contiguous()
+                                or scale.numel() * ST_ADAMW_BLOCK < n or not scale.is_contiguous() or scale.dtype != torch.float32):
             raise StError(ST_ERR_SHAPE, where)
         if out is not None and not (codes.is_cuda and scale.is_cuda):
             raise StError(ST_ERR_ARG, where)

@@ -164,3 +164,19 @@ def test_refused_gradients_change_nothing(bad, at, library):
     assert [a.grad for a in tensors.array] == [t.data_ptr() for t in first]
     tensors.set_grads(second)
     assert [a.grad for a in tensors.array] == [t.data_ptr() for t in second] and all(a is b for a, b in zip(tensors.kept[1], second))
+
+
+@pytest.mark.parametrize("dtype", [torch.uint8, torch.bool, torch.float8_e4m3fn, torch.int16, torch.float32])
+def test_codes_of_another_type_are_refused(dtype, library):
+    """Weights are int8, codes of m int8 and of v uint8, scales float32: no other type of the same size is read as one of them."""
+    refused(st.ST_ERR_SHAPE, lambda: st.st_int8_linear(dev(5, 16), dev(7, 16, dtype=dtype), dev(7)), library)
+    i8, u8 = dev(9, dtype=torch.int8), dev(9, dtype=torch.uint8)
+    refused(st.ST_ERR_SHAPE, lambda: st.st_adamw_state(dev(9, dtype=dtype), dev(1), u8, dev(1)), library)
+    if dtype != torch.uint8:
+        refused(st.ST_ERR_SHAPE, lambda: st.st_adamw_state(i8, dev(1), dev(9, dtype=dtype), dev(1)), library)
+    refused(st.ST_ERR_SHAPE, lambda: st.st_adamw_state(i8, dev(1), i8, dev(1)), library)
+    for scales in ((dev(1, dtype=torch.int32), dev(1)), (dev(1), dev(1, dtype=torch.int32))):
+        refused(st.ST_ERR_SHAPE, lambda: st.st_adamw_state(i8, scales[0], u8, scales[1]), library)
+    st.st_int8_linear(dev(5, 16), dev(7, 16, dtype=torch.int8), dev(7))
+    st.st_adamw_state(i8, dev(1), u8, dev(1))
+    assert [name for name, _ in library.calls] == ["st_int8_linear", "st_adamw_state"]
