@@ -402,6 +402,8 @@ def _dtype(t, where):
 
 def _matrix(t, where):
     """A two-dimensional tensor as the library takes it: either of its strides 1."""
+    if t is None:
+        raise StError(ST_ERR_NULL, where)
     shape = t.shape
     if len(shape) != 2:
         raise StError(ST_ERR_SHAPE, where)
@@ -423,6 +425,8 @@ def _out_matrix(t, rows, cols, where):
 
 
 def _float_vector(t, n, where):
+    if t is None:
+        raise StError(ST_ERR_NULL, where)
     if t.numel() != n or not t.is_contiguous() or (_DTYPES or _types()).get(t.dtype) != ST_F32:
         raise StError(ST_ERR_SHAPE, where)
     if not t.is_cuda:
@@ -497,6 +501,8 @@ def st_int8_linear(x, wq, w_scale, bias=None, relu: bool = False, out=None, out_
     where = "st_int8_linear"
     mx = _matrix(x, where)
     m, k = mx.rows, mx.cols
+    if wq is None:
+        raise StError(ST_ERR_NULL, where)
     if wq.dim() != 2:
         raise StError(ST_ERR_SHAPE, where)
     n, width = wq.shape
@@ -526,15 +532,18 @@ def st_int8_linear_backward(x, w, dy, y=None, dx=None, dw=None, db=None, workspa
     are given are computed; x may be None without dw, w without dx.  x, w (float weights), dy, y: float32 or bfloat16, row by row or column by
     column, y as dy.  Returns (dx, dw, db)."""
     where = "st_int8_linear_backward"
-    m, n = dy.shape
-    mats = [None if t is None else _matrix(t, where) for t in (x, w, dy, y)]
-    k = w.shape[1] if dx is not None and w is not None else x.shape[1] if dw is not None and x is not None else 1
+    mdy = _matrix(dy, where)
+    m, n = mdy.rows, mdy.cols
+    mx, mw, my = (None if t is None else _matrix(t, where) for t in (x, w, y))
+    if (dx is not None and w is None) or (dw is not None and x is None):
+        raise StError(ST_ERR_NULL, where)
+    k = mw.cols if dx is not None else mx.cols if dw is not None else 1
     dx_pitch = k if dx is None else _out_matrix(dx, m, k, where)
     if dw is not None and _dtype(dw, where) != ST_F32:
         raise StError(ST_ERR_ARG, where)
     dw_pitch = k if dw is None else _out_matrix(dw, n, k, where)
     ws = workspace if workspace is not None else _own(stream, lambda: new_int8_workspace(m, n, k, backward=True, device=dy.device))
-    _check(lib().st_int8_linear_backward(*[None if a is None else C.byref(a) for a in mats], _addr(dx),
+    _check(lib().st_int8_linear_backward(*[None if a is None else C.byref(a) for a in (mx, mw, mdy, my)], _addr(dx),
                                          ST_F32 if dx is None else _dtype(dx, where), dx_pitch, _addr(dw), dw_pitch,
                                          None if db is None else _float_vector(db, n, where),
                                          _given(ws, _int8_bytes(m, n, k, True), where), _stream(stream)), where)
@@ -552,6 +561,8 @@ class AdamWTensors:
         import torch
         where = "AdamWTensors"
         count = len(params)
+        if any(t is None for x in (params, grads, m, v, m_scales, v_scales, copies) if x is not None for t in x):
+            raise StError(ST_ERR_NULL, where)
         eight = count > 0 and m[0].dtype == torch.int8
         decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * count
         lists = [params, grads, m, v, m_scales, v_scales, copies]
@@ -591,6 +602,8 @@ class AdamWTensors:
         if len(grads) != self.count:
             raise StError(ST_ERR_SHAPE, where)
         for g, old in zip(grads, self.kept[1]):      # all of them before any is taken: a refused list changes nothing
+            if g is None:
+                raise StError(ST_ERR_NULL, where)
             if self.on_device and not g.is_cuda:
                 raise StError(ST_ERR_ARG, where)
             if g.dtype != old.dtype or g.numel() != old.numel() or not g.is_contiguous():
@@ -642,9 +655,13 @@ def st_adamw_state(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):
     import torch
     where = "st_adamw_state"
     if m_out is None and v_out is None:
+        if m is None or v is None:
+            raise StError(ST_ERR_NULL, where)
         m_out, v_out = (_own(stream, lambda: torch.empty(m.shape, dtype=torch.float32, device=m.device), result=True) for _ in range(2))
-    n = m.numel() if m_out is not None else v.numel()
+    n = (m_out if m_out is not None else v_out).numel()
     for codes, scale, out, dtype in ((m, m_scale, m_out, torch.int8), (v, v_scale, v_out, torch.uint8)):
+        if out is not None and (codes is None or scale is None):
+            raise StError(ST_ERR_NULL, where)
         if out is not None and (codes.numel() != n or codes.dtype != dtype or not codes.is_contiguous()
                                 or scale.numel() * ST_ADAMW_BLOCK < n or not scale.is_contiguous() or scale.dtype != torch.float32):
             raise StError(ST_ERR_SHAPE, where)

@@ -180,3 +180,39 @@ def test_codes_of_another_type_are_refused(dtype, library):
     st.st_int8_linear(dev(5, 16), dev(7, 16, dtype=torch.int8), dev(7))
     st.st_adamw_state(i8, dev(1), u8, dev(1))
     assert [name for name, _ in library.calls] == ["st_int8_linear", "st_adamw_state"]
+
+
+I8 = dev(7, 16, dtype=torch.int8)
+MISSING = {
+    "quantize": lambda: st.st_int8_quantize(None), "tokens": lambda: st.st_int8_linear(None, I8, dev(7)),
+    "weights": lambda: st.st_int8_linear(dev(5, 16), None, dev(7)), "scales": lambda: st.st_int8_linear(dev(5, 16), I8, None),
+    "dy": lambda: st.st_int8_linear_backward(dev(5, 16), dev(7, 16), None, dw=dev(7, 16)),
+    "dx without w": lambda: st.st_int8_linear_backward(dev(5, 16), None, dev(5, 7), dx=dev(5, 16)),
+    "dw without x": lambda: st.st_int8_linear_backward(None, dev(7, 16), dev(5, 7), dw=dev(7, 16)),
+    "dx without either": lambda: st.st_int8_linear_backward(None, None, dev(5, 7), dx=dev(5, 16)),
+    "first gradient": lambda: st.AdamWTensors([dev(4)], [None], [dev(4)], [dev(4)]),
+    "second state": lambda: st.AdamWTensors([dev(4), dev(5)], [dev(4), dev(5)], [dev(4), None], [dev(4), dev(5)]),
+    "new gradient": lambda: st.AdamWTensors([dev(4)], [dev(4)], [dev(4)], [dev(4)]).set_grads([None]),
+    "codes": lambda: st.st_adamw_state(None, None, dev(9, dtype=torch.uint8), dev(1)),
+    "codes of v": lambda: st.st_adamw_state(dev(9, dtype=torch.int8), dev(1), None, None, v_out=dev(9)),
+    "state's scales": lambda: st.st_adamw_state(dev(9, dtype=torch.int8), None, None, None, m_out=dev(9)),
+}
+DIMENSIONS = {
+    "quantize": lambda: st.st_int8_quantize(dev(16)), "tokens": lambda: st.st_int8_linear(dev(2, 3, 16), I8, dev(7)),
+    "weights": lambda: st.st_int8_linear(dev(5, 16), dev(112, dtype=torch.int8), dev(7)),
+    "dy": lambda: st.st_int8_linear_backward(dev(5, 16), None, dev(1, 5, 7), dw=dev(7, 16)),
+    "dy of one": lambda: st.st_int8_linear_backward(dev(5, 16), None, dev(7), dw=dev(7, 16)),
+    "x": lambda: st.st_int8_linear_backward(dev(5, 4, 4), None, dev(5, 7), dw=dev(7, 16)),
+    "w": lambda: st.st_int8_linear_backward(None, dev(7), dev(5, 7), dx=dev(5, 16)),
+    "y": lambda: st.st_int8_linear_backward(None, None, dev(5, 7), y=dev(35), db=dev(7)),
+}
+
+
+@pytest.mark.parametrize("name", MISSING)
+def test_missing_tensors_are_the_librarys_error(name, library):
+    refused(st.ST_ERR_NULL, MISSING[name], library)
+
+
+@pytest.mark.parametrize("name", DIMENSIONS)
+def test_matrices_have_two_dimensions(name, library):
+    refused(st.ST_ERR_SHAPE, DIMENSIONS[name], library)
