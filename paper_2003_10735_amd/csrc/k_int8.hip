@@ -611,7 +611,8 @@ static void launch(Ctx& c, const GemmPair& g)
 {
     constexpr size_t lds = (size_t)DEPTH * (BM + BN) * STAGE;
     ensure_dynamic_lds((const void*)k_int8_product<BM, BN, WM, WN, DEPTH>, lds);
-    ST_LAUNCH(c, "int8_product", (k_int8_product<BM, BN, WM, WN, DEPTH>), dim3(g.g[0].blocks + g.g[1].blocks), dim3((BM / WM) * (BN / WN) * 64), lds, g);
+    constexpr const char* name = BM == 256 ? "int8_product_256" : BM == 64 ? "int8_product_64" : DEPTH > 2 ? "int8_product_128_deep" : "int8_product_128";
+    ST_LAUNCH(c, name, (k_int8_product<BM, BN, WM, WN, DEPTH>), dim3(g.g[0].blocks + g.g[1].blocks), dim3((BM / WM) * (BN / WN) * 64), lds, g);
 }
 
 void products(Ctx& c, const Product* p, int count)
