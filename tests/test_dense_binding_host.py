@@ -216,3 +216,104 @@ def test_missing_tensors_are_the_librarys_error(name, library):
 @pytest.mark.parametrize("name", DIMENSIONS)
 def test_matrices_have_two_dimensions(name, library):
     refused(st.ST_ERR_SHAPE, DIMENSIONS[name], library)
+
+
+# Each call is right but for one argument.  name: (call with replacements, the entry point, {what is replaced: (by what, status)})
+def _linear(x=None, wq=None, scale=None, **k):
+    return st.st_int8_linear(dev(5, 16) if x is None else x, I8 if wq is None else wq, dev(7) if scale is None else scale, **k)
+
+
+def _backward(**k):
+    a = dict(x=dev(5, 16), w=dev(7, 16), dy=dev(5, 7), y=dev(5, 7), dx=dev(5, 16), dw=dev(7, 16), db=dev(7))
+    a.update(k)
+    return st.st_int8_linear_backward(**a)
+
+
+def _quantize(**k):
+    return st.st_int8_quantize(**dict(dict(x=dev(5, 16)), **k))
+
+
+def _tensors(**k):
+    a = dict(params=[dev(300), dev(2, 2)], grads=[dev(300), dev(4)], m=[dev(300, dtype=torch.int8), dev(4, dtype=torch.int8)],
+             v=[dev(300, dtype=torch.uint8), dev(4, dtype=torch.uint8)], m_scales=[dev(2), dev(1)], v_scales=[dev(2), dev(1)],
+             copies=[dev(300, dtype=torch.bfloat16), dev(4, dtype=torch.bfloat16)], weight_decay=[0.1, 0.0])
+    a.update(k)
+    return st.AdamWTensors(**a)
+
+
+def _step(**k):
+    return st.st_adamw_step(_tensors(), 1, 0.1, **dict(dict(max_norm=1.0), **k))
+
+
+def _state(**k):
+    a = dict(m=dev(300, dtype=torch.int8), m_scale=dev(2), v=dev(300, dtype=torch.uint8), v_scale=dev(2), m_out=dev(300), v_out=dev(300))
+    a.update(k)
+    return st.st_adamw_state(**a)
+
+
+HALF, BYTES = torch.float16, torch.int8
+SHAPE, ARG, SPACE = st.ST_ERR_SHAPE, st.ST_ERR_ARG, st.ST_ERR_WORKSPACE
+WRONG = {
+    "quantize": (_quantize, "st_int8_quantize", [
+        (dict(x=dev(5, 16, dtype=HALF)), ARG), (dict(x=torch.zeros(5, 16)), ARG), (dict(q=dev(4, 16, dtype=BYTES)), SHAPE),
+        (dict(q=dev(5, 15, dtype=BYTES)), SHAPE), (dict(q=dev(5, 16)), SHAPE), (dict(q=dev(16, 5, dtype=BYTES).t()), SHAPE),
+        (dict(q=torch.zeros(5, 16, dtype=BYTES)), ARG), (dict(scale=dev(4)), SHAPE), (dict(scale=dev(5, dtype=torch.bfloat16)), SHAPE),
+        (dict(scale=dev(5, 2)[:, 0]), SHAPE), (dict(scale=torch.zeros(5)), ARG),
+        (dict(x=dev(16, 5).t(), workspace=dev(8)), SPACE), (dict(x=dev(16, 5).t(), workspace=torch.zeros(1 << 20)), SPACE)]),
+    "linear": (_linear, "st_int8_linear", [
+        (dict(x=dev(5, 16, dtype=HALF)), ARG), (dict(x=torch.zeros(5, 16)), ARG), (dict(x=dev(5, 17)), SHAPE),
+        (dict(wq=dev(7, 15, dtype=BYTES)), SHAPE), (dict(wq=dev(16, 7, dtype=BYTES).t()), SHAPE), (dict(wq=torch.zeros(7, 16, dtype=BYTES)), ARG),
+        (dict(wq=dev(8, 16, dtype=BYTES)), SHAPE), (dict(scale=dev(6)), SHAPE), (dict(scale=dev(7, dtype=torch.float64)), SHAPE),
+        (dict(scale=torch.zeros(7)), ARG), (dict(bias=dev(8)), SHAPE), (dict(bias=dev(7, dtype=torch.bfloat16)), SHAPE), (dict(bias=torch.zeros(7)), ARG),
+        (dict(out=dev(5, 8)), SHAPE), (dict(out=dev(4, 7)), SHAPE), (dict(out=dev(7, 5).t()), SHAPE), (dict(out=dev(5, 7, dtype=HALF)), ARG),
+        (dict(out=torch.zeros(5, 7)), ARG), (dict(out_dtype=HALF), ARG), (dict(workspace=dev(8)), SPACE), (dict(workspace=torch.zeros(1 << 20)), SPACE)]),
+    "backward": (_backward, "st_int8_linear_backward", [
+        *[(dict([(k, t)]), s) for k, n, m in (("x", 5, 16), ("w", 7, 16), ("dy", 5, 7), ("y", 5, 7))
+          for t, s in ((dev(n, m, dtype=HALF), ARG), (torch.zeros(n, m), ARG), (dev(n, m, 1), SHAPE))],
+        (dict(dx=dev(5, 15)), SHAPE), (dict(dx=dev(4, 16)), SHAPE), (dict(dx=dev(16, 5).t()), SHAPE), (dict(dx=dev(5, 16, dtype=HALF)), ARG),
+        (dict(dx=torch.zeros(5, 16)), ARG), (dict(dw=dev(7, 15)), SHAPE), (dict(dw=dev(8, 16)), SHAPE), (dict(dw=dev(16, 7).t()), SHAPE),
+        (dict(dw=dev(7, 16, dtype=torch.bfloat16)), ARG), (dict(dw=torch.zeros(7, 16)), ARG), (dict(db=dev(8)), SHAPE),
+        (dict(db=dev(7, dtype=torch.bfloat16)), SHAPE), (dict(db=torch.zeros(7)), ARG), (dict(workspace=dev(8)), SPACE),
+        (dict(workspace=torch.zeros(1 << 20)), SPACE)]),
+    "list": (lambda **k: st.st_adamw_step(_tensors(**k), 1, 0.1), "st_adamw_step", [
+        (dict(grads=[dev(300)]), SHAPE), (dict(grads=[dev(300), dev(5)]), SHAPE), (dict(grads=[dev(300), dev(4, dtype=torch.bfloat16)]), SHAPE),
+        (dict(params=[dev(300, dtype=HALF), dev(4, dtype=HALF)]), ARG), (dict(params=[dev(300), dev(2, 2, 2)[:, :, 0]]), SHAPE),
+        (dict(m=[dev(300), dev(4)]), SHAPE), (dict(v=[dev(300, dtype=BYTES), dev(4, dtype=BYTES)]), SHAPE), (dict(m_scales=None), SHAPE),
+        (dict(v_scales=[dev(1), dev(1)]), SHAPE), (dict(m_scales=[dev(2), dev(2)]), SHAPE), (dict(m_scales=[dev(2, dtype=torch.int32), dev(1)]), SHAPE),
+        (dict(copies=[dev(300), dev(4)]), SHAPE), (dict(copies=[dev(300, dtype=torch.bfloat16)]), SHAPE), (dict(weight_decay=[0.1]), SHAPE),
+        (dict(params=[torch.zeros(300), dev(4)]), ARG), (dict(v_scales=[dev(2), torch.zeros(1)]), ARG)]),
+    "step": (_step, "st_adamw_step", [
+        (dict(grad_norm=dev(2)), SHAPE), (dict(grad_norm=dev(1, dtype=torch.float64)), SHAPE), (dict(grad_norm=torch.zeros(1)), ARG),
+        (dict(workspace=dev(8)), SPACE), (dict(workspace=torch.zeros(1 << 20)), SPACE)]),
+    "state": (_state, "st_adamw_state", [
+        (dict(m=dev(299, dtype=BYTES)), SHAPE), (dict(v=dev(301, dtype=torch.uint8)), SHAPE), (dict(m=dev(300, 2, dtype=BYTES)[:, 0]), SHAPE),
+        (dict(m_scale=dev(1)), SHAPE), (dict(v_scale=dev(2, 2)[:, 0]), SHAPE), (dict(m=torch.zeros(300, dtype=BYTES)), ARG),
+        (dict(v_scale=torch.zeros(2)), ARG), (dict(m_out=dev(300, dtype=torch.bfloat16)), SHAPE), (dict(v_out=dev(300, 2)[:, 0]), SHAPE),
+        (dict(v_out=torch.zeros(300)), ARG)]),
+}
+
+
+@pytest.mark.parametrize("name,at", [(name, i) for name, (_, _, wrong) in WRONG.items() for i in range(-1, len(wrong))])
+def test_one_wrong_argument_is_refused(name, at, library):
+    """The call as it is reaches the library; with one argument wrong it does not, and the status says what kind of fault it is."""
+    call, entry, wrong = WRONG[name]
+    if at < 0:
+        call()
+        assert [n for n, _ in library.calls] == [entry]
+    else:
+        refused(wrong[at][1], lambda: call(**wrong[at][0]), library)
+
+
+@pytest.mark.parametrize("name", WRONG)
+def test_the_librarys_own_refusals_are_raised(name, library, monkeypatch):
+    call, entry, _ = WRONG[name]
+    monkeypatch.setattr(library, entry, lambda *a: st.ST_ERR_HIP, raising=False)
+    refused(st.ST_ERR_HIP, call, library)
+
+
+def test_sizes_that_have_no_workspace_are_refused(library):
+    long = st.ST_INT8_MAX_SUM + 1
+    refused(SHAPE, lambda: st.new_int8_workspace(1, 1, long), library)
+    refused(SHAPE, lambda: st.new_int8_workspace(1, 0, 4, backward=True), library)
+    refused(SHAPE, lambda: st.st_int8_linear(dev(2, long), dev(3, long, dtype=BYTES), dev(3)), library)
+    refused(ARG, lambda: st.new_adamw_state([dev(4)], bits=16), library)
