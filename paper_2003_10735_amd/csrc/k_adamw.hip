@@ -383,8 +383,10 @@ void adamw_step(Ctx& c, const st_adamw_tensor* t, int n, const st_adamw_opts& o,
 #undef ST_SUMS
             done += (int)blocks;
         });
-        // Up to two rounds of blocks the step adds the parts itself: they are few then, and a launch of its own takes longer.
-        if (tiles > 0 && tiles <= 4096 && done <= NORM_BLOCKS) nr = NormRef{nullptr, parts, done, o.grad_norm};
+        // Up to some 2000 tiles the step adds the parts itself, every block all of them; beyond, that costs more than a launch of its own.  Lists
+        // of heads, us a call, added in each block and by a launch: 32 bits, 438 tiles 8.5 and 9.8, 1752 12.8 and 14.3, 2190 17.9 and 18.7, 2628
+        // 20.4 and 20.5, 3942 32.7 and 30.5; 8 bits, 884 tiles 13.1 and 14.4, 1768 18.1 and 18.9, 2210 29.1 and 28.9, 3978 45.8 and 44.7.
+        if (tiles > 0 && tiles <= 2048 && done <= NORM_BLOCKS) nr = NormRef{nullptr, parts, done, o.grad_norm};
         else {
             ST_LAUNCH(c, "grad_norm", k_norm, dim3(1), dim3(256), 0, parts, done, (float*)workspace, o.grad_norm);
             nr.norm = (const float*)workspace;
