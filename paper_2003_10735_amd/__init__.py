@@ -530,7 +530,7 @@ def st_int8_linear_backward(x, w, dy, y=None, dx=None, dw=None, db=None, workspa
     """Gradients of a dense layer, both products in 8-bit integers: dx [m, k] (float32 or bfloat16) = dz W, dw [n, k] float32 = dz^T x,
     db [n] float32 = sum of dz, where dz = dy, or with y (the layer's result, a layer with ReLU) dy where y > 0.  Only the outputs that
     are given are computed; x may be None without dw, w without dx.  x, w (float weights), dy, y: float32 or bfloat16, row by row or column by
-    column, y as dy.  Returns (dx, dw, db)."""
+    column, y as dy (one token: with any step).  Returns (dx, dw, db)."""
     where = "st_int8_linear_backward"
     mdy = _matrix(dy, where)
     m, n = mdy.rows, mdy.cols

@@ -143,8 +143,8 @@ __device__ __forceinline__ float run_multiplier(unsigned top, float codes2, floa
     *scale = a * (1.f / codes2);
     return codes2 * (1.f / a);
 }
-// Square root, rounded to the nearest float32, of 0 and of normal numbers from 2^-96 on (and of infinity and NaN).  The instruction's
-// result s is off by one unit in the last place at most; s (s +- unit) is s^2 beyond the middle between the two candidates, so the sign of
+// Square root, rounded to the nearest float32, of 0 and of normal numbers from 2^-96 on (and of infinity and NaN), by Tuckerman's rounding
+// test.  The instruction's result s is off by one unit in the last place at most; s (s +- unit) is s^2 beyond the middle between the two candidates, so the sign of
 // its difference from x, which a fused multiply-add has exactly, decides.
 __device__ __forceinline__ float sqrt_rn(float x)
 {

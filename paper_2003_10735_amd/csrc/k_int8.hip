@@ -90,10 +90,16 @@ template <int COUNT> __device__ __forceinline__ void store_out(const Product& p,
         asm volatile("" ::: "memory");  \
     } while (0)
 
-// BM tokens x BN channels a block, WM x WN a wavefront, DEPTH stages under way.  Large products are bound by the matrix cores at the
-// clock that they leave (8192 tokens 4096 -> 14336: 436 us, 2.2 POP/s, 54 % busy at some 1.7 GHz; the same product of zeros takes 15 % less);
-// tiles of 128 and 64 by what a compute unit gets into LDS, about 50 bytes a ns (1024 tokens 2048 -> 1024: 8.6 us, 0.28 a stage, with 3 to 8
-// stages under way alike).
+// BM tokens x BN channels a block, WM x WN a wavefront, DEPTH stages under way.  No unit is full: a stage's loads, its LDS reads and its
+// products overlap in part only, and a barrier a stage keeps the wavefronts together.  Us a launch, whole, with the loads alone and without
+// the loop's loads; then shares of the busy compute units' clocks in which LDS is read (256 bytes each; 234 measured by reads alone) and
+// the matrix cores work, and of the wavefronts' cycles that are waits:
+//   256        8192 tokens 4096 -> 14336   443   363   385    26 %   58 %   30 %
+//   128        4096 tokens 2048 -> 2048   23.7  17.4  21.4    40 %   46 %   44 %
+//   128 deep   1536 tokens 4096 -> 1536   19.7  15.2  17.1    31 %   39 %   41 %
+//   64         1024 tokens 2048 -> 1024    9.0   7.8   7.6    13 %   12 %   50 %
+// The first is 2.2 POP/s at the 1.8 GHz that the products leave (the same product of zeros takes 15 % less).  A stage of the last is 0.23 us
+// (1024 tokens 8192 -> 1024 20.4 us, half as long a sum 13.0), with 3 to 8 stages under way alike; its loads alone take 0.17, 95 bytes a ns.
 template <int BM, int BN, int WM, int WN, int DEPTH>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_int8_product(const GemmPair pair)
 {
@@ -597,8 +603,9 @@ Form form_of(const Extent* e, int count)
     for (int i = 0; i < count; ++i) {
         const int64_t stages = ceil_div(e[i].k, STAGE);
         int64_t s = stages > 16 ? stages / each : 1;
-        // (beside another product, blocks that would go on for 20 stages when the others are done: 13282 tokens 442 -> 2258 144 us backward
-        // instead of 166; 1500 tokens 8192 -> 1700, alone, 53.6 instead of 42.6, so there not)
+        // (beside another product, blocks that would go on for 20 stages when the others are done: over 26 backward passes that this changes,
+        // 24 of them drawn at random, 0.83 to 1.05 of the time without, 0.90 on average; 13282 tokens 442 -> 2258 112 us instead of 134; 1500
+        // tokens 8192 -> 1700, alone, 53.6 instead of 42.6, so there not)
         if (count > 1 && f.tile == 128 && s == 1 && stages >= each + 20) s = 2;
         s = std::max(s, ceil_div(stages, ST_INT8_MAX_SUM / STAGE));    // what int32 can hold
         f.splits[i] = (int)std::max<int64_t>(s, 1);
