@@ -174,7 +174,10 @@ def prepare(case, seed):
     if own:
         st = _library()
         s["activation"] = [st.ST_ACT_NONE, st.ST_ACT_RELU, st.ST_ACT_GELU, st.ST_ACT_GELU_TANH, st.ST_ACT_SILU][_ACTS.index(case["act"])]
-        s["workspace"] = st.new_linear_workspace(m, n, k, backward=case["op"] == "backward", dtype=dtype)
+        if case["op"] == "linear":
+            s["workspace"] = st.new_linear_workspace(s["x"], s["w"])
+        else:
+            s["workspace"] = st.new_linear_workspace(s["x"], s["w"], s["dy"], s["activation"])
     return s
 
 
