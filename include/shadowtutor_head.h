@@ -361,6 +361,76 @@ int st_adamw_step(const st_adamw_tensor* tensors, int32_t n_tensors, const st_ad
 int st_adamw_state(const int8_t* m, const float* m_scale, const uint8_t* v, const float* v_scale, int64_t n, float* m_out,
                    float* v_out, void* stream);
 
+/* ---- dense layers in bfloat16 or float32 ---------------------------------------------------
+ * The same dense layer with its products in the operands' own type (sums in float32), with what a block of layers has around it: bias,
+ * activation and a residual.  x and w have one type, either order each (a st_matrix may lie row by row or column by column, at any
+ * address that is a multiple of its type's size, with any stride).
+ *
+ *   z = x W^T + bias,   y = act(z) + residual          all in float32, each result rounded once to its type
+ *   ST_ACT_RELU z or 0 (a NaN stays one);  ST_ACT_GELU z Phi(z) with the normal distribution function;
+ *   ST_ACT_GELU_TANH z / 2 (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3)));  ST_ACT_SILU z / (1 + exp(-z))
+ * At -infinity the last three give their limit, 0. */
+#define ST_ACT_NONE 0
+#define ST_ACT_RELU 1
+#define ST_ACT_GELU 2
+#define ST_ACT_GELU_TANH 3
+#define ST_ACT_SILU 4
+#define ST_LINEAR_MAX_CHANNELS 1048576
+typedef struct st_linear_opts {      /* all zeros: nothing around the product */
+    const float* bias;               /* [n] or NULL */
+    int32_t activation;              /* ST_ACT_* */
+    int32_t residual_dtype;          /* ST_F32 | ST_BF16 */
+    const void* residual;            /* [m, n] row by row, or NULL; may be y itself (same type, same pitch) */
+    int64_t residual_pitch;
+    void* pre;                       /* [m, n] out: z, which the backward pass of an activation asks for; or NULL */
+    int64_t pre_pitch;
+    int32_t pre_dtype;
+} st_linear_opts;
+
+/* y [m, n] from x [m, k] and w [n, k]; n and k up to ST_LINEAR_MAX_CHANNELS.  y: float32 or bfloat16, row by row with y_pitch >= n.  y and pre overlap neither each
+ * other nor what is read (but for the residual in y).  opts may be NULL.
+ *   workspace  workspace_bytes >= st_linear_workspace(x, w) bytes (of these very matrices: a matrix that lies at an odd address or
+ *              with odd strides takes a copy), 256-byte aligned; 0 bytes: refused sizes */
+size_t st_linear_workspace(const st_matrix* x, const st_matrix* w);
+int st_linear(const st_matrix* x, const st_matrix* w, const st_linear_opts* opts, void* y, int32_t y_dtype, int64_t y_pitch,
+              void* workspace, size_t workspace_bytes, void* stream);
+
+/* Gradients of that layer from x [m, k], w [n, k] (one type), dy [m, n] (either type, either order) and, with an activation, pre [m, n]
+ * (z, either type, either order):
+ *   dz = dy act'(z)            rounded to the operands' type (ReLU: dy where z > 0, 0 elsewhere, whatever dy is)
+ *   dx [m, k] = dz W,   dw [n, k] (+)= dz^T x,   db [n] (+)= sum of dz over the tokens, in float32, before that rounding
+ * (The residual's gradient is dy.)  Each of dx, dw, db may be NULL and costs nothing then; x without dw and w without dx may be NULL.
+ * dx, dw: float32 or bfloat16, row by row with a pitch.  accumulate = 1 adds dw and db to what is there (several batches, one step);
+ * dx is always written anew.  Without activation pre may be NULL and is not read. */
+typedef struct st_linear_grads {
+    void* dx; int64_t dx_pitch; int32_t dx_dtype;
+    int32_t dw_dtype; void* dw; int64_t dw_pitch;
+    float* db;
+    int32_t accumulate;              /* 0 | 1 */
+} st_linear_grads;
+size_t st_linear_backward_workspace(const st_matrix* x, const st_matrix* w, const st_matrix* dy, int32_t activation);
+int st_linear_backward(const st_matrix* x, const st_matrix* w, const st_matrix* dy, const st_matrix* pre, int32_t activation,
+                       const st_linear_grads* grads, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- the norm of many gradients, and clipping ----------------------------------------------
+ * Over a list of tensors of any types together (the lists of several optimisers, whose steps take one type each):
+ *   norm = 2-norm of all grad_scale * g, sums in float64
+ *   out = grad_scale * c * g, rounded once to out's type;  c = max_norm / norm where 0 < max_norm < norm < infinity, else 1
+ * (with a norm that is no finite number nothing is clipped; grad_norm says so).  out may be grad itself (same type); otherwise no out
+ * overlaps any other tensor of the list, and no tensor is in the list twice. */
+typedef struct st_grad_tensor {      /* HOST struct of DEVICE pointers, aligned to their elements */
+    const void* grad;                /* [n] */
+    void* out;                       /* [n], or NULL in every tensor: the norm alone */
+    int64_t n;                       /* >= 0; at most 2^33, as is the sum over the list */
+    int32_t grad_dtype, out_dtype;   /* ST_F32 | ST_BF16 */
+} st_grad_tensor;
+#define ST_GRAD_MAX_TENSORS 65536
+
+/* Bytes of device scratch (0 if the list is invalid), 256-byte aligned.  max_norm 0: no clipping.  grad_norm [1] out float32, or NULL. */
+size_t st_grad_clip_workspace(const st_grad_tensor* tensors, int32_t n_tensors);
+int st_grad_clip(const st_grad_tensor* tensors, int32_t n_tensors, double grad_scale, double max_norm, float* grad_norm, void* workspace,
+                 void* stream);
+
 /* ---- scheduling arithmetic around the training step (host only, no GPU work) ------------- */
 
 /* Key-frame striding, Algorithm 2: the ratio of the next stride to the current one is linear in

@@ -24,6 +24,8 @@ ST_F32, ST_BF16 = 0, 1
 ST_NCHW, ST_NHWC = 0, 1
 ST_COMPUTE_F32, ST_COMPUTE_BF16 = 0, 1
 ST_OPTIM_SGD, ST_OPTIM_ADAM = 0, 1
+ST_ACT_NONE, ST_ACT_RELU, ST_ACT_GELU, ST_ACT_GELU_TANH, ST_ACT_SILU = 0, 1, 2, 3, 4
+ST_LINEAR_MAX_CHANNELS = 1048576
 ST_INT8_MAX_SUM = 131071
 ST_ADAMW_BLOCK = 256
 
@@ -33,7 +35,8 @@ EXPORTS = ["st_num_params", "st_workspace_bytes", "st_head_forward", "st_head_fo
            "st_next_stride", "st_schedule_bounds", "st_schedule_total_time",
            "st_graph_cache_clear", "st_graph_cache_size", "st_metric_polling",
            "st_int8_quantize_workspace", "st_int8_quantize", "st_int8_linear_workspace", "st_int8_linear",
-           "st_int8_linear_backward_workspace", "st_int8_linear_backward", "st_adamw_workspace", "st_adamw_step", "st_adamw_state"]
+           "st_int8_linear_backward_workspace", "st_int8_linear_backward", "st_adamw_workspace", "st_adamw_step", "st_adamw_state",
+           "st_linear_workspace", "st_linear", "st_linear_backward_workspace", "st_linear_backward", "st_grad_clip_workspace", "st_grad_clip"]
 
 
 class StHeadDesc(C.Structure):
@@ -86,6 +89,20 @@ class StAdamwTensor(C.Structure):
 class StAdamwOpts(C.Structure):
     _fields_ = [(k, C.c_int32) for k in ("param_dtype", "grad_dtype", "state_bits", "t")] + [
         (k, C.c_double) for k in ("lr", "beta1", "beta2", "eps", "grad_scale", "max_norm")] + [("grad_norm", C.c_void_p)]
+
+
+class StLinearOpts(C.Structure):
+    _fields_ = [("bias", C.c_void_p), ("activation", C.c_int32), ("residual_dtype", C.c_int32), ("residual", C.c_void_p),
+                ("residual_pitch", C.c_int64), ("pre", C.c_void_p), ("pre_pitch", C.c_int64), ("pre_dtype", C.c_int32)]
+
+
+class StLinearGrads(C.Structure):
+    _fields_ = [("dx", C.c_void_p), ("dx_pitch", C.c_int64), ("dx_dtype", C.c_int32), ("dw_dtype", C.c_int32), ("dw", C.c_void_p),
+                ("dw_pitch", C.c_int64), ("db", C.c_void_p), ("accumulate", C.c_int32)]
+
+
+class StGradTensor(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("grad_dtype", C.c_int32), ("out_dtype", C.c_int32)]
 
 
 class StKernelStat(C.Structure):
@@ -159,7 +176,13 @@ def lib():
                 ("st_int8_linear_backward", C.c_int, [ptr, ptr, ptr, ptr, ptr, i32, i64, ptr, i64, ptr, ptr, ptr]),
                 ("st_adamw_workspace", size, [ptr, i32]),
                 ("st_adamw_step", C.c_int, [ptr, i32, ptr, ptr, ptr]),
-                ("st_adamw_state", C.c_int, [ptr, ptr, ptr, ptr, i64, ptr, ptr, ptr])):
+                ("st_adamw_state", C.c_int, [ptr, ptr, ptr, ptr, i64, ptr, ptr, ptr]),
+                ("st_linear_workspace", size, [ptr, ptr]),
+                ("st_linear", C.c_int, [ptr, ptr, ptr, ptr, i32, i64, ptr, size, ptr]),
+                ("st_linear_backward_workspace", size, [ptr, ptr, ptr, i32]),
+                ("st_linear_backward", C.c_int, [ptr, ptr, ptr, ptr, i32, ptr, ptr, size, ptr]),
+                ("st_grad_clip_workspace", size, [ptr, i32]),
+                ("st_grad_clip", C.c_int, [ptr, i32, C.c_double, C.c_double, ptr, ptr, ptr])):
             f = getattr(L, name)
             f.restype, f.argtypes = result, args
         L.st_graph_cache_size.restype = C.c_int
@@ -672,6 +695,153 @@ def st_adamw_state(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):
                                 None if m_out is None else _float_vector(m_out, n, where),
                                 None if v_out is None else _float_vector(v_out, n, where), _stream(stream)), where)
     return m_out, v_out
+
+
+# ---------------------------------------------------------------- dense layers in bfloat16 or float32
+def _linear_bytes(x, w, dy=None, activation=ST_ACT_NONE) -> int:
+    """Bytes of scratch of a call on these matrices (StMatrix or None); 0: they are refused."""
+    refs = [None if a is None else C.byref(a) for a in (x, w, dy)]
+    return lib().st_linear_workspace(*refs[:2]) if dy is None else lib().st_linear_backward_workspace(*refs, activation)
+
+
+def new_linear_workspace(x, w, dy=None, activation: int = ST_ACT_NONE):
+    """Scratch for st_linear on matrices that lie as x and w do, or with dy for st_linear_backward (x or w may then be None where the
+    gradient that needs it is not asked for).  Most of it is for copies of matrices at odd addresses or with odd strides, and for dz."""
+    where = "new_linear_workspace"
+    like = x if x is not None else w if w is not None else dy
+    if like is None or (dy is None and (x is None or w is None)):
+        raise StError(ST_ERR_NULL, where)
+    return _scratch(_linear_bytes(*[None if t is None else _matrix(t, where) for t in (x, w, dy)], activation), like.device, where)
+
+
+def _workspace_of(workspace, nbytes, device, stream, where):
+    """(address, bytes) of the scratch of a call: as given, or made; the library says whether it is enough."""
+    if workspace is None:
+        n = nbytes()
+        workspace = _own(stream, lambda: _scratch(n, device, where))
+    elif not workspace.is_cuda:
+        raise StError(ST_ERR_WORKSPACE, where)
+    return workspace, workspace.data_ptr(), workspace.nbytes
+
+
+def st_linear(x, w, bias=None, activation: int = ST_ACT_NONE, residual=None, pre=None, out=None, out_dtype=None, workspace=None, stream=None):
+    """out [m, n] = act(x W^T + bias) + residual: x [m, k] and w [n, k] float32 or bfloat16, both of one type, either order each, any strides;
+    bias float32 [n]; residual [m, n] float32 or bfloat16, row by row, which may be out itself.  pre [m, n] (float32 or bfloat16, row by
+    row) receives x W^T + bias, which st_linear_backward asks for.  out: float32 or bfloat16, as given, else of out_dtype, else of x's type."""
+    where = "st_linear"
+    mx, mw = _matrix(x, where), _matrix(w, where)
+    m, n = mx.rows, mw.rows
+    if out is None:
+        import torch
+        out = _own(stream, lambda: torch.empty((m, n), dtype=out_dtype or x.dtype, device=x.device), result=True)
+    pitch = _out_matrix(out, m, n, where)
+    opts = None
+    if bias is not None or activation or residual is not None or pre is not None:
+        o = StLinearOpts()
+        o.activation = activation
+        if bias is not None:
+            o.bias = _float_vector(bias, n, where)
+        if residual is not None:
+            o.residual_pitch, o.residual_dtype, o.residual = _out_matrix(residual, m, n, where), _dtype(residual, where), residual.data_ptr()
+        if pre is not None:
+            o.pre_pitch, o.pre_dtype, o.pre = _out_matrix(pre, m, n, where), _dtype(pre, where), pre.data_ptr()
+        opts = C.byref(o)
+    ws, address, nbytes = _workspace_of(workspace, lambda: _linear_bytes(mx, mw), x.device, stream, where)
+    status = (_LIB or lib()).st_linear(C.byref(mx), C.byref(mw), opts, out.data_ptr(), _dtype(out, where), pitch, address, nbytes, _stream(stream))
+    if status:
+        raise StError(status, where)
+    return out
+
+
+def st_linear_backward(x, w, dy, pre=None, activation: int = ST_ACT_NONE, dx=None, dw=None, db=None, accumulate: bool = False, workspace=None,
+                       stream=None):
+    """Gradients of st_linear: dx [m, k] = dz W, dw [n, k] (+)= dz^T x (either: float32 or bfloat16), db [n] float32 (+)= sum of dz, where
+    dz = dy act'(pre); pre, what st_linear left there, is asked for with an activation.  Only the outputs that are given are computed; x may be
+    None without dw, w without dx.  accumulate=True adds to what dw and db hold.  x and w of one type; dy and pre of either; all in either
+    order.  (The residual's gradient is dy.)  Returns (dx, dw, db)."""
+    where = "st_linear_backward"
+    mdy = _matrix(dy, where)
+    m, n = mdy.rows, mdy.cols
+    if (dx is not None and w is None) or (dw is not None and x is None):
+        raise StError(ST_ERR_NULL, where)
+    mx = None if dw is None else _matrix(x, where)
+    mw = None if dx is None else _matrix(w, where)
+    mpre = _matrix(pre, where) if activation else None
+    k = mw.cols if mw is not None else mx.cols if mx is not None else 1
+    g = StLinearGrads()
+    if dx is not None:
+        g.dx_pitch, g.dx_dtype, g.dx = _out_matrix(dx, m, k, where), _dtype(dx, where), dx.data_ptr()
+    if dw is not None:
+        g.dw_pitch, g.dw_dtype, g.dw = _out_matrix(dw, n, k, where), _dtype(dw, where), dw.data_ptr()
+    if db is not None:
+        g.db = _float_vector(db, n, where)
+    g.accumulate = 1 if accumulate else 0
+    refs = [None if a is None else C.byref(a) for a in (mx, mw, mdy, mpre)]
+    ws, address, nbytes = _workspace_of(workspace, lambda: _linear_bytes(mx, mw, mdy, activation), dy.device, stream, where)
+    _check((_LIB or lib()).st_linear_backward(*refs, activation, C.byref(g), address, nbytes, _stream(stream)), where)
+    return dx, dw, db
+
+
+# ---------------------------------------------------------------- the norm of many gradients, and clipping
+class GradTensors:
+    """The list that st_grad_clip works on, in a HOST array that is filled once (the tensors are kept alive with it): gradients, contiguous,
+    float32 or bfloat16 in any mixture, and where the clipped ones go: outs (of the same lengths, either type), None in place."""
+
+    def __init__(self, grads, outs=None):
+        where = "GradTensors"
+        grads = list(grads)
+        outs = grads if outs is None else list(outs)
+        if len(outs) != len(grads):
+            raise StError(ST_ERR_SHAPE, where)
+        if any(t is None for t in grads + outs):
+            raise StError(ST_ERR_NULL, where)
+        self.count, self.kept = len(grads), (grads, outs)
+        self.array = (StGradTensor * max(self.count, 1))()
+        read, written = [], []
+        for a, g, o in zip(self.array, grads, outs):
+            if g.numel() != o.numel() or not g.is_contiguous() or not o.is_contiguous():
+                raise StError(ST_ERR_SHAPE, where)
+            a.grad, a.out, a.n, a.grad_dtype, a.out_dtype = g.data_ptr(), o.data_ptr(), g.numel(), _dtype(g, where), _dtype(o, where)
+            if a.n:
+                written.append((a.out, a.out + o.nbytes))
+                if a.grad != a.out or a.grad_dtype != a.out_dtype:
+                    read.append((a.grad, a.grad + g.nbytes))
+        # what is written is nobody else's: each result, and where it is not its own gradient every gradient too
+        spans = sorted([(*s, True) for s in written] + [(*s, False) for s in read])
+        end, end_written = 0, 0
+        for first, behind, is_written in spans:
+            if first < (end if is_written else end_written):
+                raise StError(ST_ERR_ARG, where)
+            end = max(end, behind)
+            if is_written:
+                end_written = max(end_written, behind)
+        self.device = grads[0].device if grads else "cuda"
+        self.on_device = all(t.is_cuda for t in grads + outs)
+        self._bytes = None
+
+    def norm_bytes(self) -> int:
+        """Bytes of scratch that the norm of this list asks for."""
+        if self._bytes is None:
+            self._bytes = lib().st_grad_clip_workspace(self.array, self.count)
+        return self._bytes
+
+
+def new_grad_workspace(tensors: GradTensors):
+    """Scratch for st_grad_clip of this list."""
+    return _scratch(tensors.norm_bytes(), tensors.device, "new_grad_workspace")
+
+
+def st_grad_clip(tensors: GradTensors, max_norm: float = 0.0, grad_scale: float = 1.0, grad_norm=None, workspace=None, stream=None):
+    """Every gradient of the list times grad_scale, and, where the 2-norm of all of them is above max_norm > 0, times max_norm / norm, into its
+    place in the list's outs.  grad_norm (float32 [1]) receives the norm before clipping.  A norm that is not finite clips nothing."""
+    where = "st_grad_clip"
+    if not tensors.on_device:
+        raise StError(ST_ERR_ARG, where)
+    if workspace is None:
+        workspace = _own(stream, lambda: new_grad_workspace(tensors))
+    _check((_LIB or lib()).st_grad_clip(tensors.array, tensors.count, grad_scale, max_norm,
+                                        None if grad_norm is None else _float_vector(grad_norm, 1, where),
+                                        _given(workspace, tensors.norm_bytes(), where), _stream(stream)), where)
 
 
 def st_graph_cache_clear():

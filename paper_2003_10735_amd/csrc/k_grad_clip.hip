@@ -1,0 +1,192 @@
+// The 2-norm of many gradients, and the gradients clipped by it.  A launch takes up to CLIP_PER_LAUNCH tensors, whose pointers travel with its
+// arguments.  The norm has to be known before the first value can be written, so the list is read twice.
+#include "st_clip.hpp"
+#include "st_quantize.hpp"
+
+#include <math.h>
+#include <algorithm>
+
+namespace st {
+
+constexpr int CLIP_PER_LAUNCH = 120, CLIP_BLOCKS = 2048;
+struct ClipList {
+    const void* g[CLIP_PER_LAUNCH]; void* out[CLIP_PER_LAUNCH]; long long n[CLIP_PER_LAUNCH];
+    unsigned first[CLIP_PER_LAUNCH + 1];       // first tile of each
+    uint8_t types[CLIP_PER_LAUNCH];            // bit 0: gradients in bfloat16, bit 1: results
+    int count;
+};
+static_assert(sizeof(ClipList) + 128 <= 4096, "kernel arguments");
+// values of a tile: small lists are spread over more blocks
+static int clip_tile(int64_t all) { return all <= (int64_t)CLIP_BLOCKS * 2048 ? 2048 : 8192; }
+
+// The last tensor that begins at or before the tile: every lane looks at two of them.
+__device__ __forceinline__ int clip_tensor(const ClipList& l, unsigned tile)
+{
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+#pragma unroll
+    for (int c = 0; c < CLIP_PER_LAUNCH; c += 64) {
+        const bool there = c + lane < l.count;
+        before += __popcll(__ballot(there && l.first[there ? c + lane : 0] <= tile));
+    }
+    return before - 1;
+}
+__device__ __forceinline__ double clip_block_sum(double s, double* sums)      // of 256 threads, in one order; to every thread
+{
+#pragma unroll
+    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
+    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
+    __syncthreads();
+    return (sums[0] + sums[1]) + (sums[2] + sums[3]);
+}
+
+// Squares and their sums in float64: no square of a finite gradient is infinite or vanishes, and the order of the sums does not show.
+template <class G, int RUNS> __device__ __forceinline__ double tile_squares(const void* p, long long n, long long base)
+{
+    Raw8<G> v[RUNS];
+    load_row((const G*)p, n, [&](int j) { return base + j * 2048; }, v);
+    double s = 0.0;
+#pragma unroll
+    for (int j = 0; j < RUNS; ++j)
+#pragma unroll
+        for (int k = 0; k < 8; ++k) { const double d = (double)v[j][k]; s = __builtin_fma(d, d, s); }
+    return s;
+}
+template <int RUNS> __global__ __launch_bounds__(256) void k_clip_squares(const ClipList l, unsigned tiles, double* __restrict__ parts)
+{
+    __shared__ double sums[4];
+    // a block's tiles follow one another, so that the tensor is searched once
+    const unsigned each = tiles / gridDim.x, rest = tiles - each * gridDim.x;
+    unsigned tile = blockIdx.x * each + min(blockIdx.x, rest);
+    const unsigned end = tile + each + (blockIdx.x < rest ? 1 : 0);
+    int i = clip_tensor(l, tile);
+    double s = 0.0;
+    for (; tile < end; ++tile) {
+        while (i + 1 < l.count && tile >= l.first[i + 1]) ++i;
+        const long long base = (long long)(tile - l.first[i]) * (RUNS * 2048) + threadIdx.x * 8;
+        s += l.types[i] & 1 ? tile_squares<bf16, RUNS>(l.g[i], l.n[i], base) : tile_squares<float, RUNS>(l.g[i], l.n[i], base);
+    }
+    s = clip_block_sum(s, sums);
+    if (threadIdx.x == 0) parts[blockIdx.x] = s;
+}
+
+// The norm from its parts, by every block in the same order, and the factor on the gradients.
+struct ClipFactor { double norm, factor; };
+__device__ __forceinline__ ClipFactor clip_factor(const ClipRule& r, const double* __restrict__ parts, int n, double* sums)
+{
+    double s = 0.0;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += 256) s += parts[i];
+    const double norm = sqrt(clip_block_sum(s, sums)) * r.scale;
+    return {norm, r.max_norm > 0 && norm > r.max_norm && norm < __builtin_inf() ? r.scale * (r.max_norm / norm) : r.scale};
+}
+
+template <class G, class O, int RUNS> __device__ __forceinline__ void tile_scaled(const void* p, void* q, long long n, long long base, double factor)
+{
+    Raw8<G> v[RUNS];
+    load_row((const G*)p, n, [&](int j) { return base + j * 2048; }, v);
+    O* o = (O*)q;
+    // (a factor that float32 does not hold is applied in two steps)
+    const float c = (float)factor;
+    const bool plain = fabsf(c) >= 0x1p-120f || factor == 0.0;
+    const float c1 = plain ? c : (float)(factor * 0x1p100), c2 = plain ? 1.f : 0x1p-100f;
+#pragma unroll
+    for (int j = 0; j < RUNS; ++j) {
+        const long long at = base + j * 2048;
+        float u[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) u[k] = v[j][k] * c1 * c2;
+        if (at + 8 <= n) {
+            typedef O O4 __attribute__((ext_vector_type(4)));
+            typedef O4 O4any __attribute__((aligned(sizeof(O))));
+#pragma unroll
+            for (int k = 0; k < 8; k += 4)
+                __builtin_nontemporal_store(O4{from_f32<O>(u[k]), from_f32<O>(u[k + 1]), from_f32<O>(u[k + 2]), from_f32<O>(u[k + 3])}, (O4any*)(o + at + k));
+        } else
+#pragma unroll
+            for (int k = 0; k < 8; ++k) if (at + k < n) o[at + k] = from_f32<O>(u[k]);
+    }
+}
+template <int RUNS> __global__ __launch_bounds__(256) void k_clip_scale(const ClipList l, const ClipRule r, unsigned tiles, const double* __restrict__ parts, int n_parts)
+{
+    __shared__ double sums[4];
+    const ClipFactor c = clip_factor(r, parts, n_parts, sums);
+    if (r.norm && blockIdx.x == 0 && threadIdx.x == 0) *r.norm = (float)c.norm;
+    const unsigned each = tiles / gridDim.x, rest = tiles - each * gridDim.x;
+    unsigned tile = blockIdx.x * each + min(blockIdx.x, rest);
+    const unsigned end = tile + each + (blockIdx.x < rest ? 1 : 0);
+    if (tile == end) return;
+    int i = __builtin_amdgcn_readfirstlane(clip_tensor(l, tile));
+    for (; tile < end; ++tile) {
+        while (i + 1 < l.count && tile >= l.first[i + 1]) ++i;
+        if (c.factor == 1.0 && l.g[i] == l.out[i]) continue;
+        const long long base = (long long)(tile - l.first[i]) * (RUNS * 2048) + threadIdx.x * 8;
+        switch (l.types[i]) {
+        case 0: tile_scaled<float, float, RUNS>(l.g[i], l.out[i], l.n[i], base, c.factor); break;
+        case 1: tile_scaled<bf16, float, RUNS>(l.g[i], l.out[i], l.n[i], base, c.factor); break;
+        case 2: tile_scaled<float, bf16, RUNS>(l.g[i], l.out[i], l.n[i], base, c.factor); break;
+        default: tile_scaled<bf16, bf16, RUNS>(l.g[i], l.out[i], l.n[i], base, c.factor); break;
+        }
+    }
+}
+
+// The lists of the launches that the tensors from *next on need: those without values are left out.
+static ClipList next_list(const st_grad_tensor* t, int n, int* next, int64_t tile, unsigned* tiles)
+{
+    ClipList l{};
+    unsigned at = 0;
+    for (; *next < n && l.count < CLIP_PER_LAUNCH; ++*next) {
+        const st_grad_tensor& x = t[*next];
+        if (x.n == 0) continue;
+        const int i = l.count++;
+        l.g[i] = x.grad; l.out[i] = x.out; l.n[i] = x.n; l.first[i] = at;
+        l.types[i] = (x.grad_dtype == ST_BF16 ? 1 : 0) | (x.out_dtype == ST_BF16 ? 2 : 0);
+        at += (unsigned)ceil_div(x.n, tile);
+    }
+    l.first[l.count] = at;
+    *tiles = at;
+    return l;
+}
+static int64_t all_values(const st_grad_tensor* t, int n)
+{
+    int64_t all = 0;
+    for (int i = 0; i < n; ++i) all += t[i].n;
+    return all;
+}
+int64_t clip_parts(const st_grad_tensor* t, int n)
+{
+    const int64_t tile = clip_tile(all_values(t, n));
+    int64_t parts = 0;
+    for (int next = 0; next < n;) {
+        int64_t at = 0;
+        for (int count = 0; next < n && count < CLIP_PER_LAUNCH; ++next) if (t[next].n) { at += ceil_div(t[next].n, tile); ++count; }
+        parts += std::min<int64_t>(at, CLIP_BLOCKS);
+    }
+    return parts;
+}
+void grad_clip(Ctx& c, const st_grad_tensor* t, int n, const ClipRule& r, double* parts)
+{
+    const int64_t tile = clip_tile(all_values(t, n));
+    int64_t n_parts = 0;
+    unsigned tiles = 0;
+    for (int next = 0; next < n;) {
+        const ClipList l = next_list(t, n, &next, tile, &tiles);
+        if (!tiles) continue;
+        const unsigned blocks = std::min<unsigned>(tiles, CLIP_BLOCKS);
+        if (tile == 2048) ST_LAUNCH(c, "clip_squares", k_clip_squares<1>, dim3(blocks), dim3(256), 0, l, tiles, parts + n_parts);
+        else ST_LAUNCH(c, "clip_squares", k_clip_squares<4>, dim3(blocks), dim3(256), 0, l, tiles, parts + n_parts);
+        n_parts += blocks;
+    }
+    ClipRule rule = r;
+    for (int next = r.write ? 0 : n; next < n || rule.norm;) {      // the first launch writes the norm, if only that
+        const ClipList l = next_list(t, n, &next, tile, &tiles);
+        const unsigned blocks = std::min<unsigned>(std::max(tiles, 1u), CLIP_BLOCKS);
+        if (tiles || rule.norm) {
+            if (tile == 2048) ST_LAUNCH(c, "clip_scale", k_clip_scale<1>, dim3(blocks), dim3(256), 0, l, rule, tiles, parts, (int)n_parts);
+            else ST_LAUNCH(c, "clip_scale", k_clip_scale<4>, dim3(blocks), dim3(256), 0, l, rule, tiles, parts, (int)n_parts);
+        }
+        rule.norm = nullptr;
+    }
+}
+
+}  // namespace st

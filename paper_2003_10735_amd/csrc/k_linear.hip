@@ -1,0 +1,585 @@
+// Products of bfloat16 or float32 operands on the matrix cores, with bias, activation and residual on their way out:
+//   out = act(a b^T + bias) + residual
+//
+// Either operand lies row by row along the contraction, or across it (a dense layer's gradients contract over what their operands' rows
+// are); no operand is copied to be turned.  A stage of 128 bytes of the contraction of a row (64 values, or 32 of float32) goes from
+// memory into LDS directly, 16 bytes a lane, and from there into fragments of 16 bytes a lane:
+//   v_mfma_f32_32x32x16_bf16: lane l supplies A[l % 32][8*(l/32) .. +7] and B[8*(l/32) .. +7][l % 32];
+//   v_mfma_f32_32x32x2_f32:   lane l supplies A[l % 32][l/32] and B[l/32][l % 32]: of the 16 bytes one value an instruction, so that an
+//                             instruction's two positions of the contraction lie four apart, for both operands alike;
+// both give D[8*(r/4) + 4*(l/32) + r%4][l % 32] in register r.  The rows of b (output channels) are A's, so that four registers of a lane
+// are four neighbouring channels of one token.
+//
+// Along: a row takes 128 bytes of LDS; chunk c (of 16 bytes) of row r lies in place c ^ (r / 2 % 8), so that lanes that read the same
+// chunk of sixteen consecutive rows read sixteen different groups of four banks.
+// Across: a position k of the contraction takes the tile's rows, R values next to each other.  bfloat16: ds_read_b64_tr_b16 turns 4 x 16
+// values in a group of sixteen lanes: lane j gives the address of four rows' values, 4*(j%4) .., of position j/4, and gets the four positions'
+// values of row j.  The 64 bytes that a position gives are moved by k % 4 times 64 bytes (R = 64: by 64 bytes where k / 2 is odd), so
+// that four positions of 32 rows meet no bank twice.  float32: 32 lanes read 32 rows' values at one position, the two halves of a wavefront four
+// positions apart, moved by 128 bytes.
+#include "st_linear.hpp"
+#include "st_quantize.hpp"
+
+#include <algorithm>
+
+namespace st {
+
+constexpr int BAND = 4;         // rows of tiles
+constexpr int STAGE = 128;      // bytes of the contraction a stage holds
+constexpr unsigned OUTSIDE = 0xffffff00u;      // an offset behind every buffer: a load gives zeros
+
+struct GemmArgs {
+    LinearProduct p;
+    FastDiv by_tiles, by_band;                // tiles of a split, tiles of a band of BAND rows of tiles
+    int tiles_m;
+    int splits, stages;                       // stages: of the whole contraction
+    unsigned blocks;
+};
+struct GemmPair { GemmArgs g[2]; ColumnSums sums; };
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+// 16 bytes a lane from `rsrc` + voff to LDS at `lds` + 16 * lane (the whole offset is the lanes': a scalar one takes no part in the
+// comparison with the buffer's size)
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char* lds, unsigned voff)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds, 16, (int)voff, 0, 0, 0);
+}
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const char* base, int64_t bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)(unsigned)(bytes < (int64_t)OUTSIDE ? bytes : (int64_t)OUTSIDE), 0x00020000);
+}
+
+// ------------------------------------------------------------------------------------------------- the way out
+template <int ACT, int COUNT> __device__ __forceinline__ void activate_all(float (&v)[COUNT])
+{
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i] = activate<ACT>(v[i]);
+}
+template <int COUNT> __device__ __forceinline__ void activate_all(int act, float (&v)[COUNT])
+{
+    switch (act) {
+    case ST_ACT_RELU: activate_all<ST_ACT_RELU>(v); break;
+    case ST_ACT_GELU: activate_all<ST_ACT_GELU>(v); break;
+    case ST_ACT_GELU_TANH: activate_all<ST_ACT_GELU_TANH>(v); break;
+    case ST_ACT_SILU: activate_all<ST_ACT_SILU>(v); break;
+    default: break;
+    }
+}
+// COUNT (a multiple of four, or one) values of a row from column n on, of which those below `end` exist: at once, or at the row's end one by one
+template <int COUNT> __device__ __forceinline__ void store_run(void* base, int is_bf16, int64_t at, int64_t n, int64_t end, const float (&v)[COUNT])
+{
+    if (is_bf16) {
+        bf16* o = (bf16*)base + at;
+        if (n + COUNT <= end) {
+            typedef bf16 T __attribute__((ext_vector_type(COUNT)));
+            typedef T T2 __attribute__((aligned(2)));
+            T u;
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) u[i] = (bf16)v[i];
+            *(T2*)o = u;
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) if (n + i < end) o[i] = (bf16)v[i];
+    } else {
+        float* o = (float*)base + at;
+        if (n + COUNT <= end) {
+            if constexpr (COUNT == 1) *o = v[0];
+            else
+#pragma unroll
+                for (int i = 0; i < COUNT; i += 4) *(f32x4_4*)(o + i) = f32x4_t{v[i], v[i + 1], v[i + 2], v[i + 3]};
+            return;
+        }
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) if (n + i < end) o[i] = v[i];
+    }
+}
+template <int COUNT> __device__ __forceinline__ void load_run(const void* base, int is_bf16, int64_t at, int64_t n, int64_t end, float (&v)[COUNT])
+{
+    const int there = n + COUNT <= end ? COUNT : (int)(end - n);
+    if constexpr (COUNT == 1) v[0] = is_bf16 ? (float)((const bf16*)base)[at] : ((const float*)base)[at];
+    else
+#pragma unroll
+        for (int i = 0; i < COUNT; i += 4) {
+            float u[4];
+            if (is_bf16) load4((const bf16*)base + at + i, there - i, u); else load4((const float*)base + at + i, there - i, u);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[i + j] = u[j];
+        }
+}
+// What the sums of row m, columns n .. n + COUNT - 1 (n < p.n) become.  bias: of these columns.
+template <int COUNT> __device__ __forceinline__ void finish(const LinearProduct& p, int64_t m, int64_t n, float (&v)[COUNT], const float (&bias)[COUNT])
+{
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i] += bias[i];
+    if (p.pre) store_run(p.pre, p.pre_bf16, m * p.pre_pitch + n, n, p.n, v);
+    activate_all(p.act, v);
+    if (p.residual) {
+        float r[COUNT];
+        load_run(p.residual, p.residual_bf16, m * p.residual_pitch + n, n, p.n, r);
+#pragma unroll
+        for (int i = 0; i < COUNT; ++i) v[i] += r[i];
+    }
+    store_run(p.out, p.out_bf16, m * p.out_pitch + n, n, p.n, v);
+}
+template <int COUNT> __device__ __forceinline__ void bias_of(const LinearProduct& p, int64_t n, float (&b)[COUNT])
+{
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) b[i] = p.bias && n + i < p.n ? p.bias[n + i] : 0.f;
+}
+
+// s_waitcnt vmcnt(N) alone; a barrier that memory accesses stay on their side of, without a wait of its own
+#define ST_WAIT_VM(N) __builtin_amdgcn_s_waitcnt(((N) & 15) | (((N) >> 4) << 14) | 0x0F70)
+#define ST_BARRIER()                    \
+    do {                                \
+        asm volatile("" ::: "memory");  \
+        __builtin_amdgcn_s_barrier();   \
+        asm volatile("" ::: "memory");  \
+    } while (0)
+
+// ------------------------------------------------------------------------------------------------- an operand's tile
+// R rows, loaded by WAVES wavefronts, N blocks of 32 rows of which a wavefront multiplies.
+template <class E, bool ALONG, int R, int WAVES, int N> struct Tile;
+
+template <class E, int R, int WAVES, int N> struct Tile<E, true, R, WAVES, N> {
+    static constexpr int LOADS = R / 8 / WAVES, READS = N;
+    static_assert(WAVES % 2 == 0, "a wavefront's eight rows begin at an even or at an odd multiple of eight in every load");
+    __amdgpu_buffer_rsrc_t r;
+    unsigned v, step, chunk, end;
+    unsigned row;                // of a fragment: its place in the tile
+    __device__ __forceinline__ Tile(const Operand& o, int64_t row0, int64_t rows, int64_t k, int lane, int wave, int first)
+    {
+        const int64_t pitch = o.pitch * sizeof(E);
+        end = (unsigned)k * sizeof(E);
+        r = buffer((const char*)o.p + row0 * pitch, (rows - row0 - 1) * pitch + (end + 15) / 16 * 16);      // (copies have zeros there)
+        chunk = ((lane & 7) ^ ((lane >> 4) + 4 * (wave & 1))) * 16;
+        v = (unsigned)(wave * 8 + (lane >> 3)) * (unsigned)pitch + chunk;
+        step = WAVES * 8 * (unsigned)pitch;
+        row = (unsigned)(first + (lane & 31)) * STAGE;
+    }
+    __device__ __forceinline__ void load(int s, char* to, int wave) const
+    {
+        unsigned off = v + (unsigned)s * STAGE;
+        const bool there = chunk + (unsigned)s * STAGE < end;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i, off += step) load_to_lds(r, to + (i * WAVES + wave) * 1024, there ? off : OUTSIDE);
+    }
+    __device__ __forceinline__ void fetch(const char* L, int ks, int lane, i32x4 (&f)[N]) const
+    {
+        const char* at = L + row + ((ks * 2 + (lane >> 5)) ^ (lane >> 1 & 7)) * 16;
+#pragma unroll
+        for (int i = 0; i < N; ++i) f[i] = *(const i32x4*)(at + i * 32 * STAGE);
+    }
+};
+
+template <class E, int R, int WAVES, int N> struct Tile<E, false, R, WAVES, N> {
+    static constexpr int ES = sizeof(E), KS = STAGE / ES, LANES = R * ES / 16, KPI = 64 / LANES;      // a wavefront's load: KPI positions
+    static constexpr int LOADS = R / 8 / WAVES, READS = ES == 2 ? 2 * N : 4 * N;
+    static_assert(WAVES * KPI % 8 == 0, "the places of a position are the same in every load of a wavefront");
+    const char* base; int64_t pitch, k, tail;
+    unsigned v, step, at[N];
+    static __device__ __forceinline__ unsigned moved(unsigned position)      // by how many chunks
+    {
+        if constexpr (ES == 4) return 8 * (position >> 2 & 1);
+        else if constexpr (R == 64) return 4 * (position >> 1 & 1);
+        else return 4 * (position & 3);
+    }
+    __device__ __forceinline__ Tile(const Operand& o, int64_t row0, int64_t rows, int64_t len, int lane, int wave, int first)
+    {
+        pitch = o.pitch * ES;
+        base = (const char*)o.p + row0 * ES;
+        k = len;
+        tail = ((rows - row0) * ES + 15) / 16 * 16;      // (whole chunks: what lies behind the last row inside one is memory that is there)
+        const unsigned position = wave * KPI + lane / LANES;
+        v = position * (unsigned)pitch + ((lane % LANES) ^ moved(position)) * 16;
+        step = WAVES * KPI * (unsigned)pitch;
+        const int half = lane >> 5;
+        if constexpr (ES == 2) {
+            const unsigned from = 8 * half + (lane >> 2 & 3);
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                at[i] = from * R * 2 + ((first / 8 + i * 4 + 2 * (lane >> 4 & 1) + (lane >> 1 & 1)) ^ moved(from)) * 16 + (lane & 1) * 8;
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                at[i] = 4 * half * R * 4 + (((first + i * 32 + (lane & 31)) / 4) ^ (8 * half)) * 16 + (lane & 3) * 4;
+        }
+    }
+    __device__ __forceinline__ void load(int s, char* to, int wave) const
+    {
+        const int64_t from = (int64_t)s * KS;
+        const auto r = buffer(base + from * pitch, (k - from - 1) * pitch + tail);
+        unsigned off = v;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i, off += step) load_to_lds(r, to + (i * WAVES + wave) * 1024, off);
+    }
+    __device__ __forceinline__ void fetch(const char* L, int ks, int lane, i32x4 (&f)[N]) const
+    {
+        (void)lane;
+        if constexpr (ES == 2) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                typedef __attribute__((address_space(3))) s16x4* P;
+                struct Two { s16x4 lo, hi; } t;
+                t.lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(L + at[i] + ks * 16 * R * 2));
+                t.hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(L + at[i] + (ks * 16 + 4) * R * 2));
+                f[i] = __builtin_bit_cast(i32x4, t);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f[i][j] = *(const int*)(L + at[i] + (ks * 8 + j) * R * 4);
+        }
+    }
+};
+
+template <class E> __device__ __forceinline__ f32x16 mfma(i32x4 a, i32x4 b, f32x16 c)
+{
+    if constexpr (sizeof(E) == 2) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else {
+        const f32x4 u = __builtin_bit_cast(f32x4, a), v = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(u[j], v[j], c, 0, 0, 0);
+        return c;
+    }
+}
+
+// ------------------------------------------------------------------------------------------------- a block's tile
+template <class E, int BM, int BN, int WM, int WN, int DEPTH, bool A_ALONG, bool B_ALONG>
+__device__ __forceinline__ void product_tile(const GemmArgs& g, char* lds, int64_t m0, int64_t n0, int split)
+{
+    constexpr int WAVES = (BM / WM) * (BN / WN), NA = WN / 32, NB = WM / 32, STEPS = STAGE / 32;
+    constexpr int BUF = (BM + BN) * STAGE, MINE = BN * STAGE;       // channels first, then tokens
+    const LinearProduct& p = g.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int first = (int)((int64_t)g.stages * split / g.splits), last = (int)((int64_t)g.stages * (split + 1) / g.splits);
+    const int wn = (wave % (BN / WN)) * WN, wm = (wave / (BN / WN)) * WM;
+    using Channels = Tile<E, B_ALONG, BN, WAVES, NA>;
+    using Tokens = Tile<E, A_ALONG, BM, WAVES, NB>;
+    const Channels channels(p.b, n0, p.n, p.k, lane, wave, wn);
+    const Tokens tokens(p.a, m0, p.m, p.k, lane, wave, wm);
+    auto stage = [&](int s, int buf) {
+        channels.load(s, lds + buf * BUF, wave);
+        tokens.load(s, lds + buf * BUF + MINE, wave);
+    };
+    f32x16 acc[NB][NA] = {};
+    i32x4 a[2][NA], b[2][NB];
+    auto fetch = [&](int buf, int ks, int to) {
+        channels.fetch(lds + buf * BUF, ks, lane, a[to]);
+        tokens.fetch(lds + buf * BUF + MINE, ks, lane, b[to]);
+    };
+    auto multiply = [&](int from) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int i = 0; i < NA; ++i) acc[j][i] = mfma<E>(a[from][i], b[from][j], acc[j][i]);
+    };
+    // in the instruction stream: LDS reads spread over the matrix instructions
+    auto interleave = [] {
+        constexpr int READS = Channels::READS + Tokens::READS, PRODUCTS = NA * NB * (sizeof(E) == 2 ? 1 : 4);
+        constexpr int PER = READS > PRODUCTS ? (READS + PRODUCTS - 1) / PRODUCTS : 1;
+#pragma unroll
+        for (int i = 0; i < (READS + PER - 1) / PER; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, PER, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        }
+    };
+    // DEPTH stages are under way.  A stage's last step has its operands in registers when the barrier is passed, so what follows the
+    // barrier is: the loads of the stage DEPTH later into the buffer that is done with, the next stage's first operands, the last step's
+    // products.
+    constexpr int LOADS = Channels::LOADS + Tokens::LOADS;      // of a wavefront and stage
+    static_assert((DEPTH - 1) * LOADS < 64, "the counter of loads under way");
+    constexpr int PITCH = WN + 4, RUNS = WN / 8, ROWS = 64 / RUNS;
+    const int run = lane % RUNS, row = lane / RUNS;
+    const int64_t n = n0 + wn + run * 8;
+    float bias[8];
+    bias_of(p, n, bias);
+    if (first < last) {
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) if (first + d < last) stage(first + d, d);
+        if (first + DEPTH <= last) ST_WAIT_VM((DEPTH - 1) * LOADS); else ST_WAIT_VM(0);
+        ST_BARRIER();
+        fetch(0, 0, 0);
+    }
+    for (int s = first, buf = 0; s < last; ++s) {
+#pragma unroll
+        for (int ks = 0; ks < STEPS - 1; ++ks) {
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(buf, ks + 1, (ks + 1) & 1);
+            multiply(ks & 1);
+            interleave();
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        // the next stage is there (behind it DEPTH - 2 may still be on their way), this one is read
+        if (DEPTH > 2 && s + DEPTH <= last) ST_WAIT_VM((DEPTH - 2) * LOADS); else ST_WAIT_VM(0);
+        __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0)
+        ST_BARRIER();
+        if (s + DEPTH < last) stage(s + DEPTH, buf);
+        buf = buf + 1 == DEPTH ? 0 : buf + 1;
+        if (s + 1 < last) fetch(buf, 0, 0);
+        multiply((STEPS - 1) & 1);
+    }
+
+    // Out through LDS, 32 tokens of a wavefront at a time: sums go in four neighbouring channels at a time and come out as runs along a row.
+    __syncthreads();
+    static_assert(WAVES * 32 * PITCH * 4 <= DEPTH * BUF, "room for the sums");
+    float* mine = (float*)lds + wave * 32 * PITCH;
+    const int r32 = lane & 31, half = lane >> 5;
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+#pragma unroll
+        for (int i = 0; i < NA; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q)
+                *(f32x4*)(mine + r32 * PITCH + i * 32 + q * 8 + half * 4) =
+                    f32x4{acc[j][i][q * 4], acc[j][i][q * 4 + 1], acc[j][i][q * 4 + 2], acc[j][i][q * 4 + 3]};
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int h = 0; h < 32 / ROWS; ++h) {
+            const int r = h * ROWS + row;
+            const int64_t m = m0 + wm + j * 32 + r;
+            const f32x4 lo = *(const f32x4*)(mine + r * PITCH + run * 8), hi = *(const f32x4*)(mine + r * PITCH + run * 8 + 4);
+            if (m >= p.m || n >= p.n) continue;
+            float v[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+            if (g.splits > 1) store_run(p.slabs, 0, ((int64_t)split * p.m + m) * p.n + n, n, p.n, v);
+            else finish(p, m, n, v, bias);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+template <class E, int BM, int BN, int WM, int WN, int DEPTH>
+__global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_linear_product(const GemmPair pair)
+{
+    extern __shared__ __align__(16) char lds[];
+    const unsigned both = pair.g[0].blocks + pair.g[1].blocks;
+    if (blockIdx.x >= both) {      // columns' parts, a column a thread
+        const ColumnSums& s = pair.sums;
+        const int64_t i = (int64_t)(blockIdx.x - both) * blockDim.x + threadIdx.x;
+        if (i >= s.n) return;
+        float v = 0.f;
+#pragma unroll 4
+        for (int part = 0; part < s.n_parts; ++part) v += s.parts[(int64_t)part * s.n + i];
+        s.out[i] = s.accumulate ? s.out[i] + v : v;
+        return;
+    }
+    const bool second = blockIdx.x >= pair.g[0].blocks;
+    const GemmArgs& g = pair.g[second];
+    // An XCD gets a run of consecutive tiles, ordered in bands of four tiles of tokens: what its 32 compute units work on at a time is
+    // 4 x 8 tiles, and less goes from memory to its L2 than with rows of tiles.
+    const int block = xcd_band((int)blockIdx.x - (second ? (int)pair.g[0].blocks : 0), (int)g.blocks);
+    const int split = __builtin_amdgcn_readfirstlane(fast_quot(block, g.by_tiles));
+    const int tile = block - split * (int)g.by_tiles.d;
+    const int band = __builtin_amdgcn_readfirstlane(fast_quot(tile, g.by_band)), in_band = tile - band * (int)g.by_band.d;
+    const int high = min(BAND, g.tiles_m - band * BAND);
+    const int tn = __builtin_amdgcn_readfirstlane(in_band / high), tm = band * BAND + in_band - tn * high;
+    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    if (g.p.a.along) {
+        if (g.p.b.along) product_tile<E, BM, BN, WM, WN, DEPTH, true, true>(g, lds, m0, n0, split);
+        else product_tile<E, BM, BN, WM, WN, DEPTH, true, false>(g, lds, m0, n0, split);
+    } else {
+        if (g.p.b.along) product_tile<E, BM, BN, WM, WN, DEPTH, false, true>(g, lds, m0, n0, split);
+        else product_tile<E, BM, BN, WM, WN, DEPTH, false, false>(g, lds, m0, n0, split);
+    }
+}
+
+// The slabs of split products, added in the order of the splits, and what the product's own way out does otherwise: runs of eight of a row.
+__global__ __launch_bounds__(256) void k_linear_join(const GemmPair pair, int64_t first, int64_t all)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+        const bool second = i >= first;
+        const GemmArgs& g = pair.g[second];
+        const LinearProduct& p = g.p;
+        const int64_t runs = (p.n + 7) / 8, at = second ? i - first : i, m = at / runs, n = (at - m * runs) * 8, size = p.m * p.n;
+        float v[8] = {}, bias[8];
+        bias_of(p, n, bias);
+        for (int s = 0; s < g.splits; ++s) {
+            float u[8];
+            load_run(p.slabs, 0, s * size + m * p.n + n, n, p.n, u);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += u[e];
+        }
+        finish(p, m, n, v, bias);
+    }
+}
+
+// --------------------------------------------------------------------------------------------------- few tokens
+// Up to 32 tokens, the weights along the contraction: they are read once, 16 bytes a lane straight from memory into matrix instructions of
+// 16 channels x 16 tokens (v_mfma_f32_16x16x32_bf16: lane l supplies A[l % 16][8*(l/16) .. +7] and B[8*(l/16) .. +7][l % 16] and receives
+// D[4*(l/16) + r][l % 16]; v_mfma_f32_16x16x4_f32: one value of a lane's 16 bytes an instruction).  A block takes 16 channels, each of its
+// eight wavefronts an eighth of the contraction; the eighths are added in LDS in their order.  Rows may begin at any address; the last
+// chunks of a row, those that would reach behind it, are loaded value by value.
+constexpr int FEW_WAVES = 8;
+struct FewArgs { LinearProduct p; int64_t x_row, x_step; int per_wave; };       // per_wave: bytes, a multiple of 64
+
+template <class E> __device__ __forceinline__ i32x4 load_any(const char* p)
+{
+    if constexpr (sizeof(E) == 2) return __builtin_bit_cast(i32x4, *(const u32x4_2*)p);
+    else return __builtin_bit_cast(i32x4, *(const f32x4_4*)p);
+}
+// `there` values (0 .. 16 / sizeof(E)), `step` values apart, zeros behind them
+template <class E> __device__ __forceinline__ i32x4 load_some(const char* p, int there, int64_t step)
+{
+    i32x4 v;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(E) == 2) {
+            const unsigned short* u = (const unsigned short*)p;
+            const unsigned lo = 2 * i < there ? u[2 * i * step] : 0u, hi = 2 * i + 1 < there ? u[(2 * i + 1) * step] : 0u;
+            v[i] = (int)(lo | hi << 16);
+        } else v[i] = i < there ? ((const int*)p)[i * step] : 0;
+    }
+    return v;
+}
+template <class E> __device__ __forceinline__ f32x4 mfma16(i32x4 a, i32x4 b, f32x4 c)
+{
+    if constexpr (sizeof(E) == 2) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+    else {
+        const f32x4 u = __builtin_bit_cast(f32x4, a), v = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_16x16x4f32(u[j], v[j], c, 0, 0, 0);
+        return c;
+    }
+}
+
+template <class E, int NT> __global__ __launch_bounds__(FEW_WAVES * 64) void k_linear_few(const FewArgs f)
+{
+    constexpr int ES = sizeof(E), AHEAD = 4;
+    __shared__ __align__(16) float part[FEW_WAVES * NT * 256];
+    const LinearProduct& p = f.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t n0 = (int64_t)blockIdx.x * 16;
+    const int64_t end = p.k * ES, whole = end / 64 * 64;
+    const int64_t from = (int64_t)wave * f.per_wave, to = std::min(from + f.per_wave, end), to_whole = std::min(to, whole);
+    const int64_t off = (lane >> 4) * 16;
+    const char* w = (const char*)p.b.p + std::min(n0 + (lane & 15), p.n - 1) * p.b.pitch * ES + off;      // (what is beyond the channels or the tokens is not used)
+    const char* x[NT];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) x[t] = (const char*)p.a.p + std::min<int64_t>(t * 16 + (lane & 15), p.m - 1) * f.x_row * ES + off * f.x_step;
+    f32x4 acc[NT] = {};
+    int64_t k = from;
+    if (f.x_step == 1) {
+        for (; k + AHEAD * 64 <= to_whole; k += AHEAD * 64) {
+            i32x4 a[AHEAD], b[AHEAD][NT];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                a[u] = load_any<E>(w + k + u * 64);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) b[u][t] = load_any<E>(x[t] + k + u * 64);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u)
+#pragma unroll
+                for (int t = 0; t < NT; ++t) acc[t] = mfma16<E>(a[u], b[u][t], acc[t]);
+        }
+        for (; k < to_whole; k += 64) {
+            const i32x4 a = load_any<E>(w + k);
+#pragma unroll
+            for (int t = 0; t < NT; ++t) acc[t] = mfma16<E>(a, load_any<E>(x[t] + k), acc[t]);
+        }
+    }
+    for (; k < to; k += 64) {      // the end of the rows, or tokens that lie across memory
+        const int there = (int)std::max<int64_t>(0, std::min<int64_t>(16, end - k - off)) / ES;
+        const i32x4 a = there == 16 / ES ? load_any<E>(w + k) : load_some<E>(w + k, there, 1);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) acc[t] = mfma16<E>(a, load_some<E>(x[t] + k * f.x_step, there, f.x_step), acc[t]);
+    }
+#pragma unroll
+    for (int t = 0; t < NT; ++t) *(f32x4*)(part + (wave * NT + t) * 256 + (lane & 15) * 16 + (lane >> 4) * 4) = acc[t];
+    __syncthreads();
+    for (int i = threadIdx.x; i < NT * 256; i += FEW_WAVES * 64) {
+        const int64_t m = i >> 4, n = n0 + (i & 15);
+        if (m >= p.m || n >= p.n) continue;
+        float v[1] = {0.f}, bias[1];
+        bias_of(p, n, bias);
+#pragma unroll
+        for (int u = 0; u < FEW_WAVES; ++u) v[0] += part[u * NT * 256 + i];
+        finish(p, m, n, v, bias);
+    }
+}
+
+bool linear_few(int64_t m, int64_t n, int64_t k, int is_bf16)
+{
+    (void)n; (void)k; (void)is_bf16;
+    return m <= 32;
+}
+template <class E> static void few_launch(Ctx& c, const FewArgs& f)
+{
+    const dim3 grid((unsigned)ceil_div(f.p.n, 16));
+    if (f.p.m <= 16) ST_LAUNCH(c, "linear_few", (k_linear_few<E, 1>), grid, dim3(FEW_WAVES * 64), 0, f);
+    else ST_LAUNCH(c, "linear_few", (k_linear_few<E, 2>), grid, dim3(FEW_WAVES * 64), 0, f);
+}
+void linear_product_few(Ctx& c, const LinearProduct& p, int is_bf16)
+{
+    const int64_t es = is_bf16 ? 2 : 4;
+    const FewArgs f{p, p.a.along ? p.a.pitch : 1, p.a.along ? 1 : p.a.pitch, (int)round_up(ceil_div(p.k * es, FEW_WAVES), 64)};
+    if (is_bf16) few_launch<bf16>(c, f); else few_launch<float>(c, f);
+}
+
+// --------------------------------------------------------------------------------------- choice of tile and split
+static int64_t tiles_of(const Extent& e, int tile) { return ceil_div(e.m, tile) * ceil_div(e.n, tile); }
+LinearForm linear_form(const Extent* e, int count, int is_bf16)
+{
+    const int64_t per_stage = is_bf16 ? STAGE / 2 : STAGE / 4;
+    auto total = [&](int tile) { int64_t t = 0; for (int i = 0; i < count; ++i) t += tiles_of(e[i], tile); return t; };
+    auto stages_of = [&](int tile) { int64_t w = 0; for (int i = 0; i < count; ++i) w += tiles_of(e[i], tile) * ceil_div(e[i].k, per_stage); return w; };
+    LinearForm f = {64, {1, 1}};
+    if (total(256) >= 192 && stages_of(256) > 5 * total(256)) f.tile = 256;
+    else if (total(64) > 512) f.tile = 128;
+    // every block about the same number of stages, 256 blocks, eight stages each at least
+    const int64_t each = std::max<int64_t>(8, ceil_div(stages_of(f.tile), 256));
+    for (int i = 0; i < count; ++i) {
+        const int64_t stages = ceil_div(e[i].k, per_stage);
+        int64_t s = stages > 16 ? stages / each : 1;
+        if (count > 1 && f.tile == 128 && s == 1 && stages >= each + 20) s = 2;
+        f.splits[i] = (int)std::max<int64_t>(s, 1);
+    }
+    return f;
+}
+
+template <class E, int BM, int BN, int WM, int WN, int DEPTH>
+static void launch(Ctx& c, const GemmPair& g)
+{
+    constexpr size_t lds = (size_t)DEPTH * (BM + BN) * STAGE;
+    constexpr int threads = (BM / WM) * (BN / WN) * 64;
+    ensure_dynamic_lds((const void*)k_linear_product<E, BM, BN, WM, WN, DEPTH>, lds);
+    constexpr const char* name = BM == 256 ? "linear_product_256" : BM == 64 ? "linear_product_64" : DEPTH > 2 ? "linear_product_128_deep" : "linear_product_128";
+    const unsigned grid = g.g[0].blocks + g.g[1].blocks + (unsigned)ceil_div(g.sums.n, threads);
+    ST_LAUNCH(c, name, (k_linear_product<E, BM, BN, WM, WN, DEPTH>), dim3(grid), dim3(threads), lds, g);
+}
+template <class E> static void launch_tile(Ctx& c, const GemmPair& g, int tile)
+{
+    if (tile == 256) launch<E, 256, 256, 128, 64, 2>(c, g);
+    else if (tile == 128 && g.g[0].blocks + g.g[1].blocks <= 256) launch<E, 128, 128, 64, 32, 4>(c, g);
+    else if (tile == 128) launch<E, 128, 128, 64, 32, 2>(c, g);
+    else launch<E, 64, 64, 32, 32, 4>(c, g);
+}
+
+void linear_products(Ctx& c, const LinearProduct* p, int count, int is_bf16, const ColumnSums& sums)
+{
+    if (count == 0 && sums.n == 0) return;
+    Extent e[2];
+    for (int i = 0; i < count; ++i) e[i] = {p[i].m, p[i].n, p[i].k};
+    const LinearForm f = linear_form(e, count, is_bf16);
+    GemmPair g{}, joined{};
+    g.sums = sums;
+    int n_joined = 0;
+    int64_t runs[2] = {0, 0};
+    for (int i = 0; i < count; ++i) {
+        const int64_t tm = ceil_div(p[i].m, f.tile), tn = ceil_div(p[i].n, f.tile);
+        g.g[i] = GemmArgs{p[i], fast_div((int)(tm * tn)), fast_div((int)(tn * BAND)), (int)tm, f.splits[i],
+                          (int)ceil_div(p[i].k * (is_bf16 ? 2 : 4), STAGE), (unsigned)(tm * tn * f.splits[i])};
+        if (f.splits[i] > 1) { runs[n_joined] = p[i].m * ceil_div(p[i].n, 8); joined.g[n_joined++] = g.g[i]; }
+    }
+    if (is_bf16) launch_tile<bf16>(c, g, f.tile); else launch_tile<float>(c, g, f.tile);
+    if (n_joined) {
+        const int64_t all = runs[0] + runs[1], blocks = ceil_div(all, 256);
+        ST_LAUNCH(c, "linear_join", k_linear_join, dim3((unsigned)(blocks > 8192 ? 8192 : blocks)), dim3(256), 0, joined, runs[0], all);
+    }
+}
+
+}  // namespace st

@@ -1,0 +1,209 @@
+// Operands of the dense layers' products that have to be made: copies of matrices whose addresses, strides or lengths the products' 16-byte
+// loads do not take, and dz = dy act'(z) with the sums of its columns.
+#include "st_linear.hpp"
+#include "st_quantize.hpp"
+
+#include <algorithm>
+
+namespace st {
+
+// ------------------------------------------------------------------------------------------------------ copies
+// Eight values a thread along memory, 64 runs of 64 values a block.  `turn`: through LDS, the other way round.
+struct PackArgs { PackTask t[PACK_TASKS]; unsigned first[PACK_TASKS + 1], across[PACK_TASKS]; int count; };      // first block of each; blocks along a run
+
+template <class E> __global__ __launch_bounds__(256) void k_linear_pack(const PackArgs a)
+{
+    __shared__ E turned[64][64 + 16 / sizeof(E)];
+    int i = 0;
+    while (i + 1 < a.count && blockIdx.x >= a.first[i + 1]) ++i;
+    const PackTask& t = a.t[i];
+    const unsigned block = blockIdx.x - a.first[i];
+    const int64_t o0 = (int64_t)(block / a.across[i]) * 64, i0 = (int64_t)(block % a.across[i]) * 64;
+    const int run = threadIdx.x & 7, row = threadIdx.x >> 3;
+    Raw8<E> v[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t o = std::min(o0 + h * 32 + row, t.outer - 1), at = i0 + run * 8;
+        const E* x = (const E*)t.x + o * t.pitch;
+        if (t.inner < 8) v[h].load_short(x + at, at < t.inner ? (int)(t.inner - at) : 0);
+        else {
+            v[h].load(x + run_start<8, int64_t>(at, t.inner));
+            const int64_t d = at - (t.inner - 8);
+            if (d > 0) v[h].down(d < 8 ? (int)d : 8);
+        }
+    }
+    typedef E E8 __attribute__((ext_vector_type(8)));
+    E* const to = (E*)t.to;
+    if (!t.turn) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t o = o0 + h * 32 + row, at = i0 + run * 8;
+            if (o >= t.outer || at >= t.to_pitch) continue;
+            E8 u;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = from_f32<E>(v[h][e]);
+            *(E8*)(to + o * t.to_pitch + at) = u;      // (pitches are multiples of eight)
+        }
+        return;
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) turned[run * 8 + e][h * 32 + row] = o0 + h * 32 + row < t.outer ? from_f32<E>(v[h][e]) : from_f32<E>(0.f);
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t i1 = i0 + h * 32 + row, at = o0 + run * 8;
+        if (i1 >= t.inner || at >= t.to_pitch) continue;
+        E8 u;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) u[e] = turned[h * 32 + row][run * 8 + e];
+        *(E8*)(to + i1 * t.to_pitch + at) = u;
+    }
+}
+
+void linear_pack(Ctx& c, const PackTask* t, int count, int is_bf16)
+{
+    for (int done = 0; done < count;) {      // (a launch holds fewer than 2^32 threads)
+        PackArgs a{};
+        for (; done < count && (a.count == 0 || a.first[a.count] < (1 << 22)); ++done) {
+            const int i = a.count++;
+            a.t[i] = t[done];
+            a.across[i] = (unsigned)ceil_div(t[done].inner, 64);
+            a.first[i + 1] = a.first[i] + a.across[i] * (unsigned)ceil_div(t[done].outer, 64);
+        }
+        if (is_bf16) ST_LAUNCH(c, "linear_pack", k_linear_pack<bf16>, dim3(a.first[a.count]), dim3(256), 0, a);
+        else ST_LAUNCH(c, "linear_pack", k_linear_pack<float>, dim3(a.first[a.count]), dim3(256), 0, a);
+    }
+}
+
+template <class E> __global__ __launch_bounds__(256) void k_linear_fill_zero(E* __restrict__ p, int64_t rows, int64_t cols, int64_t pitch)
+{
+    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256) p[i / cols * pitch + i % cols] = from_f32<E>(0.f);
+}
+void linear_fill_zero(Ctx& c, void* p, int is_bf16, int64_t rows, int64_t cols, int64_t pitch)
+{
+    const dim3 grid((unsigned)std::min<int64_t>(ceil_div(rows * cols, 2048), 4096));
+    if (is_bf16) ST_LAUNCH(c, "linear_fill_zero", k_linear_fill_zero<bf16>, grid, dim3(256), 0, (bf16*)p, rows, cols, pitch);
+    else ST_LAUNCH(c, "linear_fill_zero", k_linear_fill_zero<float>, grid, dim3(256), 0, (float*)p, rows, cols, pitch);
+}
+
+// ------------------------------------------------------------------------------------------------------ dz
+// A block takes 64 columns and a part of the rows, 32 rows at a time: eight threads a row, eight values each.  What lies column by column
+// goes through LDS, 64 columns x 32 rows.  dz is rounded to the operands' type; the sums of its columns are of what it was before.
+struct SlopeArgs { SlopeTask t; unsigned across; int rows_each; };
+
+template <class T> __device__ __forceinline__ void load_rows(const GradSource& s, int64_t m0, int64_t m, int64_t n0, int64_t n, float (*turned)[33], float (&v)[8])
+{
+    const int run = threadIdx.x & 7, row = threadIdx.x >> 3;
+    if (s.along) {
+        const int64_t r = std::min(m0 + row, m - 1), at = n0 + run * 8;
+        const T* x = (const T*)s.x + r * s.pitch;
+        Raw8<T> u;
+        if (n < 8) u.load_short(x + at, at < n ? (int)(n - at) : 0);
+        else {
+            u.load(x + run_start<8, int64_t>(at, n));
+            const int64_t d = at - (n - 8);
+            if (d > 0) u.down(d < 8 ? (int)d : 8);
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = u[e];
+        return;
+    }
+    const int col = threadIdx.x >> 2, part = threadIdx.x & 3;      // 64 columns, eight rows of each a thread
+    const int64_t c = std::min(n0 + col, n - 1), at = m0 + part * 8;
+    const T* x = (const T*)s.x + c * s.pitch;
+    Raw8<T> u;
+    if (m < 8) u.load_short(x + at, at < m ? (int)(m - at) : 0);
+    else {
+        u.load(x + run_start<8, int64_t>(at, m));
+        const int64_t d = at - (m - 8);
+        if (d > 0) u.down(d < 8 ? (int)d : 8);
+    }
+    __syncthreads();      // (what was there has been read)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) turned[col][part * 8 + e] = u[e];
+    __syncthreads();
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = turned[run * 8 + e][row];
+}
+
+template <class E> __device__ __forceinline__ void store_dz(void* to, int64_t at, const float (&v)[8])
+{
+    typedef E E8 __attribute__((ext_vector_type(8)));
+    E8 u;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[e] = from_f32<E>(v[e]);
+    *(E8*)((E*)to + at) = u;
+}
+
+template <class T, class Z, int ACT> __device__ __forceinline__ void slope_rows(const SlopeArgs& a, float (*turned)[33], float (*sums)[64])
+{
+    const SlopeTask& t = a.t;
+    const int64_t n0 = (int64_t)(blockIdx.x % a.across) * 64, part = blockIdx.x / a.across;
+    const int64_t from = part * a.rows_each, to = std::min(from + a.rows_each, t.m);
+    const int run = threadIdx.x & 7, row = threadIdx.x >> 3;
+    float sum[8] = {};
+    for (int64_t m0 = from; m0 < to; m0 += 32) {
+        float v[8], z[8];
+        load_rows<T>(t.dy, m0, t.m, n0, t.n, turned, v);
+        if constexpr (ACT != ST_ACT_NONE) load_rows<Z>(t.pre, m0, t.m, n0, t.n, turned, z);
+        if (m0 + row >= to) continue;      // (the last turn of the loop)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            if constexpr (ACT != ST_ACT_NONE) v[e] = slope_times<ACT>(v[e], z[e]);
+            if (n0 + run * 8 + e >= t.n) v[e] = 0.f;
+            sum[e] += v[e];
+        }
+        if (t.to && n0 + run * 8 < t.to_pitch) {
+            const int64_t at = (m0 + row) * t.to_pitch + n0 + run * 8;
+            if (t.to_bf16) store_dz<bf16>(t.to, at, v); else store_dz<float>(t.to, at, v);
+        }
+    }
+    if (!t.parts) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sums[row][run * 8 + e] = sum[e];
+    __syncthreads();
+    if (threadIdx.x < 64 && n0 + threadIdx.x < t.n) {
+        float v = 0.f;
+#pragma unroll
+        for (int r = 0; r < 32; ++r) v += sums[r][threadIdx.x];
+        t.parts[part * t.n + n0 + threadIdx.x] = v;
+    }
+}
+
+template <class T, class Z> __global__ __launch_bounds__(256) void k_linear_slope(const SlopeArgs a)
+{
+    __shared__ float turned[64][33];
+    __shared__ float sums[32][64];
+    switch (a.t.act) {
+    case ST_ACT_RELU: slope_rows<T, Z, ST_ACT_RELU>(a, turned, sums); break;
+    case ST_ACT_GELU: slope_rows<T, Z, ST_ACT_GELU>(a, turned, sums); break;
+    case ST_ACT_GELU_TANH: slope_rows<T, Z, ST_ACT_GELU_TANH>(a, turned, sums); break;
+    case ST_ACT_SILU: slope_rows<T, Z, ST_ACT_SILU>(a, turned, sums); break;
+    default: slope_rows<T, Z, ST_ACT_NONE>(a, turned, sums); break;
+    }
+}
+
+// parts of the rows: about four blocks a compute unit, 32 rows at least
+static int slope_rows_each(int64_t m, int64_t n)
+{
+    const int64_t parts = std::max<int64_t>(1, 1024 / ceil_div(n, 64));
+    return (int)round_up(std::max<int64_t>(32, ceil_div(m, parts)), 32);
+}
+int linear_slope_parts(int64_t m, int64_t n) { return (int)ceil_div(m, slope_rows_each(m, n)); }
+
+void linear_slope(Ctx& c, const SlopeTask& t)
+{
+    const SlopeArgs a{t, (unsigned)ceil_div(t.n, 64), slope_rows_each(t.m, t.n)};
+    const dim3 grid(a.across * (unsigned)linear_slope_parts(t.m, t.n));
+    if (t.dy.bf16) {
+        if (t.pre.bf16) ST_LAUNCH(c, "linear_slope", (k_linear_slope<bf16, bf16>), grid, dim3(256), 0, a);
+        else ST_LAUNCH(c, "linear_slope", (k_linear_slope<bf16, float>), grid, dim3(256), 0, a);
+    } else {
+        if (t.pre.bf16) ST_LAUNCH(c, "linear_slope", (k_linear_slope<float, bf16>), grid, dim3(256), 0, a);
+        else ST_LAUNCH(c, "linear_slope", (k_linear_slope<float, float>), grid, dim3(256), 0, a);
+    }
+}
+
+}  // namespace st

@@ -1,0 +1,324 @@
+// C entry points of the dense layers in bfloat16 or float32 and of the clipping of gradients: validation, workspace layout, order of the launches.
+#include "st_clip.hpp"
+#include "st_linear.hpp"
+
+#include <math.h>
+#include <algorithm>
+
+namespace st {
+namespace {
+
+// A launch holds fewer than 2^32 threads and 2^23 tiles.
+constexpr int64_t MAX_TOKENS = (1 << 24) - 1, MAX_CHANNELS = ST_LINEAR_MAX_CHANNELS, MAX_VALUES = (int64_t)1 << 33, MAX_STRIDE = (int64_t)1 << 40;
+
+struct Carve {      // 256-byte aligned pieces of a workspace
+    char* base; size_t used = 0;
+    void* take(size_t bytes) { void* p = base + used; used += (bytes + 255) / 256 * 256; return p; }
+};
+bool dtype_ok(int32_t d) { return d == ST_F32 || d == ST_BF16; }
+int elem(int32_t d) { return d == ST_BF16 ? 2 : 4; }
+bool is_aligned(const void* p, size_t to) { return (uintptr_t)p % to == 0; }
+bool tiles_ok(int64_t a, int64_t b) { return ceil_div(a, 64) * ceil_div(b, 64) < (1 << 23); }
+bool sizes_ok(int64_t m, int64_t n, int64_t k)
+{
+    return m >= 0 && m <= MAX_TOKENS && n >= 1 && n <= MAX_CHANNELS && k >= 1 && k <= MAX_CHANNELS && tiles_ok(m, n) && tiles_ok(m, k) && tiles_ok(n, k);
+}
+
+// Whether the matrix can be read, and whether its rows lie along memory (*along).
+int check(const st_matrix* x, int64_t rows, int64_t cols, int* along)
+{
+    if (!x) return ST_ERR_NULL;
+    if (x->rows != rows || x->cols != cols) return ST_ERR_SHAPE;
+    if (!dtype_ok(x->dtype)) return ST_ERR_ARG;
+    if (rows > 0 && !x->data) return ST_ERR_NULL;
+    if (!is_aligned(x->data, elem(x->dtype))) return ST_ERR_ARG;
+    if (x->row_stride < 0 || x->col_stride < 0 || x->row_stride > MAX_STRIDE || x->col_stride > MAX_STRIDE) return ST_ERR_SHAPE;
+    if (x->col_stride == 1 || cols == 1) *along = 1;
+    else if (x->row_stride == 1 || rows <= 1) *along = 0;
+    else return ST_ERR_SHAPE;
+    return ST_OK;
+}
+
+// An operand whose rows are x's rows (by_rows) or its columns: as it lies, or where the products cannot read it so, a copy that `pack`
+// (with room in `w`) makes.  The copy lies as x does, unless only the other order keeps a tile's offsets small.
+struct Packs { PackTask t[PACK_TASKS]; int n = 0; };
+Operand operand_of(const st_matrix& x, int along, bool by_rows, Carve& w, Packs* packs)
+{
+    const int es = elem(x.dtype);
+    const int64_t outer = along ? x.rows : x.cols, inner = along ? x.cols : x.rows;
+    // (where there is one run, or runs of one value, the step between them is whatever the caller has there)
+    const int64_t pitch = outer > 1 ? (along ? x.row_stride : x.col_stride) : round_up(inner, 16 / es);
+    const int k_along = along == (by_rows ? 1 : 0);      // the operand's rows lie along memory
+    if (operand_direct(x.data, pitch, k_along, inner, es)) return Operand{x.data, pitch, k_along};
+    const bool turn = !operand_direct(nullptr, round_up(inner, 8), k_along, round_up(inner, 8), es);
+    const int64_t to_pitch = round_up(turn ? outer : inner, 8);
+    void* to = w.take((size_t)(turn ? inner : outer) * to_pitch * es);
+    if (packs) packs->t[packs->n++] = PackTask{x.data, outer, inner, pitch, to, to_pitch, turn};
+    return Operand{to, to_pitch, turn ? !k_along : k_along};
+}
+size_t slab_bytes(const Extent* e, int count, int which, int is_bf16)
+{
+    const LinearForm f = linear_form(e, count, is_bf16);
+    return f.splits[which] > 1 ? (size_t)f.splits[which] * e[which].m * e[which].n * 4 : 0;
+}
+bool products_ok(const Extent* e, int count, int is_bf16)
+{
+    const LinearForm f = linear_form(e, count, is_bf16);
+    int64_t blocks = 0;
+    for (int i = 0; i < count; ++i) blocks += ceil_div(e[i].m, f.tile) * ceil_div(e[i].n, f.tile) * f.splits[i];
+    return blocks < (1 << 23) - 8192;      // (and the blocks of the columns' sums)
+}
+
+// The forward pass, planned: `ws` null for its size alone.
+struct LinearPlan { LinearProduct p; Packs packs; bool few; size_t bytes; };
+LinearPlan plan_linear(const st_matrix& x, int x_along, const st_matrix& w, int w_along, char* ws)
+{
+    LinearPlan l{};
+    LinearProduct& p = l.p;
+    p.m = x.rows; p.n = w.rows; p.k = x.cols;
+    const int is_bf16 = x.dtype == ST_BF16;
+    Carve c{ws};
+    l.few = w_along && linear_few(p.m, p.n, p.k, is_bf16);
+    if (l.few) {
+        p.a = Operand{x.data, x_along ? x.row_stride : x.col_stride, x_along};
+        p.b = Operand{w.data, w.row_stride, 1};
+    } else {
+        p.a = operand_of(x, x_along, true, c, &l.packs);
+        p.b = operand_of(w, w_along, true, c, &l.packs);
+        const Extent e{p.m, p.n, p.k};
+        p.slabs = (float*)c.take(p.m ? slab_bytes(&e, 1, 0, is_bf16) : 0);
+    }
+    l.bytes = c.used + 256;
+    return l;
+}
+
+// The backward pass, planned the same way for the outputs that are asked for.
+struct BackwardPlan { LinearProduct p[2]; int n_products; Packs packs; SlopeTask slope; bool slopes; ColumnSums sums; size_t bytes; };
+BackwardPlan plan_backward(const st_matrix* x, int x_along, const st_matrix* w, int w_along, const st_matrix& dy, int dy_along, int act,
+                           int dtype, bool db, char* ws)
+{
+    BackwardPlan b{};
+    Carve c{ws};
+    const int64_t m = dy.rows, n = dy.cols;
+    const int is_bf16 = dtype == ST_BF16;
+    Operand by_tokens{}, by_channels{};      // dz for dx, and for dw
+    const bool as_it_is = act == ST_ACT_NONE && dy.dtype == dtype;
+    SlopeTask& s = b.slope;
+    s.dy = GradSource{dy.data, dy.dtype == ST_BF16, dy_along ? dy.row_stride : dy.col_stride, dy_along};
+    s.act = act; s.m = m; s.n = n; s.to_bf16 = is_bf16;
+    b.slopes = db || ((x || w) && !as_it_is);
+    if (b.slopes && (x || w) && !as_it_is) {
+        s.to_pitch = round_up(n, 8);
+        s.to = c.take((size_t)m * s.to_pitch * elem(dtype));
+        by_tokens = Operand{s.to, s.to_pitch, 1};
+        by_channels = Operand{s.to, s.to_pitch, 0};
+    } else {
+        if (w) by_tokens = operand_of(dy, dy_along, true, c, &b.packs);
+        // the same matrix read the other way round, if it can be (the rows of a copy end in zeros)
+        const bool copied = w && by_tokens.p != dy.data;
+        const int64_t pitch = by_tokens.pitch;
+        if (w && operand_direct(by_tokens.p, pitch, !by_tokens.along, by_tokens.along ? n : copied ? round_up(m, 8) : m, elem(dtype)))
+            by_channels = Operand{by_tokens.p, pitch, !by_tokens.along};
+        else if (x) by_channels = operand_of(dy, dy_along, false, c, &b.packs);
+    }
+    if (db) {
+        s.parts = (float*)c.take((size_t)linear_slope_parts(m, n) * n * 4);
+        b.sums = ColumnSums{s.parts, linear_slope_parts(m, n), n, nullptr, 0};
+    }
+    Extent e[2];
+    if (x) {
+        LinearProduct& p = b.p[b.n_products];
+        p.m = n; p.n = x->cols; p.k = m;
+        p.a = by_channels;
+        p.b = operand_of(*x, x_along, false, c, &b.packs);
+        e[b.n_products++] = Extent{p.m, p.n, p.k};
+    }
+    if (w) {
+        LinearProduct& p = b.p[b.n_products];
+        p.m = m; p.n = w->cols; p.k = n;
+        p.a = by_tokens;
+        p.b = operand_of(*w, w_along, false, c, &b.packs);
+        e[b.n_products++] = Extent{p.m, p.n, p.k};
+    }
+    for (int i = 0; i < b.n_products; ++i) b.p[i].slabs = (float*)c.take(slab_bytes(e, b.n_products, i, is_bf16));
+    b.bytes = c.used + 256;
+    return b;
+}
+
+}  // namespace
+}  // namespace st
+
+using namespace st;
+
+extern "C" {
+
+static int check_linear(const st_matrix* x, const st_matrix* w, int* x_along, int* w_along)
+{
+    if (!x || !w) return ST_ERR_NULL;
+    const Extent e{std::max<int64_t>(x->rows, 1), w->rows, x->cols};
+    if (!sizes_ok(x->rows, w->rows, x->cols) || !products_ok(&e, 1, x->dtype == ST_BF16)) return ST_ERR_SHAPE;
+    if (const int v = check(x, x->rows, x->cols, x_along)) return v;
+    if (const int v = check(w, w->rows, x->cols, w_along)) return v;
+    return x->dtype == w->dtype ? ST_OK : ST_ERR_ARG;
+}
+
+size_t st_linear_workspace(const st_matrix* x, const st_matrix* w)
+{
+    int x_along = 1, w_along = 1;
+    if (check_linear(x, w, &x_along, &w_along) != ST_OK) return 0;
+    return x->rows ? plan_linear(*x, x_along, *w, w_along, nullptr).bytes : 256;
+}
+
+int st_linear(const st_matrix* x, const st_matrix* w, const st_linear_opts* opts, void* y, int32_t y_dtype, int64_t y_pitch,
+              void* workspace, size_t workspace_bytes, void* stream)
+{
+    int x_along = 1, w_along = 1;
+    if (const int v = check_linear(x, w, &x_along, &w_along)) return v;
+    const st_linear_opts none{}, &o = opts ? *opts : none;
+    const int64_t n = w->rows;
+    if (y_pitch < n || (o.residual && o.residual_pitch < n) || (o.pre && o.pre_pitch < n)) return ST_ERR_SHAPE;
+    if (!dtype_ok(y_dtype) || o.activation < ST_ACT_NONE || o.activation > ST_ACT_SILU || (o.residual && !dtype_ok(o.residual_dtype))
+        || (o.pre && !dtype_ok(o.pre_dtype)))
+        return ST_ERR_ARG;
+    if (x->rows == 0) return ST_OK;
+    if (!y) return ST_ERR_NULL;
+    if (!is_aligned(y, elem(y_dtype)) || !is_aligned(o.bias, 4) || (o.residual && !is_aligned(o.residual, elem(o.residual_dtype)))
+        || (o.pre && !is_aligned(o.pre, elem(o.pre_dtype))))
+        return ST_ERR_ARG;
+    if (o.residual == y && (o.residual_dtype != y_dtype || o.residual_pitch != y_pitch)) return ST_ERR_ARG;
+    LinearPlan l = plan_linear(*x, x_along, *w, w_along, (char*)workspace);
+    if (l.bytes > 256 && (!workspace || !is_aligned(workspace, 256) || workspace_bytes < l.bytes)) return ST_ERR_WORKSPACE;
+    LinearProduct& p = l.p;
+    p.out = y; p.out_bf16 = y_dtype == ST_BF16; p.out_pitch = y_pitch;
+    p.bias = o.bias; p.act = o.activation;
+    p.residual = o.residual; p.residual_bf16 = o.residual_dtype == ST_BF16; p.residual_pitch = o.residual_pitch;
+    p.pre = o.pre; p.pre_bf16 = o.pre_dtype == ST_BF16; p.pre_pitch = o.pre_pitch;
+    const int is_bf16 = x->dtype == ST_BF16;
+    Ctx c{(hipStream_t)stream, ST_OK};
+    if (l.few) { linear_product_few(c, p, is_bf16); return c.status; }
+    linear_pack(c, l.packs.t, l.packs.n, is_bf16);
+    linear_products(c, &p, 1, is_bf16, ColumnSums{});
+    return c.status;
+}
+
+// x and w: those that the gradients asked for need, or null
+static int check_backward(const st_matrix* x, const st_matrix* w, const st_matrix* dy, int32_t act, int* x_along, int* w_along, int* dy_along)
+{
+    if (!dy) return ST_ERR_NULL;
+    const int64_t m = dy->rows, n = dy->cols, k = w ? w->cols : x ? x->cols : 1;
+    if (!sizes_ok(m, n, k)) return ST_ERR_SHAPE;
+    if (act < ST_ACT_NONE || act > ST_ACT_SILU) return ST_ERR_ARG;
+    if (const int v = check(dy, m, n, dy_along)) return v;
+    if (x) if (const int v = check(x, m, k, x_along)) return v;
+    if (w) if (const int v = check(w, n, k, w_along)) return v;
+    if (x && w && x->dtype != w->dtype) return ST_ERR_ARG;
+    const int is_bf16 = x ? x->dtype == ST_BF16 : w && w->dtype == ST_BF16;
+    const Extent e[2] = {{n, k, std::max<int64_t>(m, 1)}, {std::max<int64_t>(m, 1), k, n}};
+    if (!products_ok(e, 2, is_bf16) || !products_ok(e, 1, is_bf16) || !products_ok(e + 1, 1, is_bf16)) return ST_ERR_SHAPE;
+    return ST_OK;
+}
+
+size_t st_linear_backward_workspace(const st_matrix* x, const st_matrix* w, const st_matrix* dy, int32_t activation)
+{
+    int x_along = 1, w_along = 1, dy_along = 1;
+    if (check_backward(x, w, dy, activation, &x_along, &w_along, &dy_along) != ST_OK) return 0;
+    if (dy->rows == 0) return 256;
+    const int dtype = x ? x->dtype : w ? w->dtype : dy->dtype;
+    size_t most = 0;      // whichever of the gradients are asked for
+    for (int which = 0; which < 4; ++which)
+        most = std::max(most, plan_backward(which & 1 ? x : nullptr, x_along, which & 2 ? w : nullptr, w_along, *dy, dy_along, activation, dtype,
+                                            true, nullptr).bytes);
+    return most;
+}
+
+int st_linear_backward(const st_matrix* x, const st_matrix* w, const st_matrix* dy, const st_matrix* pre, int32_t activation,
+                       const st_linear_grads* grads, void* workspace, size_t workspace_bytes, void* stream)
+{
+    if (!grads) return ST_ERR_NULL;
+    const st_linear_grads& o = *grads;
+    if ((o.dx && !w) || (o.dw && !x)) return ST_ERR_NULL;
+    if (!o.dx) w = nullptr;
+    if (!o.dw) x = nullptr;
+    int x_along = 1, w_along = 1, dy_along = 1, pre_along = 1;
+    if (const int v = check_backward(x, w, dy, activation, &x_along, &w_along, &dy_along)) return v;
+    const int64_t m = dy->rows, n = dy->cols, k = w ? w->cols : x ? x->cols : 1;
+    if (activation != ST_ACT_NONE) if (const int v = check(pre, m, n, &pre_along)) return v;
+    if ((o.dx && o.dx_pitch < k) || (o.dw && o.dw_pitch < k)) return ST_ERR_SHAPE;
+    if ((o.dx && !dtype_ok(o.dx_dtype)) || (o.dw && !dtype_ok(o.dw_dtype)) || (o.accumulate != 0 && o.accumulate != 1)) return ST_ERR_ARG;
+    if ((o.dx && !is_aligned(o.dx, elem(o.dx_dtype))) || (o.dw && !is_aligned(o.dw, elem(o.dw_dtype))) || !is_aligned(o.db, 4)) return ST_ERR_ARG;
+    if (!o.dx && !o.dw && !o.db) return ST_OK;
+    Ctx c{(hipStream_t)stream, ST_OK};
+    if (m == 0) {
+        if (o.accumulate) return ST_OK;
+        if (o.dw) linear_fill_zero(c, o.dw, o.dw_dtype == ST_BF16, n, k, o.dw_pitch);
+        if (o.db) linear_fill_zero(c, o.db, 0, 1, n, n);
+        return c.status;
+    }
+    const int dtype = x ? x->dtype : w ? w->dtype : dy->dtype;
+    BackwardPlan b = plan_backward(x, x_along, w, w_along, *dy, dy_along, activation, dtype, o.db != nullptr, (char*)workspace);
+    if (b.bytes > 256 && (!workspace || !is_aligned(workspace, 256) || workspace_bytes < b.bytes)) return ST_ERR_WORKSPACE;
+    if (activation != ST_ACT_NONE) b.slope.pre = GradSource{pre->data, pre->dtype == ST_BF16, pre_along ? pre->row_stride : pre->col_stride, pre_along};
+    b.sums.out = o.db; b.sums.accumulate = o.accumulate;
+    int at = 0;
+    if (x) {
+        LinearProduct& p = b.p[at++];
+        p.out = o.dw; p.out_bf16 = o.dw_dtype == ST_BF16; p.out_pitch = o.dw_pitch;
+        if (o.accumulate) { p.residual = o.dw; p.residual_bf16 = p.out_bf16; p.residual_pitch = o.dw_pitch; }
+    }
+    if (w) {
+        LinearProduct& p = b.p[at++];
+        p.out = o.dx; p.out_bf16 = o.dx_dtype == ST_BF16; p.out_pitch = o.dx_pitch;
+    }
+    if (b.slopes) linear_slope(c, b.slope);
+    linear_pack(c, b.packs.t, b.packs.n, dtype == ST_BF16);
+    linear_products(c, b.p, b.n_products, dtype == ST_BF16, b.sums);
+    return c.status;
+}
+
+static int check_grads(const st_grad_tensor* t, int32_t n)
+{
+    if (n < 0 || n > ST_GRAD_MAX_TENSORS) return ST_ERR_SHAPE;
+    if (n && !t) return ST_ERR_NULL;
+    int64_t all = 0;
+    for (int i = 0; i < n; ++i) {
+        if (t[i].n < 0 || t[i].n > MAX_VALUES) return ST_ERR_SHAPE;
+        all += t[i].n;
+        if (all > MAX_VALUES) return ST_ERR_SHAPE;
+    }
+    return ST_OK;
+}
+
+size_t st_grad_clip_workspace(const st_grad_tensor* tensors, int32_t n_tensors)
+{
+    if (check_grads(tensors, n_tensors) != ST_OK) return 0;
+    return 256 + (size_t)clip_parts(tensors, n_tensors) * sizeof(double);
+}
+
+int st_grad_clip(const st_grad_tensor* tensors, int32_t n_tensors, double grad_scale, double max_norm, float* grad_norm, void* workspace, void* stream)
+{
+    if (const int v = check_grads(tensors, n_tensors)) return v;
+    if (!((float)grad_scale > 0) || !isfinite((float)grad_scale) || !(max_norm >= 0) || !isfinite((float)max_norm)
+        || (max_norm > 0 && !((float)max_norm > 0)) || !is_aligned(grad_norm, 4))
+        return ST_ERR_ARG;
+    int with = 0, without = 0;
+    for (int i = 0; i < n_tensors; ++i) {
+        const st_grad_tensor& t = tensors[i];
+        if (!dtype_ok(t.grad_dtype) || (t.out && !dtype_ok(t.out_dtype))) return ST_ERR_ARG;
+        if (t.n == 0) continue;
+        if (!t.grad) return ST_ERR_NULL;
+        if (!is_aligned(t.grad, elem(t.grad_dtype)) || (t.out && !is_aligned(t.out, elem(t.out_dtype)))) return ST_ERR_ARG;
+        ++(t.out ? with : without);
+        if (t.out) {      // in place, or apart
+            const uintptr_t g = (uintptr_t)t.grad, o = (uintptr_t)t.out;
+            if (g == o ? t.grad_dtype != t.out_dtype : g < o + t.n * elem(t.out_dtype) && o < g + t.n * elem(t.grad_dtype)) return ST_ERR_ARG;
+        }
+    }
+    if (with && without) return ST_ERR_NULL;
+    if (!with && !grad_norm) return ST_OK;
+    if (!workspace || !is_aligned(workspace, 256)) return ST_ERR_WORKSPACE;
+    Ctx c{(hipStream_t)stream, ST_OK};
+    grad_clip(c, tensors, n_tensors, ClipRule{grad_scale, max_norm, grad_norm, with > 0}, (double*)workspace);
+    return c.status;
+}
+
+}  // extern "C"
