@@ -14,7 +14,7 @@
 // chunk of sixteen consecutive rows read sixteen different groups of four banks.
 // Across: a position k of the contraction takes the tile's rows, R values next to each other.  bfloat16: ds_read_b64_tr_b16 turns 4 x 16
 // values in a group of sixteen lanes: lane j gives the address of four rows' values, 4*(j%4) .., of position j/4, and gets the four positions'
-// values of row j.  The 64 bytes that a position gives are moved by k % 4 times 64 bytes (R = 64: by 64 bytes where k / 2 is odd), so
+// values of row j.  The 64 bytes that a position gives are moved by k % 4 times 64 bytes (R = 64: by 64 bytes where k / 2 is odd; R = 32: not), so
 // that four positions of 32 rows meet no bank twice.  float32: 32 lanes read 32 rows' values at one position, the two halves of a wavefront four
 // positions apart, moved by 128 bytes.
 #include "st_linear.hpp"
@@ -181,7 +181,8 @@ template <class E, int R, int WAVES, int N> struct Tile<E, false, R, WAVES, N> {
     unsigned v, step, at[N];
     static __device__ __forceinline__ unsigned moved(unsigned position)      // by how many chunks
     {
-        if constexpr (ES == 4) return 8 * (position >> 2 & 1);
+        if constexpr (R == 32) return 0;
+        else if constexpr (ES == 4) return 8 * (position >> 2 & 1);
         else if constexpr (R == 64) return 4 * (position >> 1 & 1);
         else return 4 * (position & 3);
     }
@@ -203,7 +204,7 @@ template <class E, int R, int WAVES, int N> struct Tile<E, false, R, WAVES, N> {
         } else {
 #pragma unroll
             for (int i = 0; i < N; ++i)
-                at[i] = 4 * half * R * 4 + (((first + i * 32 + (lane & 31)) / 4) ^ (8 * half)) * 16 + (lane & 3) * 4;
+                at[i] = 4 * half * R * 4 + (((first + i * 32 + (lane & 31)) / 4) ^ moved(4 * half)) * 16 + (lane & 3) * 4;
         }
     }
     __device__ __forceinline__ void load(int s, char* to, int wave) const
@@ -244,6 +245,23 @@ template <class E> __device__ __forceinline__ f32x16 mfma(i32x4 a, i32x4 b, f32x
         for (int j = 0; j < 4; ++j) c = __builtin_amdgcn_mfma_f32_32x32x2f32(u[j], v[j], c, 0, 0, 0);
         return c;
     }
+}
+
+// ------------------------------------------------------------------------------------------------- a block's place
+// An XCD gets a run of consecutive tiles, ordered in bands of four tiles of tokens: what its 32 compute units work on at a time is
+// 4 x 8 tiles, and less goes from memory to its L2 than with rows of tiles.
+struct Place { int second, split, tm, tn; };
+__device__ __forceinline__ Place place_of(const GemmPair& pair)
+{
+    const int second = blockIdx.x >= pair.g[0].blocks;
+    const GemmArgs& g = pair.g[second];
+    const int block = xcd_band((int)blockIdx.x - (second ? (int)pair.g[0].blocks : 0), (int)g.blocks);
+    const int split = __builtin_amdgcn_readfirstlane(fast_quot(block, g.by_tiles));
+    const int tile = block - split * (int)g.by_tiles.d;
+    const int band = __builtin_amdgcn_readfirstlane(fast_quot(tile, g.by_band)), in_band = tile - band * (int)g.by_band.d;
+    const int high = min(BAND, g.tiles_m - band * BAND);
+    const int tn = __builtin_amdgcn_readfirstlane(in_band / high);
+    return {second, split, band * BAND + in_band - tn * high, tn};
 }
 
 // ------------------------------------------------------------------------------------------------- a block's tile
@@ -352,32 +370,36 @@ __device__ __forceinline__ void product_tile(const GemmArgs& g, char* lds, int64
     }
 }
 
+// The parts of 32 columns: a column's parts are dealt out to THREADS / 32 threads, whose sums are added in their order.
+constexpr int SUM_COLUMNS = 32;
+template <int THREADS> __device__ __forceinline__ void sum_columns(const ColumnSums& s, unsigned block, float* lds)
+{
+    constexpr int GROUPS = THREADS / SUM_COLUMNS;
+    const int col = threadIdx.x % SUM_COLUMNS, group = threadIdx.x / SUM_COLUMNS;
+    const int64_t i = (int64_t)block * SUM_COLUMNS + col;
+    float v = 0.f;
+    if (i < s.n)
+#pragma unroll 8
+        for (int part = group; part < s.n_parts; part += GROUPS) v += s.parts[(int64_t)part * s.n + i];
+    lds[threadIdx.x] = v;
+    __syncthreads();
+    if (group || i >= s.n) return;
+    v = 0.f;
+#pragma unroll
+    for (int g = 0; g < GROUPS; ++g) v += lds[g * SUM_COLUMNS + col];
+    s.out[i] = s.accumulate ? s.out[i] + v : v;
+}
+
 template <class E, int BM, int BN, int WM, int WN, int DEPTH>
 __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_linear_product(const GemmPair pair)
 {
     extern __shared__ __align__(16) char lds[];
     const unsigned both = pair.g[0].blocks + pair.g[1].blocks;
-    if (blockIdx.x >= both) {      // columns' parts, a column a thread
-        const ColumnSums& s = pair.sums;
-        const int64_t i = (int64_t)(blockIdx.x - both) * blockDim.x + threadIdx.x;
-        if (i >= s.n) return;
-        float v = 0.f;
-#pragma unroll 4
-        for (int part = 0; part < s.n_parts; ++part) v += s.parts[(int64_t)part * s.n + i];
-        s.out[i] = s.accumulate ? s.out[i] + v : v;
-        return;
-    }
-    const bool second = blockIdx.x >= pair.g[0].blocks;
-    const GemmArgs& g = pair.g[second];
-    // An XCD gets a run of consecutive tiles, ordered in bands of four tiles of tokens: what its 32 compute units work on at a time is
-    // 4 x 8 tiles, and less goes from memory to its L2 than with rows of tiles.
-    const int block = xcd_band((int)blockIdx.x - (second ? (int)pair.g[0].blocks : 0), (int)g.blocks);
-    const int split = __builtin_amdgcn_readfirstlane(fast_quot(block, g.by_tiles));
-    const int tile = block - split * (int)g.by_tiles.d;
-    const int band = __builtin_amdgcn_readfirstlane(fast_quot(tile, g.by_band)), in_band = tile - band * (int)g.by_band.d;
-    const int high = min(BAND, g.tiles_m - band * BAND);
-    const int tn = __builtin_amdgcn_readfirstlane(in_band / high), tm = band * BAND + in_band - tn * high;
-    const int64_t m0 = (int64_t)tm * BM, n0 = (int64_t)tn * BN;
+    if (blockIdx.x >= both) { sum_columns<(BM / WM) * (BN / WN) * 64>(pair.sums, blockIdx.x - both, (float*)lds); return; }
+    const Place at = place_of(pair);
+    const GemmArgs& g = pair.g[at.second];
+    const int64_t m0 = (int64_t)at.tm * BM, n0 = (int64_t)at.tn * BN;
+    const int split = at.split;
     if (g.p.a.along) {
         if (g.p.b.along) product_tile<E, BM, BN, WM, WN, DEPTH, true, true>(g, lds, m0, n0, split);
         else product_tile<E, BM, BN, WM, WN, DEPTH, true, false>(g, lds, m0, n0, split);
@@ -387,22 +409,198 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_linear_product(c
     }
 }
 
-// The slabs of split products, added in the order of the splits, and what the product's own way out does otherwise: runs of eight of a row.
-__global__ __launch_bounds__(256) void k_linear_join(const GemmPair pair, int64_t first, int64_t all)
+// ------------------------------------------------------------------------------------------------- small tiles
+// 32 tokens x 32 channels a block, for products whose larger tiles would leave compute units without work: latency bounds them, so the
+// block's eight wavefronts share the contraction.  Two groups of four take its stages in turn, and of a stage each wavefront one step (two
+// LDS reads, one product); the eight sums are added in LDS in their order.
+//
+// LOOSE: operands at any address with any stride, through registers (a load's 16 bytes may begin anywhere): a chunk that would reach behind a
+// row's end is loaded from the row's last 16 bytes and moved to its place, rows and positions that do not exist are zeros.
+//
+// DEEP: where no compute unit has two blocks, twice as many stages are under way.
+constexpr int SMALL = SMALL_TILE, SMALL_GROUPS = 2, SMALL_BUF = 2 * SMALL * STAGE, SMALL_THREADS = SMALL_GROUPS * 256;
+constexpr size_t small_lds(bool loose, bool deep)
 {
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const size_t stages = (size_t)SMALL_GROUPS * (loose ? 2 : deep ? 8 : 4) * SMALL_BUF, sums = (size_t)SMALL_THREADS / 64 * SMALL * (SMALL + 4) * 4;
+    return stages > sums ? stages : sums;
+}
+
+template <class E, bool ALONG> struct LooseTile {
+    static constexpr int CH = 16 / sizeof(E), KS = STAGE / sizeof(E);
+    using Chunk = Run<E, CH>;
+    const E* base; int64_t pitch, k;
+    int position;                // of the chunk in a stage's contraction
+    int down;                    // across: by how much the row's last chunk is moved; along: nothing
+    __device__ __forceinline__ LooseTile(const Operand& o, int64_t row0, int64_t rows, int64_t len, int lane, int wave)
+    {
+        pitch = o.pitch; k = len;
+        if constexpr (ALONG) {
+            position = ((lane & 7) ^ ((lane >> 4) + 4 * (wave & 1))) * CH;
+            base = (const E*)o.p + std::min<int64_t>(row0 + wave * 8 + (lane >> 3), rows - 1) * pitch;
+            down = 0;
+        } else {
+            constexpr int LANES = SMALL / CH;
+            position = wave * (64 / LANES) + lane / LANES;
+            const int64_t at = row0 + (lane % LANES) * CH, from = std::min(at, rows - CH);
+            base = (const E*)o.p + from;
+            down = (int)std::min<int64_t>(at - from, CH);
+        }
+    }
+    __device__ __forceinline__ void load(int s, Chunk& c) const
+    {
+        const int64_t at = (int64_t)s * KS + position;
+        c.load(ALONG ? base + std::min(at, k - CH) : base + std::min(at, k - 1) * pitch);
+    }
+    __device__ __forceinline__ void store(int s, Chunk& c, char* to) const      // to: the lane's place
+    {
+        const int64_t at = (int64_t)s * KS + position;
+        if constexpr (ALONG) {
+            if (((int64_t)s + 1) * KS > k) { const int64_t d = at - (k - CH); if (d > 0) c.down((int)std::min<int64_t>(d, CH)); }
+        } else {
+            if (down) c.down(down);
+            if (at >= k) c.down(CH);
+        }
+        *(i32x4*)to = __builtin_bit_cast(i32x4, c);
+    }
+};
+
+template <class E, bool A_ALONG, bool B_ALONG, bool LOOSE, bool DEEP>
+__device__ __forceinline__ void small_tile(const GemmArgs& g, char* lds, int64_t m0, int64_t n0, int split)
+{
+    constexpr int DEPTH = LOOSE ? 2 : DEEP ? 8 : 4, AHEAD = DEEP ? 8 : 4;
+    const LinearProduct& p = g.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave >> 2, w4 = wave & 3;
+    const int first = (int)((int64_t)g.stages * split / g.splits), last = (int)((int64_t)g.stages * (split + 1) / g.splits);
+    const int turns = (last - first + SMALL_GROUPS - 1) / SMALL_GROUPS;
+    char* const own = lds + group * DEPTH * SMALL_BUF;
+    auto stage_of = [&](int turn) { return first + turn * SMALL_GROUPS + group; };
+    const Tile<E, B_ALONG, SMALL, 4, 1> channels(p.b, n0, p.n, p.k, lane, w4, 0);
+    const Tile<E, A_ALONG, SMALL, 4, 1> tokens(p.a, m0, p.m, p.k, lane, w4, 0);
+    f32x16 acc = {};
+    auto multiply = [&](const char* buf) {
+        i32x4 a[1], b[1];
+        channels.fetch(buf, w4, lane, a);
+        tokens.fetch(buf + SMALL * STAGE, w4, lane, b);
+        acc = mfma<E>(a[0], b[0], acc);
+    };
+    if constexpr (LOOSE) {
+        const LooseTile<E, B_ALONG> from_b(p.b, n0, p.n, p.k, lane, w4);
+        const LooseTile<E, A_ALONG> from_a(p.a, m0, p.m, p.k, lane, w4);
+        typename LooseTile<E, true>::Chunk c[AHEAD][2];
+        auto ask = [&](int turn, int u) { if (stage_of(turn) < last) { from_b.load(stage_of(turn), c[u][0]); from_a.load(stage_of(turn), c[u][1]); } };
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) ask(u, u);
+        for (int t = 0; t < turns; t += AHEAD)
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                if (t + u >= turns) break;
+                char* const buf = own + (u & 1) * SMALL_BUF;
+                const int s = stage_of(t + u);
+                if (s < last) {
+                    from_b.store(s, c[u][0], buf + threadIdx.x % 256 * 16);
+                    from_a.store(s, c[u][1], buf + SMALL * STAGE + threadIdx.x % 256 * 16);
+                }
+                ask(t + u + AHEAD, u);
+                __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0)
+                ST_BARRIER();
+                if (s < last) multiply(buf);
+            }
+    } else {
+        auto ask = [&](int turn) {
+            if (stage_of(turn) >= last) return;
+            char* const buf = own + turn % DEPTH * SMALL_BUF;
+            channels.load(stage_of(turn), buf, w4);
+            tokens.load(stage_of(turn), buf + SMALL * STAGE, w4);
+        };
+#pragma unroll
+        for (int t = 0; t < DEPTH - 1; ++t) ask(t);
+        for (int t = 0; t < turns; ++t) {
+            // this stage is there (two loads of each of the DEPTH - 2 behind it may be on their way), and the one before is read
+            if (stage_of(t + DEPTH - 2) < last) ST_WAIT_VM(2 * (DEPTH - 2)); else ST_WAIT_VM(0);
+            __builtin_amdgcn_s_waitcnt(0xc07f);
+            ST_BARRIER();
+            ask(t + DEPTH - 1);
+            if (stage_of(t) < last) multiply(own + t % DEPTH * SMALL_BUF);
+        }
+    }
+    __syncthreads();
+    constexpr int PITCH = SMALL + 4;
+    float* const sums = (float*)lds;
+    const int r32 = lane & 31, half = lane >> 5;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+        *(f32x4*)(sums + (wave * SMALL + r32) * PITCH + q * 8 + half * 4) = f32x4{acc[q * 4], acc[q * 4 + 1], acc[q * 4 + 2], acc[q * 4 + 3]};
+    __syncthreads();
+    const int run = threadIdx.x & 7, row = threadIdx.x >> 3;
+    const int64_t m = m0 + row, n = n0 + run * 4;
+    if (row >= SMALL || m >= p.m || n >= p.n) return;
+    float v[4] = {}, bias[4];
+    bias_of(p, n, bias);
+#pragma unroll
+    for (int w = 0; w < SMALL_GROUPS * 4; ++w) {
+        const f32x4 u = *(const f32x4*)(sums + (w * SMALL + row) * PITCH + run * 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += u[e];
+    }
+    if (g.splits > 1) store_run(p.slabs, 0, ((int64_t)split * p.m + m) * p.n + n, n, p.n, v);
+    else finish(p, m, n, v, bias);
+}
+
+template <class E, bool LOOSE, bool DEEP> __global__ __launch_bounds__(SMALL_THREADS) void k_linear_small(const GemmPair pair)
+{
+    extern __shared__ __align__(16) char lds[];
+    const unsigned both = pair.g[0].blocks + pair.g[1].blocks;
+    if (blockIdx.x >= both) { sum_columns<SMALL_THREADS>(pair.sums, blockIdx.x - both, (float*)lds); return; }
+    const Place at = place_of(pair);
+    const GemmArgs& g = pair.g[at.second];
+    const int64_t m0 = (int64_t)at.tm * SMALL, n0 = (int64_t)at.tn * SMALL;
+    if (g.p.a.along) {
+        if (g.p.b.along) small_tile<E, true, true, LOOSE, DEEP>(g, lds, m0, n0, at.split);
+        else small_tile<E, true, false, LOOSE, DEEP>(g, lds, m0, n0, at.split);
+    } else {
+        if (g.p.b.along) small_tile<E, false, true, LOOSE, DEEP>(g, lds, m0, n0, at.split);
+        else small_tile<E, false, false, LOOSE, DEEP>(g, lds, m0, n0, at.split);
+    }
+}
+
+// The slabs of split products, added in one order, and what the product's own way out does otherwise: runs of COUNT of a row.  GROUPS threads
+// share a run where there are few of them, each with some of the slabs.
+template <int GROUPS, int COUNT> __global__ __launch_bounds__(256) void k_linear_join(const GemmPair pair, int64_t first, int64_t all)
+{
+    __shared__ float sums[GROUPS > 1 ? GROUPS * (256 / GROUPS) * COUNT : 1];
+    constexpr int EACH = 256 / GROUPS;
+    const int group = threadIdx.x / EACH, mine = threadIdx.x % EACH;
+    for (int64_t base = (int64_t)blockIdx.x * EACH; base < all; base += (int64_t)gridDim.x * EACH) {
+        const int64_t i = base + mine < all ? base + mine : all - 1;
         const bool second = i >= first;
         const GemmArgs& g = pair.g[second];
         const LinearProduct& p = g.p;
-        const int64_t runs = (p.n + 7) / 8, at = second ? i - first : i, m = at / runs, n = (at - m * runs) * 8, size = p.m * p.n;
-        float v[8] = {}, bias[8];
-        bias_of(p, n, bias);
-        for (int s = 0; s < g.splits; ++s) {
-            float u[8];
-            load_run(p.slabs, 0, s * size + m * p.n + n, n, p.n, u);
+        const int64_t runs = (p.n + COUNT - 1) / COUNT, at = second ? i - first : i, m = at / runs, n = (at - m * runs) * COUNT, size = p.m * p.n;
+        float v[COUNT] = {};
+        const float* from = p.slabs + m * p.n + n;
+#pragma unroll 4
+        for (int s = group; s < g.splits; s += GROUPS) {
+            float u[COUNT];
+            load_run(from + s * size, 0, 0, n, p.n, u);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += u[e];
+            for (int e = 0; e < COUNT; ++e) v[e] += u[e];
         }
+        if constexpr (GROUPS > 1) {
+            __syncthreads();      // (the turn before has been read)
+#pragma unroll
+            for (int e = 0; e < COUNT; ++e) sums[(group * COUNT + e) * EACH + mine] = v[e];
+            __syncthreads();
+            if (group) continue;
+#pragma unroll
+            for (int e = 0; e < COUNT; ++e) {
+                v[e] = 0.f;
+#pragma unroll
+                for (int q = 0; q < GROUPS; ++q) v[e] += sums[(q * COUNT + e) * EACH + mine];
+            }
+        }
+        if (base + mine >= all) continue;
+        float bias[COUNT];
+        bias_of(p, n, bias);
         finish(p, m, n, v, bias);
     }
 }
@@ -522,14 +720,30 @@ void linear_product_few(Ctx& c, const LinearProduct& p, int is_bf16)
 
 // --------------------------------------------------------------------------------------- choice of tile and split
 static int64_t tiles_of(const Extent& e, int tile) { return ceil_div(e.m, tile) * ceil_div(e.n, tile); }
-LinearForm linear_form(const Extent* e, int count, int is_bf16)
+LinearForm linear_form(const Extent* e, int count, int is_bf16, bool odd)
 {
     const int64_t per_stage = is_bf16 ? STAGE / 2 : STAGE / 4;
     auto total = [&](int tile) { int64_t t = 0; for (int i = 0; i < count; ++i) t += tiles_of(e[i], tile); return t; };
     auto stages_of = [&](int tile) { int64_t w = 0; for (int i = 0; i < count; ++i) w += tiles_of(e[i], tile) * ceil_div(e[i].k, per_stage); return w; };
     LinearForm f = {64, {1, 1}};
     if (total(256) >= 192 && stages_of(256) > 5 * total(256)) f.tile = 256;
+    else if (total(SMALL) <= (odd ? 800 : 512)) f.tile = SMALL;
     else if (total(64) > 512) f.tile = 128;
+    for (int i = 0; i < count; ++i) f.splits[i] = 1;
+    if (f.tile == SMALL) {
+        // Stages a compute unit goes through, and what a join costs in them: us a stage about 0.13 (float32 0.2), a join 4.
+        const int64_t join = is_bf16 ? 30 : 20;
+        int64_t longest = 0, least = INT64_MAX, best = 1;
+        for (int i = 0; i < count; ++i) longest = std::max(longest, ceil_div(e[i].k, per_stage));
+        for (int64_t s = 1; s <= 16 && (s == 1 || longest >= 8 * s); s *= 2) {
+            int64_t blocks = 0;
+            for (int i = 0; i < count; ++i) blocks += tiles_of(e[i], SMALL) * std::max<int64_t>(1, std::min(s, ceil_div(e[i].k, per_stage) * s / longest));
+            const int64_t cost = ceil_div(blocks, 256) * ceil_div(longest, s) + (s > 1 ? join + s : 0);
+            if (cost < least) { least = cost; best = s; }
+        }
+        for (int i = 0; i < count; ++i) f.splits[i] = (int)std::max<int64_t>(1, std::min(best, ceil_div(e[i].k, per_stage) * best / longest));
+        return f;
+    }
     // every block about the same number of stages, 256 blocks, eight stages each at least
     const int64_t each = std::max<int64_t>(8, ceil_div(stages_of(f.tile), 256));
     for (int i = 0; i < count; ++i) {
@@ -548,37 +762,52 @@ static void launch(Ctx& c, const GemmPair& g)
     constexpr int threads = (BM / WM) * (BN / WN) * 64;
     ensure_dynamic_lds((const void*)k_linear_product<E, BM, BN, WM, WN, DEPTH>, lds);
     constexpr const char* name = BM == 256 ? "linear_product_256" : BM == 64 ? "linear_product_64" : DEPTH > 2 ? "linear_product_128_deep" : "linear_product_128";
-    const unsigned grid = g.g[0].blocks + g.g[1].blocks + (unsigned)ceil_div(g.sums.n, threads);
+    const unsigned grid = g.g[0].blocks + g.g[1].blocks + (unsigned)ceil_div(g.sums.n, SUM_COLUMNS);
     ST_LAUNCH(c, name, (k_linear_product<E, BM, BN, WM, WN, DEPTH>), dim3(grid), dim3(threads), lds, g);
+}
+template <class E, bool LOOSE, bool DEEP> static void launch_small(Ctx& c, const GemmPair& g)
+{
+    ensure_dynamic_lds((const void*)k_linear_small<E, LOOSE, DEEP>, small_lds(LOOSE, DEEP));
+    const dim3 grid(g.g[0].blocks + g.g[1].blocks + (unsigned)ceil_div(g.sums.n, SUM_COLUMNS));
+    ST_LAUNCH(c, LOOSE ? "linear_small_loose" : "linear_small", (k_linear_small<E, LOOSE, DEEP>), grid, dim3(SMALL_THREADS), small_lds(LOOSE, DEEP), g);
 }
 template <class E> static void launch_tile(Ctx& c, const GemmPair& g, int tile)
 {
-    if (tile == 256) launch<E, 256, 256, 128, 64, 2>(c, g);
+    if (tile == SMALL) {
+        const bool loose = g.g[0].p.loose || g.g[1].p.loose, deep = g.g[0].blocks + g.g[1].blocks <= 256;
+        if (loose && deep) launch_small<E, true, true>(c, g);
+        else if (loose) launch_small<E, true, false>(c, g);
+        else if (deep) launch_small<E, false, true>(c, g);
+        else launch_small<E, false, false>(c, g);
+    } else if (tile == 256) launch<E, 256, 256, 128, 64, 2>(c, g);
     else if (tile == 128 && g.g[0].blocks + g.g[1].blocks <= 256) launch<E, 128, 128, 64, 32, 4>(c, g);
     else if (tile == 128) launch<E, 128, 128, 64, 32, 2>(c, g);
     else launch<E, 64, 64, 32, 32, 4>(c, g);
 }
 
-void linear_products(Ctx& c, const LinearProduct* p, int count, int is_bf16, const ColumnSums& sums)
+void linear_products(Ctx& c, const LinearProduct* p, int count, const LinearForm& f, int is_bf16, const ColumnSums& sums)
 {
     if (count == 0 && sums.n == 0) return;
-    Extent e[2];
-    for (int i = 0; i < count; ++i) e[i] = {p[i].m, p[i].n, p[i].k};
-    const LinearForm f = linear_form(e, count, is_bf16);
     GemmPair g{}, joined{};
     g.sums = sums;
     int n_joined = 0;
-    int64_t runs[2] = {0, 0};
+    int64_t cells[2] = {0, 0};
     for (int i = 0; i < count; ++i) {
         const int64_t tm = ceil_div(p[i].m, f.tile), tn = ceil_div(p[i].n, f.tile);
         g.g[i] = GemmArgs{p[i], fast_div((int)(tm * tn)), fast_div((int)(tn * BAND)), (int)tm, f.splits[i],
                           (int)ceil_div(p[i].k * (is_bf16 ? 2 : 4), STAGE), (unsigned)(tm * tn * f.splits[i])};
-        if (f.splits[i] > 1) { runs[n_joined] = p[i].m * ceil_div(p[i].n, 8); joined.g[n_joined++] = g.g[i]; }
+        if (f.splits[i] > 1) { cells[n_joined] = p[i].m; joined.g[n_joined++] = g.g[i]; }
     }
     if (is_bf16) launch_tile<bf16>(c, g, f.tile); else launch_tile<float>(c, g, f.tile);
     if (n_joined) {
-        const int64_t all = runs[0] + runs[1], blocks = ceil_div(all, 256);
-        ST_LAUNCH(c, "linear_join", k_linear_join, dim3((unsigned)(blocks > 8192 ? 8192 : blocks)), dim3(256), 0, joined, runs[0], all);
+        // (few runs: eight threads share one)
+        auto runs = [&](int i, int count) { return cells[i] ? cells[i] * ceil_div(joined.g[i].p.n, count) : 0; };
+        const bool few = runs(0, 8) + runs(1, 8) < 1 << 16;
+        const int count = few ? 4 : 8;
+        const int64_t first = runs(0, count), all = first + runs(1, count), blocks = ceil_div(all, few ? 32 : 256);
+        const dim3 grid((unsigned)(blocks > 8192 ? 8192 : blocks));
+        if (few) ST_LAUNCH(c, "linear_join", (k_linear_join<8, 4>), grid, dim3(256), 0, joined, first, all);
+        else ST_LAUNCH(c, "linear_join", (k_linear_join<1, 8>), grid, dim3(256), 0, joined, first, all);
     }
 }
 

@@ -11,13 +11,13 @@ namespace st {
 // Eight values a thread along memory, 64 runs of 64 values a block.  `turn`: through LDS, the other way round.
 struct PackArgs { PackTask t[PACK_TASKS]; unsigned first[PACK_TASKS + 1], across[PACK_TASKS]; int count; };      // first block of each; blocks along a run
 
-template <class E> __global__ __launch_bounds__(256) void k_linear_pack(const PackArgs a)
+template <class E> __device__ __forceinline__ void pack_block(const PackArgs& a, unsigned at_block, char* lds)
 {
-    __shared__ E turned[64][64 + 16 / sizeof(E)];
+    E (*turned)[64 + 16 / sizeof(E)] = (E(*)[64 + 16 / sizeof(E)])lds;
     int i = 0;
-    while (i + 1 < a.count && blockIdx.x >= a.first[i + 1]) ++i;
+    while (i + 1 < a.count && at_block >= a.first[i + 1]) ++i;
     const PackTask& t = a.t[i];
-    const unsigned block = blockIdx.x - a.first[i];
+    const unsigned block = at_block - a.first[i];
     const int64_t o0 = (int64_t)(block / a.across[i]) * 64, i0 = (int64_t)(block % a.across[i]) * 64;
     const int run = threadIdx.x & 7, row = threadIdx.x >> 3;
     Raw8<E> v[2];
@@ -62,21 +62,6 @@ template <class E> __global__ __launch_bounds__(256) void k_linear_pack(const Pa
     }
 }
 
-void linear_pack(Ctx& c, const PackTask* t, int count, int is_bf16)
-{
-    for (int done = 0; done < count;) {      // (a launch holds fewer than 2^32 threads)
-        PackArgs a{};
-        for (; done < count && (a.count == 0 || a.first[a.count] < (1 << 22)); ++done) {
-            const int i = a.count++;
-            a.t[i] = t[done];
-            a.across[i] = (unsigned)ceil_div(t[done].inner, 64);
-            a.first[i + 1] = a.first[i] + a.across[i] * (unsigned)ceil_div(t[done].outer, 64);
-        }
-        if (is_bf16) ST_LAUNCH(c, "linear_pack", k_linear_pack<bf16>, dim3(a.first[a.count]), dim3(256), 0, a);
-        else ST_LAUNCH(c, "linear_pack", k_linear_pack<float>, dim3(a.first[a.count]), dim3(256), 0, a);
-    }
-}
-
 template <class E> __global__ __launch_bounds__(256) void k_linear_fill_zero(E* __restrict__ p, int64_t rows, int64_t cols, int64_t pitch)
 {
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * cols; i += (int64_t)gridDim.x * 256) p[i / cols * pitch + i % cols] = from_f32<E>(0.f);
@@ -91,7 +76,7 @@ void linear_fill_zero(Ctx& c, void* p, int is_bf16, int64_t rows, int64_t cols, 
 // ------------------------------------------------------------------------------------------------------ dz
 // A block takes 64 columns and a part of the rows, 32 rows at a time: eight threads a row, eight values each.  What lies column by column
 // goes through LDS, 64 columns x 32 rows.  dz is rounded to the operands' type; the sums of its columns are of what it was before.
-struct SlopeArgs { SlopeTask t; unsigned across; int rows_each; };
+struct SlopeArgs { SlopeTask t; unsigned across, blocks; int rows_each; };
 
 template <class T> __device__ __forceinline__ void load_rows(const GradSource& s, int64_t m0, int64_t m, int64_t n0, int64_t n, float (*turned)[33], float (&v)[8])
 {
@@ -137,10 +122,10 @@ template <class E> __device__ __forceinline__ void store_dz(void* to, int64_t at
     *(E8*)((E*)to + at) = u;
 }
 
-template <class T, class Z, int ACT> __device__ __forceinline__ void slope_rows(const SlopeArgs& a, float (*turned)[33], float (*sums)[64])
+template <class T, class Z, int ACT> __device__ __forceinline__ void slope_rows(const SlopeArgs& a, unsigned block, float (*turned)[33], float (*sums)[64])
 {
     const SlopeTask& t = a.t;
-    const int64_t n0 = (int64_t)(blockIdx.x % a.across) * 64, part = blockIdx.x / a.across;
+    const int64_t n0 = (int64_t)(block % a.across) * 64, part = block / a.across;
     const int64_t from = part * a.rows_each, to = std::min(from + a.rows_each, t.m);
     const int run = threadIdx.x & 7, row = threadIdx.x >> 3;
     float sum[8] = {};
@@ -172,37 +157,57 @@ template <class T, class Z, int ACT> __device__ __forceinline__ void slope_rows(
     }
 }
 
-template <class T, class Z> __global__ __launch_bounds__(256) void k_linear_slope(const SlopeArgs a)
+template <class T, class Z> __device__ __forceinline__ void slope_block(const SlopeArgs& a, unsigned block, char* lds)
 {
-    __shared__ float turned[64][33];
-    __shared__ float sums[32][64];
+    float (*turned)[33] = (float(*)[33])lds, (*sums)[64] = (float(*)[64])(lds + 64 * 33 * 4);
     switch (a.t.act) {
-    case ST_ACT_RELU: slope_rows<T, Z, ST_ACT_RELU>(a, turned, sums); break;
-    case ST_ACT_GELU: slope_rows<T, Z, ST_ACT_GELU>(a, turned, sums); break;
-    case ST_ACT_GELU_TANH: slope_rows<T, Z, ST_ACT_GELU_TANH>(a, turned, sums); break;
-    case ST_ACT_SILU: slope_rows<T, Z, ST_ACT_SILU>(a, turned, sums); break;
-    default: slope_rows<T, Z, ST_ACT_NONE>(a, turned, sums); break;
+    case ST_ACT_RELU: slope_rows<T, Z, ST_ACT_RELU>(a, block, turned, sums); break;
+    case ST_ACT_GELU: slope_rows<T, Z, ST_ACT_GELU>(a, block, turned, sums); break;
+    case ST_ACT_GELU_TANH: slope_rows<T, Z, ST_ACT_GELU_TANH>(a, block, turned, sums); break;
+    case ST_ACT_SILU: slope_rows<T, Z, ST_ACT_SILU>(a, block, turned, sums); break;
+    default: slope_rows<T, Z, ST_ACT_NONE>(a, block, turned, sums); break;
     }
 }
 
-// parts of the rows: about four blocks a compute unit, 32 rows at least
+// One launch makes all of a call's operands: dz first, whose blocks work longest, then the copies.
+struct PrepareArgs { SlopeArgs slope; PackArgs pack; };
+static_assert(sizeof(PrepareArgs) <= 4096, "kernel arguments");
+template <class E> __global__ __launch_bounds__(256) void k_linear_prepare(const PrepareArgs a)
+{
+    __shared__ __align__(16) char lds[17408];
+    static_assert(64 * 33 * 4 + 32 * 64 * 4 <= 17408 && 64 * (64 + 4) * 4 <= 17408, "room for either");
+    if (blockIdx.x >= a.slope.blocks) { pack_block<E>(a.pack, blockIdx.x - a.slope.blocks, lds); return; }
+    const SlopeTask& t = a.slope.t;
+    if (t.dy.bf16) { if (t.pre.bf16) slope_block<bf16, bf16>(a.slope, blockIdx.x, lds); else slope_block<bf16, float>(a.slope, blockIdx.x, lds); }
+    else { if (t.pre.bf16) slope_block<float, bf16>(a.slope, blockIdx.x, lds); else slope_block<float, float>(a.slope, blockIdx.x, lds); }
+}
+
+// parts of the rows: about four blocks a compute unit, 32 rows at least; no more parts than the launch that adds them reads in passing
 static int slope_rows_each(int64_t m, int64_t n)
 {
-    const int64_t parts = std::max<int64_t>(1, 1024 / ceil_div(n, 64));
+    const int64_t parts = std::min<int64_t>(128, std::max<int64_t>(1, 1024 / ceil_div(n, 64)));
     return (int)round_up(std::max<int64_t>(32, ceil_div(m, parts)), 32);
 }
 int linear_slope_parts(int64_t m, int64_t n) { return (int)ceil_div(m, slope_rows_each(m, n)); }
 
-void linear_slope(Ctx& c, const SlopeTask& t)
+void linear_prepare(Ctx& c, const SlopeTask* slope, const PackTask* t, int count, int is_bf16)
 {
-    const SlopeArgs a{t, (unsigned)ceil_div(t.n, 64), slope_rows_each(t.m, t.n)};
-    const dim3 grid(a.across * (unsigned)linear_slope_parts(t.m, t.n));
-    if (t.dy.bf16) {
-        if (t.pre.bf16) ST_LAUNCH(c, "linear_slope", (k_linear_slope<bf16, bf16>), grid, dim3(256), 0, a);
-        else ST_LAUNCH(c, "linear_slope", (k_linear_slope<bf16, float>), grid, dim3(256), 0, a);
-    } else {
-        if (t.pre.bf16) ST_LAUNCH(c, "linear_slope", (k_linear_slope<float, bf16>), grid, dim3(256), 0, a);
-        else ST_LAUNCH(c, "linear_slope", (k_linear_slope<float, float>), grid, dim3(256), 0, a);
+    PrepareArgs a{};
+    if (slope) {
+        const unsigned across = (unsigned)ceil_div(slope->n, 64);
+        a.slope = SlopeArgs{*slope, across, across * (unsigned)linear_slope_parts(slope->m, slope->n), slope_rows_each(slope->m, slope->n)};
+    }
+    for (int done = 0; done < count || a.slope.blocks;) {      // (a launch holds fewer than 2^32 threads)
+        for (; done < count && (a.pack.count == 0 || a.pack.first[a.pack.count] < (1 << 22)); ++done) {
+            const int i = a.pack.count++;
+            a.pack.t[i] = t[done];
+            a.pack.across[i] = (unsigned)ceil_div(t[done].inner, 64);
+            a.pack.first[i + 1] = a.pack.first[i] + a.pack.across[i] * (unsigned)ceil_div(t[done].outer, 64);
+        }
+        const dim3 grid(a.slope.blocks + a.pack.first[a.pack.count]);
+        if (is_bf16) ST_LAUNCH(c, "linear_prepare", k_linear_prepare<bf16>, grid, dim3(256), 0, a);
+        else ST_LAUNCH(c, "linear_prepare", k_linear_prepare<float>, grid, dim3(256), 0, a);
+        a = PrepareArgs{};
     }
 }
 

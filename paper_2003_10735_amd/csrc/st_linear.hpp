@@ -86,14 +86,17 @@ struct LinearProduct {
     const void* residual; int residual_bf16; int64_t residual_pitch;
     void* pre; int pre_bf16; int64_t pre_pitch;
     float* slabs;                // [splits, m, n] where the contraction is split
+    int loose;                   // an operand that the products' 16-byte loads do not take as it lies: small tiles load it through registers
 };
 // Sums of columns that lie as parts: out[i] (+)= sum over the parts of parts[part][i].  Done by the launch of the products.
 struct ColumnSums { const float* parts; int n_parts; int64_t n; float* out; int accumulate; };
 
+constexpr int SMALL_TILE = 32;      // small tiles take operands at any address (but rows of less than 16 bytes)
 struct LinearForm { int tile; int splits[2]; };
-LinearForm linear_form(const Extent* e, int count, int is_bf16);
-// up to two products, and sums of columns (n == 0: none), in one launch, and one more where a contraction is split
-void linear_products(Ctx& c, const LinearProduct* p, int count, int is_bf16, const ColumnSums& sums);
+// odd: an operand that small tiles take as it lies and others want copied
+LinearForm linear_form(const Extent* e, int count, int is_bf16, bool odd);
+// up to two products of that form, and sums of columns (n == 0: none), in one launch, and one more where a contraction is split
+void linear_products(Ctx& c, const LinearProduct* p, int count, const LinearForm& f, int is_bf16, const ColumnSums& sums);
 // few tokens, weights along the contraction: one launch of its own kind, whatever the alignment
 bool linear_few(int64_t m, int64_t n, int64_t k, int is_bf16);
 void linear_product_few(Ctx& c, const LinearProduct& p, int is_bf16);
@@ -103,7 +106,6 @@ void linear_product_few(Ctx& c, const LinearProduct& p, int is_bf16);
 // `turn` the copy lies the other way round: `inner` runs of `outer` values.
 struct PackTask { const void* x; int64_t outer, inner, pitch; void* to; int64_t to_pitch; int turn; };
 constexpr int PACK_TASKS = 4;
-void linear_pack(Ctx& c, const PackTask* t, int count, int is_bf16);
 void linear_fill_zero(Ctx& c, void* p, int is_bf16, int64_t rows, int64_t cols, int64_t pitch);
 
 // dz = dy act'(pre) row by row with zeros up to whole chunks (to null: not stored), and the sums of its columns as parts.
@@ -115,6 +117,7 @@ struct SlopeTask {
     float* parts;                // [linear_slope_parts(m, n), n] or null
 };
 int linear_slope_parts(int64_t m, int64_t n);
-void linear_slope(Ctx& c, const SlopeTask& t);
+// dz (or null) and the copies, in one launch
+void linear_prepare(Ctx& c, const SlopeTask* slope, const PackTask* t, int count, int is_bf16);
 
 }  // namespace st

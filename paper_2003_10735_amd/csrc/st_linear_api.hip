@@ -39,38 +39,45 @@ int check(const st_matrix* x, int64_t rows, int64_t cols, int* along)
     return ST_OK;
 }
 
-// An operand whose rows are x's rows (by_rows) or its columns: as it lies, or where the products cannot read it so, a copy that `pack`
-// (with room in `w`) makes.  The copy lies as x does, unless only the other order keeps a tile's offsets small.
+// An operand whose rows are x's rows (by_rows) or its columns: as it lies, or where the products cannot read it so, a copy that `packs`
+// makes (with room in `w`).  The copy lies as x does, unless only the other order keeps a tile's offsets small.
 struct Packs { PackTask t[PACK_TASKS]; int n = 0; };
-Operand operand_of(const st_matrix& x, int along, bool by_rows, Carve& w, Packs* packs)
+struct Lie { int64_t outer, inner, pitch; int k_along; bool direct; };      // k_along: the operand's rows lie along memory
+Lie lie_of(const st_matrix& x, int along, bool by_rows)
+{
+    Lie l{along ? x.rows : x.cols, along ? x.cols : x.rows, along ? x.row_stride : x.col_stride, along == (by_rows ? 1 : 0), false};
+    if (l.outer == 1) l.pitch = round_up(l.inner, 16 / elem(x.dtype));      // (whatever the caller has there)
+    l.direct = operand_direct(x.data, l.pitch, l.k_along, l.inner, elem(x.dtype));
+    return l;
+}
+Operand operand_of(const st_matrix& x, int along, bool by_rows, bool small, int* loose, Carve& w, Packs* packs)
 {
     const int es = elem(x.dtype);
-    const int64_t outer = along ? x.rows : x.cols, inner = along ? x.cols : x.rows;
-    // (where there is one run, or runs of one value, the step between them is whatever the caller has there)
-    const int64_t pitch = outer > 1 ? (along ? x.row_stride : x.col_stride) : round_up(inner, 16 / es);
-    const int k_along = along == (by_rows ? 1 : 0);      // the operand's rows lie along memory
-    if (operand_direct(x.data, pitch, k_along, inner, es)) return Operand{x.data, pitch, k_along};
+    const Lie l = lie_of(x, along, by_rows);
+    const int64_t outer = l.outer, inner = l.inner, pitch = l.pitch;
+    const int k_along = l.k_along;
+    if (l.direct) return Operand{x.data, pitch, k_along};
+    if (small && inner >= 16 / es) { *loose = 1; return Operand{x.data, pitch, k_along}; }
     const bool turn = !operand_direct(nullptr, round_up(inner, 8), k_along, round_up(inner, 8), es);
     const int64_t to_pitch = round_up(turn ? outer : inner, 8);
     void* to = w.take((size_t)(turn ? inner : outer) * to_pitch * es);
-    if (packs) packs->t[packs->n++] = PackTask{x.data, outer, inner, pitch, to, to_pitch, turn};
+    packs->t[packs->n++] = PackTask{x.data, outer, inner, pitch, to, to_pitch, turn};
     return Operand{to, to_pitch, turn ? !k_along : k_along};
 }
-size_t slab_bytes(const Extent* e, int count, int which, int is_bf16)
+size_t slab_bytes(const Extent* e, const LinearForm& f, int which)
 {
-    const LinearForm f = linear_form(e, count, is_bf16);
     return f.splits[which] > 1 ? (size_t)f.splits[which] * e[which].m * e[which].n * 4 : 0;
 }
 bool products_ok(const Extent* e, int count, int is_bf16)
 {
-    const LinearForm f = linear_form(e, count, is_bf16);
+    const LinearForm f = linear_form(e, count, is_bf16, false);
     int64_t blocks = 0;
     for (int i = 0; i < count; ++i) blocks += ceil_div(e[i].m, f.tile) * ceil_div(e[i].n, f.tile) * f.splits[i];
-    return blocks < (1 << 23) - 8192;      // (and the blocks of the columns' sums)
+    return blocks < (1 << 23) - 32768 - 1;      // (and the blocks of the columns' sums)
 }
 
 // The forward pass, planned: `ws` null for its size alone.
-struct LinearPlan { LinearProduct p; Packs packs; bool few; size_t bytes; };
+struct LinearPlan { LinearProduct p; LinearForm form; Packs packs; bool few; size_t bytes; };
 LinearPlan plan_linear(const st_matrix& x, int x_along, const st_matrix& w, int w_along, char* ws)
 {
     LinearPlan l{};
@@ -83,17 +90,19 @@ LinearPlan plan_linear(const st_matrix& x, int x_along, const st_matrix& w, int 
         p.a = Operand{x.data, x_along ? x.row_stride : x.col_stride, x_along};
         p.b = Operand{w.data, w.row_stride, 1};
     } else {
-        p.a = operand_of(x, x_along, true, c, &l.packs);
-        p.b = operand_of(w, w_along, true, c, &l.packs);
         const Extent e{p.m, p.n, p.k};
-        p.slabs = (float*)c.take(p.m ? slab_bytes(&e, 1, 0, is_bf16) : 0);
+        l.form = linear_form(&e, 1, is_bf16, !lie_of(x, x_along, true).direct || !lie_of(w, w_along, true).direct);
+        const bool small = l.form.tile == SMALL_TILE;
+        p.a = operand_of(x, x_along, true, small, &p.loose, c, &l.packs);
+        p.b = operand_of(w, w_along, true, small, &p.loose, c, &l.packs);
+        p.slabs = (float*)c.take(slab_bytes(&e, l.form, 0));
     }
     l.bytes = c.used + 256;
     return l;
 }
 
 // The backward pass, planned the same way for the outputs that are asked for.
-struct BackwardPlan { LinearProduct p[2]; int n_products; Packs packs; SlopeTask slope; bool slopes; ColumnSums sums; size_t bytes; };
+struct BackwardPlan { LinearProduct p[2]; LinearForm form; int n_products; Packs packs; SlopeTask slope; bool slopes; ColumnSums sums; size_t bytes; };
 BackwardPlan plan_backward(const st_matrix* x, int x_along, const st_matrix* w, int w_along, const st_matrix& dy, int dy_along, int act,
                            int dtype, bool db, char* ws)
 {
@@ -103,44 +112,49 @@ BackwardPlan plan_backward(const st_matrix* x, int x_along, const st_matrix* w, 
     const int is_bf16 = dtype == ST_BF16;
     Operand by_tokens{}, by_channels{};      // dz for dx, and for dw
     const bool as_it_is = act == ST_ACT_NONE && dy.dtype == dtype;
+    Extent e[2];
+    if (x) e[b.n_products++] = Extent{n, x->cols, m};
+    if (w) e[b.n_products++] = Extent{m, w->cols, n};
+    const bool odd = (x && !lie_of(*x, x_along, false).direct) || (w && !lie_of(*w, w_along, false).direct)
+                     || (as_it_is && ((w && !lie_of(dy, dy_along, true).direct) || (x && !lie_of(dy, dy_along, false).direct)));
+    b.form = b.n_products ? linear_form(e, b.n_products, is_bf16, odd) : LinearForm{SMALL_TILE, {1, 1}};
+    const bool small = b.form.tile == SMALL_TILE;
+    int loose = 0;
     SlopeTask& s = b.slope;
     s.dy = GradSource{dy.data, dy.dtype == ST_BF16, dy_along ? dy.row_stride : dy.col_stride, dy_along};
     s.act = act; s.m = m; s.n = n; s.to_bf16 = is_bf16;
     b.slopes = db || ((x || w) && !as_it_is);
-    if (b.slopes && (x || w) && !as_it_is) {
+    if ((x || w) && !as_it_is) {
         s.to_pitch = round_up(n, 8);
         s.to = c.take((size_t)m * s.to_pitch * elem(dtype));
         by_tokens = Operand{s.to, s.to_pitch, 1};
         by_channels = Operand{s.to, s.to_pitch, 0};
     } else {
-        if (w) by_tokens = operand_of(dy, dy_along, true, c, &b.packs);
+        if (w) by_tokens = operand_of(dy, dy_along, true, small, &loose, c, &b.packs);
         // the same matrix read the other way round, if it can be (the rows of a copy end in zeros)
         const bool copied = w && by_tokens.p != dy.data;
         const int64_t pitch = by_tokens.pitch;
         if (w && operand_direct(by_tokens.p, pitch, !by_tokens.along, by_tokens.along ? n : copied ? round_up(m, 8) : m, elem(dtype)))
             by_channels = Operand{by_tokens.p, pitch, !by_tokens.along};
-        else if (x) by_channels = operand_of(dy, dy_along, false, c, &b.packs);
+        else if (x) by_channels = operand_of(dy, dy_along, false, small, &loose, c, &b.packs);
     }
     if (db) {
         s.parts = (float*)c.take((size_t)linear_slope_parts(m, n) * n * 4);
         b.sums = ColumnSums{s.parts, linear_slope_parts(m, n), n, nullptr, 0};
     }
-    Extent e[2];
+    int at = 0;
     if (x) {
-        LinearProduct& p = b.p[b.n_products];
-        p.m = n; p.n = x->cols; p.k = m;
+        LinearProduct& p = b.p[at++];
         p.a = by_channels;
-        p.b = operand_of(*x, x_along, false, c, &b.packs);
-        e[b.n_products++] = Extent{p.m, p.n, p.k};
+        p.b = operand_of(*x, x_along, false, small, &loose, c, &b.packs);
     }
     if (w) {
-        LinearProduct& p = b.p[b.n_products];
-        p.m = m; p.n = w->cols; p.k = n;
+        LinearProduct& p = b.p[at++];
         p.a = by_tokens;
-        p.b = operand_of(*w, w_along, false, c, &b.packs);
-        e[b.n_products++] = Extent{p.m, p.n, p.k};
+        p.b = operand_of(*w, w_along, false, small, &loose, c, &b.packs);
     }
-    for (int i = 0; i < b.n_products; ++i) b.p[i].slabs = (float*)c.take(slab_bytes(e, b.n_products, i, is_bf16));
+    for (int i = 0; i < b.n_products; ++i) { LinearProduct& p = b.p[i]; p.m = e[i].m; p.n = e[i].n; p.k = e[i].k; p.loose = loose; }
+    for (int i = 0; i < b.n_products; ++i) b.p[i].slabs = (float*)c.take(slab_bytes(e, b.form, i));
     b.bytes = c.used + 256;
     return b;
 }
@@ -196,8 +210,8 @@ int st_linear(const st_matrix* x, const st_matrix* w, const st_linear_opts* opts
     const int is_bf16 = x->dtype == ST_BF16;
     Ctx c{(hipStream_t)stream, ST_OK};
     if (l.few) { linear_product_few(c, p, is_bf16); return c.status; }
-    linear_pack(c, l.packs.t, l.packs.n, is_bf16);
-    linear_products(c, &p, 1, is_bf16, ColumnSums{});
+    linear_prepare(c, nullptr, l.packs.t, l.packs.n, is_bf16);
+    linear_products(c, &p, 1, l.form, is_bf16, ColumnSums{});
     return c.status;
 }
 
@@ -269,9 +283,8 @@ int st_linear_backward(const st_matrix* x, const st_matrix* w, const st_matrix* 
         LinearProduct& p = b.p[at++];
         p.out = o.dx; p.out_bf16 = o.dx_dtype == ST_BF16; p.out_pitch = o.dx_pitch;
     }
-    if (b.slopes) linear_slope(c, b.slope);
-    linear_pack(c, b.packs.t, b.packs.n, dtype == ST_BF16);
-    linear_products(c, b.p, b.n_products, dtype == ST_BF16, b.sums);
+    linear_prepare(c, b.slopes ? &b.slope : nullptr, b.packs.t, b.packs.n, dtype == ST_BF16);
+    linear_products(c, b.p, b.n_products, b.form, dtype == ST_BF16, b.sums);
     return c.status;
 }
 
