@@ -40,14 +40,18 @@ struct GemmPair { GemmArgs g[2]; ColumnSums sums; };
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 // 16 bytes a lane from `rsrc` + voff to LDS at `lds` + 16 * lane (the whole offset is the lanes': a scalar one takes no part in the
-// comparison with the buffer's size)
-__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t rsrc, char* lds, unsigned voff)
+// comparison with the buffer's size).  Written out, because the compiler has every transposing LDS read wait for all loads of its own
+// builtin that are under way, whatever they write (8192 tokens 4096 -> 4096, dz^T x: 256 us that way); the waits that are needed stand
+// where the stages change.  No register is written.  The pause covers a scalar register that a vector instruction has written just before, and M0.
+__device__ __forceinline__ void load_to_lds(i32x4 rsrc, char* lds, unsigned voff)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (__attribute__((address_space(3))) void*)lds, 16, (int)voff, 0, 0, 0);
+    const unsigned to = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "memory");      // (M0: nothing else of these kernels asks for it)
 }
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer(const char* base, int64_t bytes)
+__device__ __forceinline__ i32x4 buffer(const char* base, int64_t bytes)
 {
-    return __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, (int)(unsigned)(bytes < (int64_t)OUTSIDE ? bytes : (int64_t)OUTSIDE), 0x00020000);
+    const uint64_t at = (uint64_t)base;
+    return i32x4{(int)(unsigned)at, (int)(unsigned)(at >> 32 & 0xffff), (int)(unsigned)(bytes < (int64_t)OUTSIDE ? bytes : (int64_t)OUTSIDE), 0x00020000};
 }
 
 // ------------------------------------------------------------------------------------------------- the way out
@@ -145,25 +149,29 @@ template <class E, bool ALONG, int R, int WAVES, int N> struct Tile;
 template <class E, int R, int WAVES, int N> struct Tile<E, true, R, WAVES, N> {
     static constexpr int LOADS = R / 8 / WAVES, READS = N;
     static_assert(WAVES % 2 == 0, "a wavefront's eight rows begin at an even or at an odd multiple of eight in every load");
-    __amdgpu_buffer_rsrc_t r;
-    unsigned v, step, chunk, end;
+    i32x4 r;
+    unsigned v, step, by, left;     // left: bytes of the row from the lane's chunk on; by: what a turn moves on
     unsigned row;                // of a fragment: its place in the tile
-    __device__ __forceinline__ Tile(const Operand& o, int64_t row0, int64_t rows, int64_t k, int lane, int wave, int first)
+    // stages s0, s0 + every, .. are loaded in turn
+    __device__ __forceinline__ Tile(const Operand& o, int64_t row0, int64_t rows, int64_t k, int lane, int wave, int first, int s0, int every)
     {
         const int64_t pitch = o.pitch * sizeof(E);
-        end = (unsigned)k * sizeof(E);
-        r = buffer((const char*)o.p + row0 * pitch, (rows - row0 - 1) * pitch + (end + 15) / 16 * 16);      // (copies have zeros there)
-        chunk = ((lane & 7) ^ ((lane >> 4) + 4 * (wave & 1))) * 16;
+        const unsigned end = ((unsigned)k * sizeof(E) + 15) / 16 * 16;      // (copies have zeros there)
+        r = buffer((const char*)o.p + row0 * pitch, (rows - row0 - 1) * pitch + end);
+        const unsigned chunk = ((lane & 7) ^ ((lane >> 4) + 4 * (wave & 1))) * 16 + (unsigned)s0 * STAGE;
         v = (unsigned)(wave * 8 + (lane >> 3)) * (unsigned)pitch + chunk;
+        left = end - chunk;
+        by = every * STAGE;
         step = WAVES * 8 * (unsigned)pitch;
         row = (unsigned)(first + (lane & 31)) * STAGE;
     }
-    __device__ __forceinline__ void load(int s, char* to, int wave) const
+    __device__ __forceinline__ void load(char* to, int wave)
     {
-        unsigned off = v + (unsigned)s * STAGE;
-        const bool there = chunk + (unsigned)s * STAGE < end;
+        unsigned off = v;
+        const bool there = (int)left > 0;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i, off += step) load_to_lds(r, to + (i * WAVES + wave) * 1024, there ? off : OUTSIDE);
+        v += by; left -= by;
     }
     __device__ __forceinline__ void fetch(const char* L, int ks, int lane, i32x4 (&f)[N]) const
     {
@@ -177,7 +185,7 @@ template <class E, int R, int WAVES, int N> struct Tile<E, false, R, WAVES, N> {
     static constexpr int ES = sizeof(E), KS = STAGE / ES, LANES = R * ES / 16, KPI = 64 / LANES;      // a wavefront's load: KPI positions
     static constexpr int LOADS = R / 8 / WAVES, READS = ES == 2 ? 2 * N : 4 * N;
     static_assert(WAVES * KPI % 8 == 0, "the places of a position are the same in every load of a wavefront");
-    const char* base; int64_t pitch, k, tail;
+    const char* base; int64_t left, by;      // of the next stage: its first position, and the bytes from there to the matrix's end
     unsigned v, step, at[N];
     static __device__ __forceinline__ unsigned moved(unsigned position)      // by how many chunks
     {
@@ -186,12 +194,13 @@ template <class E, int R, int WAVES, int N> struct Tile<E, false, R, WAVES, N> {
         else if constexpr (R == 64) return 4 * (position >> 1 & 1);
         else return 4 * (position & 3);
     }
-    __device__ __forceinline__ Tile(const Operand& o, int64_t row0, int64_t rows, int64_t len, int lane, int wave, int first)
+    __device__ __forceinline__ Tile(const Operand& o, int64_t row0, int64_t rows, int64_t len, int lane, int wave, int first, int s0, int every)
     {
-        pitch = o.pitch * ES;
-        base = (const char*)o.p + row0 * ES;
-        k = len;
-        tail = ((rows - row0) * ES + 15) / 16 * 16;      // (whole chunks: what lies behind the last row inside one is memory that is there)
+        const int64_t pitch = o.pitch * ES, from0 = (int64_t)s0 * KS * pitch;
+        by = (int64_t)every * KS * pitch;
+        base = (const char*)o.p + row0 * ES + from0;
+        // (whole chunks: what lies behind the last row inside one is memory that is there)
+        left = (len - 1) * pitch + ((rows - row0) * ES + 15) / 16 * 16 - from0;
         const unsigned position = wave * KPI + lane / LANES;
         v = position * (unsigned)pitch + ((lane % LANES) ^ moved(position)) * 16;
         step = WAVES * KPI * (unsigned)pitch;
@@ -207,13 +216,13 @@ template <class E, int R, int WAVES, int N> struct Tile<E, false, R, WAVES, N> {
                 at[i] = 4 * half * R * 4 + (((first + i * 32 + (lane & 31)) / 4) ^ moved(4 * half)) * 16 + (lane & 3) * 4;
         }
     }
-    __device__ __forceinline__ void load(int s, char* to, int wave) const
+    __device__ __forceinline__ void load(char* to, int wave)
     {
-        const int64_t from = (int64_t)s * KS;
-        const auto r = buffer(base + from * pitch, (k - from - 1) * pitch + tail);
+        const auto r = buffer(base, left);
         unsigned off = v;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i, off += step) load_to_lds(r, to + (i * WAVES + wave) * 1024, off);
+        base += by; left -= by;
     }
     __device__ __forceinline__ void fetch(const char* L, int ks, int lane, i32x4 (&f)[N]) const
     {
@@ -266,7 +275,7 @@ __device__ __forceinline__ Place place_of(const GemmPair& pair)
 
 // ------------------------------------------------------------------------------------------------- a block's tile
 template <class E, int BM, int BN, int WM, int WN, int DEPTH, bool A_ALONG, bool B_ALONG>
-__device__ __forceinline__ void product_tile(const GemmArgs& g, char* lds, int64_t m0, int64_t n0, int split)
+__device__ __forceinline__ void product_tile(const GemmArgs& g, char* lds, int64_t m0, int64_t n0, int split, f32x16 (&acc)[WM / 32][WN / 32])
 {
     constexpr int WAVES = (BM / WM) * (BN / WN), NA = WN / 32, NB = WM / 32, STEPS = STAGE / 32;
     constexpr int BUF = (BM + BN) * STAGE, MINE = BN * STAGE;       // channels first, then tokens
@@ -276,13 +285,12 @@ __device__ __forceinline__ void product_tile(const GemmArgs& g, char* lds, int64
     const int wn = (wave % (BN / WN)) * WN, wm = (wave / (BN / WN)) * WM;
     using Channels = Tile<E, B_ALONG, BN, WAVES, NA>;
     using Tokens = Tile<E, A_ALONG, BM, WAVES, NB>;
-    const Channels channels(p.b, n0, p.n, p.k, lane, wave, wn);
-    const Tokens tokens(p.a, m0, p.m, p.k, lane, wave, wm);
-    auto stage = [&](int s, int buf) {
-        channels.load(s, lds + buf * BUF, wave);
-        tokens.load(s, lds + buf * BUF + MINE, wave);
+    Channels channels(p.b, n0, p.n, p.k, lane, wave, wn, first, 1);
+    Tokens tokens(p.a, m0, p.m, p.k, lane, wave, wm, first, 1);
+    auto next_stage = [&](int buf) {
+        channels.load(lds + buf * BUF, wave);
+        tokens.load(lds + buf * BUF + MINE, wave);
     };
-    f32x16 acc[NB][NA] = {};
     i32x4 a[2][NA], b[2][NB];
     auto fetch = [&](int buf, int ks, int to) {
         channels.fetch(lds + buf * BUF, ks, lane, a[to]);
@@ -309,14 +317,9 @@ __device__ __forceinline__ void product_tile(const GemmArgs& g, char* lds, int64
     // products.
     constexpr int LOADS = Channels::LOADS + Tokens::LOADS;      // of a wavefront and stage
     static_assert((DEPTH - 1) * LOADS < 64, "the counter of loads under way");
-    constexpr int PITCH = WN + 4, RUNS = WN / 8, ROWS = 64 / RUNS;
-    const int run = lane % RUNS, row = lane / RUNS;
-    const int64_t n = n0 + wn + run * 8;
-    float bias[8];
-    bias_of(p, n, bias);
     if (first < last) {
 #pragma unroll
-        for (int d = 0; d < DEPTH; ++d) if (first + d < last) stage(first + d, d);
+        for (int d = 0; d < DEPTH; ++d) if (first + d < last) next_stage(d);
         if (first + DEPTH <= last) ST_WAIT_VM((DEPTH - 1) * LOADS); else ST_WAIT_VM(0);
         ST_BARRIER();
         fetch(0, 0, 0);
@@ -334,28 +337,40 @@ __device__ __forceinline__ void product_tile(const GemmArgs& g, char* lds, int64
         if (DEPTH > 2 && s + DEPTH <= last) ST_WAIT_VM((DEPTH - 2) * LOADS); else ST_WAIT_VM(0);
         __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0)
         ST_BARRIER();
-        if (s + DEPTH < last) stage(s + DEPTH, buf);
+        if (s + DEPTH < last) next_stage(buf);
         buf = buf + 1 == DEPTH ? 0 : buf + 1;
         if (s + 1 < last) fetch(buf, 0, 0);
         multiply((STEPS - 1) & 1);
     }
 
-    // Out through LDS, 32 tokens of a wavefront at a time: sums go in four neighbouring channels at a time and come out as runs along a row.
+}
+
+// Out through LDS, 32 tokens of a wavefront at a time: sums go in four neighbouring channels at a time and come out as runs along a row.
+template <int BM, int BN, int WM, int WN, int DEPTH>
+__device__ __forceinline__ void tile_out(const GemmArgs& g, char* lds, int64_t m0, int64_t n0, int split, const f32x16 (&acc)[WM / 32][WN / 32])
+{
+    constexpr int WAVES = (BM / WM) * (BN / WN), PITCH = WN + 4, RUNS = WN / 8, ROWS = 64 / RUNS;
+    static_assert(WAVES * 32 * PITCH * 4 <= DEPTH * (BM + BN) * STAGE, "room for the sums");
+    const LinearProduct& p = g.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int wn = (wave % (BN / WN)) * WN, wm = (wave / (BN / WN)) * WM;
+    const int run = lane % RUNS, row = lane / RUNS, r32 = lane & 31, half = lane >> 5;
+    const int64_t n = n0 + wn + run * 8;
+    float bias[8];
+    bias_of(p, n, bias);
     __syncthreads();
-    static_assert(WAVES * 32 * PITCH * 4 <= DEPTH * BUF, "room for the sums");
     float* mine = (float*)lds + wave * 32 * PITCH;
-    const int r32 = lane & 31, half = lane >> 5;
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
+    for (int j = 0; j < WM / 32; ++j) {
 #pragma unroll
-        for (int i = 0; i < NA; ++i)
+        for (int i = 0; i < WN / 32; ++i)
 #pragma unroll
             for (int q = 0; q < 4; ++q)
                 *(f32x4*)(mine + r32 * PITCH + i * 32 + q * 8 + half * 4) =
                     f32x4{acc[j][i][q * 4], acc[j][i][q * 4 + 1], acc[j][i][q * 4 + 2], acc[j][i][q * 4 + 3]};
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
-#pragma unroll
+#pragma unroll 1
         for (int h = 0; h < 32 / ROWS; ++h) {
             const int r = h * ROWS + row;
             const int64_t m = m0 + wm + j * 32 + r;
@@ -400,13 +415,15 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_linear_product(c
     const GemmArgs& g = pair.g[at.second];
     const int64_t m0 = (int64_t)at.tm * BM, n0 = (int64_t)at.tn * BN;
     const int split = at.split;
+    f32x16 acc[WM / 32][WN / 32] = {};
     if (g.p.a.along) {
-        if (g.p.b.along) product_tile<E, BM, BN, WM, WN, DEPTH, true, true>(g, lds, m0, n0, split);
-        else product_tile<E, BM, BN, WM, WN, DEPTH, true, false>(g, lds, m0, n0, split);
+        if (g.p.b.along) product_tile<E, BM, BN, WM, WN, DEPTH, true, true>(g, lds, m0, n0, split, acc);
+        else product_tile<E, BM, BN, WM, WN, DEPTH, true, false>(g, lds, m0, n0, split, acc);
     } else {
-        if (g.p.b.along) product_tile<E, BM, BN, WM, WN, DEPTH, false, true>(g, lds, m0, n0, split);
-        else product_tile<E, BM, BN, WM, WN, DEPTH, false, false>(g, lds, m0, n0, split);
+        if (g.p.b.along) product_tile<E, BM, BN, WM, WN, DEPTH, false, true>(g, lds, m0, n0, split, acc);
+        else product_tile<E, BM, BN, WM, WN, DEPTH, false, false>(g, lds, m0, n0, split, acc);
     }
+    tile_out<BM, BN, WM, WN, DEPTH>(g, lds, m0, n0, split, acc);
 }
 
 // ------------------------------------------------------------------------------------------------- small tiles
@@ -465,7 +482,7 @@ template <class E, bool ALONG> struct LooseTile {
 };
 
 template <class E, bool A_ALONG, bool B_ALONG, bool LOOSE, bool DEEP>
-__device__ __forceinline__ void small_tile(const GemmArgs& g, char* lds, int64_t m0, int64_t n0, int split)
+__device__ __forceinline__ void small_tile(const GemmArgs& g, char* lds, int64_t m0, int64_t n0, int split, f32x16& acc)
 {
     constexpr int DEPTH = LOOSE ? 2 : DEEP ? 8 : 4, AHEAD = DEEP ? 8 : 4;
     const LinearProduct& p = g.p;
@@ -474,9 +491,8 @@ __device__ __forceinline__ void small_tile(const GemmArgs& g, char* lds, int64_t
     const int turns = (last - first + SMALL_GROUPS - 1) / SMALL_GROUPS;
     char* const own = lds + group * DEPTH * SMALL_BUF;
     auto stage_of = [&](int turn) { return first + turn * SMALL_GROUPS + group; };
-    const Tile<E, B_ALONG, SMALL, 4, 1> channels(p.b, n0, p.n, p.k, lane, w4, 0);
-    const Tile<E, A_ALONG, SMALL, 4, 1> tokens(p.a, m0, p.m, p.k, lane, w4, 0);
-    f32x16 acc = {};
+    Tile<E, B_ALONG, SMALL, 4, 1> channels(p.b, n0, p.n, p.k, lane, w4, 0, first + group, SMALL_GROUPS);
+    Tile<E, A_ALONG, SMALL, 4, 1> tokens(p.a, m0, p.m, p.k, lane, w4, 0, first + group, SMALL_GROUPS);
     auto multiply = [&](const char* buf) {
         i32x4 a[1], b[1];
         channels.fetch(buf, w4, lane, a);
@@ -509,8 +525,8 @@ __device__ __forceinline__ void small_tile(const GemmArgs& g, char* lds, int64_t
         auto ask = [&](int turn) {
             if (stage_of(turn) >= last) return;
             char* const buf = own + turn % DEPTH * SMALL_BUF;
-            channels.load(stage_of(turn), buf, w4);
-            tokens.load(stage_of(turn), buf + SMALL * STAGE, w4);
+            channels.load(buf, w4);
+            tokens.load(buf + SMALL * STAGE, w4);
         };
 #pragma unroll
         for (int t = 0; t < DEPTH - 1; ++t) ask(t);
@@ -523,6 +539,12 @@ __device__ __forceinline__ void small_tile(const GemmArgs& g, char* lds, int64_t
             if (stage_of(t) < last) multiply(own + t % DEPTH * SMALL_BUF);
         }
     }
+}
+
+__device__ __forceinline__ void small_out(const GemmArgs& g, char* lds, int64_t m0, int64_t n0, int split, const f32x16& acc)
+{
+    const LinearProduct& p = g.p;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     __syncthreads();
     constexpr int PITCH = SMALL + 4;
     float* const sums = (float*)lds;
@@ -554,13 +576,15 @@ template <class E, bool LOOSE, bool DEEP> __global__ __launch_bounds__(SMALL_THR
     const Place at = place_of(pair);
     const GemmArgs& g = pair.g[at.second];
     const int64_t m0 = (int64_t)at.tm * SMALL, n0 = (int64_t)at.tn * SMALL;
+    f32x16 acc = {};
     if (g.p.a.along) {
-        if (g.p.b.along) small_tile<E, true, true, LOOSE, DEEP>(g, lds, m0, n0, at.split);
-        else small_tile<E, true, false, LOOSE, DEEP>(g, lds, m0, n0, at.split);
+        if (g.p.b.along) small_tile<E, true, true, LOOSE, DEEP>(g, lds, m0, n0, at.split, acc);
+        else small_tile<E, true, false, LOOSE, DEEP>(g, lds, m0, n0, at.split, acc);
     } else {
-        if (g.p.b.along) small_tile<E, false, true, LOOSE, DEEP>(g, lds, m0, n0, at.split);
-        else small_tile<E, false, false, LOOSE, DEEP>(g, lds, m0, n0, at.split);
+        if (g.p.b.along) small_tile<E, false, true, LOOSE, DEEP>(g, lds, m0, n0, at.split, acc);
+        else small_tile<E, false, false, LOOSE, DEEP>(g, lds, m0, n0, at.split, acc);
     }
+    small_out(g, lds, m0, n0, at.split, acc);
 }
 
 // The slabs of split products, added in one order, and what the product's own way out does otherwise: runs of COUNT of a row.  GROUPS threads
