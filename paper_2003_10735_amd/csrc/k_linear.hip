@@ -312,9 +312,9 @@ __device__ __forceinline__ void product_tile(const GemmArgs& g, char* lds, int64
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         }
     };
-    // DEPTH stages are under way.  A stage's last step has its operands in registers when the barrier is passed, so what follows the
-    // barrier is: the loads of the stage DEPTH later into the buffer that is done with, the next stage's first operands, the last step's
-    // products.
+    // DEPTH stages are under way.  A stage's last step has its operands in registers when the barrier is passed; what follows the barrier
+    // is the loads of the stage DEPTH later into the buffer that is done with, and the next stage's first operands.  (8192 tokens 4096 -> 14336
+    // with the last step's products before the barrier 814 us, behind these loads 828; half stages, twice as many, 870.)
     constexpr int LOADS = Channels::LOADS + Tokens::LOADS;      // of a wavefront and stage
     static_assert((DEPTH - 1) * LOADS < 64, "the counter of loads under way");
     if (first < last) {
@@ -336,11 +336,11 @@ __device__ __forceinline__ void product_tile(const GemmArgs& g, char* lds, int64
         // the next stage is there (behind it DEPTH - 2 may still be on their way), this one is read
         if (DEPTH > 2 && s + DEPTH <= last) ST_WAIT_VM((DEPTH - 2) * LOADS); else ST_WAIT_VM(0);
         __builtin_amdgcn_s_waitcnt(0xc07f);    // lgkmcnt(0)
+        multiply((STEPS - 1) & 1);
         ST_BARRIER();
         if (s + DEPTH < last) next_stage(buf);
         buf = buf + 1 == DEPTH ? 0 : buf + 1;
         if (s + 1 < last) fetch(buf, 0, 0);
-        multiply((STEPS - 1) & 1);
     }
 
 }
@@ -445,12 +445,12 @@ constexpr size_t small_lds(bool loose, bool deep)
 template <class E, bool ALONG> struct LooseTile {
     static constexpr int CH = 16 / sizeof(E), KS = STAGE / sizeof(E);
     using Chunk = Run<E, CH>;
-    const E* base; int64_t pitch, k;
+    const E* base; int64_t pitch, k;      // k: positions of the contraction that can be read
     int position;                // of the chunk in a stage's contraction
     int down;                    // across: by how much the row's last chunk is moved; along: nothing
     __device__ __forceinline__ LooseTile(const Operand& o, int64_t row0, int64_t rows, int64_t len, int lane, int wave)
     {
-        pitch = o.pitch; k = len;
+        pitch = o.pitch; k = ALONG ? o.inner : len;
         if constexpr (ALONG) {
             position = ((lane & 7) ^ ((lane >> 4) + 4 * (wave & 1))) * CH;
             base = (const E*)o.p + std::min<int64_t>(row0 + wave * 8 + (lane >> 3), rows - 1) * pitch;
@@ -458,7 +458,7 @@ template <class E, bool ALONG> struct LooseTile {
         } else {
             constexpr int LANES = SMALL / CH;
             position = wave * (64 / LANES) + lane / LANES;
-            const int64_t at = row0 + (lane % LANES) * CH, from = std::min(at, rows - CH);
+            const int64_t at = row0 + (lane % LANES) * CH, from = std::min(at, o.inner - CH);
             base = (const E*)o.p + from;
             down = (int)std::min<int64_t>(at - from, CH);
         }

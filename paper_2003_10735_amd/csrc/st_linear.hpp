@@ -65,8 +65,8 @@ template <int ACT> __device__ __forceinline__ float slope_times(float dy, float 
 
 // ------------------------------------------------------------------ operands of a product
 // Rows of an operand, `pitch` elements apart: along == 1, a row's values (the contraction) lie next to each other; 0: the values of one
-// position of the contraction do.
-struct Operand { const void* p; int64_t pitch; int along; };
+// position of the contraction do.  inner: how many values next to each other can be read, 16 bytes of them at least.
+struct Operand { const void* p; int64_t pitch; int along; int64_t inner; };
 // What the products take of a matrix with `inner` values next to each other: 16-byte aligned, whole 16-byte chunks between two runs, a
 // contraction of whole chunks where it lies along memory, and tiles that 32-bit offsets reach.  (Across, a position behind the last one has
 // to lie behind the buffer's end: runs do not overlap.)

@@ -56,13 +56,13 @@ Operand operand_of(const st_matrix& x, int along, bool by_rows, bool small, int*
     const Lie l = lie_of(x, along, by_rows);
     const int64_t outer = l.outer, inner = l.inner, pitch = l.pitch;
     const int k_along = l.k_along;
-    if (l.direct) return Operand{x.data, pitch, k_along};
-    if (small && inner >= 16 / es) { *loose = 1; return Operand{x.data, pitch, k_along}; }
+    if (l.direct) return Operand{x.data, pitch, k_along, round_up(inner, 16 / es)};      // (whole aligned chunks are there)
+    if (small && inner >= 16 / es) { *loose = 1; return Operand{x.data, pitch, k_along, inner}; }
     const bool turn = !operand_direct(nullptr, round_up(inner, 8), k_along, round_up(inner, 8), es);
     const int64_t to_pitch = round_up(turn ? outer : inner, 8);
     void* to = w.take((size_t)(turn ? inner : outer) * to_pitch * es);
     packs->t[packs->n++] = PackTask{x.data, outer, inner, pitch, to, to_pitch, turn};
-    return Operand{to, to_pitch, turn ? !k_along : k_along};
+    return Operand{to, to_pitch, turn ? !k_along : k_along, to_pitch};
 }
 size_t slab_bytes(const Extent* e, const LinearForm& f, int which)
 {
@@ -87,8 +87,8 @@ LinearPlan plan_linear(const st_matrix& x, int x_along, const st_matrix& w, int 
     Carve c{ws};
     l.few = w_along && linear_few(p.m, p.n, p.k, is_bf16);
     if (l.few) {
-        p.a = Operand{x.data, x_along ? x.row_stride : x.col_stride, x_along};
-        p.b = Operand{w.data, w.row_stride, 1};
+        p.a = Operand{x.data, x_along ? x.row_stride : x.col_stride, x_along, x_along ? p.k : p.m};
+        p.b = Operand{w.data, w.row_stride, 1, p.k};
     } else {
         const Extent e{p.m, p.n, p.k};
         l.form = linear_form(&e, 1, is_bf16, !lie_of(x, x_along, true).direct || !lie_of(w, w_along, true).direct);
@@ -127,15 +127,15 @@ BackwardPlan plan_backward(const st_matrix* x, int x_along, const st_matrix* w, 
     if ((x || w) && !as_it_is) {
         s.to_pitch = round_up(n, 8);
         s.to = c.take((size_t)m * s.to_pitch * elem(dtype));
-        by_tokens = Operand{s.to, s.to_pitch, 1};
-        by_channels = Operand{s.to, s.to_pitch, 0};
+        by_tokens = Operand{s.to, s.to_pitch, 1, s.to_pitch};
+        by_channels = Operand{s.to, s.to_pitch, 0, s.to_pitch};
     } else {
         if (w) by_tokens = operand_of(dy, dy_along, true, small, &loose, c, &b.packs);
         // the same matrix read the other way round, if it can be (the rows of a copy end in zeros)
         const bool copied = w && by_tokens.p != dy.data;
         const int64_t pitch = by_tokens.pitch;
         if (w && operand_direct(by_tokens.p, pitch, !by_tokens.along, by_tokens.along ? n : copied ? round_up(m, 8) : m, elem(dtype)))
-            by_channels = Operand{by_tokens.p, pitch, !by_tokens.along};
+            by_channels = Operand{by_tokens.p, pitch, !by_tokens.along, by_tokens.inner};
         else if (x) by_channels = operand_of(dy, dy_along, false, small, &loose, c, &b.packs);
     }
     if (db) {

@@ -1,4 +1,5 @@
-"""A trainable 1x1 layer between a frozen front part's features and the head, trained together with the head.
+"""Trainable parts between a frozen front part's features and the head, trained together with the head: a 1x1 layer in 8-bit integers
+(DenseFront) and a residual block of two layers in bfloat16 (DenseBlockFront).
 
 The layer maps every cell of the feature map (a token) from the front's channels to the head's.  Its products run in 8-bit integers
 (st_int8_linear, st_int8_linear_backward), its gradient comes from the head's full backward pass (st_partial_distill with feature_grad),
@@ -81,3 +82,86 @@ class DenseFront:
             self._last.record()
         st.st_int8_quantize(self.weight, *self.quantized)
         return self.loss[0]
+
+
+class DenseBlockFront:
+    """features = cells + act(cells W1^T + b1) W2^T + b2 for every cell of the feature map: two st_linear, the second with the residual in its
+    epilogue.  w1 [hidden, desc.c_in], b1 [hidden], w2 [desc.c_in, hidden], b2 [desc.c_in] are float32 and used in place; the products take
+    bfloat16 copies of the matrices, which the optimiser's step writes.  desc describes the head behind the block (its feature type and
+    layout are chosen here: bfloat16, channels last).
+
+    backward() adds one key frame's (or batch's) gradients to those that are there; apply() brings their sum over the frames to its mean, clips
+    it by the norm over all four tensors (st_grad_clip: the matrices and the biases are two lists of the optimiser, whose states have
+    state_bits and 32 bits) and steps.  step() does both.  A list whose own gradients hold a value that is not finite takes no step."""
+
+    def __init__(self, desc: st.HeadDesc, w1, b1, w2, b2, activation: int = st.ST_ACT_GELU, lr: float = 1e-3, weight_decay: float = 0.0,
+                 max_norm: float = 1.0, state_bits: int = 8):
+        import torch
+        self.desc = replace(desc, feat_dtype=st.ST_BF16, feat_layout=st.ST_NHWC)
+        self.params, self.activation, self.lr, self.max_norm = (w1, b1, w2, b2), activation, lr, max_norm
+        self.frames, self.steps = 0, 0           # of the gradients that are there; steps enqueued
+        d, device = self.desc, w1.device
+        hidden, cells = w1.shape[0], d.n * d.h * d.w
+        self.grads = [torch.zeros_like(p) for p in self.params]
+        dw1, db1, dw2, db2 = self.grads
+        self.copies = [w.to(torch.bfloat16) for w in (w1, w2)]
+        self.matrices = st.AdamWTensors([w1, w2], [dw1, dw2], copies=self.copies, weight_decay=weight_decay, **st.new_adamw_state([w1, w2], state_bits))
+        self.biases = st.AdamWTensors([b1, b2], [db1, db2], **st.new_adamw_state([b1, b2], 32))
+        self.all_grads = st.GradTensors(self.grads)
+        empty = lambda *shape, dtype=torch.bfloat16: torch.empty(shape, dtype=dtype, device=device)      # noqa: E731
+        self.features = empty(d.n, d.h, d.w, d.c_in)
+        self.feature_grad = empty(d.n, d.c_in, d.h, d.w, dtype=torch.float32)
+        self.pre, self.hidden, self.hidden_grad = (empty(cells, hidden) for _ in range(3))
+        self.loss, self.grad_norm = empty(2, dtype=torch.float32), empty(1, dtype=torch.float32)
+        self.workspace = st.new_workspace(self.desc, device)
+        self.norm_workspace = st.new_grad_workspace(self.all_grads)
+        self.step_workspaces = [st.new_adamw_workspace(t) for t in (self.matrices, self.biases)]
+        self.linear_workspaces = None
+
+    def forward(self, cells):
+        """cells [n*h*w, desc.c_in] bfloat16 -> the head's features [n, h, w, c_in] bfloat16."""
+        w1, w2 = self.copies
+        _, b1, _, b2 = self.params
+        y = self.features.view(-1, self.desc.c_in)
+        if self.linear_workspaces is None:       # for cells that lie as these do
+            dy = self._feature_rows()
+            self.linear_workspaces = (st.new_linear_workspace(cells, w1), st.new_linear_workspace(self.hidden, w2),
+                                      st.new_linear_workspace(self.hidden, w2, dy), st.new_linear_workspace(cells, None, self.hidden_grad, self.activation))
+        ws = self.linear_workspaces
+        st.st_linear(cells, w1, b1, self.activation, pre=self.pre, out=self.hidden, workspace=ws[0])
+        st.st_linear(self.hidden, w2, b2, residual=cells, out=y, workspace=ws[1])
+        return self.features
+
+    def _feature_rows(self):
+        """The head's gradient of the features, a cell a row.  (One frame's lies channel by channel: its cells' rows are its columns.)"""
+        d, g = self.desc, self.feature_grad
+        return g[0].view(d.c_in, d.h * d.w).t() if d.n == 1 else g.permute(0, 2, 3, 1).reshape(-1, d.c_in)
+
+    def backward(self, cells, labels, head_params, head_lr: float):
+        """Forward pass, the head's step on one key frame (or batch), and the block's gradients, added to those of earlier frames.  Returns
+        the loss before the head's step (on the device)."""
+        st.st_partial_distill(self.desc, self.forward(cells), labels, head_params, 1, head_lr, losses=self.loss, feature_grad=self.feature_grad,
+                              workspace=self.workspace)
+        dw1, db1, dw2, db2 = self.grads
+        more, ws = self.frames > 0, self.linear_workspaces
+        st.st_linear_backward(self.hidden, self.copies[1], self._feature_rows(), dx=self.hidden_grad, dw=dw2, db=db2, accumulate=more, workspace=ws[2])
+        st.st_linear_backward(cells, None, self.hidden_grad, self.pre, self.activation, dw=dw1, db=db1, accumulate=more, workspace=ws[3])
+        self.frames += 1
+        return self.loss[0]
+
+    def apply(self):
+        """One step with the mean of the gradients that are there."""
+        if not self.frames:
+            return
+        st.st_grad_clip(self.all_grads, max_norm=self.max_norm, grad_scale=1.0 / self.frames, grad_norm=self.grad_norm, workspace=self.norm_workspace)
+        self.frames = 0
+        self.steps += 1
+        for tensors, ws in zip((self.matrices, self.biases), self.step_workspaces):
+            # (a limit that nothing finite reaches: a list with other values is left out)
+            st.st_adamw_step(tensors, self.steps, self.lr, max_norm=3e38, workspace=ws)
+
+    def step(self, cells, labels, head_params, head_lr: float):
+        """backward() and apply().  Returns the loss before the step (on the device)."""
+        loss = self.backward(cells, labels, head_params, head_lr)
+        self.apply()
+        return loss
