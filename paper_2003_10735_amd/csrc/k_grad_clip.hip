@@ -81,52 +81,82 @@ __device__ __forceinline__ ClipFactor clip_factor(const ClipRule& r, const doubl
     return {norm, r.max_norm > 0 && norm > r.max_norm && norm < __builtin_inf() ? r.scale * (r.max_norm / norm) : r.scale};
 }
 
-template <class G, class O, int RUNS> __device__ __forceinline__ void tile_scaled(const void* p, void* q, long long n, long long base, double factor)
+// A thread's values of a tile on their way: asked for, and later scaled and stored.  Runs are as long as 16 bytes of the wider of the two
+// types, so that a wavefront's stores are whole lines: eight values where both are bfloat16, else four.  (436 M bfloat16 values into float32 with runs
+// of eight 299 us, most of it in halves of lines.)
+template <int RUNS> struct Pending { Run<bf16, 8> b8[RUNS]; Run<bf16, 4> b4[2 * RUNS]; Run<float, 4> f4[2 * RUNS]; };
+constexpr int BOTH_BF16 = 3;
+template <int V> __device__ __forceinline__ long long run_at(long long tile_base, int j) { return tile_base + j * (256 * V) + threadIdx.x * V; }
+template <int V, class G, int COUNT> __device__ __forceinline__ void ask_runs(const void* g, long long n, long long base, Run<G, V> (&v)[COUNT])
 {
-    Raw8<G> v[RUNS];
-    load_row((const G*)p, n, [&](int j) { return base + j * 2048; }, v);
+    if (n < V) {
+#pragma unroll
+        for (int j = 0; j < COUNT; ++j) { const long long at = run_at<V>(base, j); v[j].load_short((const G*)g + at, at < n ? (int)(n - at) : 0); }
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < COUNT; ++j) v[j].template load<true>((const G*)g + run_start<V, long long>(run_at<V>(base, j), n));
+}
+template <int RUNS> __device__ __forceinline__ void ask_tile(const ClipList& l, unsigned tile, int i, Pending<RUNS>& p)
+{
+    const long long base = (long long)(tile - l.first[i]) * (RUNS * 2048);
+    if (l.types[i] == BOTH_BF16) ask_runs<8>(l.g[i], l.n[i], base, p.b8);
+    else if (l.types[i] & 1) ask_runs<4>(l.g[i], l.n[i], base, p.b4);
+    else ask_runs<4>(l.g[i], l.n[i], base, p.f4);
+}
+template <class O, int V, class G, int COUNT> __device__ __forceinline__ void store_runs(void* q, long long n, long long base, Run<G, V> (&v)[COUNT], float c1, float c2)
+{
     O* o = (O*)q;
-    // (a factor that float32 does not hold is applied in two steps)
-    const float c = (float)factor;
-    const bool plain = fabsf(c) >= 0x1p-120f || factor == 0.0;
-    const float c1 = plain ? c : (float)(factor * 0x1p100), c2 = plain ? 1.f : 0x1p-100f;
 #pragma unroll
-    for (int j = 0; j < RUNS; ++j) {
-        const long long at = base + j * 2048;
-        float u[8];
+    for (int j = 0; j < COUNT; ++j) {
+        const long long at = run_at<V>(base, j);
+        if (at >= n) continue;
+        if (at + V > n && n >= V) v[j].down((int)(at - (n - V)));
+        float u[V];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) u[k] = v[j][k] * c1 * c2;
-        if (at + 8 <= n) {
-            typedef O O4 __attribute__((ext_vector_type(4)));
-            typedef O4 O4any __attribute__((aligned(sizeof(O))));
+        for (int k = 0; k < V; ++k) u[k] = v[j][k] * c1 * c2;
+        if (at + V <= n) {
+            typedef O OV __attribute__((ext_vector_type(V)));
+            typedef OV OVany __attribute__((aligned(sizeof(O))));
+            OV w;
 #pragma unroll
-            for (int k = 0; k < 8; k += 4)
-                __builtin_nontemporal_store(O4{from_f32<O>(u[k]), from_f32<O>(u[k + 1]), from_f32<O>(u[k + 2]), from_f32<O>(u[k + 3])}, (O4any*)(o + at + k));
+            for (int k = 0; k < V; ++k) w[k] = from_f32<O>(u[k]);
+            __builtin_nontemporal_store(w, (OVany*)(o + at));
         } else
 #pragma unroll
-            for (int k = 0; k < 8; ++k) if (at + k < n) o[at + k] = from_f32<O>(u[k]);
+            for (int k = 0; k < V; ++k) if (at + k < n) o[at + k] = from_f32<O>(u[k]);
     }
 }
+template <int RUNS> __device__ __forceinline__ void store_tile(const ClipList& l, unsigned tile, int i, Pending<RUNS>& p, float c1, float c2)
+{
+    const long long n = l.n[i], base = (long long)(tile - l.first[i]) * (RUNS * 2048);
+    switch (l.types[i]) {
+    case 0: store_runs<float, 4>(l.out[i], n, base, p.f4, c1, c2); break;
+    case 1: store_runs<float, 4>(l.out[i], n, base, p.b4, c1, c2); break;
+    case 2: store_runs<bf16, 4>(l.out[i], n, base, p.f4, c1, c2); break;
+    default: store_runs<bf16, 8>(l.out[i], n, base, p.b8, c1, c2); break;
+    }
+}
+// The blocks go through the list side by side; a block's first tile is on its way while it adds the norm's parts.
 template <int RUNS> __global__ __launch_bounds__(256) void k_clip_scale(const ClipList l, const ClipRule r, unsigned tiles, const double* __restrict__ parts, int n_parts)
 {
     __shared__ double sums[4];
+    Pending<RUNS> p;
+    unsigned tile = blockIdx.x;
+    int i = tile < tiles ? __builtin_amdgcn_readfirstlane(clip_tensor(l, tile)) : 0;
+    if (tile < tiles) ask_tile(l, tile, i, p);
     const ClipFactor c = clip_factor(r, parts, n_parts, sums);
     if (r.norm && blockIdx.x == 0 && threadIdx.x == 0) *r.norm = (float)c.norm;
-    const unsigned each = tiles / gridDim.x, rest = tiles - each * gridDim.x;
-    unsigned tile = blockIdx.x * each + min(blockIdx.x, rest);
-    const unsigned end = tile + each + (blockIdx.x < rest ? 1 : 0);
-    if (tile == end) return;
-    int i = __builtin_amdgcn_readfirstlane(clip_tensor(l, tile));
-    for (; tile < end; ++tile) {
+    // (a factor that float32 does not hold is applied in two steps)
+    const float factor = (float)c.factor;
+    const bool plain = fabsf(factor) >= 0x1p-120f;
+    const float c1 = plain ? factor : (float)(c.factor * 0x1p100), c2 = plain ? 1.f : 0x1p-100f;
+    while (tile < tiles) {
+        if (c.factor != 1.0 || l.g[i] != l.out[i]) store_tile(l, tile, i, p, c1, c2);
+        tile += gridDim.x;
+        if (tile >= tiles) break;
         while (i + 1 < l.count && tile >= l.first[i + 1]) ++i;
-        if (c.factor == 1.0 && l.g[i] == l.out[i]) continue;
-        const long long base = (long long)(tile - l.first[i]) * (RUNS * 2048) + threadIdx.x * 8;
-        switch (l.types[i]) {
-        case 0: tile_scaled<float, float, RUNS>(l.g[i], l.out[i], l.n[i], base, c.factor); break;
-        case 1: tile_scaled<bf16, float, RUNS>(l.g[i], l.out[i], l.n[i], base, c.factor); break;
-        case 2: tile_scaled<float, bf16, RUNS>(l.g[i], l.out[i], l.n[i], base, c.factor); break;
-        default: tile_scaled<bf16, bf16, RUNS>(l.g[i], l.out[i], l.n[i], base, c.factor); break;
-        }
+        ask_tile(l, tile, i, p);
     }
 }
 

@@ -743,40 +743,43 @@ void linear_product_few(Ctx& c, const LinearProduct& p, int is_bf16)
 }
 
 // --------------------------------------------------------------------------------------- choice of tile and split
-static int64_t tiles_of(const Extent& e, int tile) { return ceil_div(e.m, tile) * ceil_div(e.n, tile); }
-LinearForm linear_form(const Extent* e, int count, int is_bf16, bool odd)
+// What a call is estimated to take, us: a stage of 128 bytes of a tile takes `stage` of a compute unit's time (as much where it is alone as
+// where two blocks share the unit's throughput), a block `block` to begin and to end; half of what blocks leave idle that do not divide among 256
+// compute units is lost; parts of a split contraction cost a join, copies of odd operands a launch and their bytes.  Fitted to 140 forward and
+// backward calls of 33 .. 12000 tokens, 96 .. 14336 channels, each with every tile and 1 .. 16 splits: what it chooses takes 1.03 (float32 1.04) times
+// the best of them, geometric mean, where thresholds on the number of tiles took 1.06 (1.13).
+struct TileCost { int tile; double stage[2], block[2]; };      // float32, bfloat16
+constexpr TileCost TILE_COSTS[] = {{SMALL, {0.20, 0.13}, {1.0, 1.0}}, {64, {0.64, 0.26}, {0.6, 0.6}}, {128, {2.24, 0.57}, {1.5, 1.0}}, {256, {8.2, 1.72}, {5.0, 5.0}}};
+constexpr double JOIN_US = 4.0, JOIN_BYTE_US = 3e-7, COPY_US = 1.5, COPY_BYTE_US = 6e-7;
+constexpr int MOST_SPLITS = 32, LEAST_STAGES = 8;
+LinearForm linear_form(const Extent* e, int count, int is_bf16, int64_t copied, bool prepared)
 {
-    const int64_t per_stage = is_bf16 ? STAGE / 2 : STAGE / 4;
-    auto total = [&](int tile) { int64_t t = 0; for (int i = 0; i < count; ++i) t += tiles_of(e[i], tile); return t; };
-    auto stages_of = [&](int tile) { int64_t w = 0; for (int i = 0; i < count; ++i) w += tiles_of(e[i], tile) * ceil_div(e[i].k, per_stage); return w; };
-    LinearForm f = {64, {1, 1}};
-    if (total(256) >= 192 && stages_of(256) > 5 * total(256)) f.tile = 256;
-    else if (total(SMALL) <= (odd ? 800 : 512)) f.tile = SMALL;
-    else if (total(64) > 512) f.tile = 128;
-    for (int i = 0; i < count; ++i) f.splits[i] = 1;
-    if (f.tile == SMALL) {
-        // Stages a compute unit goes through, and what a join costs in them: us a stage about 0.13 (float32 0.2), a join 4.
-        const int64_t join = is_bf16 ? 30 : 20;
-        int64_t longest = 0, least = INT64_MAX, best = 1;
-        for (int i = 0; i < count; ++i) longest = std::max(longest, ceil_div(e[i].k, per_stage));
-        for (int64_t s = 1; s <= 16 && (s == 1 || longest >= 8 * s); s *= 2) {
+    LinearForm best = {64, {1, 1}};
+    double least = 1e300;
+    int64_t stages[2] = {1, 1}, longest = 1;
+    for (int i = 0; i < count; ++i) { stages[i] = ceil_div(e[i].k * (is_bf16 ? 2 : 4), STAGE); longest = std::max(longest, stages[i]); }
+    for (const TileCost& c : TILE_COSTS)
+        for (int64_t s = 1; s <= MOST_SPLITS && (s == 1 || longest >= LEAST_STAGES * s); s *= 2) {
+            const double stage = c.stage[is_bf16], block = c.block[is_bf16];
+            LinearForm f = {c.tile, {1, 1}};
+            double work = 0, alone = 0, slabs = 0;
             int64_t blocks = 0;
-            for (int i = 0; i < count; ++i) blocks += tiles_of(e[i], SMALL) * std::max<int64_t>(1, std::min(s, ceil_div(e[i].k, per_stage) * s / longest));
-            const int64_t cost = ceil_div(blocks, 256) * ceil_div(longest, s) + (s > 1 ? join + s : 0);
-            if (cost < least) { least = cost; best = s; }
+            bool joined = false;
+            for (int i = 0; i < count; ++i) {
+                const int64_t tiles = ceil_div(e[i].m, c.tile) * ceil_div(e[i].n, c.tile), k = std::max<int64_t>(1, std::min(s, stages[i] * s / longest));
+                f.splits[i] = (int)k;
+                work += (double)(tiles * stages[i]);
+                blocks += tiles * k;
+                alone = std::max(alone, (double)(ceil_div(stages[i], k) * ceil_div(tiles * k, c.tile == 256 ? 256 : 512)) * stage);
+                if (k > 1) { joined = true; slabs += (double)e[i].m * e[i].n * k * 4; }
+            }
+            if (c.tile == SMALL && blocks > 2048) continue;      // (43 tokens, gradients of 1601 -> 2582: 4233 of them, 28 us, 128 x 128 13)
+            const double rounds = (double)ceil_div(blocks, 256), idle = rounds * 256 / blocks - 1;
+            const double us = std::max(work * stage / 256 * (1 + 0.5 * idle) + rounds * block, alone + block) + (joined ? JOIN_US + slabs * JOIN_BYTE_US : 0)
+                              + (c.tile != SMALL && copied ? (prepared ? 0 : COPY_US) + copied * COPY_BYTE_US : 0);
+            if (us < least) { least = us; best = f; }
         }
-        for (int i = 0; i < count; ++i) f.splits[i] = (int)std::max<int64_t>(1, std::min(best, ceil_div(e[i].k, per_stage) * best / longest));
-        return f;
-    }
-    // every block about the same number of stages, 256 blocks, eight stages each at least
-    const int64_t each = std::max<int64_t>(8, ceil_div(stages_of(f.tile), 256));
-    for (int i = 0; i < count; ++i) {
-        const int64_t stages = ceil_div(e[i].k, per_stage);
-        int64_t s = stages > 16 ? stages / each : 1;
-        if (count > 1 && f.tile == 128 && s == 1 && stages >= each + 20) s = 2;
-        f.splits[i] = (int)std::max<int64_t>(s, 1);
-    }
-    return f;
+    return best;
 }
 
 template <class E, int BM, int BN, int WM, int WN, int DEPTH>

@@ -8,57 +8,57 @@
 namespace st {
 
 // ------------------------------------------------------------------------------------------------------ copies
-// Eight values a thread along memory, 64 runs of 64 values a block.  `turn`: through LDS, the other way round.
+// Eight values a thread along memory: 32 runs of 256 values a block, all of its loads under way at once.  `turn`: 64 x 64 through LDS, the other
+// way round.
 struct PackArgs { PackTask t[PACK_TASKS]; unsigned first[PACK_TASKS + 1], across[PACK_TASKS]; int count; };      // first block of each; blocks along a run
+constexpr int PACK_RUNS = 32, PACK_VALUES = 256, TURN = 64;
 
 template <class E> __device__ __forceinline__ void pack_block(const PackArgs& a, unsigned at_block, char* lds)
 {
-    E (*turned)[64 + 16 / sizeof(E)] = (E(*)[64 + 16 / sizeof(E)])lds;
     int i = 0;
     while (i + 1 < a.count && at_block >= a.first[i + 1]) ++i;
     const PackTask& t = a.t[i];
-    const unsigned block = at_block - a.first[i];
-    const int64_t o0 = (int64_t)(block / a.across[i]) * 64, i0 = (int64_t)(block % a.across[i]) * 64;
-    const int run = threadIdx.x & 7, row = threadIdx.x >> 3;
-    Raw8<E> v[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int64_t o = std::min(o0 + h * 32 + row, t.outer - 1), at = i0 + run * 8;
-        const E* x = (const E*)t.x + o * t.pitch;
-        if (t.inner < 8) v[h].load_short(x + at, at < t.inner ? (int)(t.inner - at) : 0);
-        else {
-            v[h].load(x + run_start<8, int64_t>(at, t.inner));
-            const int64_t d = at - (t.inner - 8);
-            if (d > 0) v[h].down(d < 8 ? (int)d : 8);
-        }
-    }
+    const unsigned block = at_block - a.first[i], down = block / a.across[i], along = block - down * a.across[i];
+    const int ROWS = t.turn ? TURN : PACK_RUNS, VALUES = t.turn ? TURN : PACK_VALUES, LANES = VALUES / 8;
+    const int64_t o0 = (int64_t)down * ROWS, i0 = (int64_t)along * VALUES;
+    const int run = threadIdx.x % LANES, row = threadIdx.x / LANES, step = 256 / LANES;
     typedef E E8 __attribute__((ext_vector_type(8)));
     E* const to = (E*)t.to;
-    if (!t.turn) {
+    constexpr int COUNT = PACK_RUNS * PACK_VALUES / 8 / 256;      // (turned: two of them)
+    Raw8<E> v[COUNT];
+    const int64_t at = i0 + run * 8;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t o = o0 + h * 32 + row, at = i0 + run * 8;
-            if (o >= t.outer || at >= t.to_pitch) continue;
-            E8 u;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] = from_f32<E>(v[h][e]);
-            *(E8*)(to + o * t.to_pitch + at) = u;      // (pitches are multiples of eight)
-        }
-        return;
+    for (int h = 0; h < COUNT; ++h) {
+        if (h * step >= ROWS) break;
+        const E* x = (const E*)t.x + std::min(o0 + h * step + row, t.outer - 1) * t.pitch;
+        if (t.inner < 8) v[h].load_short(x + at, at < t.inner ? (int)(t.inner - at) : 0);
+        else v[h].load(x + run_start<8, int64_t>(at, t.inner));
     }
+    const int64_t d = t.inner < 8 ? 0 : at - (t.inner - 8);
+    E (*turned)[TURN + 16 / sizeof(E)] = (E(*)[TURN + 16 / sizeof(E)])lds;
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < COUNT; ++h) {
+        if (h * step >= ROWS) break;
+        if (d > 0) v[h].down(d < 8 ? (int)d : 8);
+        const int64_t o = o0 + h * step + row;
+        E8 u;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) turned[run * 8 + e][h * 32 + row] = o0 + h * 32 + row < t.outer ? from_f32<E>(v[h][e]) : from_f32<E>(0.f);
+        for (int e = 0; e < 8; ++e) u[e] = from_f32<E>(v[h][e]);
+        if (!t.turn) { if (o < t.outer && at < t.to_pitch) *(E8*)(to + o * t.to_pitch + at) = u; }      // (pitches are multiples of eight)
+        else
+#pragma unroll
+            for (int e = 0; e < 8; ++e) turned[run * 8 + e][h * step + row] = o < t.outer ? u[e] : from_f32<E>(0.f);
+    }
+    if (!t.turn) return;
     __syncthreads();
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const int64_t i1 = i0 + h * 32 + row, at = o0 + run * 8;
-        if (i1 >= t.inner || at >= t.to_pitch) continue;
+        const int64_t i1 = i0 + h * 32 + row, o1 = o0 + run * 8;
+        if (i1 >= t.inner || o1 >= t.to_pitch) continue;
         E8 u;
 #pragma unroll
         for (int e = 0; e < 8; ++e) u[e] = turned[h * 32 + row][run * 8 + e];
-        *(E8*)(to + i1 * t.to_pitch + at) = u;
+        *(E8*)(to + i1 * t.to_pitch + o1) = u;
     }
 }
 
@@ -201,8 +201,8 @@ void linear_prepare(Ctx& c, const SlopeTask* slope, const PackTask* t, int count
         for (; done < count && (a.pack.count == 0 || a.pack.first[a.pack.count] < (1 << 22)); ++done) {
             const int i = a.pack.count++;
             a.pack.t[i] = t[done];
-            a.pack.across[i] = (unsigned)ceil_div(t[done].inner, 64);
-            a.pack.first[i + 1] = a.pack.first[i] + a.pack.across[i] * (unsigned)ceil_div(t[done].outer, 64);
+            a.pack.across[i] = (unsigned)ceil_div(t[done].inner, t[done].turn ? TURN : PACK_VALUES);
+            a.pack.first[i + 1] = a.pack.first[i] + a.pack.across[i] * (unsigned)ceil_div(t[done].outer, t[done].turn ? TURN : PACK_RUNS);
         }
         const dim3 grid(a.slope.blocks + a.pack.first[a.pack.count]);
         if (is_bf16) ST_LAUNCH(c, "linear_prepare", k_linear_prepare<bf16>, grid, dim3(256), 0, a);

@@ -93,8 +93,8 @@ struct ColumnSums { const float* parts; int n_parts; int64_t n; float* out; int 
 
 constexpr int SMALL_TILE = 32;      // small tiles take operands at any address (but rows of less than 16 bytes)
 struct LinearForm { int tile; int splits[2]; };
-// odd: an operand that small tiles take as it lies and others want copied
-LinearForm linear_form(const Extent* e, int count, int is_bf16, bool odd);
+// copied: bytes of operands that small tiles take as they lie and others want copied; prepared: a launch that could copy them is there anyway
+LinearForm linear_form(const Extent* e, int count, int is_bf16, int64_t copied, bool prepared);
 // up to two products of that form, and sums of columns (n == 0: none), in one launch, and one more where a contraction is split
 void linear_products(Ctx& c, const LinearProduct* p, int count, const LinearForm& f, int is_bf16, const ColumnSums& sums);
 // few tokens, weights along the contraction: one launch of its own kind, whatever the alignment

@@ -50,6 +50,10 @@ Lie lie_of(const st_matrix& x, int along, bool by_rows)
     l.direct = operand_direct(x.data, l.pitch, l.k_along, l.inner, elem(x.dtype));
     return l;
 }
+int64_t copied_bytes(const st_matrix& x, int along, bool by_rows)
+{
+    return lie_of(x, along, by_rows).direct ? 0 : x.rows * x.cols * elem(x.dtype);
+}
 Operand operand_of(const st_matrix& x, int along, bool by_rows, bool small, int* loose, Carve& w, Packs* packs)
 {
     const int es = elem(x.dtype);
@@ -68,12 +72,16 @@ size_t slab_bytes(const Extent* e, const LinearForm& f, int which)
 {
     return f.splits[which] > 1 ? (size_t)f.splits[which] * e[which].m * e[which].n * 4 : 0;
 }
+// (whatever tile is chosen: large tiles are chosen where small ones are many; the columns' sums have blocks too)
 bool products_ok(const Extent* e, int count, int is_bf16)
 {
-    const LinearForm f = linear_form(e, count, is_bf16, false);
-    int64_t blocks = 0;
-    for (int i = 0; i < count; ++i) blocks += ceil_div(e[i].m, f.tile) * ceil_div(e[i].n, f.tile) * f.splits[i];
-    return blocks < (1 << 23) - 32768 - 1;      // (and the blocks of the columns' sums)
+    for (int odd = 0; odd < 2; ++odd) {
+        const LinearForm f = linear_form(e, count, is_bf16, odd, true);
+        int64_t blocks = 0;
+        for (int i = 0; i < count; ++i) blocks += ceil_div(e[i].m, f.tile) * ceil_div(e[i].n, f.tile) * f.splits[i];
+        if (blocks >= (1 << 23) - 32768 - 1) return false;
+    }
+    return true;
 }
 
 // The forward pass, planned: `ws` null for its size alone.
@@ -91,7 +99,7 @@ LinearPlan plan_linear(const st_matrix& x, int x_along, const st_matrix& w, int 
         p.b = Operand{w.data, w.row_stride, 1, p.k};
     } else {
         const Extent e{p.m, p.n, p.k};
-        l.form = linear_form(&e, 1, is_bf16, !lie_of(x, x_along, true).direct || !lie_of(w, w_along, true).direct);
+        l.form = linear_form(&e, 1, is_bf16, copied_bytes(x, x_along, true) + copied_bytes(w, w_along, true), false);
         const bool small = l.form.tile == SMALL_TILE;
         p.a = operand_of(x, x_along, true, small, &p.loose, c, &l.packs);
         p.b = operand_of(w, w_along, true, small, &p.loose, c, &l.packs);
@@ -115,9 +123,9 @@ BackwardPlan plan_backward(const st_matrix* x, int x_along, const st_matrix* w, 
     Extent e[2];
     if (x) e[b.n_products++] = Extent{n, x->cols, m};
     if (w) e[b.n_products++] = Extent{m, w->cols, n};
-    const bool odd = (x && !lie_of(*x, x_along, false).direct) || (w && !lie_of(*w, w_along, false).direct)
-                     || (as_it_is && ((w && !lie_of(dy, dy_along, true).direct) || (x && !lie_of(dy, dy_along, false).direct)));
-    b.form = b.n_products ? linear_form(e, b.n_products, is_bf16, odd) : LinearForm{SMALL_TILE, {1, 1}};
+    const int64_t copied = (x ? copied_bytes(*x, x_along, false) : 0) + (w ? copied_bytes(*w, w_along, false) : 0)
+                           + (as_it_is && w ? copied_bytes(dy, dy_along, true) : as_it_is && x ? copied_bytes(dy, dy_along, false) : 0);
+    b.form = b.n_products ? linear_form(e, b.n_products, is_bf16, copied, db || !as_it_is) : LinearForm{SMALL_TILE, {1, 1}};
     const bool small = b.form.tile == SMALL_TILE;
     int loose = 0;
     SlopeTask& s = b.slope;
