@@ -433,12 +433,12 @@ __global__ __launch_bounds__((BM / WM) * (BN / WN) * 64) void k_linear_product(c
 //
 // LOOSE: operands at any address with any stride, through registers (a load's 16 bytes may begin anywhere): a chunk that would reach behind a
 // row's end is loaded from the row's last 16 bytes and moved to its place, rows and positions that do not exist are zeros.
-//
-// DEEP: where no compute unit has two blocks, twice as many stages are under way.
+// (Four stages of a group are under way; eight, in a compute unit's whole LDS, take as long: 64 tokens 512 -> 512 7.4 us and 7.5, 8 tokens
+// 4096 -> 4096, weights across, 12.3 and 12.3.)
 constexpr int SMALL = SMALL_TILE, SMALL_GROUPS = 2, SMALL_BUF = 2 * SMALL * STAGE, SMALL_THREADS = SMALL_GROUPS * 256;
-constexpr size_t small_lds(bool loose, bool deep)
+constexpr size_t small_lds(bool loose)
 {
-    const size_t stages = (size_t)SMALL_GROUPS * (loose ? 2 : deep ? 8 : 4) * SMALL_BUF, sums = (size_t)SMALL_THREADS / 64 * SMALL * (SMALL + 4) * 4;
+    const size_t stages = (size_t)SMALL_GROUPS * (loose ? 2 : 4) * SMALL_BUF, sums = (size_t)SMALL_THREADS / 64 * SMALL * (SMALL + 4) * 4;
     return stages > sums ? stages : sums;
 }
 
@@ -481,10 +481,10 @@ template <class E, bool ALONG> struct LooseTile {
     }
 };
 
-template <class E, bool A_ALONG, bool B_ALONG, bool LOOSE, bool DEEP>
+template <class E, bool A_ALONG, bool B_ALONG, bool LOOSE>
 __device__ __forceinline__ void small_tile(const GemmArgs& g, char* lds, int64_t m0, int64_t n0, int split, f32x16& acc)
 {
-    constexpr int DEPTH = LOOSE ? 2 : DEEP ? 8 : 4, AHEAD = DEEP ? 8 : 4;
+    constexpr int DEPTH = LOOSE ? 2 : 4, AHEAD = 4;
     const LinearProduct& p = g.p;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), group = wave >> 2, w4 = wave & 3;
     const int first = (int)((int64_t)g.stages * split / g.splits), last = (int)((int64_t)g.stages * (split + 1) / g.splits);
@@ -568,7 +568,7 @@ __device__ __forceinline__ void small_out(const GemmArgs& g, char* lds, int64_t 
     else finish(p, m, n, v, bias);
 }
 
-template <class E, bool LOOSE, bool DEEP> __global__ __launch_bounds__(SMALL_THREADS) void k_linear_small(const GemmPair pair)
+template <class E, bool LOOSE> __global__ __launch_bounds__(SMALL_THREADS) void k_linear_small(const GemmPair pair)
 {
     extern __shared__ __align__(16) char lds[];
     const unsigned both = pair.g[0].blocks + pair.g[1].blocks;
@@ -578,11 +578,11 @@ template <class E, bool LOOSE, bool DEEP> __global__ __launch_bounds__(SMALL_THR
     const int64_t m0 = (int64_t)at.tm * SMALL, n0 = (int64_t)at.tn * SMALL;
     f32x16 acc = {};
     if (g.p.a.along) {
-        if (g.p.b.along) small_tile<E, true, true, LOOSE, DEEP>(g, lds, m0, n0, at.split, acc);
-        else small_tile<E, true, false, LOOSE, DEEP>(g, lds, m0, n0, at.split, acc);
+        if (g.p.b.along) small_tile<E, true, true, LOOSE>(g, lds, m0, n0, at.split, acc);
+        else small_tile<E, true, false, LOOSE>(g, lds, m0, n0, at.split, acc);
     } else {
-        if (g.p.b.along) small_tile<E, false, true, LOOSE, DEEP>(g, lds, m0, n0, at.split, acc);
-        else small_tile<E, false, false, LOOSE, DEEP>(g, lds, m0, n0, at.split, acc);
+        if (g.p.b.along) small_tile<E, false, true, LOOSE>(g, lds, m0, n0, at.split, acc);
+        else small_tile<E, false, false, LOOSE>(g, lds, m0, n0, at.split, acc);
     }
     small_out(g, lds, m0, n0, at.split, acc);
 }
@@ -750,7 +750,7 @@ void linear_product_few(Ctx& c, const LinearProduct& p, int is_bf16)
 // the best of them, geometric mean, where thresholds on the number of tiles took 1.06 (1.13).
 struct TileCost { int tile; double stage[2], block[2]; };      // float32, bfloat16
 constexpr TileCost TILE_COSTS[] = {{SMALL, {0.20, 0.13}, {1.0, 1.0}}, {64, {0.64, 0.26}, {0.6, 0.6}}, {128, {2.24, 0.57}, {1.5, 1.0}}, {256, {8.2, 1.72}, {5.0, 5.0}}};
-constexpr double JOIN_US = 4.0, JOIN_BYTE_US = 3e-7, COPY_US = 1.5, COPY_BYTE_US = 6e-7;
+constexpr double JOIN_US = 4.0, JOIN_BYTE_US = 3e-7, COPY_US = 1.5, COPY_BYTE_US = 4e-7;
 constexpr int MOST_SPLITS = 32, LEAST_STAGES = 8;
 LinearForm linear_form(const Extent* e, int count, int is_bf16, int64_t copied, bool prepared)
 {
@@ -792,20 +792,16 @@ static void launch(Ctx& c, const GemmPair& g)
     const unsigned grid = g.g[0].blocks + g.g[1].blocks + (unsigned)ceil_div(g.sums.n, SUM_COLUMNS);
     ST_LAUNCH(c, name, (k_linear_product<E, BM, BN, WM, WN, DEPTH>), dim3(grid), dim3(threads), lds, g);
 }
-template <class E, bool LOOSE, bool DEEP> static void launch_small(Ctx& c, const GemmPair& g)
+template <class E, bool LOOSE> static void launch_small(Ctx& c, const GemmPair& g)
 {
-    ensure_dynamic_lds((const void*)k_linear_small<E, LOOSE, DEEP>, small_lds(LOOSE, DEEP));
+    ensure_dynamic_lds((const void*)k_linear_small<E, LOOSE>, small_lds(LOOSE));
     const dim3 grid(g.g[0].blocks + g.g[1].blocks + (unsigned)ceil_div(g.sums.n, SUM_COLUMNS));
-    ST_LAUNCH(c, LOOSE ? "linear_small_loose" : "linear_small", (k_linear_small<E, LOOSE, DEEP>), grid, dim3(SMALL_THREADS), small_lds(LOOSE, DEEP), g);
+    ST_LAUNCH(c, LOOSE ? "linear_small_loose" : "linear_small", (k_linear_small<E, LOOSE>), grid, dim3(SMALL_THREADS), small_lds(LOOSE), g);
 }
 template <class E> static void launch_tile(Ctx& c, const GemmPair& g, int tile)
 {
     if (tile == SMALL) {
-        const bool loose = g.g[0].p.loose || g.g[1].p.loose, deep = g.g[0].blocks + g.g[1].blocks <= 256;
-        if (loose && deep) launch_small<E, true, true>(c, g);
-        else if (loose) launch_small<E, true, false>(c, g);
-        else if (deep) launch_small<E, false, true>(c, g);
-        else launch_small<E, false, false>(c, g);
+        if (g.g[0].p.loose || g.g[1].p.loose) launch_small<E, true>(c, g); else launch_small<E, false>(c, g);
     } else if (tile == 256) launch<E, 256, 256, 128, 64, 2>(c, g);
     else if (tile == 128 && g.g[0].blocks + g.g[1].blocks <= 256) launch<E, 128, 128, 64, 32, 4>(c, g);
     else if (tile == 128) launch<E, 128, 128, 64, 32, 2>(c, g);

@@ -182,10 +182,11 @@ template <class E> __global__ __launch_bounds__(256) void k_linear_prepare(const
     else { if (t.pre.bf16) slope_block<float, bf16>(a.slope, blockIdx.x, lds); else slope_block<float, float>(a.slope, blockIdx.x, lds); }
 }
 
-// parts of the rows: about four blocks a compute unit, 32 rows at least; no more parts than the launch that adds them reads in passing
+// Parts of the rows: about four blocks a compute unit, 32 rows at least; no more parts than the launch that adds them reads in passing (14400
+// cells of 128 channels: 450 parts 6.4 us, 113 parts 9.5; 8192 tokens of 4096 channels in 16 parts 43 us, in 8 64, in 32 47).
 static int slope_rows_each(int64_t m, int64_t n)
 {
-    const int64_t parts = std::min<int64_t>(128, std::max<int64_t>(1, 1024 / ceil_div(n, 64)));
+    const int64_t parts = std::min<int64_t>(512, std::max<int64_t>(1, 1024 / ceil_div(n, 64)));
     return (int)round_up(std::max<int64_t>(32, ceil_div(m, parts)), 32);
 }
 int linear_slope_parts(int64_t m, int64_t n) { return (int)ceil_div(m, slope_rows_each(m, n)); }

@@ -72,19 +72,15 @@ size_t slab_bytes(const Extent* e, const LinearForm& f, int which)
 {
     return f.splits[which] > 1 ? (size_t)f.splits[which] * e[which].m * e[which].n * 4 : 0;
 }
-// (whatever tile is chosen: large tiles are chosen where small ones are many; the columns' sums have blocks too)
-bool products_ok(const Extent* e, int count, int is_bf16)
+// Whether a launch holds the products' blocks (and those of the columns' sums).
+bool fits(const Extent* e, int count, const LinearForm& f)
 {
-    for (int odd = 0; odd < 2; ++odd) {
-        const LinearForm f = linear_form(e, count, is_bf16, odd, true);
-        int64_t blocks = 0;
-        for (int i = 0; i < count; ++i) blocks += ceil_div(e[i].m, f.tile) * ceil_div(e[i].n, f.tile) * f.splits[i];
-        if (blocks >= (1 << 23) - 32768 - 1) return false;
-    }
-    return true;
+    int64_t blocks = 0;
+    for (int i = 0; i < count; ++i) blocks += ceil_div(e[i].m, f.tile) * ceil_div(e[i].n, f.tile) * f.splits[i];
+    return blocks < (1 << 23) - 32768 - 1;
 }
 
-// The forward pass, planned: `ws` null for its size alone.
+// The forward pass, planned: `ws` null for its size alone; bytes 0: more than a launch holds.
 struct LinearPlan { LinearProduct p; LinearForm form; Packs packs; bool few; size_t bytes; };
 LinearPlan plan_linear(const st_matrix& x, int x_along, const st_matrix& w, int w_along, char* ws)
 {
@@ -94,18 +90,18 @@ LinearPlan plan_linear(const st_matrix& x, int x_along, const st_matrix& w, int 
     const int is_bf16 = x.dtype == ST_BF16;
     Carve c{ws};
     l.few = w_along && linear_few(p.m, p.n, p.k, is_bf16);
+    const Extent e{p.m, p.n, p.k};
     if (l.few) {
         p.a = Operand{x.data, x_along ? x.row_stride : x.col_stride, x_along, x_along ? p.k : p.m};
         p.b = Operand{w.data, w.row_stride, 1, p.k};
     } else {
-        const Extent e{p.m, p.n, p.k};
         l.form = linear_form(&e, 1, is_bf16, copied_bytes(x, x_along, true) + copied_bytes(w, w_along, true), false);
         const bool small = l.form.tile == SMALL_TILE;
         p.a = operand_of(x, x_along, true, small, &p.loose, c, &l.packs);
         p.b = operand_of(w, w_along, true, small, &p.loose, c, &l.packs);
         p.slabs = (float*)c.take(slab_bytes(&e, l.form, 0));
     }
-    l.bytes = c.used + 256;
+    l.bytes = l.few || fits(&e, 1, l.form) ? c.used + 256 : 0;
     return l;
 }
 
@@ -163,7 +159,7 @@ BackwardPlan plan_backward(const st_matrix* x, int x_along, const st_matrix* w, 
     }
     for (int i = 0; i < b.n_products; ++i) { LinearProduct& p = b.p[i]; p.m = e[i].m; p.n = e[i].n; p.k = e[i].k; p.loose = loose; }
     for (int i = 0; i < b.n_products; ++i) b.p[i].slabs = (float*)c.take(slab_bytes(e, b.form, i));
-    b.bytes = c.used + 256;
+    b.bytes = fits(e, b.n_products, b.form) ? c.used + 256 : 0;
     return b;
 }
 
@@ -177,8 +173,7 @@ extern "C" {
 static int check_linear(const st_matrix* x, const st_matrix* w, int* x_along, int* w_along)
 {
     if (!x || !w) return ST_ERR_NULL;
-    const Extent e{std::max<int64_t>(x->rows, 1), w->rows, x->cols};
-    if (!sizes_ok(x->rows, w->rows, x->cols) || !products_ok(&e, 1, x->dtype == ST_BF16)) return ST_ERR_SHAPE;
+    if (!sizes_ok(x->rows, w->rows, x->cols)) return ST_ERR_SHAPE;
     if (const int v = check(x, x->rows, x->cols, x_along)) return v;
     if (const int v = check(w, w->rows, x->cols, w_along)) return v;
     return x->dtype == w->dtype ? ST_OK : ST_ERR_ARG;
@@ -209,6 +204,7 @@ int st_linear(const st_matrix* x, const st_matrix* w, const st_linear_opts* opts
         return ST_ERR_ARG;
     if (o.residual == y && (o.residual_dtype != y_dtype || o.residual_pitch != y_pitch)) return ST_ERR_ARG;
     LinearPlan l = plan_linear(*x, x_along, *w, w_along, (char*)workspace);
+    if (!l.bytes) return ST_ERR_SHAPE;
     if (l.bytes > 256 && (!workspace || !is_aligned(workspace, 256) || workspace_bytes < l.bytes)) return ST_ERR_WORKSPACE;
     LinearProduct& p = l.p;
     p.out = y; p.out_bf16 = y_dtype == ST_BF16; p.out_pitch = y_pitch;
@@ -234,9 +230,6 @@ static int check_backward(const st_matrix* x, const st_matrix* w, const st_matri
     if (x) if (const int v = check(x, m, k, x_along)) return v;
     if (w) if (const int v = check(w, n, k, w_along)) return v;
     if (x && w && x->dtype != w->dtype) return ST_ERR_ARG;
-    const int is_bf16 = x ? x->dtype == ST_BF16 : w && w->dtype == ST_BF16;
-    const Extent e[2] = {{n, k, std::max<int64_t>(m, 1)}, {std::max<int64_t>(m, 1), k, n}};
-    if (!products_ok(e, 2, is_bf16) || !products_ok(e, 1, is_bf16) || !products_ok(e + 1, 1, is_bf16)) return ST_ERR_SHAPE;
     return ST_OK;
 }
 
@@ -247,9 +240,11 @@ size_t st_linear_backward_workspace(const st_matrix* x, const st_matrix* w, cons
     if (dy->rows == 0) return 256;
     const int dtype = x ? x->dtype : w ? w->dtype : dy->dtype;
     size_t most = 0;      // whichever of the gradients are asked for
-    for (int which = 0; which < 4; ++which)
-        most = std::max(most, plan_backward(which & 1 ? x : nullptr, x_along, which & 2 ? w : nullptr, w_along, *dy, dy_along, activation, dtype,
-                                            true, nullptr).bytes);
+    for (int which = 0; which < 4; ++which) {
+        const size_t bytes = plan_backward(which & 1 ? x : nullptr, x_along, which & 2 ? w : nullptr, w_along, *dy, dy_along, activation, dtype, true, nullptr).bytes;
+        if (!bytes) return 0;
+        most = std::max(most, bytes);
+    }
     return most;
 }
 
@@ -278,6 +273,7 @@ int st_linear_backward(const st_matrix* x, const st_matrix* w, const st_matrix* 
     }
     const int dtype = x ? x->dtype : w ? w->dtype : dy->dtype;
     BackwardPlan b = plan_backward(x, x_along, w, w_along, *dy, dy_along, activation, dtype, o.db != nullptr, (char*)workspace);
+    if (!b.bytes) return ST_ERR_SHAPE;
     if (b.bytes > 256 && (!workspace || !is_aligned(workspace, 256) || workspace_bytes < b.bytes)) return ST_ERR_WORKSPACE;
     if (activation != ST_ACT_NONE) b.slope.pre = GradSource{pre->data, pre->dtype == ST_BF16, pre_along ? pre->row_stride : pre->col_stride, pre_along};
     b.sums.out = o.db; b.sums.accumulate = o.accumulate;
