@@ -32,7 +32,7 @@ struct GemmArgs {
     LinearProduct p;
     FastDiv by_tiles, by_band;                // tiles of a split, tiles of a band of BAND rows of tiles
     int tiles_m;
-    int splits, stages;                       // stages: of the whole contraction
+    int splits, stages, once;                 // stages: of the whole contraction, once: of one of its terms
     unsigned blocks;
 };
 struct GemmPair { GemmArgs g[2]; ColumnSums sums; };
@@ -245,6 +245,11 @@ template <class E, int R, int WAVES, int N> struct Tile<E, false, R, WAVES, N> {
     }
 };
 
+template <class E> __device__ __forceinline__ Operand second_term(const LinearProduct& p)
+{
+    return Operand{(const E*)p.a.p + p.a_second, p.a.pitch, p.a.along, p.a.inner};
+}
+
 template <class E> __device__ __forceinline__ f32x16 mfma(i32x4 a, i32x4 b, f32x16 c)
 {
     if constexpr (sizeof(E) == 2) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -285,9 +290,16 @@ __device__ __forceinline__ void product_tile(const GemmArgs& g, char* lds, int64
     const int wn = (wave % (BN / WN)) * WN, wm = (wave / (BN / WN)) * WM;
     using Channels = Tile<E, B_ALONG, BN, WAVES, NA>;
     using Tokens = Tile<E, A_ALONG, BM, WAVES, NB>;
-    Channels channels(p.b, n0, p.n, p.k, lane, wave, wn, first, 1);
-    Tokens tokens(p.a, m0, p.m, p.k, lane, wave, wm, first, 1);
+    int coming = first < g.once ? first : first - g.once;      // the stage of its term that is loaded next
+    Channels channels(p.b, n0, p.n, p.k, lane, wave, wn, coming, 1);
+    Tokens tokens(first < g.once ? p.a : second_term<E>(p), m0, p.m, p.k, lane, wave, wm, coming, 1);
     auto next_stage = [&](int buf) {
+        if (coming == g.once) {
+            coming = 0;
+            channels = Channels(p.b, n0, p.n, p.k, lane, wave, wn, 0, 1);
+            tokens = Tokens(second_term<E>(p), m0, p.m, p.k, lane, wave, wm, 0, 1);
+        }
+        ++coming;
         channels.load(lds + buf * BUF, wave);
         tokens.load(lds + buf * BUF + MINE, wave);
     };
@@ -446,9 +458,11 @@ template <class E, bool ALONG> struct LooseTile {
     static constexpr int CH = 16 / sizeof(E), KS = STAGE / sizeof(E);
     using Chunk = Run<E, CH>;
     const E* base; int64_t pitch, k;      // k: positions of the contraction that can be read
+    int once; int64_t second;             // stages of a term; from a term to the next
     int position;                // of the chunk in a stage's contraction
     int down;                    // across: by how much the row's last chunk is moved; along: nothing
-    __device__ __forceinline__ LooseTile(const Operand& o, int64_t row0, int64_t rows, int64_t len, int lane, int wave)
+    __device__ __forceinline__ LooseTile(const Operand& o, int64_t row0, int64_t rows, int64_t len, int lane, int wave, int once_, int64_t second_)
+        : once(once_), second(second_)
     {
         pitch = o.pitch; k = ALONG ? o.inner : len;
         if constexpr (ALONG) {
@@ -465,11 +479,12 @@ template <class E, bool ALONG> struct LooseTile {
     }
     __device__ __forceinline__ void load(int s, Chunk& c) const
     {
-        const int64_t at = (int64_t)s * KS + position;
-        c.load(ALONG ? base + std::min(at, k - CH) : base + std::min(at, k - 1) * pitch);
+        const int64_t at = (int64_t)(s < once ? s : s - once) * KS + position;
+        c.load((ALONG ? base + std::min(at, k - CH) : base + std::min(at, k - 1) * pitch) + (s < once ? 0 : second));
     }
     __device__ __forceinline__ void store(int s, Chunk& c, char* to) const      // to: the lane's place
     {
+        if (s >= once) s -= once;
         const int64_t at = (int64_t)s * KS + position;
         if constexpr (ALONG) {
             if (((int64_t)s + 1) * KS > k) { const int64_t d = at - (k - CH); if (d > 0) c.down((int)std::min<int64_t>(d, CH)); }
@@ -491,8 +506,12 @@ __device__ __forceinline__ void small_tile(const GemmArgs& g, char* lds, int64_t
     const int turns = (last - first + SMALL_GROUPS - 1) / SMALL_GROUPS;
     char* const own = lds + group * DEPTH * SMALL_BUF;
     auto stage_of = [&](int turn) { return first + turn * SMALL_GROUPS + group; };
-    Tile<E, B_ALONG, SMALL, 4, 1> channels(p.b, n0, p.n, p.k, lane, w4, 0, first + group, SMALL_GROUPS);
-    Tile<E, A_ALONG, SMALL, 4, 1> tokens(p.a, m0, p.m, p.k, lane, w4, 0, first + group, SMALL_GROUPS);
+    using Channels = Tile<E, B_ALONG, SMALL, 4, 1>;
+    using Tokens = Tile<E, A_ALONG, SMALL, 4, 1>;
+    bool in_second = first + group >= g.once;
+    const int begin = first + group - (in_second ? g.once : 0);
+    Channels channels(p.b, n0, p.n, p.k, lane, w4, 0, begin, SMALL_GROUPS);
+    Tokens tokens(in_second ? second_term<E>(p) : p.a, m0, p.m, p.k, lane, w4, 0, begin, SMALL_GROUPS);
     auto multiply = [&](const char* buf) {
         i32x4 a[1], b[1];
         channels.fetch(buf, w4, lane, a);
@@ -500,8 +519,8 @@ __device__ __forceinline__ void small_tile(const GemmArgs& g, char* lds, int64_t
         acc = mfma<E>(a[0], b[0], acc);
     };
     if constexpr (LOOSE) {
-        const LooseTile<E, B_ALONG> from_b(p.b, n0, p.n, p.k, lane, w4);
-        const LooseTile<E, A_ALONG> from_a(p.a, m0, p.m, p.k, lane, w4);
+        const LooseTile<E, B_ALONG> from_b(p.b, n0, p.n, p.k, lane, w4, g.once, 0);
+        const LooseTile<E, A_ALONG> from_a(p.a, m0, p.m, p.k, lane, w4, g.once, p.a_second);
         typename LooseTile<E, true>::Chunk c[AHEAD][2];
         auto ask = [&](int turn, int u) { if (stage_of(turn) < last) { from_b.load(stage_of(turn), c[u][0]); from_a.load(stage_of(turn), c[u][1]); } };
 #pragma unroll
@@ -523,7 +542,13 @@ __device__ __forceinline__ void small_tile(const GemmArgs& g, char* lds, int64_t
             }
     } else {
         auto ask = [&](int turn) {
-            if (stage_of(turn) >= last) return;
+            const int s = stage_of(turn);
+            if (s >= last) return;
+            if (!in_second && s >= g.once) {
+                in_second = true;
+                channels = Channels(p.b, n0, p.n, p.k, lane, w4, 0, s - g.once, SMALL_GROUPS);
+                tokens = Tokens(second_term<E>(p), m0, p.m, p.k, lane, w4, 0, s - g.once, SMALL_GROUPS);
+            }
             char* const buf = own + turn % DEPTH * SMALL_BUF;
             channels.load(buf, w4);
             tokens.load(buf + SMALL * STAGE, w4);
@@ -817,8 +842,9 @@ void linear_products(Ctx& c, const LinearProduct* p, int count, const LinearForm
     int64_t cells[2] = {0, 0};
     for (int i = 0; i < count; ++i) {
         const int64_t tm = ceil_div(p[i].m, f.tile), tn = ceil_div(p[i].n, f.tile);
+        const int once = (int)ceil_div(p[i].k * (is_bf16 ? 2 : 4), STAGE);
         g.g[i] = GemmArgs{p[i], fast_div((int)(tm * tn)), fast_div((int)(tn * BAND)), (int)tm, f.splits[i],
-                          (int)ceil_div(p[i].k * (is_bf16 ? 2 : 4), STAGE), (unsigned)(tm * tn * f.splits[i])};
+                          p[i].a_second ? 2 * once : once, once, (unsigned)(tm * tn * f.splits[i])};
         if (f.splits[i] > 1) { cells[n_joined] = p[i].m; joined.g[n_joined++] = g.g[i]; }
     }
     if (is_bf16) launch_tile<bf16>(c, g, f.tile); else launch_tile<float>(c, g, f.tile);

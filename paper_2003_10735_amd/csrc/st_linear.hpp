@@ -86,6 +86,7 @@ struct LinearProduct {
     const void* residual; int residual_bf16; int64_t residual_pitch;
     void* pre; int pre_bf16; int64_t pre_pitch;
     float* slabs;                // [splits, m, n] where the contraction is split
+    int64_t a_second;            // > 0: a has a second term, that many elements behind the first, whose product with b is added
     int loose;                   // an operand that the products' 16-byte loads do not take as it lies: small tiles load it through registers
 };
 // Sums of columns that lie as parts: out[i] (+)= sum over the parts of parts[part][i].  Done by the launch of the products.
@@ -108,12 +109,13 @@ struct PackTask { const void* x; int64_t outer, inner, pitch; void* to; int64_t 
 constexpr int PACK_TASKS = 4;
 void linear_fill_zero(Ctx& c, void* p, int is_bf16, int64_t rows, int64_t cols, int64_t pitch);
 
-// dz = dy act'(pre) row by row with zeros up to whole chunks (to null: not stored), and the sums of its columns as parts.
+// dz = dy act'(pre) row by row with zeros up to whole chunks (to null: not stored), and the sums of its columns as parts.  second > 0: what a
+// rounding to bfloat16 leaves of it as a second term, that many elements behind the first.
 struct GradSource { const void* x; int bf16; int64_t pitch; int along; };
 struct SlopeTask {
     GradSource dy, pre;          // pre.x null without activation
     int act; int64_t m, n;
-    void* to; int to_bf16; int64_t to_pitch;
+    void* to; int to_bf16; int64_t to_pitch, second;
     float* parts;                // [linear_slope_parts(m, n), n] or null
 };
 int linear_slope_parts(int64_t m, int64_t n);

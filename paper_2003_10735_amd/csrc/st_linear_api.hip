@@ -116,9 +116,11 @@ BackwardPlan plan_backward(const st_matrix* x, int x_along, const st_matrix* w, 
     const int is_bf16 = dtype == ST_BF16;
     Operand by_tokens{}, by_channels{};      // dz for dx, and for dw
     const bool as_it_is = act == ST_ACT_NONE && dy.dtype == dtype;
+    // float32 gradients beside bfloat16 operands: two terms, each a contraction of its own
+    const int terms = is_bf16 && dy.dtype == ST_F32 ? 2 : 1;
     Extent e[2];
-    if (x) e[b.n_products++] = Extent{n, x->cols, m};
-    if (w) e[b.n_products++] = Extent{m, w->cols, n};
+    if (x) e[b.n_products++] = Extent{n, x->cols, m * terms};
+    if (w) e[b.n_products++] = Extent{m, w->cols, n * terms};
     const int64_t copied = (x ? copied_bytes(*x, x_along, false) : 0) + (w ? copied_bytes(*w, w_along, false) : 0)
                            + (as_it_is && w ? copied_bytes(dy, dy_along, true) : as_it_is && x ? copied_bytes(dy, dy_along, false) : 0);
     b.form = b.n_products ? linear_form(e, b.n_products, is_bf16, copied, db || !as_it_is) : LinearForm{SMALL_TILE, {1, 1}};
@@ -130,7 +132,8 @@ BackwardPlan plan_backward(const st_matrix* x, int x_along, const st_matrix* w, 
     b.slopes = db || ((x || w) && !as_it_is);
     if ((x || w) && !as_it_is) {
         s.to_pitch = round_up(n, 8);
-        s.to = c.take((size_t)m * s.to_pitch * elem(dtype));
+        s.second = terms == 2 ? m * s.to_pitch : 0;
+        s.to = c.take((size_t)m * s.to_pitch * elem(dtype) * terms);
         by_tokens = Operand{s.to, s.to_pitch, 1, s.to_pitch};
         by_channels = Operand{s.to, s.to_pitch, 0, s.to_pitch};
     } else {
@@ -157,7 +160,7 @@ BackwardPlan plan_backward(const st_matrix* x, int x_along, const st_matrix* w, 
         p.a = by_tokens;
         p.b = operand_of(*w, w_along, false, small, &loose, c, &b.packs);
     }
-    for (int i = 0; i < b.n_products; ++i) { LinearProduct& p = b.p[i]; p.m = e[i].m; p.n = e[i].n; p.k = e[i].k; p.loose = loose; }
+    for (int i = 0; i < b.n_products; ++i) { LinearProduct& p = b.p[i]; p.m = e[i].m; p.n = e[i].n; p.k = e[i].k / terms; p.a_second = s.second; p.loose = loose; }
     for (int i = 0; i < b.n_products; ++i) b.p[i].slabs = (float*)c.take(slab_bytes(e, b.form, i));
     b.bytes = fits(e, b.n_products, b.form) ? c.used + 256 : 0;
     return b;

@@ -5,7 +5,7 @@ products (exact of bfloat16, rounded of float32) in float32 in any order is with
 slices add a few roundings, the bias one).  An activation moves by at most 1.13 times its argument; the factor beside z (a distribution
 function) is within 2^-19: a polynomial of 2e-7, an exponential, a reciprocal and a dozen roundings of 2^-24.  A slope is within 2^-17 of dy: near
 |z| = 5, where the tanh form's sigmoid rounds to one, 2^-23 meets a factor of 33.  dz is rounded to the operands' type (2^-8 relative for
-bfloat16), each result to its own.
+bfloat16, 2^-16 where dy is float32: two terms), each result to its own.
 """
 import math
 
@@ -128,6 +128,22 @@ def test_gradients_of_whole_numbers_are_exact(m, n, k, dtype):
                 assert (dx[:, k:] == 7).all() and (dw[n:] == 7).all() and (dw[:, k:] == 7).all()
 
 
+@pytest.mark.parametrize("m,n,k", [(3, 16, 8), (40, 31, 3), (70, 130, 257), (97, 96, 40), (64, 64, 2000), (300, 1000, 72), (2000, 90, 100), (1030, 520, 200), (2100, 1030, 136),
+                                   (1500, 1100, 67), (4100, 1500, 96)])
+def test_float32_gradients_beside_bfloat16_operands_keep_sixteen_bits(m, n, k):
+    """Whole numbers of up to ten bits, which one bfloat16 does not hold and two do: exact again (sums below 2^24)."""
+    for i, order in enumerate(ORDERS):
+        x, w, dy, z = whole((m, k), 1, "bf16", 1), whole((n, k), 2, "bf16", 1), whole((m, n), 3, "f32", 700), whole((m, n), 4, "bf16")
+        dz = dy.double() * (z > 0)
+        dx, dw, db = torch.empty(m, k, device="cuda"), torch.empty(n, k, device="cuda"), torch.empty(n, device="cuda")
+        st.st_linear_backward(laid(x, ORDERS[(i + 1) % 4]), laid(w, ORDERS[(i + 2) % 4]), laid(dy, order), z, st.ST_ACT_RELU, dx, dw, db)
+        assert torch.equal(dx.double(), mm64(dz, w.t())) and torch.equal(dw.double(), mm64(dz.t(), x.t())) and torch.equal(db.double(), dz.sum(0)), order
+    dy[1, 2], z[1, 2] = float("inf"), 1.0
+    st.st_linear_backward(x, w, dy, z, st.ST_ACT_RELU, dx, dw, db)
+    want = torch.where(w[2] != 0, torch.sign(w[2].float()) * math.inf, math.nan)      # an infinity times zero is none
+    assert torch.equal(torch.nan_to_num(dx[1], 7.0), torch.nan_to_num(want, 7.0)) and torch.isfinite(dx[0]).all() and math.isinf(float(db[2]))
+
+
 @pytest.mark.parametrize("out", ["bf16", "f32"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("act", list(ACTS))
@@ -159,11 +175,12 @@ def test_gradients(m, n, k, act, dtype, dy_type, dw_type):
     st.st_linear_backward(x, w, dy, z, ACTS[act], dx, dw, db)
     dz = dy.double() * slope64(z, act)
     slope_far = 0 * dz.abs() if act in ("none", "relu") else 2.0 ** -17 * dy.double().abs()
-    half = 2.0 ** -8 if dtype == "bf16" else EPS
+    half = EPS if dtype == "f32" else 2.0 ** -8 if dy_type == "bf16" else 2.0 ** -16
     dz_far = slope_far + (0 if act in ("none", "relu") and dy_type == dtype else half) * (dz.abs() + slope_far)
     top = dz.abs() + dz_far
-    assert within(dx, mm64(dz, w.t()), mm64(dz_far + (n + 16) * EPS * top, w.t().abs()))
-    assert within(dw, mm64(dz.t(), x.t()), mm64((dz_far + (m + 16) * EPS * top).t(), x.t().abs()))
+    terms = 2 if dtype == "bf16" and dy_type == "f32" else 1
+    assert within(dx, mm64(dz, w.t()), mm64(dz_far + (terms * n + 16) * EPS * top, w.t().abs()))
+    assert within(dw, mm64(dz.t(), x.t()), mm64((dz_far + (terms * m + 16) * EPS * top).t(), x.t().abs()))
     assert within(db, dz.sum(0), (slope_far + (m + 16) * EPS * top).sum(0))
 
 
