@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 from functools import lru_cache
 
@@ -698,10 +699,21 @@ def st_adamw_state(m, m_scale, v, v_scale, m_out=None, v_out=None, stream=None):
 
 
 # ---------------------------------------------------------------- dense layers in bfloat16 or float32
-def _linear_bytes(x, w, dy=None, activation=ST_ACT_NONE) -> int:
-    """Bytes of scratch of a call on these matrices (StMatrix or None); 0: they are refused."""
-    refs = [None if a is None else C.byref(a) for a in (x, w, dy)]
-    return lib().st_linear_workspace(*refs[:2]) if dy is None else lib().st_linear_backward_workspace(*refs, activation)
+# (a call's structs as bytes in one go: filling ctypes fields one by one costs a third of a microsecond each more)
+_MATRIX_BYTES, _OPTS_BYTES, _GRADS_BYTES = struct.Struct("@Piqqqq"), struct.Struct("@PiiPqPqi4x"), struct.Struct("@PqiiPqPi4x")
+
+
+def _packed(t, where):
+    """A two-dimensional tensor as the bytes of an st_matrix, its rows and its columns."""
+    if t is None:
+        raise StError(ST_ERR_NULL, where)
+    shape = t.shape
+    if len(shape) != 2:
+        raise StError(ST_ERR_SHAPE, where)
+    if not t.is_cuda:
+        raise StError(ST_ERR_ARG, where)
+    rows, cols = shape
+    return _MATRIX_BYTES.pack(t.data_ptr(), _dtype(t, where), rows, cols, *t.stride()), rows, cols
 
 
 def new_linear_workspace(x, w, dy=None, activation: int = ST_ACT_NONE):
@@ -711,17 +723,15 @@ def new_linear_workspace(x, w, dy=None, activation: int = ST_ACT_NONE):
     like = x if x is not None else w if w is not None else dy
     if like is None or (dy is None and (x is None or w is None)):
         raise StError(ST_ERR_NULL, where)
-    return _scratch(_linear_bytes(*[None if t is None else _matrix(t, where) for t in (x, w, dy)], activation), like.device, where)
+    mx, mw, mdy = (None if t is None else _packed(t, where)[0] for t in (x, w, dy))
+    nbytes = lib().st_linear_workspace(mx, mw) if dy is None else lib().st_linear_backward_workspace(mx, mw, mdy, activation)
+    return _scratch(nbytes, like.device, where)
 
 
-def _workspace_of(workspace, nbytes, device, stream, where):
-    """(address, bytes) of the scratch of a call: as given, or made; the library says whether it is enough."""
-    if workspace is None:
-        n = nbytes()
-        workspace = _own(stream, lambda: _scratch(n, device, where))
-    elif not workspace.is_cuda:
+def _workspace(workspace, where):
+    if not workspace.is_cuda:
         raise StError(ST_ERR_WORKSPACE, where)
-    return workspace, workspace.data_ptr(), workspace.nbytes
+    return workspace.data_ptr(), workspace.nbytes
 
 
 def st_linear(x, w, bias=None, activation: int = ST_ACT_NONE, residual=None, pre=None, out=None, out_dtype=None, workspace=None, stream=None):
@@ -729,25 +739,21 @@ def st_linear(x, w, bias=None, activation: int = ST_ACT_NONE, residual=None, pre
     bias float32 [n]; residual [m, n] float32 or bfloat16, row by row, which may be out itself.  pre [m, n] (float32 or bfloat16, row by
     row) receives x W^T + bias, which st_linear_backward asks for.  out: float32 or bfloat16, as given, else of out_dtype, else of x's type."""
     where = "st_linear"
-    mx, mw = _matrix(x, where), _matrix(w, where)
-    m, n = mx.rows, mw.rows
+    mx, m, _ = _packed(x, where)
+    mw, n, _ = _packed(w, where)
     if out is None:
         import torch
         out = _own(stream, lambda: torch.empty((m, n), dtype=out_dtype or x.dtype, device=x.device), result=True)
     pitch = _out_matrix(out, m, n, where)
     opts = None
     if bias is not None or activation or residual is not None or pre is not None:
-        o = StLinearOpts()
-        o.activation = activation
-        if bias is not None:
-            o.bias = _float_vector(bias, n, where)
-        if residual is not None:
-            o.residual_pitch, o.residual_dtype, o.residual = _out_matrix(residual, m, n, where), _dtype(residual, where), residual.data_ptr()
-        if pre is not None:
-            o.pre_pitch, o.pre_dtype, o.pre = _out_matrix(pre, m, n, where), _dtype(pre, where), pre.data_ptr()
-        opts = C.byref(o)
-    ws, address, nbytes = _workspace_of(workspace, lambda: _linear_bytes(mx, mw), x.device, stream, where)
-    status = (_LIB or lib()).st_linear(C.byref(mx), C.byref(mw), opts, out.data_ptr(), _dtype(out, where), pitch, address, nbytes, _stream(stream))
+        r = (0, 0, 0) if residual is None else (residual.data_ptr(), _out_matrix(residual, m, n, where), _dtype(residual, where))
+        z = (0, 0, 0) if pre is None else (pre.data_ptr(), _out_matrix(pre, m, n, where), _dtype(pre, where))
+        opts = _OPTS_BYTES.pack(0 if bias is None else _float_vector(bias, n, where), activation, r[2], r[0], r[1], z[0], z[1], z[2])
+    if workspace is None:
+        workspace = _own(stream, lambda: new_linear_workspace(x, w))
+    address, nbytes = _workspace(workspace, where)
+    status = (_LIB or lib()).st_linear(mx, mw, opts, out.data_ptr(), _dtype(out, where), pitch, address, nbytes, _stream(stream))
     if status:
         raise StError(status, where)
     return out
@@ -760,25 +766,28 @@ def st_linear_backward(x, w, dy, pre=None, activation: int = ST_ACT_NONE, dx=Non
     None without dw, w without dx.  accumulate=True adds to what dw and db hold.  x and w of one type; dy and pre of either; all in either
     order.  (The residual's gradient is dy.)  Returns (dx, dw, db)."""
     where = "st_linear_backward"
-    mdy = _matrix(dy, where)
-    m, n = mdy.rows, mdy.cols
+    mdy, m, n = _packed(dy, where)
     if (dx is not None and w is None) or (dw is not None and x is None):
         raise StError(ST_ERR_NULL, where)
-    mx = None if dw is None else _matrix(x, where)
-    mw = None if dx is None else _matrix(w, where)
-    mpre = _matrix(pre, where) if activation else None
-    k = mw.cols if mw is not None else mx.cols if mx is not None else 1
-    g = StLinearGrads()
-    if dx is not None:
-        g.dx_pitch, g.dx_dtype, g.dx = _out_matrix(dx, m, k, where), _dtype(dx, where), dx.data_ptr()
+    mx = mw = mpre = None
+    k = 1
+    a = b = (0, 0, 0)
     if dw is not None:
-        g.dw_pitch, g.dw_dtype, g.dw = _out_matrix(dw, n, k, where), _dtype(dw, where), dw.data_ptr()
-    if db is not None:
-        g.db = _float_vector(db, n, where)
-    g.accumulate = 1 if accumulate else 0
-    refs = [None if a is None else C.byref(a) for a in (mx, mw, mdy, mpre)]
-    ws, address, nbytes = _workspace_of(workspace, lambda: _linear_bytes(mx, mw, mdy, activation), dy.device, stream, where)
-    _check((_LIB or lib()).st_linear_backward(*refs, activation, C.byref(g), address, nbytes, _stream(stream)), where)
+        mx, _, k = _packed(x, where)
+    if dx is not None:
+        mw, _, k = _packed(w, where)
+        a = dx.data_ptr(), _out_matrix(dx, m, k, where), _dtype(dx, where)
+    if dw is not None:
+        b = dw.data_ptr(), _out_matrix(dw, n, k, where), _dtype(dw, where)
+    if activation:
+        mpre = _packed(pre, where)[0]
+    grads = _GRADS_BYTES.pack(a[0], a[1], a[2], b[2], b[0], b[1], 0 if db is None else _float_vector(db, n, where), 1 if accumulate else 0)
+    if workspace is None:
+        workspace = _own(stream, lambda: new_linear_workspace(None if dw is None else x, None if dx is None else w, dy, activation))
+    address, nbytes = _workspace(workspace, where)
+    status = (_LIB or lib()).st_linear_backward(mx, mw, mdy, mpre, activation, grads, address, nbytes, _stream(stream))
+    if status:
+        raise StError(status, where)
     return dx, dw, db
 
 

@@ -45,13 +45,15 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // where the stages change.  No register is written.  The pause covers a scalar register that a vector instruction has written just before, and M0.
 __device__ __forceinline__ void load_to_lds(i32x4 rsrc, char* lds, unsigned voff)
 {
-    const unsigned to = (unsigned)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    const unsigned to = (unsigned)__builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) char*)lds);
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "memory");      // (M0: nothing else of these kernels asks for it)
 }
 __device__ __forceinline__ i32x4 buffer(const char* base, int64_t bytes)
 {
     const uint64_t at = (uint64_t)base;
-    return i32x4{(int)(unsigned)at, (int)(unsigned)(at >> 32 & 0xffff), (int)(unsigned)(bytes < (int64_t)OUTSIDE ? bytes : (int64_t)OUTSIDE), 0x00020000};
+    const unsigned size = (unsigned)(bytes < (int64_t)OUTSIDE ? bytes : (int64_t)OUTSIDE);
+    return i32x4{__builtin_amdgcn_readfirstlane((int)(unsigned)at), __builtin_amdgcn_readfirstlane((int)(unsigned)(at >> 32 & 0xffff)),
+                 __builtin_amdgcn_readfirstlane((int)size), 0x00020000};
 }
 
 // ------------------------------------------------------------------------------------------------- the way out

@@ -195,3 +195,12 @@ def test_calls_that_get_through(library):
     st.st_grad_clip(st.GradTensors([dev(4), dev(5, dtype=B)]), 1.0, 0.5, dev(1))
     (a, x), (b, y), (c, z) = library.calls
     assert (a, b, c) == ("st_linear", "st_linear_backward", "st_grad_clip") and x[4:6] == (st.ST_F32, 8) and y[4] == st.ST_ACT_GELU and z[1:4] == (2, 0.5, 1.0)
+
+
+def test_structs_as_bytes_are_the_structs():
+    """What the binding packs in one go lies as the ctypes structures do."""
+    for packed, values, cls in ((st._MATRIX_BYTES, (P, 1, 3, 16, 40, 1), st.StMatrix), (st._OPTS_BYTES, (P, 2, 1, P + 8, 9, P + 16, 10, 1), st.StLinearOpts),
+                                (st._GRADS_BYTES, (P, 16, 1, 1, P + 8, 17, P + 16, 1), st.StLinearGrads)):
+        assert packed.size == C.sizeof(cls)
+        got = cls.from_buffer_copy(packed.pack(*values))
+        assert tuple(getattr(got, name) for name, _ in cls._fields_) == values
