@@ -785,19 +785,21 @@ LinearForm linear_form(const Extent* e, int count, int is_bf16, int64_t copied, 
     double least = 1e300;
     int64_t stages[2] = {1, 1}, longest = 1;
     for (int i = 0; i < count; ++i) { stages[i] = ceil_div(e[i].k * (is_bf16 ? 2 : 4), STAGE); longest = std::max(longest, stages[i]); }
-    for (const TileCost& c : TILE_COSTS)
+    for (const TileCost& c : TILE_COSTS) {
+        int64_t tiles[2] = {0, 0};
+        for (int i = 0; i < count; ++i) tiles[i] = ceil_div(e[i].m, c.tile) * ceil_div(e[i].n, c.tile);
+        const double stage = c.stage[is_bf16], block = c.block[is_bf16];
         for (int64_t s = 1; s <= MOST_SPLITS && (s == 1 || longest >= LEAST_STAGES * s); s *= 2) {
-            const double stage = c.stage[is_bf16], block = c.block[is_bf16];
             LinearForm f = {c.tile, {1, 1}};
             double work = 0, alone = 0, slabs = 0;
             int64_t blocks = 0;
             bool joined = false;
             for (int i = 0; i < count; ++i) {
-                const int64_t tiles = ceil_div(e[i].m, c.tile) * ceil_div(e[i].n, c.tile), k = std::max<int64_t>(1, std::min(s, stages[i] * s / longest));
+                const int64_t k = std::max<int64_t>(1, std::min(s, stages[i] * s / longest));
                 f.splits[i] = (int)k;
-                work += (double)(tiles * stages[i]);
-                blocks += tiles * k;
-                alone = std::max(alone, (double)(ceil_div(stages[i], k) * ceil_div(tiles * k, c.tile == 256 ? 256 : 512)) * stage);
+                work += (double)(tiles[i] * stages[i]);
+                blocks += tiles[i] * k;
+                alone = std::max(alone, (double)(ceil_div(stages[i], k) * ceil_div(tiles[i] * k, c.tile == 256 ? 256 : 512)) * stage);
                 if (k > 1) { joined = true; slabs += (double)e[i].m * e[i].n * k * 4; }
             }
             if (c.tile == SMALL && blocks > 2048) continue;      // (43 tokens, gradients of 1601 -> 2582: 4233 of them, 28 us, 128 x 128 13)
@@ -806,6 +808,7 @@ LinearForm linear_form(const Extent* e, int count, int is_bf16, int64_t copied, 
                               + (c.tile != SMALL && copied ? (prepared ? 0 : COPY_US) + copied * COPY_BYTE_US : 0);
             if (us < least) { least = us; best = f; }
         }
+    }
     return best;
 }
 
