@@ -403,7 +403,7 @@ int st_linear(const st_matrix* x, const st_matrix* w, const st_linear_opts* opts
  *   dx [m, k] = dz W,   dw [n, k] (+)= dz^T x,   db [n] (+)= sum of dz over the tokens, in float32, before that rounding
  * (The residual's gradient is dy.)  Each of dx, dw, db may be NULL and costs nothing then; x without dw and w without dx may be NULL.
  * dx, dw: float32 or bfloat16, row by row with a pitch.  accumulate = 1 adds dw and db to what is there (several batches, one step);
- * dx is always written anew.  Without activation pre may be NULL and is not read. */
+ * dx is always written anew.  Without activation pre may be NULL and is not read.  What is written overlaps nothing that is read. */
 typedef struct st_linear_grads {
     void* dx; int64_t dx_pitch; int32_t dx_dtype;
     int32_t dw_dtype; void* dw; int64_t dw_pitch;

@@ -1,5 +1,6 @@
 // AdamW over a list of tensors.  A launch takes up to ST_ADAMW_PER_LAUNCH tensors, whose pointers travel with its arguments; every block
 // takes one tile of one of them.
+#include "st_lists.hpp"
 #include "st_quantize.hpp"
 
 #include <algorithm>
@@ -27,20 +28,6 @@ struct GradList {
     int count;
 };
 static_assert(sizeof(TensorList) + sizeof(AdamwConstants) + 64 <= 4096 && sizeof(GradList) + 64 <= 4096, "kernel arguments");
-
-// The last tensor that begins at or before the tile (tensors without values own no tile and are not in the list).  Every lane looks at a
-// few of them: one trip to memory, where a search by halves takes one after the other.
-template <int MOST> __device__ __forceinline__ int tensor_of(const unsigned* first, int n, unsigned tile)
-{
-    const int lane = threadIdx.x & 63;
-    int before = 0;
-#pragma unroll
-    for (int c = 0; c < MOST; c += 64) {
-        const bool there = c + lane < n;
-        before += __popcll(__ballot(there && first[there ? c + lane : 0] <= tile));
-    }
-    return before - 1;
-}
 
 // What a step writes is read by the next one: its stores do not ask for room in L2.
 template <class T> __device__ __forceinline__ void store4(T* p, int n, const float (&v)[4])
@@ -72,14 +59,6 @@ template <bool NT = false> __device__ __forceinline__ void store_codes(void* p, 
         return;
     }
     for (int e = 0; e < n; ++e) ((uint8_t*)p)[e] = (uint8_t)(c >> (8 * e));
-}
-__device__ __forceinline__ double block_sum(double s, double* sums)      // of 256 threads, in one order; to every thread
-{
-#pragma unroll
-    for (int d = 32; d; d >>= 1) s += __shfl_xor(s, d);
-    if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = s;
-    __syncthreads();
-    return (sums[0] + sums[1]) + (sums[2] + sums[3]);
 }
 
 // ------------------------------------------------------------------------------------------------------ norm

@@ -281,6 +281,17 @@ __device__ __forceinline__ Place place_of(const GemmPair& pair)
 }
 
 // ------------------------------------------------------------------------------------------------- a block's tile
+// BM tokens x BN channels a block, WM x WN a wavefront.  Us of a launch with plain epilogue, and what that is:
+//   256        8192 tokens 4096 -> 14336   814   1.18 PFLOP/s (the library's plain product 1.40), of which 68 us do not grow with the sums: a
+//              block's first loads and its way out, 7 blocks one after the other on a compute unit.  Half of the matrix cores' time is waits;
+//              operands of zeros, which leave the clock higher, 654
+//              both gradients, 8192 tokens 4096 -> 4096   433   1.27 PFLOP/s (the library's 1.17: it turns operands on the way)
+//   128        4096 tokens 2048 -> 2048   40   0.86 PFLOP/s, two blocks a compute unit: L2 gives 9 TB/s for its tiles
+//   64         2048 tokens 1024 -> 1024   11.3   0.38 PFLOP/s, 16 stages of 0.26 us two a compute unit
+//   float32    8192 tokens 4096 -> 4096   1940   0.142 PFLOP/s of the instruction's 0.157 (the library 0.149)
+// Tried: 128 x 128 a wavefront, four of them (912 us in the first row's place); stages of 64 bytes, 4 or 5 under way (870); a higher
+// wavefront priority around the products (833); 256 x 128 tiles (40 shapes of 500 .. 14000 tokens: 1.007 of the time); blocks that stay and ask for their
+// next tile's stages before the way out (the same shapes: 1.09, for the registers that takes).
 template <class E, int BM, int BN, int WM, int WN, int DEPTH, bool A_ALONG, bool B_ALONG>
 __device__ __forceinline__ void product_tile(const GemmArgs& g, char* lds, int64_t m0, int64_t n0, int split, f32x16 (&acc)[WM / 32][WN / 32])
 {
@@ -661,7 +672,8 @@ template <int GROUPS, int COUNT> __global__ __launch_bounds__(256) void k_linear
 // 16 channels x 16 tokens (v_mfma_f32_16x16x32_bf16: lane l supplies A[l % 16][8*(l/16) .. +7] and B[8*(l/16) .. +7][l % 16] and receives
 // D[4*(l/16) + r][l % 16]; v_mfma_f32_16x16x4_f32: one value of a lane's 16 bytes an instruction).  A block takes 16 channels, each of its
 // eight wavefronts an eighth of the contraction; the eighths are added in LDS in their order.  Rows may begin at any address; the last
-// chunks of a row, those that would reach behind it, are loaded value by value.
+// chunks of a row, those that would reach behind it, are loaded value by value.  Bytes bound it: 1 token 2048 -> 5632 6 us (23 MB, 3.9 TB/s), 12 tokens
+// 4096 -> 4096 8 us (34 MB, 4.2 TB/s); twice as many loads under way, with twice the registers, take 0.6 us longer.
 constexpr int FEW_WAVES = 8;
 struct FewArgs { LinearProduct p; int64_t x_row, x_step; int per_wave; };       // per_wave: bytes, a multiple of 64
 
@@ -751,6 +763,7 @@ template <class E, int NT> __global__ __launch_bounds__(FEW_WAVES * 64) void k_l
     }
 }
 
+// (Against the tiles, us a call: see the test of both sides below the choice of a tile.)
 bool linear_few(int64_t m, int64_t n, int64_t k, int is_bf16)
 {
     (void)n; (void)k; (void)is_bf16;

@@ -116,14 +116,16 @@ class DenseBlockFront:
         self.workspace = st.new_workspace(self.desc, device)
         self.norm_workspace = st.new_grad_workspace(self.all_grads)
         self.step_workspaces = [st.new_adamw_workspace(t) for t in (self.matrices, self.biases)]
-        self.linear_workspaces = None
+        self.linear_workspaces = self.cells_lie = None
 
     def forward(self, cells):
         """cells [n*h*w, desc.c_in] bfloat16 -> the head's features [n, h, w, c_in] bfloat16."""
         w1, w2 = self.copies
         _, b1, _, b2 = self.params
         y = self.features.view(-1, self.desc.c_in)
-        if self.linear_workspaces is None:       # for cells that lie as these do
+        lie = cells.stride(), cells.data_ptr() % 16
+        if self.cells_lie != lie:       # scratch is for cells that lie as these do
+            self.cells_lie = lie
             dy = self._feature_rows()
             self.linear_workspaces = (st.new_linear_workspace(cells, w1), st.new_linear_workspace(self.hidden, w2),
                                       st.new_linear_workspace(self.hidden, w2, dy), st.new_linear_workspace(cells, None, self.hidden_grad, self.activation))
