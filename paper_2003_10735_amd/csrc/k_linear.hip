@@ -763,11 +763,16 @@ template <class E, int NT> __global__ __launch_bounds__(FEW_WAVES * 64) void k_l
     }
 }
 
-// (Against the tiles, us a call: see the test of both sides below the choice of a tile.)
-bool linear_few(int64_t m, int64_t n, int64_t k, int is_bf16)
+// Where a wavefront's eighth of a row is short, or the tokens are so few that reading them in every block does not count.  Against the tiles, us a
+// call: 1 token 3000 -> 2000 6.7 and 9.8, 8 tokens 4096 -> 4096 9.3 and 12.5, 20 11.9 and 12.9, 16 tokens 1024 -> 12000 8.1 and 9.0; but 16 tokens
+// 4096 -> 14336 37 and 28, 8192 -> 1000 16.7 and 10.6, 32 tokens 4096 -> 4096 13.4 and 12.8.  Rows of bfloat16 at odd addresses, whose 16 bytes the
+// card fetches in pieces: 16 tokens 1001 -> 3001 7.3 and 7.7, 20 8.5 and 7.6, 20 tokens 4097 -> 4097 51 and 19.  float32: 16 tokens 2048 -> 5632 17.1
+// and 19.4, 8 tokens 4096 -> 4096 14.5 and 23.1, 16 tokens 4096 -> 14336 67 and 56, 32 tokens 8192 -> 500 43 and 12.
+bool linear_few(int64_t m, int64_t n, int64_t k, int is_bf16, bool aligned)
 {
-    (void)n; (void)k; (void)is_bf16;
-    return m <= 32;
+    if (m > 32 || k > 4096) return false;
+    if (is_bf16) return aligned ? m <= 8 || (m <= 20 && (n <= 4096 || k <= 1024)) : m <= 16 && k <= 1024;
+    return k <= 2048 || m <= 8 || (m <= 20 && n >= 2000 && n <= 8192);
 }
 template <class E> static void few_launch(Ctx& c, const FewArgs& f)
 {

@@ -98,8 +98,8 @@ struct LinearForm { int tile; int splits[2]; };
 LinearForm linear_form(const Extent* e, int count, int is_bf16, int64_t copied, bool prepared);
 // up to two products of that form, and sums of columns (n == 0: none), in one launch, and one more where a contraction is split
 void linear_products(Ctx& c, const LinearProduct* p, int count, const LinearForm& f, int is_bf16, const ColumnSums& sums);
-// few tokens, weights along the contraction: one launch of its own kind, whatever the alignment
-bool linear_few(int64_t m, int64_t n, int64_t k, int is_bf16);
+// few tokens, weights along the contraction: one launch of its own kind, whatever the alignment.  aligned: rows of whole 16-byte chunks
+bool linear_few(int64_t m, int64_t n, int64_t k, int is_bf16, bool aligned);
 void linear_product_few(Ctx& c, const LinearProduct& p, int is_bf16);
 
 // ------------------------------------------------------------------ operands made for a product

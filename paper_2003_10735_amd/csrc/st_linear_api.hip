@@ -89,7 +89,7 @@ LinearPlan plan_linear(const st_matrix& x, int x_along, const st_matrix& w, int 
     p.m = x.rows; p.n = w.rows; p.k = x.cols;
     const int is_bf16 = x.dtype == ST_BF16;
     Carve c{ws};
-    l.few = w_along && linear_few(p.m, p.n, p.k, is_bf16);
+    l.few = w_along && linear_few(p.m, p.n, p.k, is_bf16, is_aligned(w.data, 16) && (w.row_stride * elem(w.dtype) % 16 == 0 || p.n == 1));
     const Extent e{p.m, p.n, p.k};
     if (l.few) {
         p.a = Operand{x.data, x_along ? x.row_stride : x.col_stride, x_along, x_along ? p.k : p.m};

@@ -88,7 +88,7 @@ def mm64(a, b_t):
 
 
 # every form: few tokens, small tiles (aligned, loose, split), 64, 128 and 256, copies, splits of the contraction
-SHAPES = [(1, 1, 1), (1, 300, 37), (1, 515, 1000), (3, 16, 8), (17, 70, 129), (32, 33, 64), (33, 1, 5), (40, 31, 3), (33, 64, 64), (70, 130, 257), (97, 96, 40),
+SHAPES = [(1, 1, 1), (1, 300, 37), (1, 515, 1000), (3, 16, 8), (17, 70, 129), (18, 90, 64), (20, 40, 1016), (32, 33, 64), (33, 1, 5), (40, 31, 3), (33, 64, 64), (70, 130, 257), (97, 96, 40),
           (64, 64, 4096), (50, 40, 5000), (300, 1000, 72), (1030, 520, 200), (2100, 1030, 136), (1500, 1100, 67), (4100, 3100, 96), (4096, 3200, 400)]
 
 
