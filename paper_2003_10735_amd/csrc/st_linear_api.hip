@@ -139,9 +139,9 @@ BackwardPlan plan_backward(const st_matrix* x, int x_along, const st_matrix* w, 
     } else {
         if (w) by_tokens = operand_of(dy, dy_along, true, small, &loose, c, &b.packs);
         // the same matrix read the other way round, if it can be (the rows of a copy end in zeros)
-        const bool copied = w && by_tokens.p != dy.data;
+        const bool is_copy = b.packs.n > 0;
         const int64_t pitch = by_tokens.pitch;
-        if (w && operand_direct(by_tokens.p, pitch, !by_tokens.along, by_tokens.along ? n : copied ? round_up(m, 8) : m, elem(dtype)))
+        if (w && operand_direct(by_tokens.p, pitch, !by_tokens.along, by_tokens.along ? n : is_copy ? round_up(m, 8) : m, elem(dtype)))
             by_channels = Operand{by_tokens.p, pitch, !by_tokens.along, by_tokens.inner};
         else if (x) by_channels = operand_of(dy, dy_along, false, small, &loose, c, &b.packs);
     }
@@ -243,8 +243,8 @@ size_t st_linear_backward_workspace(const st_matrix* x, const st_matrix* w, cons
     if (dy->rows == 0) return 256;
     const int dtype = x ? x->dtype : w ? w->dtype : dy->dtype;
     size_t most = 0;      // whichever of the gradients are asked for
-    for (int which = 0; which < 4; ++which) {
-        const size_t bytes = plan_backward(which & 1 ? x : nullptr, x_along, which & 2 ? w : nullptr, w_along, *dy, dy_along, activation, dtype, true, nullptr).bytes;
+    for (int which = 0; which < 8; ++which) {
+        const size_t bytes = plan_backward(which & 1 ? x : nullptr, x_along, which & 2 ? w : nullptr, w_along, *dy, dy_along, activation, dtype, which & 4, nullptr).bytes;
         if (!bytes) return 0;
         most = std::max(most, bytes);
     }

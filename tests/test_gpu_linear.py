@@ -278,6 +278,19 @@ def test_only_what_is_asked_for():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", [(75, 95, 46), (513, 8, 2360), (310, 272, 928), (3, 72, 800)])
+def test_a_workspace_serves_whatever_is_asked_for(m, n, k, dtype):
+    """Scratch made once for all three gradients, and any of them asked for: operands at odd addresses, which are copied or not as the call sees fit."""
+    x, w, dy = whole((m, k + 1), 1, dtype)[:, 1:], whole((k, n + 1), 2, dtype).t()[1:], whole((n, m), 3, dtype).t()
+    ws = st.new_linear_workspace(x, w, dy)
+    want = mm64(dy, w.t()), mm64(dy.t(), x.t()), dy.double().sum(0)
+    for which in range(1, 8):
+        outs = [torch.full(s, 7.0, device="cuda") if which >> i & 1 else None for i, s in enumerate([(m, k), (n, k), (n,)])]
+        st.st_linear_backward(x, w, dy, dx=outs[0], dw=outs[1], db=outs[2], workspace=ws)
+        assert all(o is None or torch.equal(o.double(), v) for o, v in zip(outs, want)), which
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_no_tokens(dtype):
     x, w, dy = torch.empty(0, 8, dtype=DT[dtype], device="cuda"), rand((5, 8), 1, dtype), torch.empty(0, 5, dtype=DT[dtype], device="cuda")
     assert st.st_linear(x, w).shape == (0, 5)
