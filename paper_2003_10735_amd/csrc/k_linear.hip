@@ -283,14 +283,16 @@ __device__ __forceinline__ Place place_of(const GemmPair& pair)
 // ------------------------------------------------------------------------------------------------- a block's tile
 // BM tokens x BN channels a block, WM x WN a wavefront.  Us of a launch with plain epilogue, and what that is:
 //   256        8192 tokens 4096 -> 14336   814   1.18 PFLOP/s (the library's plain product 1.40), of which 68 us do not grow with the sums: a
-//              block's first loads and its way out, 7 blocks one after the other on a compute unit.  Half of the matrix cores' time is waits;
-//              operands of zeros, which leave the clock higher, 654
+//              block's first loads and its way out, 7 blocks one after the other on a compute unit.  The stages' loads alone take 682 (360 where
+//              all of them hit L2), the products alone 670; on operands of zeros, which leave the clock higher, the products take 501 and all of
+//              it 654: loads into LDS, and the clock under load.  LDS reads alone take 245
 //              both gradients, 8192 tokens 4096 -> 4096   433   1.27 PFLOP/s (the library's 1.17: it turns operands on the way)
 //   128        4096 tokens 2048 -> 2048   40   0.86 PFLOP/s, two blocks a compute unit: L2 gives 9 TB/s for its tiles
 //   64         2048 tokens 1024 -> 1024   11.3   0.38 PFLOP/s, 16 stages of 0.26 us two a compute unit
 //   float32    8192 tokens 4096 -> 4096   1940   0.142 PFLOP/s of the instruction's 0.157 (the library 0.149)
 // Tried: 128 x 128 a wavefront, four of them (912 us in the first row's place); stages of 64 bytes, 4 or 5 under way (870); a higher
-// wavefront priority around the products (833); 256 x 128 tiles (40 shapes of 500 .. 14000 tokens: 1.007 of the time); blocks that stay and ask for their
+// wavefront priority around the products (833); a stage's loads spread over the last step's products (834 against 836 with activation, the tiles of 64 and
+// 128 1.03 of the time); 256 x 128 tiles (40 shapes of 500 .. 14000 tokens: 1.007 of the time); blocks that stay and ask for their
 // next tile's stages before the way out (the same shapes: 1.09, for the registers that takes).
 template <class E, int BM, int BN, int WM, int WN, int DEPTH, bool A_ALONG, bool B_ALONG>
 __device__ __forceinline__ void product_tile(const GemmArgs& g, char* lds, int64_t m0, int64_t n0, int split, f32x16 (&acc)[WM / 32][WN / 32])
