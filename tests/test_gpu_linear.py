@@ -291,6 +291,22 @@ def test_a_workspace_serves_whatever_is_asked_for(m, n, k, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,n,k", [(16, st.ST_LINEAR_MAX_CHANNELS, 8), (40, 24, st.ST_LINEAR_MAX_CHANNELS), ((1 << 24) - 1, 8, 9)])
+def test_the_longest(m, n, k, dtype):
+    """The most channels and the most tokens: sums of up to 2^24 products stay below 2^24 and are exact in any order."""
+    x, w, dy = whole((m, k), 1, dtype, 1), whole((n, k), 2, dtype, 1), whole((m, n), 3, dtype, 1)
+    y = st.st_linear(x, w, out_dtype=torch.float32)
+    for at in range(0, m, 1 << 20):
+        assert torch.equal(y[at:at + (1 << 20)].double(), mm64(x[at:at + (1 << 20)], w))
+    dx, dw, db = torch.empty(m, k, device="cuda"), torch.empty(n, k, device="cuda"), torch.empty(n, device="cuda")
+    st.st_linear_backward(x, w, dy, dx=dx, dw=dw, db=db)
+    for at in range(0, m, 1 << 20):
+        assert torch.equal(dx[at:at + (1 << 20)].double(), mm64(dy[at:at + (1 << 20)], w.t()))
+    parts = [(dy[at:at + (1 << 20)], x[at:at + (1 << 20)]) for at in range(0, m, 1 << 20)]
+    assert torch.equal(dw.double(), sum(mm64(p.t(), q.t()) for p, q in parts)) and torch.equal(db.double(), sum(p.double().sum(0) for p, _ in parts))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_no_tokens(dtype):
     x, w, dy = torch.empty(0, 8, dtype=DT[dtype], device="cuda"), rand((5, 8), 1, dtype), torch.empty(0, 5, dtype=DT[dtype], device="cuda")
     assert st.st_linear(x, w).shape == (0, 5)
