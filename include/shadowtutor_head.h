@@ -397,9 +397,11 @@ int st_linear(const st_matrix* x, const st_matrix* w, const st_linear_opts* opts
 
 /* Gradients of that layer from x [m, k], w [n, k] (one type), dy [m, n] (either type, either order) and, with an activation, pre [m, n]
  * (z, either type, either order):
- *   dz = dy act'(z)            rounded to the operands' type; a float32 dy beside bfloat16 operands to two bfloat16 terms (2^-16 off at
- *                              most), at the price of two products each (an infinity in x or w may then give NaN where one product gives
- *                              an infinity).  (ReLU: dy where z > 0, 0 elsewhere, whatever dy is)
+ *   dz = dy act'(z)            rounded to the operands' type (2^-8 for bfloat16), but two bfloat16 terms (2^-16 off at most) beside bfloat16
+ *                              operands where dy is float32, and in a dx or dw in float32 where the activation is none that leaves dy or 0:
+ *                              whoever asks for a result in float32 gets its bits, at the price of two products each (an infinity in x or
+ *                              w may then give NaN where one product gives an infinity).  (ReLU: dy where z > 0, 0 elsewhere, whatever
+ *                              dy is)
  *   dx [m, k] = dz W,   dw [n, k] (+)= dz^T x,   db [n] (+)= sum of dz over the tokens, in float32, before that rounding
  * (The residual's gradient is dy.)  Each of dx, dw, db may be NULL and costs nothing then; x without dw and w without dx may be NULL.
  * dx, dw: float32 or bfloat16, row by row with a pitch.  accumulate = 1 adds dw and db to what is there (several batches, one step);

@@ -762,8 +762,9 @@ def st_linear(x, w, bias=None, activation: int = ST_ACT_NONE, residual=None, pre
 def st_linear_backward(x, w, dy, pre=None, activation: int = ST_ACT_NONE, dx=None, dw=None, db=None, accumulate: bool = False, workspace=None,
                        stream=None):
     """Gradients of st_linear: dx [m, k] = dz W, dw [n, k] (+)= dz^T x (either: float32 or bfloat16), db [n] float32 (+)= sum of dz, where
-    dz = dy act'(pre); pre, what st_linear left there, is asked for with an activation.  Only the outputs that are given are computed; x may be
-    None without dw, w without dx.  accumulate=True adds to what dw and db hold.  x and w of one type; dy and pre of either; all in either
+    dz = dy act'(pre); pre, what st_linear left there, is asked for with an activation.  Beside bfloat16 operands dz keeps sixteen bits for a dx or dw
+    in float32 (and wherever dy is float32), at the price of two products, and eight for one in bfloat16.  Only the outputs that are given are
+    computed; x may be None without dw, w without dx.  accumulate=True adds to what dw and db hold.  x and w of one type; dy and pre of either; all in either
     order.  (The residual's gradient is dy.)  Returns (dx, dw, db)."""
     where = "st_linear_backward"
     mdy, m, n = _packed(dy, where)

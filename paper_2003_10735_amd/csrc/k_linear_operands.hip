@@ -75,7 +75,7 @@ void linear_fill_zero(Ctx& c, void* p, int is_bf16, int64_t rows, int64_t cols, 
 
 // ------------------------------------------------------------------------------------------------------ dz
 // A block takes 64 columns and a part of the rows, 32 rows at a time: eight threads a row, eight values each.  What lies column by column
-// goes through LDS, 64 columns x 32 rows.  dz is rounded to the operands' type, float32 gradients beside bfloat16 operands to two bfloat16
+// goes through LDS, 64 columns x 32 rows.  dz is rounded to the operands' type, or where a product asks for them to two bfloat16
 // terms (2^-16 off at most, where one is 2^-8); the sums of its columns are of what it was before.  8192 tokens x 4096 channels: 43 us, 4.7 TB/s.
 struct SlopeArgs { SlopeTask t; unsigned across, blocks; int rows_each; };
 
