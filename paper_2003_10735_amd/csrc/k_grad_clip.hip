@@ -11,7 +11,7 @@
 
 namespace st {
 
-constexpr int CLIP_PER_LAUNCH = 120, CLIP_BLOCKS = 2048;
+constexpr int CLIP_PER_LAUNCH = 120, CLIP_BLOCKS = 2048, CLIP_READS = 1 << 14;
 struct ClipList {
     const void* g[CLIP_PER_LAUNCH]; void* out[CLIP_PER_LAUNCH]; long long n[CLIP_PER_LAUNCH];
     unsigned first[CLIP_PER_LAUNCH + 1];       // first tile of each
@@ -34,6 +34,13 @@ template <class G, int RUNS> __device__ __forceinline__ double tile_squares(cons
         for (int k = 0; k < 8; ++k) { const double d = (double)v[j][k]; s = __builtin_fma(d, d, s); }
     return s;
 }
+__device__ __forceinline__ double sum_of_parts(const double* __restrict__ parts, int n, double* sums)
+{
+    double s = 0.0;
+#pragma unroll 4
+    for (int i = threadIdx.x; i < n; i += 256) s += parts[i];
+    return block_sum(s, sums);
+}
 template <int RUNS> __global__ __launch_bounds__(256) void k_clip_squares(const ClipList l, unsigned tiles, double* __restrict__ parts)
 {
     __shared__ double sums[4];
@@ -52,14 +59,22 @@ template <int RUNS> __global__ __launch_bounds__(256) void k_clip_squares(const 
     if (threadIdx.x == 0) parts[blockIdx.x] = s;
 }
 
+// All parts as one, behind the last.  Every block of every launch reads all parts otherwise, which grows with the square of the list; one block that adds
+// them is a launch of 10 - 20 us.  Without it and with it, us a call: 240 tensors of 200 000 values (2 launches, 4096 parts) 85 and 106, 800 of 20 000
+// (7, 2400) 71 and 70 - 84, 480 of 200 000 (4, 8192) 191 - 234 and 172 - 216, 2000 of 2000 (17, 2000) 161 - 164 and 120, 10 000 of 1000 (84, 10 000) 920 and 710, 65 536 of
+// 1000 (547, 65 536) 9220 and 4760 - 5300.  So it runs where launches times parts pass CLIP_READS.
+__global__ __launch_bounds__(256) void k_clip_norm(double* __restrict__ parts, int n)
+{
+    __shared__ double sums[4];
+    const double s = sum_of_parts(parts, n, sums);
+    if (threadIdx.x == 0) parts[n] = s;
+}
+
 // The norm from its parts, by every block in the same order, and the factor on the gradients.
 struct ClipFactor { double norm, factor; };
 __device__ __forceinline__ ClipFactor clip_factor(const ClipRule& r, const double* __restrict__ parts, int n, double* sums)
 {
-    double s = 0.0;
-#pragma unroll 4
-    for (int i = threadIdx.x; i < n; i += 256) s += parts[i];
-    const double norm = sqrt(block_sum(s, sums)) * r.scale;
+    const double norm = sqrt(sum_of_parts(parts, n, sums)) * r.scale;
     return {norm, r.max_norm > 0 && norm > r.max_norm && norm < __builtin_inf() ? r.scale * (r.max_norm / norm) : r.scale};
 }
 
@@ -179,15 +194,21 @@ int64_t clip_parts(const st_grad_tensor* t, int n)
 void grad_clip(Ctx& c, const st_grad_tensor* t, int n, const ClipRule& r, double* parts)
 {
     const int64_t tile = clip_tile(all_values(t, n));
-    int64_t n_parts = 0;
+    int64_t n_parts = 0, launches = 0;
     unsigned tiles = 0;
     for (int next = 0; next < n;) {
         const ClipList l = next_list(t, n, &next, tile, &tiles);
         if (!tiles) continue;
+        ++launches;
         const unsigned blocks = std::min<unsigned>(tiles, CLIP_BLOCKS);
         if (tile == 2048) ST_LAUNCH(c, "clip_squares", k_clip_squares<1>, dim3(blocks), dim3(256), 0, l, tiles, parts + n_parts);
         else ST_LAUNCH(c, "clip_squares", k_clip_squares<4>, dim3(blocks), dim3(256), 0, l, tiles, parts + n_parts);
         n_parts += blocks;
+    }
+    if (r.write && launches * n_parts > CLIP_READS) {
+        ST_LAUNCH(c, "clip_norm", k_clip_norm, dim3(1), dim3(256), 0, parts, (int)n_parts);
+        parts += n_parts;
+        n_parts = 1;
     }
     ClipRule rule = r;
     for (int next = r.write ? 0 : n; next < n || rule.norm;) {      // the first launch writes the norm, if only that

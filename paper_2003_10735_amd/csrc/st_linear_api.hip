@@ -324,7 +324,7 @@ static int check_grads(const st_grad_tensor* t, int32_t n)
 size_t st_grad_clip_workspace(const st_grad_tensor* tensors, int32_t n_tensors)
 {
     if (check_grads(tensors, n_tensors) != ST_OK) return 0;
-    return 256 + (size_t)clip_parts(tensors, n_tensors) * sizeof(double);
+    return 256 + (size_t)clip_parts(tensors, n_tensors) * sizeof(double);      // (room for one more: their sum)
 }
 
 int st_grad_clip(const st_grad_tensor* tensors, int32_t n_tensors, double grad_scale, double max_norm, float* grad_norm, void* workspace, void* stream)
