@@ -388,7 +388,8 @@ typedef struct st_linear_opts {      /* all zeros: nothing around the product */
 } st_linear_opts;
 
 /* y [m, n] from x [m, k] and w [n, k]; n and k up to ST_LINEAR_MAX_CHANNELS.  y: float32 or bfloat16, row by row with y_pitch >= n.  y and pre overlap neither each
- * other nor what is read (but for the residual in y).  opts may be NULL.
+ * other nor what is read (but for the residual in y): ST_ERR_ARG where they do, unless they are rows of two different pitches that lie
+ * between each other, which is not looked into.  opts may be NULL.
  *   workspace  workspace_bytes >= st_linear_workspace(x, w) bytes (of these very matrices: a matrix that lies at an odd address or
  *              with odd strides takes a copy), 256-byte aligned; 0 bytes: refused sizes */
 size_t st_linear_workspace(const st_matrix* x, const st_matrix* w);
@@ -405,7 +406,8 @@ int st_linear(const st_matrix* x, const st_matrix* w, const st_linear_opts* opts
  *   dx [m, k] = dz W,   dw [n, k] (+)= dz^T x,   db [n] (+)= sum of dz over the tokens, in float32, before that rounding
  * (The residual's gradient is dy.)  Each of dx, dw, db may be NULL and costs nothing then; x without dw and w without dx may be NULL.
  * dx, dw: float32 or bfloat16, row by row with a pitch.  accumulate = 1 adds dw and db to what is there (several batches, one step);
- * dx is always written anew.  Without activation pre may be NULL and is not read.  What is written overlaps nothing that is read. */
+ * dx is always written anew.  Without activation pre may be NULL and is not read.  What is written overlaps nothing else that is
+ * written or read (ST_ERR_ARG, as for st_linear). */
 typedef struct st_linear_grads {
     void* dx; int64_t dx_pitch; int32_t dx_dtype;
     int32_t dw_dtype; void* dw; int64_t dw_pitch;

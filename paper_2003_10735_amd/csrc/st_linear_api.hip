@@ -1,6 +1,7 @@
 // C entry points of the dense layers in bfloat16 or float32 and of the clipping of gradients: validation, workspace layout, order of the launches.
 #include "st_clip.hpp"
 #include "st_linear.hpp"
+#include "st_overlap.hpp"
 
 #include <math.h>
 #include <algorithm>
@@ -38,6 +39,33 @@ int check(const st_matrix* x, int64_t rows, int64_t cols, int* along)
     else return ST_ERR_SHAPE;
     return ST_OK;
 }
+
+// What a call touches: a result row by row, a matrix that lies either way (checked), a vector.  No memory reaches FARTHEST from one run to the next.
+constexpr int64_t FARTHEST = (int64_t)1 << 39;
+Runs runs_of(const void* p, int32_t dtype, int64_t count, int64_t values, int64_t pitch)
+{
+    return Runs{(uint64_t)p, count, values * elem(dtype), std::min(pitch, FARTHEST / elem(dtype)) * elem(dtype)};
+}
+Runs runs_of(const st_matrix& x, int along)
+{
+    return runs_of(x.data, x.dtype, along ? x.rows : x.cols, along ? x.cols : x.rows, along ? x.row_stride : x.col_stride);
+}
+Runs runs_of(const float* p, int64_t n) { return Runs{(uint64_t)p, 1, n * 4, 0}; }
+// Whether one of the `written` overlaps another or one of the `read` (places at address 0 are not there).
+struct Touched {
+    Runs written[3], read[5];
+    int n_written = 0, n_read = 0;
+    void writes(const Runs& r) { if (r.at) written[n_written++] = r; }
+    void reads(const Runs& r) { if (r.at) read[n_read++] = r; }
+    bool overlap() const
+    {
+        for (int i = 0; i < n_written; ++i) {
+            for (int j = 0; j < i; ++j) if (st::overlap(written[i], written[j])) return true;
+            for (int j = 0; j < n_read; ++j) if (st::overlap(written[i], read[j])) return true;
+        }
+        return false;
+    }
+};
 
 // An operand whose rows are x's rows (by_rows) or its columns: as it lies, or where the products cannot read it so, a copy that `packs`
 // makes (with room in `w`).  The copy lies as x does, unless only the other order keeps a tile's offsets small.
@@ -219,6 +247,13 @@ int st_linear(const st_matrix* x, const st_matrix* w, const st_linear_opts* opts
     LinearPlan l = plan_linear(*x, x_along, *w, w_along, (char*)workspace);
     if (!l.bytes) return ST_ERR_SHAPE;
     if (l.bytes > 256 && (!workspace || !is_aligned(workspace, 256) || workspace_bytes < l.bytes)) return ST_ERR_WORKSPACE;
+    const int64_t m = x->rows;
+    Touched t;
+    t.writes(runs_of(y, y_dtype, m, n, y_pitch));
+    if (o.pre) t.writes(runs_of(o.pre, o.pre_dtype, m, n, o.pre_pitch));
+    t.reads(runs_of(*x, x_along)); t.reads(runs_of(*w, w_along)); t.reads(runs_of(o.bias, n));
+    if (o.residual && o.residual != y) t.reads(runs_of(o.residual, o.residual_dtype, m, n, o.residual_pitch));
+    if (t.overlap()) return ST_ERR_ARG;
     LinearProduct& p = l.p;
     p.out = y; p.out_bf16 = y_dtype == ST_BF16; p.out_pitch = y_pitch;
     p.bias = o.bias; p.act = o.activation;
@@ -291,6 +326,15 @@ int st_linear_backward(const st_matrix* x, const st_matrix* w, const st_matrix* 
     BackwardPlan b = plan_backward(x, x_along, o.dw_dtype, w, w_along, o.dx_dtype, *dy, dy_along, activation, dtype, o.db != nullptr, (char*)workspace);
     if (!b.bytes) return ST_ERR_SHAPE;
     if (b.bytes > 256 && (!workspace || !is_aligned(workspace, 256) || workspace_bytes < b.bytes)) return ST_ERR_WORKSPACE;
+    Touched t;
+    if (o.dx) t.writes(runs_of(o.dx, o.dx_dtype, m, k, o.dx_pitch));
+    if (o.dw) t.writes(runs_of(o.dw, o.dw_dtype, n, k, o.dw_pitch));
+    t.writes(runs_of(o.db, n));
+    if (x) t.reads(runs_of(*x, x_along));
+    if (w) t.reads(runs_of(*w, w_along));
+    t.reads(runs_of(*dy, dy_along));
+    if (activation != ST_ACT_NONE) t.reads(runs_of(*pre, pre_along));
+    if (t.overlap()) return ST_ERR_ARG;
     if (activation != ST_ACT_NONE) b.slope.pre = GradSource{pre->data, pre->dtype == ST_BF16, pre_along ? pre->row_stride : pre->col_stride, pre_along};
     b.sums.out = o.db; b.sums.accumulate = o.accumulate;
     int at = 0;
