@@ -42,11 +42,12 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 // 16 bytes a lane from `rsrc` + voff to LDS at `lds` + 16 * lane (the whole offset is the lanes': a scalar one takes no part in the
 // comparison with the buffer's size).  Written out, because the compiler has every transposing LDS read wait for all loads of its own
 // builtin that are under way, whatever they write (8192 tokens 4096 -> 4096, dz^T x: 256 us that way); the waits that are needed stand
-// where the stages change.  No register is written.  The pause covers a scalar register that a vector instruction has written just before, and M0.
+// where the stages change.  No register is written; M0, which holds the place in LDS, is an operand, so that the compiler sets it and knows what it
+// holds.  The pause covers M0 and a scalar register that a vector instruction has written just before.
 __device__ __forceinline__ void load_to_lds(i32x4 rsrc, char* lds, unsigned voff)
 {
     const unsigned to = (unsigned)__builtin_amdgcn_readfirstlane((int)(uintptr_t)(__attribute__((address_space(3))) char*)lds);
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(to), "v"(voff), "s"(rsrc) : "memory");      // (M0: nothing else of these kernels asks for it)
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(to), "v"(voff), "s"(rsrc) : "memory");
 }
 __device__ __forceinline__ i32x4 buffer(const char* base, int64_t bytes)
 {
