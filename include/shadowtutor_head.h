@@ -422,8 +422,10 @@ int st_linear_backward(const st_matrix* x, const st_matrix* w, const st_matrix* 
  * Over a list of tensors of any types together (the lists of several optimisers, whose steps take one type each):
  *   norm = 2-norm of all grad_scale * g, sums in float64
  *   out = grad_scale * c * g, rounded once to out's type;  c = max_norm / norm where 0 < max_norm < norm < infinity, else 1
- * (with a norm that is no finite number nothing is clipped; grad_norm says so).  out may be grad itself (same type); otherwise no out
- * overlaps any other tensor of the list, and no tensor is in the list twice. */
+ * The norm is a float64 there: with one that is no finite number nothing is clipped, with any other the gradients are.  grad_norm is that norm as a
+ * float32, so it is infinite or NaN in the first case, and infinite in the second too where the norm is finite but more than float32 holds (3.4e38):
+ * whoever leaves out steps whose grad_norm is not finite leaves out those as well.
+ * out may be grad itself (same type); otherwise no out overlaps any other tensor of the list, and no tensor is in the list twice. */
 typedef struct st_grad_tensor {      /* HOST struct of DEVICE pointers, aligned to their elements */
     const void* grad;                /* [n] */
     void* out;                       /* [n], or NULL in every tensor: the norm alone */

@@ -735,7 +735,8 @@ def _workspace(workspace, where):
 
 
 def st_linear(x, w, bias=None, activation: int = ST_ACT_NONE, residual=None, pre=None, out=None, out_dtype=None, workspace=None, stream=None):
-    """out [m, n] = act(x W^T + bias) + residual: x [m, k] and w [n, k] float32 or bfloat16, both of one type, either order each, any strides;
+    """out [m, n] = act(x W^T + bias) + residual: x [m, k] and w [n, k] float32 or bfloat16, both of one type, row by row or column by
+    column each at any distance (one stride is 1);
     bias float32 [n]; residual [m, n] float32 or bfloat16, row by row, which may be out itself.  pre [m, n] (float32 or bfloat16, row by
     row) receives x W^T + bias, which st_linear_backward asks for.  out: float32 or bfloat16, as given, else of out_dtype, else of x's type."""
     where = "st_linear"
@@ -843,7 +844,8 @@ def new_grad_workspace(tensors: GradTensors):
 
 def st_grad_clip(tensors: GradTensors, max_norm: float = 0.0, grad_scale: float = 1.0, grad_norm=None, workspace=None, stream=None):
     """Every gradient of the list times grad_scale, and, where the 2-norm of all of them is above max_norm > 0, times max_norm / norm, into its
-    place in the list's outs.  grad_norm (float32 [1]) receives the norm before clipping.  A norm that is not finite clips nothing."""
+    place in the list's outs.  grad_norm (float32 [1]) receives the norm before clipping.  A norm that is not finite clips nothing; one that is but passes
+    float32's range clips, and grad_norm is infinite in either case."""
     where = "st_grad_clip"
     if not tensors.on_device:
         raise StError(ST_ERR_ARG, where)
