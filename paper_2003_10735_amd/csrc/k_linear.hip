@@ -771,6 +771,13 @@ template <class E, int NT> __global__ __launch_bounds__(FEW_WAVES * 64) void k_l
 // 4096 -> 14336 37 and 28, 8192 -> 1000 16.7 and 10.6, 32 tokens 4096 -> 4096 13.4 and 12.8.  Rows of bfloat16 at odd addresses, whose 16 bytes the
 // card fetches in pieces: 16 tokens 1001 -> 3001 7.3 and 7.7, 20 8.5 and 7.6, 20 tokens 4097 -> 4097 51 and 19.  float32: 16 tokens 2048 -> 5632 17.1
 // and 19.4, 8 tokens 4096 -> 4096 14.5 and 23.1, 16 tokens 4096 -> 14336 67 and 56, 32 tokens 8192 -> 500 43 and 12.
+// Beyond 4096, weights that no cache holds, 1, 4, 8 and 16 tokens here against one time of the tiles (which hardly depends on the tokens), a call in a graph:
+// 5632 -> 2048 10.8, 11.5, 12.3, 14.3 and 11.9; 8192 -> 1024 13.7 - 18.4 and 11.2; 16384 -> 500 24.7 - 33.7 and 11.8; 14336 -> 4096 29.2, 31.2, 32.7, 37.7 and
+// 29.1; 8192 -> 8192 29.0, 31.5, 34.8, 41.0 and 33.3: a tenth to be had for one token of some shapes, twice the time to be lost in others.  float32, 1
+// token: 5632 -> 2048 19.1 and 19.0, 14336 -> 4096 51 and 62.  At odd addresses, 1, 4 and 8 tokens: 1001 -> 3001 5.5, 6.6, 6.8 and 7.3, 8.9, 8.5; 2049 -> 2049 9.2, 11.6,
+// 12.7 and 14.0, 15.1, 15.0; 4097 -> 4097 17.9, 27.1, 31.0 and 24.0, 25.4, 25.3; 14337 -> 1001 47.9, 64.6, 72.1 and 17.2, 18.3, 18.3: the limit of 1024 keeps clear of
+// what is lost at long rows and leaves up to a third at 1025 .. 4096 with few tokens.  Tokens that lie column by column, whose values are loaded one by one: 8 tokens
+// 1024 -> 4096 6.8 and 6.8, 4096 -> 4096 21.5 and 14.4, which the rule does not tell apart.
 bool linear_few(int64_t m, int64_t n, int64_t k, int is_bf16, bool aligned)
 {
     if (m > 32 || k > 4096) return false;
@@ -849,6 +856,10 @@ template <class E, bool LOOSE> static void launch_small(Ctx& c, const GemmPair& 
     const dim3 grid(g.g[0].blocks + g.g[1].blocks + (unsigned)ceil_div(g.sums.n, SUM_COLUMNS));
     ST_LAUNCH(c, LOOSE ? "linear_small_loose" : "linear_small", (k_linear_small<E, LOOSE>), grid, dim3(SMALL_THREADS), small_lds(LOOSE), g);
 }
+// 128 x 128 with four stages under way takes a compute unit's LDS, with two a half.  Up to 256 blocks each has a unit for itself; beyond, two side by side are worth
+// more than the depth.  Four stages and two, us: bfloat16 135 blocks (3384 tokens 1416 -> 584) 19.8 and 25.5, 184 (408 tokens 3088 -> 5784) 36.0 and 48.7, 230 (5824
+// tokens 5976 -> 520) 76 and 98; 264 blocks (992 tokens 216 -> 4176) 15.4 and 11.1, 288 (2296 tokens 3008 -> 2024) 57 and 41, 550 (6976 tokens 2144 -> 1200) 72 and 70.
+// float32, whose products take longer than loads: 207 - 252 blocks 0.98 - 1.00 of the deep one's time either way, 410 - 684 blocks 0.88 - 0.95.
 template <class E> static void launch_tile(Ctx& c, const GemmPair& g, int tile)
 {
     if (tile == SMALL) {
