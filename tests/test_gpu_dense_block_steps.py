@@ -91,3 +91,29 @@ def test_a_recorded_step_is_an_eager_one():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(held(block), before if bad is not None else seen[3])) and block.steps == 3
+
+
+@pytest.mark.parametrize("bad", [None, float("nan")])
+def test_a_step_recorded_right_behind_eager_ones(bad):
+    """The count of the eager steps is settled while the graph is recorded."""
+    values = [None, bad, None]
+    block, seen = run(values, 1, 32)
+    desc, cells, params, labels, head = setup()
+    again = DenseBlockFront(desc, *params, lr=3e-3, weight_decay=0.01, state_bits=32)
+    for value in values[:2]:
+        again.backward(cells, labels, head, head_lr=0.0)
+        spoil(again, 1, value)
+        again.apply()
+    again.frames = 1
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        again.apply()
+    again.backward(cells, labels, head, head_lr=0.0)
+    before, grads = [t.clone() for t in held(again)], [g.clone() for g in again.grads]
+    for _ in range(3):
+        for t, b in zip((*held(again), *again.grads), (*before, *grads)):
+            t.copy_(b)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(held(again), seen[3])) and again.steps == block.steps == (3 if bad is None else 2)
